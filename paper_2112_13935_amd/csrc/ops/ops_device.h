@@ -1,0 +1,124 @@
+// Device-side helpers of the operators: values in fp32 and bf16, activations, the dropout's mask.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../aet_device.h"
+#include "aet_ops.h"
+
+namespace aet_ops {
+
+typedef __bf16 bf16;
+typedef bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef bf16 bf4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f8 __attribute__((ext_vector_type(8)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+// V values from memory that is aligned to the type only (ALIGNED: to all V of them), as floats, and back:
+// one rounding, to nearest even.
+template <typename T, int V>
+struct Vec {
+    typedef T type __attribute__((ext_vector_type(V)));
+};
+template <typename T>
+struct Vec<T, 1> {
+    typedef T type;
+};
+template <typename T, int V>
+__device__ __forceinline__ void load(const T *p, float (&v)[V]) {
+    if constexpr (V == 1) {
+        v[0] = (float)p[0];
+    } else {
+        const auto raw = *(const typename Vec<T, V>::type *)p;
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (float)raw[i];
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store(T *p, const float (&v)[V]) {
+    if constexpr (V == 1) {
+        p[0] = (T)v[0];
+    } else {
+        typename Vec<T, V>::type raw;
+#pragma unroll
+        for (int i = 0; i < V; ++i) raw[i] = (T)v[i];
+        *(typename Vec<T, V>::type *)p = raw;
+    }
+}
+
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+// Phi(z) and exp(-z^2 / 2).  Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: erfc(u) =
+// (a1 t + ... + a5 t^5) exp(-u^2), t = 1 / (1 + p u), u >= 0, with an error of at most 1.5e-7; Phi has half of
+// it, which is about the rounding of 1 + erf.
+__device__ __forceinline__ float normal_cdf(float z, float &e) {
+    const float u = __builtin_fabsf(z) * 0.70710678f;
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, u, 1.0f));
+    float s = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
+    s = __builtin_fmaf(t, s, 1.421413741f);
+    s = __builtin_fmaf(t, s, -0.284496736f);
+    s = __builtin_fmaf(t, s, 0.254829592f);
+    e = exp_fast(-u * u);
+    const float tail = 0.5f * t * s * e;
+    return z < 0 ? tail : 1.0f - tail;
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if constexpr (ACT == AET_ACT_RELU) return z <= 0 ? 0.0f : z;
+    if constexpr (ACT == AET_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
+    if constexpr (ACT == AET_ACT_GELU) {
+        float e;
+        return z * normal_cdf(z, e);
+    }
+    return z;
+}
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+    if constexpr (ACT == AET_ACT_RELU) return z > 0 ? 1.0f : 0.0f;
+    if constexpr (ACT == AET_ACT_SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
+        return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
+    }
+    if constexpr (ACT == AET_ACT_GELU) {
+        float e;
+        const float c = normal_cdf(z, e);
+        return __builtin_fmaf(z * 0.39894228f, e, c);
+    }
+    return 1.0f;
+}
+
+// The dropout of a call: rows of `half` counters.
+struct Drop {
+    uint64_t key;      // of the stream
+    uint64_t first;    // counter of the first row's first pair
+    uint64_t half;     // ceil(cols / 2)
+    uint32_t least;    // a value stays where its half of the hash is no less; 0: everything stays
+    float scale;
+};
+__device__ __forceinline__ uint64_t drop_row(const Drop &d, int64_t row) { return d.first + (uint64_t)row * d.half; }
+// The hash of columns 2 j (lower half) and 2 j + 1 (upper half) of the row whose counters begin at q.
+__device__ __forceinline__ uint64_t drop_hash(const Drop &d, uint64_t q, int j) {
+    return aet::splitmix_at(d.key, q + (uint32_t)j);
+}
+// v[i]: columns col .. col + V - 1
+template <int V>
+__device__ __forceinline__ void drop_apply(const Drop &d, uint64_t q, int col, float (&v)[V]) {
+    if constexpr (V == 1) {
+        const uint64_t h = drop_hash(d, q, col >> 1);
+        v[0] = (uint32_t)(col & 1 ? h >> 32 : h) >= d.least ? v[0] * d.scale : 0.0f;
+    } else {   // col is even
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            const uint64_t h = drop_hash(d, q, (col + i) >> 1);
+            v[i] = (uint32_t)h >= d.least ? v[i] * d.scale : 0.0f;
+            v[i + 1] = (uint32_t)(h >> 32) >= d.least ? v[i + 1] * d.scale : 0.0f;
+        }
+    }
+}
+
+}  // namespace aet_ops
