@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../per_device.h"
 #include "ops_device.h"
 
 namespace aet_ops {

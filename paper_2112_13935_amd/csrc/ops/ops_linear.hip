@@ -1,90 +1,30 @@
 // The linear layer with bias, activation, dropout and residual in its epilogue, and its gradient.
 #include "ops_internal.h"
+#include "ops_tiles.h"
 
 namespace aet_ops {
 
-// C[m][n] = sum over k of A(m, k) B(n, k) for each client; what is done with a sum is the epilogue's.
-struct Operand {
-    const void *p;
-    int64_t client, row, k;   // strides
-};
+static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-struct ForwardEpilogue {
-    aet_in bias, residual;
-    aet_out y, pre;
-    int rows, act;
-    Drop d;
-};
-struct StoreEpilogue {
-    aet_out c;
-};
-
-__device__ __forceinline__ float act_any(int act, float z) {
-    switch (act) {
-    case AET_ACT_RELU: return act_value<AET_ACT_RELU>(z);
-    case AET_ACT_SILU: return act_value<AET_ACT_SILU>(z);
-    case AET_ACT_GELU: return act_value<AET_ACT_GELU>(z);
-    default: return z;
-    }
+static Product forward_product(const aet_linear &a) {
+    Product p = {};
+    p.a = {a.x.p, a.x.client, a.x.row, false};
+    p.b = {a.w.p, a.w.client, a.w.row, false};
+    p.clients = a.n;
+    p.M = a.rows;
+    p.N = a.out;
+    p.K = a.in;
+    p.e = {a.bias, a.residual, a.y, a.pre, a.rows, a.act, make_drop(a.p, a.seed, a.first_row, a.out)};
+    return p;
 }
-__device__ __forceinline__ float slope_any(int act, float z) {
-    switch (act) {
-    case AET_ACT_RELU: return act_slope<AET_ACT_RELU>(z);
-    case AET_ACT_SILU: return act_slope<AET_ACT_SILU>(z);
-    case AET_ACT_GELU: return act_slope<AET_ACT_GELU>(z);
-    default: return 1.0f;
-    }
-}
-
-template <typename T>
-__device__ __forceinline__ void finish(const ForwardEpilogue &e, int c, int m, int n, float v) {
-    if (e.bias.p) v += (float)((const T *)e.bias.p)[c * e.bias.client + n];
-    if (e.pre.p) ((T *)e.pre.p)[c * e.pre.client + m * e.pre.row + n] = (T)v;
-    float w[1] = {act_any(e.act, v)};
-    if (e.d.least) drop_apply(e.d, drop_row(e.d, (int64_t)c * e.rows + m), n, w);
-    if (e.residual.p) w[0] += (float)((const T *)e.residual.p)[c * e.residual.client + m * e.residual.row + n];
-    ((T *)e.y.p)[c * e.y.client + m * e.y.row + n] = (T)w[0];
-}
-template <typename T>
-__device__ __forceinline__ void finish(const StoreEpilogue &e, int c, int m, int n, float v) {
-    ((T *)e.c.p)[c * e.c.client + m * e.c.row + n] = (T)v;
-}
-
-// 16 x 16 values a workgroup, one a thread.
-template <typename T, class E>
-__global__ __launch_bounds__(256) void k_product(Operand a, Operand b, int M, int N, int K, E e) {
-    __shared__ float sa[16][17], sb[16][17];
-    const int tn = (N + 15) / 16, tm = (M + 15) / 16;
-    const int c = blockIdx.x / (tn * tm), t = blockIdx.x % (tn * tm), m0 = t / tn * 16, n0 = t % tn * 16;
-    const int i = threadIdx.x / 16, j = threadIdx.x % 16;
-    float acc = 0;
-    for (int k0 = 0; k0 < K; k0 += 16) {
-        sa[i][j] = m0 + i < M && k0 + j < K ? (float)((const T *)a.p)[c * a.client + (m0 + i) * a.row + (k0 + j) * a.k] : 0.0f;
-        sb[i][j] = n0 + i < N && k0 + j < K ? (float)((const T *)b.p)[c * b.client + (n0 + i) * b.row + (k0 + j) * b.k] : 0.0f;
-        __syncthreads();
-        for (int k = 0; k < 16; ++k) acc += sa[i][k] * sb[j][k];
-        __syncthreads();
-    }
-    if (m0 + i < M && n0 + j < N) finish<T>(e, c, m0 + i, n0 + j, acc);
-}
-
-template <typename T, class E>
-static void product(const Operand &a, const Operand &b, int n, int M, int N, int K, const E &e, hipStream_t s) {
-    const int64_t blocks = n * ceil_div(M, 16) * ceil_div(N, 16);
-    if (blocks) k_product<T><<<(int)blocks, 256, 0, s>>>(a, b, M, N, K, e);
-}
-
-size_t linear_forward_workspace(const aet_linear &) { return 0; }
-hipError_t launch_linear_forward(const aet_linear &a, void *, hipStream_t s) {
-    const Operand x = {a.x.p, a.x.client, a.x.row, 1}, w = {a.w.p, a.w.client, a.w.row, 1};
-    const ForwardEpilogue e = {a.bias, a.residual, a.y, a.pre, a.rows, a.act, make_drop(a.p, a.seed, a.first_row, a.out)};
-    a.dtype == AET_F32 ? product<float>(x, w, a.n, a.rows, a.out, a.in, e, s) : product<bf16>(x, w, a.n, a.rows, a.out, a.in, e, s);
-    return hipGetLastError();
+size_t linear_forward_workspace(const aet_linear &a) { return product_workspace(a.dtype, forward_product(a)); }
+hipError_t launch_linear_forward(const aet_linear &a, void *workspace, hipStream_t s) {
+    return launch_product(a.dtype, forward_product(a), workspace, s);
 }
 
 // dz, and db: a thread per column.
 template <typename T>
-__global__ __launch_bounds__(256) void k_dz(aet_linear_grad a, Drop d, T *dz) {
+__global__ __launch_bounds__(256) void k_dz(aet_linear_grad a, Drop d, T *dz, int64_t dz_row) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= (int64_t)a.n * a.out) return;
     const int64_t c = i / a.out;
@@ -93,27 +33,71 @@ __global__ __launch_bounds__(256) void k_dz(aet_linear_grad a, Drop d, T *dz) {
     for (int r = 0; r < a.rows; ++r) {
         float v[1] = {(float)((const T *)a.dy.p)[c * a.dy.client + r * a.dy.row + col]};
         if (d.least) drop_apply(d, drop_row(d, c * a.rows + r), col, v);
-        if (a.act) v[0] *= slope_any(a.act, (float)((const T *)a.pre.p)[c * a.pre.client + r * a.pre.row + col]);
+        if (a.act) {
+            const float z = (float)((const T *)a.pre.p)[c * a.pre.client + r * a.pre.row + col];
+            v[0] *= a.act == AET_ACT_RELU ? act_slope<AET_ACT_RELU>(z) : a.act == AET_ACT_SILU ? act_slope<AET_ACT_SILU>(z) : act_slope<AET_ACT_GELU>(z);
+        }
         sum += v[0];
-        dz[(c * a.rows + r) * a.out + col] = (T)v[0];
+        if (dz) dz[(c * a.rows + r) * dz_row + col] = (T)v[0];
     }
     if (a.db.p) ((T *)a.db.p)[c * a.db.client + col] = (T)sum;
 }
 
-size_t linear_backward_workspace(const aet_linear_grad &a) {
-    return (size_t)a.n * a.rows * a.out * (a.dtype == AET_F32 ? 4 : 2);
+// dz has a place of its own unless it is dy.
+struct BackwardPlan {
+    bool own_dz;
+    int64_t dz_row;
+    Product dx, dw;
+    size_t dz_bytes, bytes;
+};
+static BackwardPlan plan(const aet_linear_grad &a, char *workspace) {
+    BackwardPlan b = {};
+    b.own_dz = a.p > 0 || a.act != AET_ACT_NONE;
+    const int e = a.dtype == AET_F32 ? 4 : 2;
+    b.dz_row = ceil_div((int64_t)a.out * e, 16) * 16 / e;
+    b.dz_bytes = b.own_dz && (a.dx.p || a.dw.p) ? up256((size_t)a.n * a.rows * b.dz_row * e) : 0;
+    Operand dz = {a.dy.p, a.dy.client, a.dy.row, false};
+    if (b.own_dz) dz = {workspace, a.rows * b.dz_row, b.dz_row, false};
+    const Drop none = {};
+    if (a.dx.p) {
+        b.dx.a = dz;
+        b.dx.b = {a.w.p, a.w.client, a.w.row, true};
+        b.dx.clients = a.n;
+        b.dx.M = a.rows;
+        b.dx.N = a.in;
+        b.dx.K = a.out;
+        b.dx.e = {{}, {}, a.dx, {}, a.rows, AET_ACT_NONE, none};
+    }
+    if (a.dw.p) {
+        dz.by_columns = true;
+        b.dw.a = dz;
+        b.dw.b = {a.x.p, a.x.client, a.x.row, true};
+        b.dw.clients = a.n;
+        b.dw.M = a.out;
+        b.dw.N = a.in;
+        b.dw.K = a.rows;
+        b.dw.e = {{}, {}, a.dw, {}, a.out, AET_ACT_NONE, none};
+    }
+    const size_t x = product_workspace(a.dtype, b.dx), w = product_workspace(a.dtype, b.dw);
+    b.bytes = b.dz_bytes + (x > w ? x : w);
+    return b;
 }
+
+size_t linear_backward_workspace(const aet_linear_grad &a) { return plan(a, nullptr).bytes; }
+
 template <typename T>
-static void backward(const aet_linear_grad &a, T *dz, hipStream_t s) {
+static hipError_t backward(const aet_linear_grad &a, char *workspace, hipStream_t s) {
+    const BackwardPlan b = plan(a, workspace);
     const int64_t columns = (int64_t)a.n * a.out;
-    if (columns) k_dz<T><<<(int)ceil_div(columns, 256), 256, 0, s>>>(a, make_drop(a.p, a.seed, a.first_row, a.out), dz);
-    const int64_t client = (int64_t)a.rows * a.out;
-    if (a.dx.p) product<T>({dz, client, a.out, 1}, {a.w.p, a.w.client, 1, a.w.row}, a.n, a.rows, a.in, a.out, StoreEpilogue{a.dx}, s);
-    if (a.dw.p) product<T>({dz, client, 1, a.out}, {a.x.p, a.x.client, 1, a.x.row}, a.n, a.out, a.in, a.rows, StoreEpilogue{a.dw}, s);
+    if (columns && (b.dz_bytes || a.db.p))
+        k_dz<T><<<(int)ceil_div(columns, 256), 256, 0, s>>>(a, make_drop(a.p, a.seed, a.first_row, a.out), b.dz_bytes ? (T *)workspace : nullptr, b.dz_row);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && a.dx.p) e = launch_product(a.dtype, b.dx, workspace + b.dz_bytes, s);
+    if (e == hipSuccess && a.dw.p) e = launch_product(a.dtype, b.dw, workspace + b.dz_bytes, s);
+    return e;
 }
 hipError_t launch_linear_backward(const aet_linear_grad &a, void *workspace, hipStream_t s) {
-    a.dtype == AET_F32 ? backward<float>(a, (float *)workspace, s) : backward<bf16>(a, (bf16 *)workspace, s);
-    return hipGetLastError();
+    return a.dtype == AET_F32 ? backward<float>(a, (char *)workspace, s) : backward<bf16>(a, (char *)workspace, s);
 }
 
 }  // namespace aet_ops

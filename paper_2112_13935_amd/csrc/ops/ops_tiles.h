@@ -1,0 +1,24 @@
+// C[m][n] = sum over k of A(m, k) B(n, k) on the matrix cores, a tile of C per workgroup.
+#pragma once
+#include "ops_epilogue.h"
+
+namespace aet_ops {
+
+// By rows: element (r, k) is at p + client * c + row * r + k.  By columns: at p + client * c + row * k + r.
+struct Operand {
+    const void *p;
+    int64_t client, row;
+    bool by_columns;
+};
+
+struct Product {
+    Operand a, b;
+    int clients, M, N, K;
+    Epilogue e;
+};
+
+// Bytes of scratch that the product wants (for sums that are split along k).
+size_t product_workspace(int dtype, const Product &p);
+hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStream_t s);
+
+}  // namespace aet_ops

@@ -1,0 +1,432 @@
+// Products on the matrix cores, for the linear layer and its gradient: a tile of C per workgroup, staged through LDS.
+//
+// bf16: v_mfma_f32_32x32x16_bf16.  fp32: the same unit, each value in three bf16 parts and six products (split_bf16.h),
+// which holds 24 bits at 6/16 of the fp32 unit's time.
+//
+// A stage of BK along k of both operands lies in LDS in pieces of 16 bytes (8 values, in one part): by rows as [row][BK],
+// by columns as [k][row], so that both are copied as they lie in memory and no transposition is made on the way.  A lane
+// of the matrix unit wants 8 consecutive k of one row: by rows one ds_read_b128, by columns two ds_read_b64_tr_b16, which
+// hand 16 lanes the transpose of 4 pieces of memory.  The pieces of a row are permuted by exclusive or with the row's number
+// (by columns: in groups of 4 with k), so that the lanes that read together find different banks.
+#include "ops_internal.h"
+#include "ops_tiles.h"
+
+#include "../split_bf16.h"
+
+namespace aet_ops {
+
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char *lds_ptr;
+
+struct Shape {
+    int M, N, K;
+    int tiles_n, tiles;       // tiles of C: in a row, of a client
+    int slices, slice_k;      // parts of the sum (slice_k a multiple of BK); partial sums go to `partial` where there are several
+    int blocks;
+    float *partial;           // [slice][client][M][N]
+    int clients;
+};
+
+// Workgroups go to the XCDs in turn: each XCD gets consecutive tiles, whose operands meet in its L2.
+__device__ __forceinline__ int xcd_order(int id, int blocks) {
+    const int q = blocks / 8, r = blocks % 8, x = id % 8;
+    return x * q + (x < r ? x : r) + id / 8;
+}
+
+// ---- staging -----------------------------------------------------------------------------
+
+// Piece (r, c) of an operand's stage: by rows row r, values 8 c .. of the stage; by columns k = r, rows 8 c ..
+template <int R, int BK, bool COLS>
+struct Stage {
+    static constexpr int kPieces = R * BK / 8;
+    static constexpr int kWidth = COLS ? R / 8 : BK / 8;   // pieces side by side
+    static constexpr int kBytes = R * BK * 2;              // of a part
+    static __device__ __forceinline__ int slot(int r, int c) {
+        if constexpr (COLS) return r * kWidth + (c ^ ((r & 3 & (R / 32 - 1)) << 2));
+        else return r * kWidth + (c ^ (BK == 64 ? r & 7 : (r >> 1) & 3));
+    }
+    // Lane addresses of fragment t (rows 32 t ..): 8 k of row 32 t + lane % 32 from k = 16 ks + 8 (lane / 32) on
+    static __device__ __forceinline__ bf8 fragment(lds_ptr part, int t, int ks, int lane) {
+        if constexpr (COLS) {
+            const int i = lane & 15, j = i >> 2, k = 16 * ks + 8 * (lane >> 5) + j;
+            const int c = (4 * t + 2 * (lane >> 4 & 1) + (i >> 1 & 1)) ^ ((j & (R / 32 - 1)) << 2);
+            const lds_ptr at = part + k * (R * 2) + c * 16 + (i & 1) * 8;
+            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)at);
+            const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(at + 4 * R * 2));
+            typedef short s8 __attribute__((ext_vector_type(8)));
+            const s8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_bit_cast(bf8, both);
+        } else {
+            const int r = lane & 31, c = 2 * ks + (lane >> 5);
+            return *(__attribute__((address_space(3))) bf8 *)(part + t * (32 * BK * 2) + slot(r, c) * 16);
+        }
+    }
+};
+
+// Through registers: any alignment, any end of rows and sums.
+template <typename T, int R, int BK, bool COLS, int THREADS>
+struct RegStage {
+    using S = Stage<R, BK, COLS>;
+    static constexpr int kCount = S::kPieces / THREADS;
+    static_assert(S::kPieces % THREADS == 0 && THREADS % S::kWidth == 0, "whole pieces a thread");
+    static constexpr int kStep = THREADS / S::kWidth;   // rows between a thread's pieces
+    float raw[kCount][8];
+    const T *p;          // the thread's first piece of the next stage
+    int64_t row;
+    int r, c, left;      // left: by rows, k until the end of the sum; by columns, likewise
+    int rows;            // rows of C there are from the tile's first on
+
+    __device__ __forceinline__ void begin(const Operand &o, int64_t client, int r0, int rows_all, int k0, int k1) {
+        r = threadIdx.x / S::kWidth;
+        c = threadIdx.x % S::kWidth;
+        row = o.row;
+        rows = rows_all - r0;
+        left = k1 - k0;
+        p = (const T *)o.p + client * o.client + (COLS ? (int64_t)(k0 + r) * row + r0 + 8 * c : (int64_t)(r0 + r) * row + k0 + 8 * c);
+    }
+    __device__ __forceinline__ void load() {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const int ri = r + i * kStep;
+            const bool in = ri < (COLS ? left : rows);
+            const int count = in ? (COLS ? rows : left) - 8 * c : 0;
+            const T *at = p + (int64_t)(i * kStep) * row;
+            if (count >= 8) {
+                load8(at, raw[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) raw[i][e] = e < count ? (float)at[e] : 0.0f;
+            }
+        }
+        p += COLS ? BK * row : BK;
+        left -= BK;
+    }
+    // parts: of kBytes each
+    __device__ __forceinline__ void store(lds_ptr to) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const lds_ptr at = to + S::slot(r + i * kStep, c) * 16;
+            if constexpr (sizeof(T) == 2) {
+                bf8 v;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = (bf16)raw[i][e];
+                *(__attribute__((address_space(3))) bf8 *)at = v;
+            } else {
+                aet::Split8 s = aet::split8<false>(raw[i]);
+                uint32_t seen = 0;
+                aet::split_watch(seen, s);
+                if (aet::split_over(seen)) s = aet::split8<true>(raw[i]);   // something infinite, NaN or next to it
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *(__attribute__((address_space(3))) bf8 *)(at + q * S::kBytes) = s.p[q];
+            }
+        }
+    }
+};
+
+// From memory into LDS, without registers: 16-byte aligned pieces, sums of whole stages, whole pieces of rows.  Rows past
+// the last are read from the last again: they become rows of C that are not stored.
+template <int R, int BK, bool COLS, int THREADS>
+struct DirectStage {
+    using S = Stage<R, BK, COLS>;
+    static constexpr int kCount = S::kPieces / THREADS;
+    const char *p;              // the stage's first byte, the same for all threads
+    uint32_t at[kCount];
+    int64_t step;
+
+    __device__ __forceinline__ void begin(const Operand &o, int64_t client, int r0, int rows_all, int k0, int) {
+        const int rows = rows_all - r0;
+        p = (const char *)((const bf16 *)o.p + client * o.client + (COLS ? (int64_t)k0 * o.row + r0 : (int64_t)r0 * o.row + k0));
+        step = (COLS ? BK * o.row : BK) * 2;
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const int q = threadIdx.x + i * THREADS, r = q / S::kWidth, s = q % S::kWidth;
+            const int c = S::slot(r, s) - r * S::kWidth;   // the permutation is its own inverse
+            if (COLS) {
+                const int last = rows - 8;
+                at[i] = (uint32_t)r * (uint32_t)(o.row * 2) + (uint32_t)(8 * c < last ? 8 * c : last) * 2;
+            } else {
+                at[i] = (uint32_t)(r < rows ? r : rows - 1) * (uint32_t)(o.row * 2) + c * 16;
+            }
+        }
+    }
+    __device__ __forceinline__ void load(lds_ptr to) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+#pragma unroll
+        for (int i = 0; i < kCount; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p + at[i]),
+                                             (__attribute__((address_space(3))) void *)(to + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+        p += step;
+    }
+};
+
+// ---- the kernel --------------------------------------------------------------------------
+
+template <typename T>
+struct Parts {
+    static constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
+};
+
+// BM x BN of C, waves WR x WC; a wave has BM / WR x BN / WC in fragments of 32 x 32.
+template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT>
+struct Tile {
+    static constexpr int kThreads = 64 * WR * WC;
+    static constexpr int FM = BM / WR / 32, FN = BN / WC / 32;
+    static constexpr int kParts = Parts<T>::kParts;
+    using SA = Stage<BM, BK, TA>;
+    using SB = Stage<BN, BK, TB>;
+    static constexpr int kStage = kParts * (SA::kBytes + SB::kBytes);
+    static constexpr int kBuffers = sizeof(T) == 2 ? 2 : 1;
+    static constexpr int kEpilogue = WR * WC * 32 * (FN * 32 + 4) * 4;
+    static constexpr int kLds = kStage * kBuffers > kEpilogue ? kStage * kBuffers : kEpilogue;
+};
+
+template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT>
+__global__ __launch_bounds__(64 * WR * WC) void k_tiles(Operand oa, Operand ob, Shape s, Epilogue e) {
+    using L = Tile<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>;
+    constexpr int FM = L::FM, FN = L::FN, P = L::kParts;
+    using SA = typename L::SA;
+    using SB = typename L::SB;
+    extern __shared__ __attribute__((aligned(1024))) char lds_all[];
+    const lds_ptr lds = (lds_ptr)lds_all;
+
+    int id = xcd_order(blockIdx.x, s.blocks);
+    const int tile = id % s.tiles;
+    id /= s.tiles;
+    const int slice = id % s.slices;
+    const int64_t client = id / s.slices;
+    // eight rows of tiles at a time, column after column
+    const int tiles_m = s.tiles / s.tiles_n, group = tile / (8 * s.tiles_n) * 8;
+    const int high = tiles_m - group < 8 ? tiles_m - group : 8, in = tile - group * s.tiles_n;
+    const int m0 = (group + in % high) * BM, n0 = in / high * BN;
+    const int k0 = slice * s.slice_k, k1 = k0 + s.slice_k < s.K ? k0 + s.slice_k : s.K;
+
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int wr = wave / WC, wc = wave % WC;
+
+    f16v acc[FN][FM], corr[P == 3 ? FN : 1][P == 3 ? FM : 1];
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+            acc[i][j] = f16v{};
+            if constexpr (P == 3) corr[i][j] = f16v{};
+        }
+
+    const auto compute = [&](lds_ptr a, lds_ptr b) {
+#pragma unroll
+        for (int ks = 0; ks < BK / 16; ++ks) {
+            bf8 fa[FM][P], fb[FN][P];
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+#pragma unroll
+                for (int i = 0; i < FN; ++i) fb[i][q] = SB::fragment(b + q * SB::kBytes, wc * FN + i, ks, lane);
+#pragma unroll
+                for (int j = 0; j < FM; ++j) fa[j][q] = SA::fragment(a + q * SA::kBytes, wr * FM + j, ks, lane);
+            }
+            if constexpr (P == 1) {
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+#pragma unroll
+                    for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[i][0], fa[j][0], acc[i][j], 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 6; ++q)
+#pragma unroll
+                    for (int i = 0; i < FN; ++i)
+#pragma unroll
+                        for (int j = 0; j < FM; ++j) aet::split_mfma(q, fb[i], fa[j], acc[i][j], corr[i][j]);
+            }
+        }
+    };
+
+    const int stages = (k1 - k0 + BK - 1) / BK;
+    constexpr int kPartA = P * SA::kBytes;
+    if constexpr (DIRECT) {
+        DirectStage<BM, BK, TA, L::kThreads> la;
+        DirectStage<BN, BK, TB, L::kThreads> lb;
+        la.begin(oa, client, m0, s.M, k0, k1);
+        lb.begin(ob, client, n0, s.N, k0, k1);
+        if (stages > 0) {
+            la.load(lds);
+            lb.load(lds + kPartA);
+        }
+        for (int i = 0; i < stages; ++i) {
+            const lds_ptr now = lds + (i & 1) * L::kStage, next = lds + ((i & 1) ^ 1) * L::kStage;
+            // this stage has arrived, and everybody is done with the one before
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (i + 1 < stages) {
+                la.load(next);
+                lb.load(next + kPartA);
+            }
+            compute(now, now + kPartA);
+        }
+    } else {
+        RegStage<T, BM, BK, TA, L::kThreads> la;
+        RegStage<T, BN, BK, TB, L::kThreads> lb;
+        la.begin(oa, client, m0, s.M, k0, k1);
+        lb.begin(ob, client, n0, s.N, k0, k1);
+        la.load();
+        lb.load();
+        for (int i = 0; i < stages; ++i) {
+            const lds_ptr now = lds + (L::kBuffers == 2 ? (i & 1) * L::kStage : 0);
+            if constexpr (L::kBuffers == 1) __syncthreads();
+            la.store(now);
+            lb.store(now + kPartA);
+            __syncthreads();
+            if (i + 1 < stages) {
+                la.load();
+                lb.load();
+            }
+            compute(now, now + kPartA);
+        }
+    }
+    __syncthreads();
+
+    // A lane has, of row m0 + lane % 32 of a fragment, four columns at a time: through LDS, a wave for itself, to lanes
+    // with 8 columns each, in whole lines of memory.
+    constexpr int W = FN * 32, LINE = W + 4;
+    __attribute__((address_space(3))) float *mine = (__attribute__((address_space(3))) float *)lds + wave * (32 * LINE);
+    const int col = n0 + wc * W + lane % (W / 8) * 8;
+    const int count = s.N - col;
+    float bias[8];
+    bias8<T>(e, client, col, s.slices > 1 ? 0 : count, bias);
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                f4 v;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v[x] = P == 3 ? aet::split_sum(acc[i][j][4 * q + x], corr[P == 3 ? i : 0][P == 3 ? j : 0][4 * q + x]) : acc[i][j][4 * q + x];
+                *(__attribute__((address_space(3))) f4 *)(mine + (lane & 31) * LINE + i * 32 + 8 * q + 4 * (lane >> 5)) = v;
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < 32; r += 512 / W) {
+            const int line = r + lane / (W / 8);
+            const int64_t row = m0 + (wr * FM + j) * 32 + line;
+            float v[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f4 x = *(__attribute__((address_space(3))) f4 *)(mine + line * LINE + lane % (W / 8) * 8 + 4 * h);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) v[4 * h + y] = x[y] + bias[4 * h + y];
+            }
+            if (row < s.M && count > 0) {
+                if (s.slices > 1) store_some(s.partial + (((int64_t)slice * s.clients + client) * s.M + row) * s.N + col, count, v);
+                else finish8<T>(e, client, row, col, count, v);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Adds the slices of a split sum, in their order, and ends it.  A thread has 8 columns.
+template <typename T>
+__global__ __launch_bounds__(256) void k_join(Shape s, Epilogue e) {
+    const int wide = (s.N + 7) / 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t line = i / wide;
+    if (line >= (int64_t)s.clients * s.M) return;
+    const int col = (int)(i - line * wide) * 8, count = s.N - col;
+    const int64_t client = line / s.M, row = line - client * s.M;
+    float v[8];
+    bias8<T>(e, client, col, count, v);
+    for (int k = 0; k < s.slices; ++k) {
+        float x[8];
+        load_some(s.partial + ((int64_t)k * s.clients * s.M + line) * s.N + col, count, x);
+#pragma unroll
+        for (int y = 0; y < 8; ++y) v[y] += x[y];
+    }
+    finish8<T>(e, client, row, col, count, v);
+}
+
+// ---- the choice --------------------------------------------------------------------------
+
+// Whether the operand's stages of BK can go straight into LDS.
+static bool direct(const Operand &o, int rows, int K, int BK) {
+    const int64_t across = o.by_columns ? BK : 256;
+    return aligned16(o.p, 2, o.client, o.row) && o.row * 2 * across < (INT64_C(1) << 31) && K % BK == 0 && K > 0 &&
+           (!o.by_columns || rows % 8 == 0);
+}
+
+template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT>
+static hipError_t run_tiles(const Product &p, Shape s, hipStream_t stream) {
+    using L = Tile<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>;
+    const auto kernel = k_tiles<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>;
+    if constexpr (L::kLds > 64 * 1024) {
+        static aet::PerDevice allowed;
+        int dev = 0, ok = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        e = allowed.get(dev, &ok, [&](int *v) {
+            *v = 1;
+            return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kLds);
+        });
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<s.blocks, L::kThreads, L::kLds, stream>>>(p.a, p.b, s, p.e);
+    return hipGetLastError();
+}
+
+struct Choice {
+    int bm, bn, bk, slices;
+};
+static Choice choose(int dtype, const Product &p) {
+    Choice c;
+    if (dtype == AET_F32) {
+        c = {128, 128, 32, 1};
+    } else {
+        c = {128, 128, 64, 1};
+        if (p.M >= 256 && p.N >= 256 && p.clients * ceil_div(p.M, 256) * ceil_div(p.N, 256) >= 192) c.bm = c.bn = 256;
+    }
+    const int64_t tiles = p.clients * ceil_div(p.M, c.bm) * ceil_div(p.N, c.bn), stages = ceil_div(p.K, c.bk);
+    while (tiles * c.slices < 128 && stages / (c.slices * 2) >= 4) c.slices *= 2;
+    return c;
+}
+
+size_t product_workspace(int dtype, const Product &p) {
+    const Choice c = choose(dtype, p);
+    return c.slices > 1 ? (size_t)c.slices * p.clients * p.M * p.N * sizeof(float) : 0;
+}
+
+template <typename T, bool TA, bool TB>
+static hipError_t run_product(const Product &p, void *workspace, hipStream_t stream) {
+    const Choice c = choose(sizeof(T) == 4 ? AET_F32 : AET_BF16, p);
+    Shape s = {p.M, p.N, p.K};
+    s.clients = p.clients;
+    s.tiles_n = (int)ceil_div(p.N, c.bn);
+    const int64_t tiles = ceil_div(p.M, c.bm) * s.tiles_n, blocks = tiles * p.clients * c.slices;
+    if (!blocks) return hipSuccess;
+    if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+    s.tiles = (int)tiles;
+    s.blocks = (int)blocks;
+    s.slices = c.slices;
+    s.slice_k = (int)ceil_div(ceil_div(p.K, c.bk), c.slices) * c.bk;
+    s.partial = (float *)workspace;
+    hipError_t e;
+    if constexpr (sizeof(T) == 4) {
+        e = run_tiles<T, 128, 128, 32, 2, 2, TA, TB, false>(p, s, stream);
+    } else {
+        const bool d = direct(p.a, p.M, p.K, c.bk) && direct(p.b, p.N, p.K, c.bk);
+        if (c.bm == 256) e = d ? run_tiles<T, 256, 256, 64, 2, 4, TA, TB, true>(p, s, stream) : run_tiles<T, 256, 256, 64, 2, 4, TA, TB, false>(p, s, stream);
+        else e = d ? run_tiles<T, 128, 128, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 128, 128, 64, 2, 2, TA, TB, false>(p, s, stream);
+    }
+    if (e != hipSuccess || s.slices == 1) return e;
+    k_join<T><<<(int)ceil_div((int64_t)p.clients * p.M * ceil_div(p.N, 8), 256), 256, 0, stream>>>(s, p.e);
+    return hipGetLastError();
+}
+
+hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStream_t s) {
+    const bool f32 = dtype == AET_F32;
+    if (!p.a.by_columns && !p.b.by_columns) return f32 ? run_product<float, false, false>(p, workspace, s) : run_product<bf16, false, false>(p, workspace, s);
+    if (!p.a.by_columns) return f32 ? run_product<float, false, true>(p, workspace, s) : run_product<bf16, false, true>(p, workspace, s);
+    return f32 ? run_product<float, true, true>(p, workspace, s) : run_product<bf16, true, true>(p, workspace, s);
+}
+
+}  // namespace aet_ops

@@ -76,6 +76,25 @@ def test_backward(ops, size, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size,pad", [((2, 2568, 2624, 2632), 0), ((2, 2568, 2624, 2632), 3), ((1, 3000, 700, 4104), 0)], ids=str)
+def test_large(ops, size, pad, dtype):
+    """Many tiles of the largest kind, whole and at the edges."""
+    n, rows, inp, out = size
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(pad)
+    x, w, b = rand(g, (n, rows, inp), dt, pad=pad), rand(g, (n, out, inp), dt, inp ** -0.5), rand(g, (n, out), dt)
+    dy, pre = rand(g, (n, rows, out), dt), rand(g, (n, rows, out), dt)
+    y, z = ops.aet_linear_forward(x, w, b, act="gelu", p=0.1, seed=1, keep_pre=True)
+    got = ops.aet_linear_backward(dy, x, w, pre, act="gelu", p=0.1, seed=1)
+    torch.cuda.synchronize()
+    wy, wz = O.linear_forward(d64(x), d64(w), d64(b), None, "gelu", 0.1, 1, 0, dt)
+    O.near(y, wy, "y")
+    O.near(z, wz, "pre")
+    for what, a, b_ in zip(("dx", "dw", "db"), got, O.linear_backward(d64(dy), d64(x), d64(w), d64(pre), "gelu", 0.1, 1, 0, dt)):
+        O.near(a, b_, what)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("pad,skip", [(1, 0), (8, 0), (0, 1), (5, 3), (24, 8)])
 @pytest.mark.parametrize("size", [(2, 9, 56, 40), (1, 150, 264, 136), (1, 256, 128, 256)], ids=str)
 def test_strides_and_alignment(ops, size, pad, skip, dtype):
