@@ -18,35 +18,41 @@ typedef float f8 __attribute__((ext_vector_type(8)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
-// V values from memory that is aligned to the type only (ALIGNED: to all V of them), as floats, and back:
-// one rounding, to nearest even.
+// V values in memory, in one wide access whatever their alignment beyond the type's own.
 template <typename T, int V>
-struct Vec {
-    typedef T type __attribute__((ext_vector_type(V)));
-};
-template <typename T>
-struct Vec<T, 1> {
-    typedef T type;
+struct Wide {
+    typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T))));
 };
 template <typename T, int V>
-__device__ __forceinline__ void load(const T *p, float (&v)[V]) {
-    if constexpr (V == 1) {
-        v[0] = (float)p[0];
-    } else {
-        const auto raw = *(const typename Vec<T, V>::type *)p;
+using wide = typename Wide<T, V>::type;
+
+// The first count (may be below 0, or V and more) of V values; the rest are 0.
+template <typename T, int V>
+__device__ __forceinline__ wide<T, V> load_raw(const T *p, int count) {
+    if (count >= V) return *(const wide<T, V> *)p;
+    wide<T, V> v;
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (float)raw[i];
-    }
+    for (int i = 0; i < V; ++i) v[i] = i < count ? p[i] : (T)0.0f;
+    return v;
 }
 template <typename T, int V>
-__device__ __forceinline__ void store(T *p, const float (&v)[V]) {
-    if constexpr (V == 1) {
-        p[0] = (T)v[0];
-    } else {
-        typename Vec<T, V>::type raw;
+__device__ __forceinline__ void load_some(const T *p, int count, float (&v)[V]) {
+    const wide<T, V> raw = load_raw<T, V>(p, count);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (float)raw[i];
+}
+// One rounding, to nearest even.
+template <typename T, int V>
+__device__ __forceinline__ void store_some(T *p, int count, const float (&v)[V]) {
+    if (count >= V) {
+        wide<T, V> raw;
 #pragma unroll
         for (int i = 0; i < V; ++i) raw[i] = (T)v[i];
-        *(typename Vec<T, V>::type *)p = raw;
+        *(wide<T, V> *)p = raw;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < count) p[i] = (T)v[i];
     }
 }
 
@@ -92,6 +98,36 @@ __device__ __forceinline__ float act_slope(float z) {
     return 1.0f;
 }
 
+template <int ACT, int V>
+__device__ __forceinline__ void act_each(float (&v)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = act_value<ACT>(v[i]);
+}
+template <int V>
+__device__ __forceinline__ void act_each(int act, float (&v)[V]) {
+    switch (act) {
+    case AET_ACT_RELU: act_each<AET_ACT_RELU>(v); break;
+    case AET_ACT_SILU: act_each<AET_ACT_SILU>(v); break;
+    case AET_ACT_GELU: act_each<AET_ACT_GELU>(v); break;
+    default: break;
+    }
+}
+// v times the slope at z
+template <int ACT, int V>
+__device__ __forceinline__ void slope_each(const float (&z)[V], float (&v)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] *= act_slope<ACT>(z[i]);
+}
+template <int V>
+__device__ __forceinline__ void slope_each(int act, const float (&z)[V], float (&v)[V]) {
+    switch (act) {
+    case AET_ACT_RELU: slope_each<AET_ACT_RELU>(z, v); break;
+    case AET_ACT_SILU: slope_each<AET_ACT_SILU>(z, v); break;
+    case AET_ACT_GELU: slope_each<AET_ACT_GELU>(z, v); break;
+    default: break;
+    }
+}
+
 // The dropout of a call: rows of `half` counters.
 struct Drop {
     uint64_t key;      // of the stream
@@ -105,19 +141,14 @@ __device__ __forceinline__ uint64_t drop_row(const Drop &d, int64_t row) { retur
 __device__ __forceinline__ uint64_t drop_hash(const Drop &d, uint64_t q, int j) {
     return aet::splitmix_at(d.key, q + (uint32_t)j);
 }
-// v[i]: columns col .. col + V - 1
+// v[i]: columns col .. col + V - 1, col even
 template <int V>
 __device__ __forceinline__ void drop_apply(const Drop &d, uint64_t q, int col, float (&v)[V]) {
-    if constexpr (V == 1) {
-        const uint64_t h = drop_hash(d, q, col >> 1);
-        v[0] = (uint32_t)(col & 1 ? h >> 32 : h) >= d.least ? v[0] * d.scale : 0.0f;
-    } else {   // col is even
 #pragma unroll
-        for (int i = 0; i < V; i += 2) {
-            const uint64_t h = drop_hash(d, q, (col + i) >> 1);
-            v[i] = (uint32_t)h >= d.least ? v[i] * d.scale : 0.0f;
-            v[i + 1] = (uint32_t)(h >> 32) >= d.least ? v[i + 1] * d.scale : 0.0f;
-        }
+    for (int i = 0; i < V; i += 2) {
+        const uint64_t h = drop_hash(d, q, (col + i) >> 1);
+        v[i] = (uint32_t)h >= d.least ? v[i] * d.scale : 0.0f;
+        v[i + 1] = (uint32_t)(h >> 32) >= d.least ? v[i + 1] * d.scale : 0.0f;
     }
 }
 

@@ -1,151 +1,610 @@
 // Group normalisation with an activation, channels last, and its gradient.
+//
+// Bound by memory.  A thread has V neighbouring channels (16 bytes) of several positions, whatever groups they belong to;
+// sums are kept by channel and come together by group in the end, so that memory is read in whole lines also where
+// a group has few channels.  Where a sample's groups fit the registers of a workgroup, one kernel reads every value once
+// (k_norm_whole, k_norm_back_whole): mean first, then the squares of the differences from it.  Larger samples take
+// three: sums of strips of positions, their union by group, and a second pass over the values.
 #include "ops_internal.h"
 
 namespace aet_ops {
 
-__device__ __forceinline__ float block_sum(float v, float *lds) {   // 256 threads
+constexpr int kThreads = 512;
+
+// How a sample is dealt out.  A workgroup has `span` channels (the last of a sample: what is left), in `pieces` of V.
+struct NormShape {
+    int channels, span, spans, span_groups;
+    int pieces, lanes;      // threads side by side; positions at a time
+    int threads;            // pieces * lanes, in whole waves
+    int strips, strip;      // positions' parts (three kernels only)
+    float *sums;            // whole: [sample][2][channels]; else [sample][strips][2][channels]
+    float *stats;           // [sample][2][groups], three kernels only: mean and rstd, or s1 and s2 (both by number)
+};
+
+struct Where {
+    int64_t sample, client, in_batch;
+    int ch0, chans, piece, lane, ch, count;   // ch, count: the thread's first channel, and how many it has
+    int group[8];                             // of its channels
+};
+template <int V>
+__device__ __forceinline__ Where where(const NormShape &s, int batch, int width, int64_t block) {
+    Where w;
+    w.sample = block / s.spans;
+    w.ch0 = (int)(block % s.spans) * s.span;
+    w.chans = s.channels - w.ch0 < s.span ? s.channels - w.ch0 : s.span;
+    w.client = w.sample / batch;
+    w.in_batch = w.sample - w.client * batch;
+    w.lane = threadIdx.x / s.pieces;
+    w.piece = threadIdx.x - w.lane * s.pieces;
+    w.ch = w.ch0 + w.piece * V;
+    w.count = w.lane < s.lanes ? w.chans - w.piece * V : 0;
+    if (w.count > V) w.count = V;
+    int g = w.ch / width, k = w.ch - g * width;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        w.group[e] = g;
+        if (++k == width) {
+            k = 0;
+            ++g;
+        }
+    }
+    return w;
+}
+
+// Sums by channel over the workgroup's threads: tot[k], k < chans.  lds: threads * V floats.
+template <int V>
+__device__ __forceinline__ void channel_sums(const NormShape &s, const Where &w, const float (&v)[V], float *lds, float *tot) {
+    const int line = s.pieces * V;
+    __syncthreads();
+    if (w.lane < s.lanes) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) lds[w.lane * line + w.piece * V + e] = v[e];
+    }
+    __syncthreads();
+    // up to 16 threads a channel, then one
+    int parts = blockDim.x / line;
+    parts = parts > 16 ? 16 : parts < 1 ? 1 : parts;
+    if (parts > s.lanes) parts = s.lanes;
+    const int part = threadIdx.x / line;
+    if (parts > 1) {
+        float sum = 0;
+        if (part < parts)
+            for (int l = part; l < s.lanes; l += parts) sum += lds[l * line + threadIdx.x - part * line];
+        __syncthreads();
+        if (part < parts) lds[threadIdx.x] = sum;
+        __syncthreads();
+    } else {
+        parts = s.lanes;
+    }
+    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
+        float sum = 0;
+        for (int l = 0; l < parts; ++l) sum += lds[l * line + k];
+        tot[k] = sum;
+    }
+    __syncthreads();
+}
+// Sums of a group's channels, a wave per group: out[g] = scale * sum of tot[k] (* by[k])
+__device__ __forceinline__ void group_sums(const float *tot, const float *by, int groups, int width, float scale, float *out) {
+    const int waves = blockDim.x / 64, lane = threadIdx.x % 64;
+    for (int g = threadIdx.x / 64; g < groups; g += waves) {
+        float sum = 0;
+        for (int k = lane; k < width; k += 64) sum += by ? tot[g * width + k] * by[g * width + k] : tot[g * width + k];
+        sum = aet::wave_sum(sum);
+        if (lane == 0) out[g] = sum * scale;
+    }
+    __syncthreads();
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void params(const aet_in &p, int64_t client, int ch, int count, float none, float (&v)[V]) {
+    if (p.p && count > 0) {
+        load_some((const T *)p.p + client * p.client + ch, count, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = none;
+    }
+}
+// from[group of the thread's channel - first]
+template <int V>
+__device__ __forceinline__ void by_channel(const Where &w, int first, const float *from, float (&v)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = e < w.count ? from[w.group[e] - first] : 0.0f;
+}
+
+// ---- a sample's groups in registers ------------------------------------------------------
+
+template <typename T, int V, int N>
+__global__ __launch_bounds__(kThreads) void k_norm_whole(aet_group_norm a, NormShape s) {
+    extern __shared__ float lds[];   // threads * V, then by channel, then by group
+    float *const tot = lds + s.threads * V, *const stat = tot + s.span;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x);
+    const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
+    T *y = (T *)a.y.p + w.client * a.y.client + w.in_batch * a.y.sample + w.ch;
+    wide<T, V> raw[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int pos = w.lane + i * s.lanes;
+        raw[i] = load_raw<T, V>(x + pos * a.x.row, pos < a.positions ? w.count : 0);
+    }
+    float acc[V] = {};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += (float)raw[i][e];
+    const int groups = w.chans / a.width, g0 = w.ch0 / a.width;
+    const float inv = 1.0f / ((float)a.positions * (float)a.width);
+    channel_sums(s, w, acc, lds, tot);
+    group_sums(tot, nullptr, groups, a.width, inv, stat);
+    float mean[V], scale[V], beta[V];
+    by_channel(w, g0, stat, mean);
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[e] = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (w.lane + i * s.lanes < a.positions) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = (float)raw[i][e] - mean[e];
+                acc[e] += d * d;
+            }
+        }
+    channel_sums(s, w, acc, lds, tot);
+    if (a.mean)
+        for (int g = threadIdx.x; g < groups; g += blockDim.x) a.mean[w.sample * a.groups + g0 + g] = stat[g];
+    __syncthreads();
+    group_sums(tot, nullptr, groups, a.width, inv, stat);
+    for (int g = threadIdx.x; g < groups; g += blockDim.x) {
+        stat[g] = 1.0f / __builtin_sqrtf(stat[g] + a.eps);
+        if (a.rstd) a.rstd[w.sample * a.groups + g0 + g] = stat[g];
+    }
+    __syncthreads();
+    by_channel(w, g0, stat, scale);
+    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, acc);
+    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+#pragma unroll
+    for (int e = 0; e < V; ++e) scale[e] *= acc[e];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int pos = w.lane + i * s.lanes;
+        if (pos >= a.positions || w.count <= 0) continue;
+        float v[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = __builtin_fmaf((float)raw[i][e] - mean[e], scale[e], beta[e]);
+        act_each(a.act, v);
+        store_some(y + pos * a.y.row, w.count, v);
+    }
+}
+
+// d = dy * act'(t) at one position, and x^
+template <typename T, int V>
+__device__ __forceinline__ void slopes(int act, const wide<T, V> &x, const wide<T, V> &dy, const float (&mean)[V], const float (&rstd)[V],
+                                       const float (&gamma)[V], const float (&beta)[V], float (&d)[V], float (&xh)[V]) {
+    float t[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        xh[e] = ((float)x[e] - mean[e]) * rstd[e];
+        t[e] = __builtin_fmaf(xh[e], gamma[e], beta[e]);
+        d[e] = (float)dy[e];
+    }
+    slope_each(act, t, d);
+}
+
+template <typename T, int V, int N>
+__global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_grad a, NormShape s) {
+    extern __shared__ float lds[];
+    float *const totA = lds + s.threads * V, *const totB = totA + s.span, *const gam = totB + s.span, *const stat = gam + s.span;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x);
+    const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
+    const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
+    wide<T, V> rx[N], rd[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int pos = w.lane + i * s.lanes, count = pos < a.positions ? w.count : 0;
+        rx[i] = load_raw<T, V>(x + pos * a.x.row, count);
+        rd[i] = load_raw<T, V>(dy + pos * a.dy.row, count);
+    }
+    const int groups = w.chans / a.width, g0 = w.ch0 / a.width;
+    float mean[V], rstd[V], gamma[V], beta[V];
+    by_channel(w, 0, a.mean + w.sample * a.groups, mean);
+    by_channel(w, 0, a.rstd + w.sample * a.groups, rstd);
+    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
+    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+    float A[V] = {}, B[V] = {};
+    float d[N][V];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float xh[V];
+        slopes<T, V>(a.act, rx[i], rd[i], mean, rstd, gamma, beta, d[i], xh);   // dy is 0 where there is no position
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            A[e] += d[i][e];
+            B[e] += d[i][e] * xh[e];
+        }
+    }
+    channel_sums(s, w, A, lds, totA);
+    channel_sums(s, w, B, lds, totB);
+    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
+        float *to = s.sums + w.sample * 2 * s.channels + w.ch0 + k;
+        to[0] = totA[k];
+        to[s.channels] = totB[k];
+        gam[k] = a.gamma.p ? (float)((const T *)a.gamma.p)[w.client * a.gamma.client + w.ch0 + k] : 1.0f;
+    }
+    __syncthreads();
+    if (!a.dx.p) return;
+    const float inv = 1.0f / ((float)a.positions * (float)a.width);
+    group_sums(totA, gam, groups, a.width, inv, stat);
+    group_sums(totB, gam, groups, a.width, inv, stat + groups);
+    T *dx = (T *)a.dx.p + w.client * a.dx.client + w.in_batch * a.dx.sample + w.ch;
+    by_channel(w, g0, stat, A);
+    by_channel(w, g0, stat + groups, B);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int pos = w.lane + i * s.lanes;
+        if (pos >= a.positions || w.count <= 0) continue;
+        float v[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = (d[i][e] * gamma[e] - A[e] - ((float)rx[i][e] - mean[e]) * rstd[e] * B[e]) * rstd[e];
+        store_some(dx + pos * a.dx.row, w.count, v);
+    }
+}
+
+// ---- larger samples ----------------------------------------------------------------------
+
+// Of a strip's values of a channel: their mean, and the sum of squares of the differences from it.
+template <typename T, int V>
+__global__ __launch_bounds__(kThreads) void k_norm_strips(aet_group_norm a, NormShape s) {
+    extern __shared__ float lds[];
+    float *const tot = lds + s.threads * V;
+    const int strip = blockIdx.x % s.strips;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.strips);
+    const int first = strip * s.strip, end = first + s.strip < a.positions ? first + s.strip : a.positions;
+    const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
+    // about the strip's first value, so that the squares do not cancel where the mean is far from 0
+    const wide<T, V> about = load_raw<T, V>(x + first * a.x.row, w.count);
+    float S[V] = {}, Q[V] = {};
+    if (w.count > 0) {
+#pragma unroll 4
+        for (int pos = first + w.lane; pos < end; pos += s.lanes) {
+            const wide<T, V> v = load_raw<T, V>(x + pos * a.x.row, w.count);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = (float)v[e] - (float)about[e];
+                S[e] += d;
+                Q[e] += d * d;
+            }
+        }
+    }
+    float *to = s.sums + (w.sample * s.strips + strip) * 2 * s.channels + w.ch0;
+    const float inv = 1.0f / (float)(end - first);
+    channel_sums(s, w, S, lds, tot);
+    const T *about0 = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + first * a.x.row + w.ch0;
+    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
+        const float off = tot[k];
+        to[k] = (float)about0[k] + off * inv;
+        to[s.channels + k] = off * off * inv;
+    }
+    channel_sums(s, w, Q, lds, tot);
+    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
+        const float m2 = tot[k] - to[s.channels + k];
+        to[s.channels + k] = m2 < 0 ? 0.0f : m2;
+    }
+}
+
+// The union of a group's strips and channels (Chan, Golub and LeVeque 1983): one workgroup per sample and group.
+__device__ __forceinline__ float block_sum(float v, float *lds) {
     v = aet::wave_sum(v);
     __syncthreads();
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
     __syncthreads();
     return lds[0] + lds[1] + lds[2] + lds[3];
 }
-
-// One workgroup per sample and group.
-template <typename T, int ACT>
-__global__ __launch_bounds__(256) void k_norm(aet_group_norm a) {
+__global__ __launch_bounds__(256) void k_norm_union(aet_group_norm a, NormShape s) {
     __shared__ float lds[4];
     const int64_t sample = blockIdx.x / a.groups;
-    const int g = blockIdx.x % a.groups;
-    const int64_t c = sample / a.batch, b = sample % a.batch;
-    const T *x = (const T *)a.x.p + c * a.x.client + b * a.x.sample + g * a.width;
-    T *y = (T *)a.y.p + c * a.y.client + b * a.y.sample + g * a.width;
-    const int64_t count = (int64_t)a.positions * a.width;
-    float s = 0;
-    for (int64_t i = threadIdx.x; i < count; i += 256) s += (float)x[i / a.width * a.x.row + i % a.width];
-    const float mean = count ? block_sum(s, lds) / (float)count : 0.0f;
-    s = 0;
-    for (int64_t i = threadIdx.x; i < count; i += 256) {
-        const float d = (float)x[i / a.width * a.x.row + i % a.width] - mean;
-        s += d * d;
+    const int ch = (int)(blockIdx.x % a.groups) * a.width;
+    const float *from = s.sums + sample * s.strips * 2 * s.channels + ch;
+    const int64_t entries = (int64_t)s.strips * a.width;
+    const float inv = 1.0f / ((float)a.positions * (float)a.width);
+    const float first = from[0];
+    float sum = 0;
+    for (int64_t i = threadIdx.x; i < entries; i += 256) {
+        const int strip = (int)(i / a.width), k = (int)(i % a.width), left = a.positions - strip * s.strip;
+        sum += (float)(left < s.strip ? left : s.strip) * (from[(int64_t)strip * 2 * s.channels + k] - first);
     }
-    const float rstd = 1.0f / __builtin_sqrtf((count ? block_sum(s, lds) / (float)count : 0.0f) + a.eps);
-    if (threadIdx.x == 0) {
-        if (a.mean) a.mean[blockIdx.x] = mean;
-        if (a.rstd) a.rstd[blockIdx.x] = rstd;
+    const float mean = first + block_sum(sum, lds) * inv;
+    sum = 0;
+    for (int64_t i = threadIdx.x; i < entries; i += 256) {
+        const int strip = (int)(i / a.width), k = (int)(i % a.width), left = a.positions - strip * s.strip;
+        const float *at = from + (int64_t)strip * 2 * s.channels + k;
+        const float d = at[0] - mean;
+        sum += at[s.channels] + (float)(left < s.strip ? left : s.strip) * d * d;
     }
-    for (int64_t i = threadIdx.x; i < count; i += 256) {
-        const int k = (int)(i % a.width), ch = g * a.width + k;
-        const float gamma = a.gamma.p ? (float)((const T *)a.gamma.p)[c * a.gamma.client + ch] : 1.0f;
-        const float beta = a.beta.p ? (float)((const T *)a.beta.p)[c * a.beta.client + ch] : 0.0f;
-        const float t = ((float)x[i / a.width * a.x.row + k] - mean) * rstd * gamma + beta;
-        y[i / a.width * a.y.row + k] = (T)act_value<ACT>(t);
+    const float rstd = 1.0f / __builtin_sqrtf(block_sum(sum, lds) * inv + a.eps);
+    if (threadIdx.x) return;
+    const int64_t at = sample * 2 * a.groups + ch / a.width;
+    s.stats[at] = mean;
+    s.stats[at + a.groups] = rstd;
+    if (a.mean) a.mean[blockIdx.x] = mean;
+    if (a.rstd) a.rstd[blockIdx.x] = rstd;
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(kThreads) void k_norm_apply(aet_group_norm a, NormShape s) {
+    const int strip = blockIdx.x % s.strips;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.strips);
+    if (w.count <= 0) return;
+    const int first = strip * s.strip, end = first + s.strip < a.positions ? first + s.strip : a.positions;
+    const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
+    T *y = (T *)a.y.p + w.client * a.y.client + w.in_batch * a.y.sample + w.ch;
+    float mean[V], scale[V], gamma[V], beta[V];
+    const float *stat = s.stats + w.sample * 2 * a.groups;
+    by_channel(w, 0, stat, mean);
+    by_channel(w, 0, stat + a.groups, scale);
+    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
+    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+#pragma unroll
+    for (int e = 0; e < V; ++e) scale[e] *= gamma[e];
+#pragma unroll 4
+    for (int pos = first + w.lane; pos < end; pos += s.lanes) {
+        const wide<T, V> raw = load_raw<T, V>(x + pos * a.x.row, w.count);
+        float v[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = __builtin_fmaf((float)raw[e] - mean[e], scale[e], beta[e]);
+        act_each(a.act, v);
+        store_some(y + pos * a.y.row, w.count, v);
     }
 }
 
-// One workgroup per sample and group; sums: A and B of each sample and channel.
-template <typename T, int ACT>
-__global__ __launch_bounds__(256) void k_norm_back(aet_group_norm_grad a, float *sums) {
+template <typename T, int V>
+__global__ __launch_bounds__(kThreads) void k_norm_back_strips(aet_group_norm_grad a, NormShape s) {
+    extern __shared__ float lds[];
+    float *const tot = lds + s.threads * V;
+    const int strip = blockIdx.x % s.strips;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.strips);
+    const int first = strip * s.strip, end = first + s.strip < a.positions ? first + s.strip : a.positions;
+    const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
+    const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
+    float mean[V], rstd[V], gamma[V], beta[V], A[V] = {}, B[V] = {};
+    by_channel(w, 0, a.mean + w.sample * a.groups, mean);
+    by_channel(w, 0, a.rstd + w.sample * a.groups, rstd);
+    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
+    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+    if (w.count > 0) {
+#pragma unroll 4
+        for (int pos = first + w.lane; pos < end; pos += s.lanes) {
+            float d[V], xh[V];
+            slopes<T, V>(a.act, load_raw<T, V>(x + pos * a.x.row, w.count), load_raw<T, V>(dy + pos * a.dy.row, w.count), mean, rstd, gamma, beta, d, xh);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                A[e] += d[e];
+                B[e] += d[e] * xh[e];
+            }
+        }
+    }
+    float *to = s.sums + (w.sample * s.strips + strip) * 2 * s.channels + w.ch0;
+    channel_sums(s, w, A, lds, tot);
+    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) to[k] = tot[k];
+    channel_sums(s, w, B, lds, tot);
+    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) to[s.channels + k] = tot[k];
+}
+
+// The strips' sums by channel go to the first strip's place; s1 and s2, divided by their number, to the group's.
+template <typename T>
+__global__ __launch_bounds__(256) void k_norm_back_union(aet_group_norm_grad a, NormShape s) {
     __shared__ float lds[4];
-    const int64_t sample = blockIdx.x / a.groups;
-    const int g = blockIdx.x % a.groups;
-    const int64_t c = sample / a.batch, b = sample % a.batch;
-    const int64_t C = (int64_t)a.groups * a.width;
-    const T *x = (const T *)a.x.p + c * a.x.client + b * a.x.sample + g * a.width;
-    const T *dy = (const T *)a.dy.p + c * a.dy.client + b * a.dy.sample + g * a.width;
-    const float mean = a.mean[blockIdx.x], rstd = a.rstd[blockIdx.x];
+    const int64_t sample = blockIdx.x / a.groups, client = sample / a.batch;
+    const int ch = (int)(blockIdx.x % a.groups) * a.width;
+    float *from = s.sums + sample * s.strips * 2 * s.channels + ch;
+    const float inv = 1.0f / ((float)a.positions * (float)a.width);
     float s1 = 0, s2 = 0;
-    for (int k = 0; k < a.width; ++k) {
-        const int ch = g * a.width + k;
-        const float gamma = a.gamma.p ? (float)((const T *)a.gamma.p)[c * a.gamma.client + ch] : 1.0f;
-        const float beta = a.beta.p ? (float)((const T *)a.beta.p)[c * a.beta.client + ch] : 0.0f;
+    for (int k = threadIdx.x; k < a.width; k += 256) {
         float A = 0, B = 0;
-        for (int i = threadIdx.x; i < a.positions; i += 256) {
-            const float xh = ((float)x[i * a.x.row + k] - mean) * rstd;
-            const float d = (float)dy[i * a.dy.row + k] * act_slope<ACT>(xh * gamma + beta);
-            A += d;
-            B += d * xh;
+#pragma unroll 8
+        for (int i = 0; i < s.strips; ++i) {
+            A += from[(int64_t)i * 2 * s.channels + k];
+            B += from[((int64_t)i * 2 + 1) * s.channels + k];
         }
-        A = block_sum(A, lds);
-        B = block_sum(B, lds);
-        s1 += gamma * A;
-        s2 += gamma * B;
-        if (threadIdx.x == 0) {
-            sums[(sample * 2 + 0) * C + ch] = A;
-            sums[(sample * 2 + 1) * C + ch] = B;
-        }
+        from[k] = A;
+        from[s.channels + k] = B;
+        const float gamma = a.gamma.p ? (float)((const T *)a.gamma.p)[client * a.gamma.client + ch + k] : 1.0f;
+        s1 += A * gamma;
+        s2 += B * gamma;
     }
-    if (!a.dx.p) return;
-    T *dx = (T *)a.dx.p + c * a.dx.client + b * a.dx.sample + g * a.width;
-    const int64_t count = (int64_t)a.positions * a.width;
-    s1 /= (float)count;
-    s2 /= (float)count;
-    for (int64_t i = threadIdx.x; i < count; i += 256) {
-        const int k = (int)(i % a.width), ch = g * a.width + k;
-        const int64_t pos = i / a.width;
-        const float gamma = a.gamma.p ? (float)((const T *)a.gamma.p)[c * a.gamma.client + ch] : 1.0f;
-        const float beta = a.beta.p ? (float)((const T *)a.beta.p)[c * a.beta.client + ch] : 0.0f;
-        const float xh = ((float)x[pos * a.x.row + k] - mean) * rstd;
-        const float d = (float)dy[pos * a.dy.row + k] * act_slope<ACT>(xh * gamma + beta) * gamma;
-        dx[pos * a.dx.row + k] = (T)((d - s1 - xh * s2) * rstd);
+    s1 = block_sum(s1, lds) * inv;
+    s2 = block_sum(s2, lds) * inv;
+    if (threadIdx.x) return;
+    const int64_t at = sample * 2 * a.groups + ch / a.width;
+    s.stats[at] = s1;
+    s.stats[at + a.groups] = s2;
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(kThreads) void k_norm_back_apply(aet_group_norm_grad a, NormShape s) {
+    const int strip = blockIdx.x % s.strips;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.strips);
+    if (w.count <= 0) return;
+    const int first = strip * s.strip, end = first + s.strip < a.positions ? first + s.strip : a.positions;
+    const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
+    const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
+    T *dx = (T *)a.dx.p + w.client * a.dx.client + w.in_batch * a.dx.sample + w.ch;
+    float mean[V], rstd[V], gamma[V], beta[V], s1[V], s2[V];
+    by_channel(w, 0, a.mean + w.sample * a.groups, mean);
+    by_channel(w, 0, a.rstd + w.sample * a.groups, rstd);
+    by_channel(w, 0, s.stats + w.sample * 2 * a.groups, s1);
+    by_channel(w, 0, s.stats + (w.sample * 2 + 1) * a.groups, s2);
+    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
+    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+#pragma unroll 4
+    for (int pos = first + w.lane; pos < end; pos += s.lanes) {
+        float d[V], xh[V];
+        slopes<T, V>(a.act, load_raw<T, V>(x + pos * a.x.row, w.count), load_raw<T, V>(dy + pos * a.dy.row, w.count), mean, rstd, gamma, beta, d, xh);
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] = (d[e] * gamma[e] - s1[e] - xh[e] * s2[e]) * rstd[e];
+        store_some(dx + pos * a.dx.row, w.count, d);
     }
 }
 
-// One thread per client and channel.
+// dgamma and dbeta: samples' sums, 64 channels a workgroup, four samples at a time.  apart: between samples, in floats.
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm_params(aet_group_norm_grad a, const float *sums, int clients, int64_t samples) {
-    const int64_t C = (int64_t)a.groups * a.width, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= clients * C) return;
-    const int64_t c = i / C, ch = i % C;
+__global__ __launch_bounds__(256) void k_norm_params(aet_group_norm_grad a, const float *sums, int64_t apart, int channels, int across, int64_t samples) {
+    __shared__ float lds[2][4][64];
+    const int64_t client = blockIdx.x / across;
+    const int k = threadIdx.x % 64, part = threadIdx.x / 64, ch = blockIdx.x % across * 64 + k;
     float A = 0, B = 0;
-    for (int64_t k = c * samples; k < (c + 1) * samples; ++k) {
-        A += sums[(k * 2 + 0) * C + ch];
-        B += sums[(k * 2 + 1) * C + ch];
+    if (ch < channels) {
+#pragma unroll 8
+        for (int64_t i = client * samples + part; i < (client + 1) * samples; i += 4) {
+            A += sums[i * apart + ch];
+            B += sums[i * apart + channels + ch];
+        }
     }
-    if (a.dbeta.p) ((T *)a.dbeta.p)[c * a.dbeta.client + ch] = (T)A;
-    if (a.dgamma.p) ((T *)a.dgamma.p)[c * a.dgamma.client + ch] = (T)B;
+    lds[0][part][k] = A;
+    lds[1][part][k] = B;
+    __syncthreads();
+    if (part || ch >= channels) return;
+    if (a.dbeta.p) ((T *)a.dbeta.p)[client * a.dbeta.client + ch] = (T)(lds[0][0][k] + lds[0][1][k] + lds[0][2][k] + lds[0][3][k]);
+    if (a.dgamma.p) ((T *)a.dgamma.p)[client * a.dgamma.client + ch] = (T)(lds[1][0][k] + lds[1][1][k] + lds[1][2][k] + lds[1][3][k]);
 }
 
-size_t group_norm_forward_workspace(const aet_group_norm &) { return 0; }
-size_t group_norm_backward_workspace(const aet_group_norm_grad &a) {
-    return a.positions ? (size_t)a.n * a.batch * 2 * a.groups * a.width * sizeof(float) : 0;
+// No positions: the statistics of nothing.
+__global__ __launch_bounds__(256) void k_norm_nothing(float *mean, float *rstd, float eps, int64_t count) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= count) return;
+    if (mean) mean[i] = 0.0f;
+    if (rstd) rstd[i] = 1.0f / __builtin_sqrtf(eps);
 }
+
+// ---- the choice --------------------------------------------------------------------------
+
+static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+struct NormPlan {
+    bool whole;
+    int n;             // positions a thread has (whole)
+    NormShape s;
+    size_t lds, sums_bytes, bytes;
+};
+
+static void deal(NormShape &s, int V, int span) {
+    s.span = span;
+    s.spans = (int)ceil_div(s.channels, span);
+    s.pieces = (int)ceil_div(span, V);
+}
+
+static NormPlan make_plan(int64_t samples, int positions, int groups, int width, int V, bool back) {
+    NormPlan p = {};
+    NormShape &s = p.s;
+    s.channels = groups * width;
+    // Whole groups: as many as fit the registers, of those as give 512 workgroups, but 64 bytes of neighbouring channels
+    // unless that leaves fewer than 128.
+    const int most = back ? 8 : 16;
+    const int64_t lanes = ceil_div(positions, most), fit_pieces = lanes > kThreads ? 0 : kThreads / lanes;
+    int64_t fit = (fit_pieces < 256 ? fit_pieces : 256) * V / width;
+    if (fit > groups) fit = groups;
+    if (fit > 0) {
+        const auto at_least_1 = [](int64_t v) { return v < 1 ? 1 : v; };
+        int64_t best = at_least_1(samples * groups / 512);
+        if (best < ceil_div(4 * V, width)) best = ceil_div(4 * V, width);
+        if (best > at_least_1(samples * groups / 128)) best = at_least_1(samples * groups / 128);
+        if (best > fit) best = fit;
+        s.span_groups = (int)ceil_div(groups, ceil_div(groups, best));
+    }
+    const int best = s.span_groups;
+    p.whole = best && (best == groups || best * width >= 2 * V || samples * positions * s.channels < (1 << 22));
+    if (p.whole) {
+        deal(s, V, best * width);
+        s.lanes = kThreads / s.pieces;
+        if (s.lanes > positions) s.lanes = positions;
+        p.n = (int)ceil_div(positions, s.lanes);
+        s.threads = (int)ceil_div(s.pieces * s.lanes, 64) * 64;
+        s.strips = 1;
+        s.strip = positions;
+        p.lds = sizeof(float) * ((size_t)s.threads * V + (back ? 3 : 1) * s.span + 2 * best);
+        p.sums_bytes = back ? up256((size_t)samples * 2 * s.channels * sizeof(float)) : 0;
+        p.bytes = p.sums_bytes;
+        return p;
+    }
+    deal(s, V, s.channels < 256 * V ? s.channels : 256 * V);
+    s.lanes = kThreads / s.pieces;
+    // strips of 8 positions a thread or more, as many as give every compute unit several workgroups
+    const int64_t wanted = ceil_div(4096, samples * s.spans), most_strips = ceil_div(positions, (int64_t)s.lanes * 8);
+    s.strip = (int)ceil_div(ceil_div(positions, wanted < most_strips ? wanted : most_strips), s.lanes) * s.lanes;
+    s.strips = (int)ceil_div(positions, s.strip);
+    s.threads = (int)ceil_div(s.pieces * s.lanes, 64) * 64;
+    p.lds = sizeof(float) * ((size_t)s.threads * V + s.span);
+    p.sums_bytes = up256((size_t)samples * s.strips * 2 * s.channels * sizeof(float));
+    p.bytes = p.sums_bytes + up256((size_t)samples * 2 * groups * sizeof(float));
+    return p;
+}
+static int vec(int dtype) { return dtype == AET_F32 ? 4 : 8; }
+static NormPlan plan(const aet_group_norm &a) {
+    return make_plan((int64_t)a.n * a.batch, a.positions, a.groups, a.width, vec(a.dtype), false);
+}
+static NormPlan plan(const aet_group_norm_grad &a) {
+    return make_plan((int64_t)a.n * a.batch, a.positions, a.groups, a.width, vec(a.dtype), true);
+}
+
+size_t group_norm_forward_workspace(const aet_group_norm &a) { return a.n && a.batch && a.positions ? plan(a).bytes : 0; }
+size_t group_norm_backward_workspace(const aet_group_norm_grad &a) { return a.n && a.batch && a.positions ? plan(a).bytes : 0; }
 
 template <typename T>
-static void norm(const aet_group_norm &a, hipStream_t s, int blocks) {
-    switch (a.act) {
-    case AET_ACT_RELU: k_norm<T, AET_ACT_RELU><<<blocks, 256, 0, s>>>(a); break;
-    case AET_ACT_SILU: k_norm<T, AET_ACT_SILU><<<blocks, 256, 0, s>>>(a); break;
-    case AET_ACT_GELU: k_norm<T, AET_ACT_GELU><<<blocks, 256, 0, s>>>(a); break;
-    default: k_norm<T, AET_ACT_NONE><<<blocks, 256, 0, s>>>(a);
+static hipError_t forward(const aet_group_norm &a, char *workspace, hipStream_t s) {
+    constexpr int V = 16 / sizeof(T);
+    const int64_t samples = (int64_t)a.n * a.batch;
+    if (!a.positions) {
+        if (a.mean || a.rstd) k_norm_nothing<<<(int)ceil_div(samples * a.groups, 256), 256, 0, s>>>(a.mean, a.rstd, a.eps, samples * a.groups);
+        return hipGetLastError();
     }
-}
-hipError_t launch_group_norm_forward(const aet_group_norm &a, void *, hipStream_t s) {
-    const int64_t blocks = (int64_t)a.n * a.batch * a.groups;
-    if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
-    a.dtype == AET_F32 ? norm<float>(a, s, (int)blocks) : norm<bf16>(a, s, (int)blocks);
+    NormPlan p = plan(a);
+    p.s.sums = (float *)workspace;
+    p.s.stats = (float *)(workspace + p.sums_bytes);
+    const int64_t blocks = samples * p.s.spans * p.s.strips;
+    if (blocks > INT32_MAX || samples * a.groups > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (p.whole) {
+        if (p.n <= 4) k_norm_whole<T, V, 4><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+        else if (p.n <= 8) k_norm_whole<T, V, 8><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+        else k_norm_whole<T, V, 16><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+    } else {
+        k_norm_strips<T, V><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+        k_norm_union<<<(int)(samples * a.groups), 256, 0, s>>>(a, p.s);
+        k_norm_apply<T, V><<<(int)blocks, p.s.threads, 0, s>>>(a, p.s);
+    }
     return hipGetLastError();
 }
+hipError_t launch_group_norm_forward(const aet_group_norm &a, void *workspace, hipStream_t s) {
+    return a.dtype == AET_F32 ? forward<float>(a, (char *)workspace, s) : forward<bf16>(a, (char *)workspace, s);
+}
 
 template <typename T>
-static void norm_back(const aet_group_norm_grad &a, float *sums, hipStream_t s, int blocks) {
-    if (blocks) switch (a.act) {
-    case AET_ACT_RELU: k_norm_back<T, AET_ACT_RELU><<<blocks, 256, 0, s>>>(a, sums); break;
-    case AET_ACT_SILU: k_norm_back<T, AET_ACT_SILU><<<blocks, 256, 0, s>>>(a, sums); break;
-    case AET_ACT_GELU: k_norm_back<T, AET_ACT_GELU><<<blocks, 256, 0, s>>>(a, sums); break;
-    default: k_norm_back<T, AET_ACT_NONE><<<blocks, 256, 0, s>>>(a, sums);
+static hipError_t backward(const aet_group_norm_grad &a, char *workspace, hipStream_t s) {
+    constexpr int V = 16 / sizeof(T);
+    const int64_t samples = a.positions ? (int64_t)a.n * a.batch : 0, channels = (int64_t)a.groups * a.width;
+    NormPlan p = {};
+    if (samples) {
+        p = plan(a);
+        p.s.sums = (float *)workspace;
+        p.s.stats = (float *)(workspace + p.sums_bytes);
+        const int64_t blocks = samples * p.s.spans * p.s.strips;
+        if (blocks > INT32_MAX || samples * a.groups > INT32_MAX) return hipErrorInvalidConfiguration;
+        if (p.whole) {
+            if (p.n <= 4) k_norm_back_whole<T, V, 4><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+            else k_norm_back_whole<T, V, 8><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+        } else {
+            k_norm_back_strips<T, V><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+            k_norm_back_union<T><<<(int)(samples * a.groups), 256, 0, s>>>(a, p.s);
+            if (a.dx.p) k_norm_back_apply<T, V><<<(int)blocks, p.s.threads, 0, s>>>(a, p.s);
+        }
     }
-    if (!a.dgamma.p && !a.dbeta.p) return;
-    const bool shared = (a.dgamma.p && !a.dgamma.client) || (a.dbeta.p && !a.dbeta.client);
-    const int clients = shared ? 1 : a.n;
-    const int64_t samples = blocks ? (int64_t)a.batch * (shared ? a.n : 1) : 0;
-    k_norm_params<T><<<(int)ceil_div((int64_t)clients * a.groups * a.width, 256), 256, 0, s>>>(a, sums, clients, samples);
+    if (a.dgamma.p || a.dbeta.p) {
+        const bool shared = (a.dgamma.p && !a.dgamma.client) || (a.dbeta.p && !a.dbeta.client);
+        const int clients = shared ? 1 : a.n, across = (int)ceil_div(channels, 64);
+        if ((int64_t)clients * across > INT32_MAX) return hipErrorInvalidConfiguration;
+        k_norm_params<T><<<clients * across, 256, 0, s>>>(a, p.s.sums, (int64_t)p.s.strips * 2 * channels, (int)channels, across, samples / clients);
+    }
+    return hipGetLastError();
 }
 hipError_t launch_group_norm_backward(const aet_group_norm_grad &a, void *workspace, hipStream_t s) {
-    const int64_t blocks = a.positions ? (int64_t)a.n * a.batch * a.groups : 0;
-    if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
-    a.dtype == AET_F32 ? norm_back<float>(a, (float *)workspace, s, (int)blocks) : norm_back<bf16>(a, (float *)workspace, s, (int)blocks);
-    return hipGetLastError();
+    return a.dtype == AET_F32 ? backward<float>(a, (char *)workspace, s) : backward<bf16>(a, (char *)workspace, s);
 }
 
 }  // namespace aet_ops

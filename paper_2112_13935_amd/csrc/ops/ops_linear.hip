@@ -22,42 +22,85 @@ hipError_t launch_linear_forward(const aet_linear &a, void *workspace, hipStream
     return launch_product(a.dtype, forward_product(a), workspace, s);
 }
 
-// dz, and db: a thread per column.
+// dz = dropout'(dy) * act'(z), and its sums over rows.  A workgroup has 32 pieces of 8 columns of a strip of a client's
+// rows, eight rows at a time; the sums of several strips go to `partial` and are added by k_db, in their order.
+struct DzShape {
+    int across, strips, strip;   // workgroups: side by side, one below the other; rows of a strip
+    int64_t dz_row;
+    float *partial;              // [strip][client][out]
+};
+
 template <typename T>
-__global__ __launch_bounds__(256) void k_dz(aet_linear_grad a, Drop d, T *dz, int64_t dz_row) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (int64_t)a.n * a.out) return;
-    const int64_t c = i / a.out;
-    const int col = (int)(i - c * a.out);
-    float sum = 0;
-    for (int r = 0; r < a.rows; ++r) {
-        float v[1] = {(float)((const T *)a.dy.p)[c * a.dy.client + r * a.dy.row + col]};
-        if (d.least) drop_apply(d, drop_row(d, c * a.rows + r), col, v);
-        if (a.act) {
-            const float z = (float)((const T *)a.pre.p)[c * a.pre.client + r * a.pre.row + col];
-            v[0] *= a.act == AET_ACT_RELU ? act_slope<AET_ACT_RELU>(z) : a.act == AET_ACT_SILU ? act_slope<AET_ACT_SILU>(z) : act_slope<AET_ACT_GELU>(z);
+__global__ __launch_bounds__(256) void k_dz(aet_linear_grad a, Drop d, DzShape s, T *dz) {
+    __shared__ float lds[8][256];
+    const int per = s.across * s.strips;
+    const int64_t client = blockIdx.x / per;
+    const int b = blockIdx.x % per, strip = b / s.across, tx = threadIdx.x % 32, ty = threadIdx.x / 32;
+    const int col = (b % s.across * 32 + tx) * 8, count = a.out - col;
+    const int64_t first = (int64_t)strip * s.strip, end = first + s.strip < a.rows ? first + s.strip : a.rows;
+    const T *dy = (const T *)a.dy.p + client * a.dy.client + col;
+    const T *pre = a.act ? (const T *)a.pre.p + client * a.pre.client + col : nullptr;
+    float sum[8] = {};
+    if (count > 0) {
+#pragma unroll 4
+        for (int64_t r = first + ty; r < end; r += 8) {
+            float v[8];
+            load_some(dy + r * a.dy.row, count, v);
+            if (d.least) drop_apply(d, drop_row(d, client * a.rows + r), col, v);
+            if (pre) {
+                float z[8];
+                load_some(pre + r * a.pre.row, count, z);
+                slope_each(a.act, z, v);
+            }
+            if (dz) store_some(dz + (client * a.rows + r) * s.dz_row + col, count, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += v[i];
         }
-        sum += v[0];
-        if (dz) dz[(c * a.rows + r) * dz_row + col] = (T)v[0];
     }
-    if (a.db.p) ((T *)a.db.p)[c * a.db.client + col] = (T)sum;
+    if (!a.db.p) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) lds[ty][tx * 8 + i] = sum[i];
+    __syncthreads();
+    const int mine = b % s.across * 256 + threadIdx.x;
+    if (mine >= a.out) return;
+    float total = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) total += lds[i][threadIdx.x];
+    if (s.strips == 1) ((T *)a.db.p)[client * a.db.client + mine] = (T)total;
+    else s.partial[((int64_t)strip * a.n + client) * a.out + mine] = total;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_db(aet_linear_grad a, DzShape s) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)a.n * a.out;
+    if (i >= all) return;
+    float total = 0;
+#pragma unroll 8
+    for (int k = 0; k < s.strips; ++k) total += s.partial[k * all + i];
+    ((T *)a.db.p)[i / a.out * a.db.client + i % a.out] = (T)total;
 }
 
 // dz has a place of its own unless it is dy.
 struct BackwardPlan {
-    bool own_dz;
-    int64_t dz_row;
+    DzShape dz;
     Product dx, dw;
-    size_t dz_bytes, bytes;
+    size_t dz_bytes, db_bytes, bytes;
 };
 static BackwardPlan plan(const aet_linear_grad &a, char *workspace) {
     BackwardPlan b = {};
-    b.own_dz = a.p > 0 || a.act != AET_ACT_NONE;
+    const bool own = (a.p > 0 || a.act != AET_ACT_NONE) && (a.dx.p || a.dw.p);
     const int e = a.dtype == AET_F32 ? 4 : 2;
-    b.dz_row = ceil_div((int64_t)a.out * e, 16) * 16 / e;
-    b.dz_bytes = b.own_dz && (a.dx.p || a.dw.p) ? up256((size_t)a.n * a.rows * b.dz_row * e) : 0;
+    b.dz.dz_row = ceil_div((int64_t)a.out * e, 16) * 16 / e;
+    b.dz.across = (int)ceil_div(a.out, 256);
+    // strips of at least 64 rows, as many as give every compute unit several workgroups
+    const int64_t wanted = ceil_div(2048, (int64_t)a.n * b.dz.across + 1), most = ceil_div(a.rows, 64);
+    b.dz.strip = (int)ceil_div(ceil_div(a.rows, wanted < most ? wanted : most > 0 ? most : 1), 8) * 8;
+    b.dz.strips = a.rows ? (int)ceil_div(a.rows, b.dz.strip) : 1;
+    b.dz_bytes = own ? up256((size_t)a.n * a.rows * b.dz.dz_row * e) : 0;
+    b.db_bytes = a.db.p && b.dz.strips > 1 ? up256((size_t)b.dz.strips * a.n * a.out * sizeof(float)) : 0;
+    b.dz.partial = (float *)(workspace + b.dz_bytes);
     Operand dz = {a.dy.p, a.dy.client, a.dy.row, false};
-    if (b.own_dz) dz = {workspace, a.rows * b.dz_row, b.dz_row, false};
+    if (own) dz = {workspace, a.rows * b.dz.dz_row, b.dz.dz_row, false};
     const Drop none = {};
     if (a.dx.p) {
         b.dx.a = dz;
@@ -79,7 +122,7 @@ static BackwardPlan plan(const aet_linear_grad &a, char *workspace) {
         b.dw.e = {{}, {}, a.dw, {}, a.out, AET_ACT_NONE, none};
     }
     const size_t x = product_workspace(a.dtype, b.dx), w = product_workspace(a.dtype, b.dw);
-    b.bytes = b.dz_bytes + (x > w ? x : w);
+    b.bytes = b.dz_bytes + b.db_bytes + (x > w ? x : w);
     return b;
 }
 
@@ -88,12 +131,17 @@ size_t linear_backward_workspace(const aet_linear_grad &a) { return plan(a, null
 template <typename T>
 static hipError_t backward(const aet_linear_grad &a, char *workspace, hipStream_t s) {
     const BackwardPlan b = plan(a, workspace);
-    const int64_t columns = (int64_t)a.n * a.out;
-    if (columns && (b.dz_bytes || a.db.p))
-        k_dz<T><<<(int)ceil_div(columns, 256), 256, 0, s>>>(a, make_drop(a.p, a.seed, a.first_row, a.out), b.dz_bytes ? (T *)workspace : nullptr, b.dz_row);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && a.dx.p) e = launch_product(a.dtype, b.dx, workspace + b.dz_bytes, s);
-    if (e == hipSuccess && a.dw.p) e = launch_product(a.dtype, b.dw, workspace + b.dz_bytes, s);
+    char *const more = workspace + b.dz_bytes + b.db_bytes;
+    hipError_t e = hipSuccess;
+    if (a.out && (b.dz_bytes || a.db.p)) {
+        const int64_t blocks = (int64_t)a.n * b.dz.across * b.dz.strips;
+        if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+        k_dz<T><<<(int)blocks, 256, 0, s>>>(a, make_drop(a.p, a.seed, a.first_row, a.out), b.dz, b.dz_bytes ? (T *)workspace : nullptr);
+        if (a.db.p && b.dz.strips > 1) k_db<T><<<(int)ceil_div((int64_t)a.n * a.out, 256), 256, 0, s>>>(a, b.dz);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && a.dx.p) e = launch_product(a.dtype, b.dx, more, s);
+    if (e == hipSuccess && a.dw.p) e = launch_product(a.dtype, b.dw, more, s);
     return e;
 }
 hipError_t launch_linear_backward(const aet_linear_grad &a, void *workspace, hipStream_t s) {

@@ -70,7 +70,7 @@ struct RegStage {
     static constexpr int kCount = S::kPieces / THREADS;
     static_assert(S::kPieces % THREADS == 0 && THREADS % S::kWidth == 0, "whole pieces a thread");
     static constexpr int kStep = THREADS / S::kWidth;   // rows between a thread's pieces
-    float raw[kCount][8];
+    wide<T, 8> raw[kCount];
     const T *p;          // the thread's first piece of the next stage
     int64_t row;
     int r, c, left;      // left: by rows, k until the end of the sum; by columns, likewise
@@ -90,13 +90,7 @@ struct RegStage {
             const int ri = r + i * kStep;
             const bool in = ri < (COLS ? left : rows);
             const int count = in ? (COLS ? rows : left) - 8 * c : 0;
-            const T *at = p + (int64_t)(i * kStep) * row;
-            if (count >= 8) {
-                load8(at, raw[i]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) raw[i][e] = e < count ? (float)at[e] : 0.0f;
-            }
+            raw[i] = load_raw<T, 8>(p + (int64_t)(i * kStep) * row, count);
         }
         p += COLS ? BK * row : BK;
         left -= BK;
@@ -107,15 +101,15 @@ struct RegStage {
         for (int i = 0; i < kCount; ++i) {
             const lds_ptr at = to + S::slot(r + i * kStep, c) * 16;
             if constexpr (sizeof(T) == 2) {
-                bf8 v;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = (bf16)raw[i][e];
-                *(__attribute__((address_space(3))) bf8 *)at = v;
+                *(__attribute__((address_space(3))) bf8 *)at = raw[i];
             } else {
-                aet::Split8 s = aet::split8<false>(raw[i]);
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = raw[i][e];
+                aet::Split8 s = aet::split8<false>(v);
                 uint32_t seen = 0;
                 aet::split_watch(seen, s);
-                if (aet::split_over(seen)) s = aet::split8<true>(raw[i]);   // something infinite, NaN or next to it
+                if (aet::split_over(seen)) s = aet::split8<true>(v);   // something infinite, NaN or next to it
 #pragma unroll
                 for (int q = 0; q < 3; ++q) *(__attribute__((address_space(3))) bf8 *)(at + q * S::kBytes) = s.p[q];
             }
