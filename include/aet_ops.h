@@ -25,7 +25,7 @@
  *     (AET_EHIP) what was enqueued is not to be used.  aet_ops_last_error() describes the
  *     problem of the calling thread's last failed call.  Nothing aborts or throws across the
  *     boundary.  Calls are thread safe.
- *   - Sizes of 0 are legal: sums over nothing are 0.
+ *   - Sizes of 0 are legal: sums over nothing are 0.  The largest is 2^30.
  *   - The same call gives the same bits every time.
  */
 #ifndef AET_OPS_H

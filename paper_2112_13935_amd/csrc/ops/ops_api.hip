@@ -3,6 +3,8 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <initializer_list>
+
 #include "ops_internal.h"
 
 namespace aet_ops {
@@ -62,6 +64,15 @@ static const char *bad_out(const void *p, int dtype, int nd, const int64_t *coun
     return nullptr;
 }
 
+constexpr int kMostSize = 1 << 30;
+static bool bad_sizes(std::initializer_list<int64_t> sizes, const char **why) {
+    for (int64_t v : sizes)
+        if (v < 0 || v > kMostSize) {
+            *why = "a size is negative or over 2^30";
+            return true;
+        }
+    return false;
+}
 static bool bad_common(int dtype, int act, const char **why) {
     if (dtype != AET_F32 && dtype != AET_BF16) *why = "dtype is neither AET_F32 nor AET_BF16";
     else if (act < AET_ACT_NONE || act > AET_ACT_GELU) *why = "act is none of the AET_ACT_ values";
@@ -89,7 +100,7 @@ static aet_status check(const aet_linear *a) {
     const char *why;
     if (!a) return fail(AET_EINVAL, "the record is NULL");
     if (bad_common(a->dtype, a->act, &why)) return fail(AET_EINVAL, "%s", why);
-    if (a->n < 0 || a->rows < 0 || a->in < 0 || a->out < 0) return fail(AET_EINVAL, "a size is negative");
+    if (bad_sizes({a->n, a->rows, a->in, a->out}, &why)) return fail(AET_EINVAL, "%s", why);
     if (bad_drop(a->p, a->first_row, (int64_t)a->n * a->rows, &why)) return fail(AET_EINVAL, "%s", why);
     if (!a->n || !a->rows || !a->out) return AET_OK;
     const int64_t nr[2] = {a->n, a->rows}, no[2] = {a->n, a->out};
@@ -113,7 +124,7 @@ static aet_status check(const aet_linear *a) {
 static void fold(aet_linear &a) {
     if (a.n <= 1) return;
     auto flat = [&](const void *p, int64_t client, int64_t row) { return !p || client == a.rows * row; };
-    if (a.w.client || (a.bias.p && a.bias.client) || (int64_t)a.n * a.rows > INT32_MAX) return;
+    if (a.w.client || (a.bias.p && a.bias.client) || (int64_t)a.n * a.rows > kMostSize) return;
     if (!flat(a.x.p, a.x.client, a.x.row) || !flat(a.residual.p, a.residual.client, a.residual.row) ||
         !flat(a.y.p, a.y.client, a.y.row) || !flat(a.pre.p, a.pre.client, a.pre.row))
         return;
@@ -125,7 +136,7 @@ static aet_status check(const aet_linear_grad *a, bool *shared) {
     const char *why;
     if (!a) return fail(AET_EINVAL, "the record is NULL");
     if (bad_common(a->dtype, a->act, &why)) return fail(AET_EINVAL, "%s", why);
-    if (a->n < 0 || a->rows < 0 || a->in < 0 || a->out < 0) return fail(AET_EINVAL, "a size is negative");
+    if (bad_sizes({a->n, a->rows, a->in, a->out}, &why)) return fail(AET_EINVAL, "%s", why);
     if (bad_drop(a->p, a->first_row, (int64_t)a->n * a->rows, &why)) return fail(AET_EINVAL, "%s", why);
     *shared = a->n > 1 && ((a->dw.p && !a->dw.client) || (a->db.p && !a->db.client));
     const int64_t n = *shared ? 1 : a->n;   // gradients of parameters
@@ -152,7 +163,7 @@ static aet_status check(const aet_linear_grad *a, bool *shared) {
         if (!flat(a->dy.p, a->dy.client, a->dy.row) || !flat(a->x.p, a->x.client, a->x.row) ||
             !flat(a->pre.p, a->pre.client, a->pre.row) || !flat(a->dx.p, a->dx.client, a->dx.row))
             return fail(AET_EINVAL, "one W for all clients: rows have to lie client after client (client = rows * row)");
-        if ((int64_t)a->n * a->rows > INT32_MAX) return fail(AET_EINVAL, "one W for all clients: more than 2^31 - 1 rows");
+        if ((int64_t)a->n * a->rows > kMostSize) return fail(AET_EINVAL, "one W for all clients: more than 2^30 rows");
     }
     return AET_OK;
 }
@@ -169,7 +180,7 @@ template <class A>
 static aet_status check_norm(const A *a) {
     const char *why;
     if (bad_common(a->dtype, a->act, &why)) return fail(AET_EINVAL, "%s", why);
-    if (a->n < 0 || a->batch < 0 || a->positions < 0) return fail(AET_EINVAL, "a size is negative");
+    if (bad_sizes({a->n, a->batch, a->positions}, &why)) return fail(AET_EINVAL, "%s", why);
     if (a->groups < 1 || a->width < 1 || (int64_t)a->groups * a->width > (1 << 24))
         return fail(AET_EINVAL, "groups and width have to be positive, with at most 2^24 channels");
     const int64_t one[1] = {a->n};
@@ -222,7 +233,7 @@ static aet_status run_dropout(const aet_dropout *a, bool residual, void *hip_str
     const char *why;
     if (!a) return fail(AET_EINVAL, "the record is NULL");
     if (bad_common(a->dtype, AET_ACT_NONE, &why)) return fail(AET_EINVAL, "%s", why);
-    if (a->n < 0 || a->rows < 0 || a->cols < 0) return fail(AET_EINVAL, "a size is negative");
+    if (bad_sizes({a->n, a->rows, a->cols}, &why)) return fail(AET_EINVAL, "%s", why);
     if (bad_drop(a->p, a->first_row, (int64_t)a->n * a->rows, &why)) return fail(AET_EINVAL, "%s", why);
     if (!residual && a->residual.p) return fail(AET_EINVAL, "the gradient takes no residual");
     if (!a->n || !a->rows || !a->cols) return AET_OK;
@@ -233,7 +244,7 @@ static aet_status run_dropout(const aet_dropout *a, bool residual, void *hip_str
     AET_CHECK("y", bad_out(a->y.p, a->dtype, 2, nr, ys, a->cols));
     aet_dropout b = *a;
     auto flat = [&](const void *p, int64_t client, int64_t row) { return !p || client == b.rows * row; };
-    if (b.n > 1 && (int64_t)b.n * b.rows <= INT32_MAX && flat(b.x.p, b.x.client, b.x.row) && flat(b.y.p, b.y.client, b.y.row) &&
+    if (b.n > 1 && (int64_t)b.n * b.rows <= kMostSize && flat(b.x.p, b.x.client, b.x.row) && flat(b.y.p, b.y.client, b.y.row) &&
         flat(b.residual.p, b.residual.client, b.residual.row)) {
         b.rows *= b.n;
         b.n = 1;

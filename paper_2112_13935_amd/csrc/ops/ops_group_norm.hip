@@ -16,7 +16,8 @@ struct NormShape {
     int channels, span, spans, span_groups;
     int pieces, lanes;      // threads side by side; positions at a time
     int threads;            // pieces * lanes, in whole waves
-    int strips, strip;      // positions' parts (three kernels only)
+    int strips, strip;      // positions' parts: for the sums (three kernels only)
+    int parts, part;        // and for the second pass
     float *sums;            // whole: [sample][2][channels]; else [sample][strips][2][channels]
     float *stats;           // [sample][2][groups], three kernels only: mean and rstd, or s1 and s2 (both by number)
 };
@@ -39,10 +40,12 @@ __device__ __forceinline__ Where where(const NormShape &s, int batch, int width,
     w.ch = w.ch0 + w.piece * V;
     w.count = w.lane < s.lanes ? w.chans - w.piece * V : 0;
     if (w.count > V) w.count = V;
+    // (channels that are not there have the group of one that is, so that nothing has to be tested to read what it has)
     int g = w.ch / width, k = w.ch - g * width;
+    const int last = (w.ch0 + w.chans - 1) / width;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        w.group[e] = g;
+        w.group[e] = g < last ? g : last;
         if (++k == width) {
             k = 0;
             ++g;
@@ -108,7 +111,7 @@ __device__ __forceinline__ void params(const aet_in &p, int64_t client, int ch, 
 template <int V>
 __device__ __forceinline__ void by_channel(const Where &w, int first, const float *from, float (&v)[V]) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = e < w.count ? from[w.group[e] - first] : 0.0f;
+    for (int e = 0; e < V; ++e) v[e] = from[w.group[e] - first];
 }
 
 // ---- a sample's groups in registers ------------------------------------------------------
@@ -250,6 +253,23 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_gra
 
 // ---- larger samples ----------------------------------------------------------------------
 
+// load(position, slot, count) and then use(position, slot, count) for a thread's positions, four of them at a time: their
+// loads are on their way together.  With whole pieces the count is a constant there.
+template <class L, class U>
+__device__ __forceinline__ void each_position(int pos, int end, int step, int count, int V, L load, U use) {
+    const auto some = [&](int have) {
+        for (; pos < end; pos += 4 * step) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load(pos + i * step < end ? pos + i * step : end - 1, i, have);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (pos + i * step < end) use(pos + i * step, i, have);
+        }
+    };
+    if (count >= V) some(V);
+    else if (count > 0) some(count);
+}
+
 // Of a strip's values of a channel: their mean, and the sum of squares of the differences from it.
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void k_norm_strips(aet_group_norm a, NormShape s) {
@@ -257,23 +277,21 @@ __global__ __launch_bounds__(kThreads) void k_norm_strips(aet_group_norm a, Norm
     float *const tot = lds + s.threads * V;
     const int strip = blockIdx.x % s.strips;
     const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.strips);
-    const int first = strip * s.strip, end = first + s.strip < a.positions ? first + s.strip : a.positions;
+    const int first = strip * s.strip, end = a.positions - first < s.strip ? a.positions : first + s.strip;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     // about the strip's first value, so that the squares do not cancel where the mean is far from 0
     const wide<T, V> about = load_raw<T, V>(x + first * a.x.row, w.count);
     float S[V] = {}, Q[V] = {};
-    if (w.count > 0) {
-#pragma unroll 4
-        for (int pos = first + w.lane; pos < end; pos += s.lanes) {
-            const wide<T, V> v = load_raw<T, V>(x + pos * a.x.row, w.count);
+    wide<T, V> raw[4];
+    each_position(first + w.lane, end, s.lanes, w.count, V, [&](int pos, int i, int count) { raw[i] = load_raw<T, V>(x + pos * a.x.row, count); },
+                  [&](int, int i, int) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float d = (float)v[e] - (float)about[e];
-                S[e] += d;
-                Q[e] += d * d;
-            }
+        for (int e = 0; e < V; ++e) {
+            const float d = (float)raw[i][e] - (float)about[e];
+            S[e] += d;
+            Q[e] += d * d;
         }
-    }
+    });
     float *to = s.sums + (w.sample * s.strips + strip) * 2 * s.channels + w.ch0;
     const float inv = 1.0f / (float)(end - first);
     channel_sums(s, w, S, lds, tot);
@@ -330,10 +348,10 @@ __global__ __launch_bounds__(256) void k_norm_union(aet_group_norm a, NormShape 
 
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void k_norm_apply(aet_group_norm a, NormShape s) {
-    const int strip = blockIdx.x % s.strips;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.strips);
+    const int part = blockIdx.x % s.parts;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.parts);
     if (w.count <= 0) return;
-    const int first = strip * s.strip, end = first + s.strip < a.positions ? first + s.strip : a.positions;
+    const int first = part * s.part, end = a.positions - first < s.part ? a.positions : first + s.part;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     T *y = (T *)a.y.p + w.client * a.y.client + w.in_batch * a.y.sample + w.ch;
     float mean[V], scale[V], gamma[V], beta[V];
@@ -344,15 +362,15 @@ __global__ __launch_bounds__(kThreads) void k_norm_apply(aet_group_norm a, NormS
     params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
 #pragma unroll
     for (int e = 0; e < V; ++e) scale[e] *= gamma[e];
-#pragma unroll 4
-    for (int pos = first + w.lane; pos < end; pos += s.lanes) {
-        const wide<T, V> raw = load_raw<T, V>(x + pos * a.x.row, w.count);
+    wide<T, V> raw[4];
+    each_position(first + w.lane, end, s.lanes, w.count, V, [&](int pos, int i, int count) { raw[i] = load_raw<T, V>(x + pos * a.x.row, count); },
+                  [&](int pos, int i, int count) {
         float v[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = __builtin_fmaf((float)raw[e] - mean[e], scale[e], beta[e]);
+        for (int e = 0; e < V; ++e) v[e] = __builtin_fmaf((float)raw[i][e] - mean[e], scale[e], beta[e]);
         act_each(a.act, v);
-        store_some(y + pos * a.y.row, w.count, v);
-    }
+        store_some(y + pos * a.y.row, count, v);
+    });
 }
 
 template <typename T, int V>
@@ -361,7 +379,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_strips(aet_group_norm_gr
     float *const tot = lds + s.threads * V;
     const int strip = blockIdx.x % s.strips;
     const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.strips);
-    const int first = strip * s.strip, end = first + s.strip < a.positions ? first + s.strip : a.positions;
+    const int first = strip * s.strip, end = a.positions - first < s.strip ? a.positions : first + s.strip;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
     float mean[V], rstd[V], gamma[V], beta[V], A[V] = {}, B[V] = {};
@@ -369,18 +387,20 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_strips(aet_group_norm_gr
     by_channel(w, 0, a.rstd + w.sample * a.groups, rstd);
     params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
     params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
-    if (w.count > 0) {
-#pragma unroll 4
-        for (int pos = first + w.lane; pos < end; pos += s.lanes) {
-            float d[V], xh[V];
-            slopes<T, V>(a.act, load_raw<T, V>(x + pos * a.x.row, w.count), load_raw<T, V>(dy + pos * a.dy.row, w.count), mean, rstd, gamma, beta, d, xh);
+    wide<T, V> rx[4], rd[4];
+    const auto load = [&](int pos, int i, int count) {
+        rx[i] = load_raw<T, V>(x + pos * a.x.row, count);
+        rd[i] = load_raw<T, V>(dy + pos * a.dy.row, count);
+    };
+    each_position(first + w.lane, end, s.lanes, w.count, V, load, [&](int pos, int i, int count) {
+        float d[V], xh[V];
+        slopes<T, V>(a.act, rx[i], rd[i], mean, rstd, gamma, beta, d, xh);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                A[e] += d[e];
-                B[e] += d[e] * xh[e];
-            }
+        for (int e = 0; e < V; ++e) {
+            A[e] += d[e];
+            B[e] += d[e] * xh[e];
         }
-    }
+    });
     float *to = s.sums + (w.sample * s.strips + strip) * 2 * s.channels + w.ch0;
     channel_sums(s, w, A, lds, tot);
     for (int k = threadIdx.x; k < w.chans; k += blockDim.x) to[k] = tot[k];
@@ -420,10 +440,10 @@ __global__ __launch_bounds__(256) void k_norm_back_union(aet_group_norm_grad a, 
 
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void k_norm_back_apply(aet_group_norm_grad a, NormShape s) {
-    const int strip = blockIdx.x % s.strips;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.strips);
+    const int part = blockIdx.x % s.parts;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.parts);
     if (w.count <= 0) return;
-    const int first = strip * s.strip, end = first + s.strip < a.positions ? first + s.strip : a.positions;
+    const int first = part * s.part, end = a.positions - first < s.part ? a.positions : first + s.part;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
     T *dx = (T *)a.dx.p + w.client * a.dx.client + w.in_batch * a.dx.sample + w.ch;
@@ -434,14 +454,18 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_apply(aet_group_norm_gra
     by_channel(w, 0, s.stats + (w.sample * 2 + 1) * a.groups, s2);
     params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
     params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
-#pragma unroll 4
-    for (int pos = first + w.lane; pos < end; pos += s.lanes) {
+    wide<T, V> rx[4], rd[4];
+    const auto load = [&](int pos, int i, int count) {
+        rx[i] = load_raw<T, V>(x + pos * a.x.row, count);
+        rd[i] = load_raw<T, V>(dy + pos * a.dy.row, count);
+    };
+    each_position(first + w.lane, end, s.lanes, w.count, V, load, [&](int pos, int i, int count) {
         float d[V], xh[V];
-        slopes<T, V>(a.act, load_raw<T, V>(x + pos * a.x.row, w.count), load_raw<T, V>(dy + pos * a.dy.row, w.count), mean, rstd, gamma, beta, d, xh);
+        slopes<T, V>(a.act, rx[i], rd[i], mean, rstd, gamma, beta, d, xh);
 #pragma unroll
         for (int e = 0; e < V; ++e) d[e] = (d[e] * gamma[e] - s1[e] - xh[e] * s2[e]) * rstd[e];
-        store_some(dx + pos * a.dx.row, w.count, d);
-    }
+        store_some(dx + pos * a.dx.row, count, d);
+    });
 }
 
 // dgamma and dbeta: samples' sums, 64 channels a workgroup, four samples at a time.  apart: between samples, in floats.
@@ -526,10 +550,15 @@ static NormPlan make_plan(int64_t samples, int positions, int groups, int width,
     }
     deal(s, V, s.channels < 256 * V ? s.channels : 256 * V);
     s.lanes = kThreads / s.pieces;
-    // strips of 8 positions a thread or more, as many as give every compute unit several workgroups
-    const int64_t wanted = ceil_div(4096, samples * s.spans), most_strips = ceil_div(positions, (int64_t)s.lanes * 8);
+    // Sums: as many strips as give every compute unit four workgroups, of 8 positions a thread or more (a workgroup's
+    // own sums and their union cost as much as some 10 positions: gradient of 128 samples of 4096 x 320 in bf16, 1024 workgroups
+    // 170 us, 4096 220 us).  Second pass: short parts, 4 positions a thread (177 us; with 1024 workgroups 191 us).
+    const int64_t wanted = ceil_div(1024, samples * s.spans), most_strips = ceil_div(positions, (int64_t)s.lanes * 8);
     s.strip = (int)ceil_div(ceil_div(positions, wanted < most_strips ? wanted : most_strips), s.lanes) * s.lanes;
     s.strips = (int)ceil_div(positions, s.strip);
+    s.part = 4 * s.lanes;
+    while (s.part < positions && samples * s.spans * ceil_div(positions, s.part) > 8192) s.part *= 2;
+    s.parts = (int)ceil_div(positions, s.part);
     s.threads = (int)ceil_div(s.pieces * s.lanes, 64) * 64;
     p.lds = sizeof(float) * ((size_t)s.threads * V + s.span);
     p.sums_bytes = up256((size_t)samples * s.strips * 2 * s.channels * sizeof(float));
@@ -559,7 +588,7 @@ static hipError_t forward(const aet_group_norm &a, char *workspace, hipStream_t 
     p.s.sums = (float *)workspace;
     p.s.stats = (float *)(workspace + p.sums_bytes);
     const int64_t blocks = samples * p.s.spans * p.s.strips;
-    if (blocks > INT32_MAX || samples * a.groups > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (blocks > INT32_MAX || samples * p.s.spans * p.s.parts > INT32_MAX || samples * a.groups > INT32_MAX) return hipErrorInvalidConfiguration;
     if (p.whole) {
         if (p.n <= 4) k_norm_whole<T, V, 4><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
         else if (p.n <= 8) k_norm_whole<T, V, 8><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
@@ -567,7 +596,7 @@ static hipError_t forward(const aet_group_norm &a, char *workspace, hipStream_t 
     } else {
         k_norm_strips<T, V><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
         k_norm_union<<<(int)(samples * a.groups), 256, 0, s>>>(a, p.s);
-        k_norm_apply<T, V><<<(int)blocks, p.s.threads, 0, s>>>(a, p.s);
+        k_norm_apply<T, V><<<(int)(samples * p.s.spans * p.s.parts), p.s.threads, 0, s>>>(a, p.s);
     }
     return hipGetLastError();
 }
@@ -585,14 +614,14 @@ static hipError_t backward(const aet_group_norm_grad &a, char *workspace, hipStr
         p.s.sums = (float *)workspace;
         p.s.stats = (float *)(workspace + p.sums_bytes);
         const int64_t blocks = samples * p.s.spans * p.s.strips;
-        if (blocks > INT32_MAX || samples * a.groups > INT32_MAX) return hipErrorInvalidConfiguration;
+        if (blocks > INT32_MAX || samples * p.s.spans * p.s.parts > INT32_MAX || samples * a.groups > INT32_MAX) return hipErrorInvalidConfiguration;
         if (p.whole) {
             if (p.n <= 4) k_norm_back_whole<T, V, 4><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
             else k_norm_back_whole<T, V, 8><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
         } else {
             k_norm_back_strips<T, V><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
             k_norm_back_union<T><<<(int)(samples * a.groups), 256, 0, s>>>(a, p.s);
-            if (a.dx.p) k_norm_back_apply<T, V><<<(int)blocks, p.s.threads, 0, s>>>(a, p.s);
+            if (a.dx.p) k_norm_back_apply<T, V><<<(int)(samples * p.s.spans * p.s.parts), p.s.threads, 0, s>>>(a, p.s);
         }
     }
     if (a.dgamma.p || a.dbeta.p) {

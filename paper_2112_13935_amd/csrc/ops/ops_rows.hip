@@ -1,0 +1,119 @@
+// The linear layer for few rows a client (single requests, small mini-batches).
+//
+// Bound by reading W once.  A workgroup has 16 outputs of a client and all its rows, its waves parts of the sum; operands
+// go from memory straight into the lanes that want them (v_mfma_f32_16x16x32_bf16; v_mfma_f32_16x16x4_f32, whose four
+// k of a step are taken from places 4 apart so that a lane reads 16 bytes), several steps ahead of their use.  The waves'
+// sums meet in LDS.
+#include "ops_internal.h"
+#include "ops_tiles.h"
+
+namespace aet_ops {
+
+template <typename T>
+struct Step;
+template <>
+struct Step<bf16> {
+    static constexpr int kDepth = 32, kLane = 8;   // k of a step, and of a lane
+    static __device__ __forceinline__ f4 product(const wide<bf16, 8> &a, const wide<bf16, 8> &b, f4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16((bf8)a, (bf8)b, c, 0, 0, 0);
+    }
+};
+template <>
+struct Step<float> {
+    static constexpr int kDepth = 16, kLane = 4;
+    static __device__ __forceinline__ f4 product(const wide<float, 4> &a, const wide<float, 4> &b, f4 c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+};
+
+struct RowsShape {
+    int M, N, K;
+    int tiles_n;    // workgroups of a client
+};
+
+// G: groups of 16 rows.  AHEAD steps of a wave are on their way at a time.
+template <typename T, int G, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_rows(Operand ox, Operand ow, RowsShape s, Epilogue e) {
+    using S = Step<T>;
+    constexpr int AHEAD = G == 1 ? 8 : 4;
+    __shared__ float lds[WAVES][G * 16][20];
+    const int64_t client = blockIdx.x / s.tiles_n;
+    const int n0 = (int)(blockIdx.x % s.tiles_n) * 16;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int line = lane % 16, kl = lane / 16 * S::kLane;
+    // lines past the last are read from the last again, and not stored
+    const T *w = (const T *)ow.p + client * ow.client + (int64_t)(n0 + line < s.N ? n0 + line : s.N - 1) * ow.row + kl;
+    const T *x[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+        x[g] = (const T *)ox.p + client * ox.client + (int64_t)(16 * g + line < s.M ? 16 * g + line : s.M - 1) * ox.row + kl;
+    f4 acc[G] = {};
+    const int whole = s.K / S::kDepth;   // steps
+    // a wave's steps: AHEAD in a row, then those of the others
+    for (int i0 = wave * AHEAD; i0 < whole; i0 += WAVES * AHEAD) {
+        wide<T, S::kLane> a[AHEAD], b[AHEAD][G];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int64_t k = (int64_t)(i0 + i < whole ? i0 + i : whole - 1) * S::kDepth;
+            a[i] = *(const wide<T, S::kLane> *)(w + k);
+#pragma unroll
+            for (int g = 0; g < G; ++g) b[i][g] = *(const wide<T, S::kLane> *)(x[g] + k);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (i0 + i < whole)
+#pragma unroll
+                for (int g = 0; g < G; ++g) acc[g] = S::product(a[i], b[i][g], acc[g]);
+    }
+    const int rest = s.K - whole * S::kDepth;   // the sum's end, less than a step
+    if (rest && wave == WAVES - 1) {
+        const int64_t k = (int64_t)whole * S::kDepth;
+        const wide<T, S::kLane> a = load_raw<T, S::kLane>(w + k, rest - kl);
+#pragma unroll
+        for (int g = 0; g < G; ++g) acc[g] = S::product(a, load_raw<T, S::kLane>(x[g] + k, rest - kl), acc[g]);
+    }
+    // lane: row lane % 16, outputs 4 (lane / 16) ..
+#pragma unroll
+    for (int g = 0; g < G; ++g) *(f4 *)&lds[wave][16 * g + line][lane / 16 * 4] = acc[g];
+    __syncthreads();
+    const int row = threadIdx.x / 2, half = threadIdx.x % 2 * 8, count = s.N - n0 - half;
+    if (row >= G * 16 || row >= s.M || count <= 0) return;
+    float v[8];
+    bias8<T>(e, client, n0 + half, count, v);
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+        const f4 lo = *(const f4 *)&lds[i][row][half], hi = *(const f4 *)&lds[i][row][half + 4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            v[y] += lo[y];
+            v[4 + y] += hi[y];
+        }
+    }
+    finish8<T>(e, client, row, n0 + half, count, v);
+}
+
+bool rows_fit(const Product &p) { return !p.a.by_columns && !p.b.by_columns && p.M <= 32; }
+
+template <typename T>
+static hipError_t run(const Product &p, hipStream_t stream) {
+    const RowsShape s = {p.M, p.N, p.K, (int)ceil_div(p.N, 16)};
+    const int64_t blocks = (int64_t)p.clients * s.tiles_n;
+    if (!blocks || !p.M) return hipSuccess;
+    if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+    // waves: what the sum keeps busy
+    const bool deep = p.K >= 16 * 4 * Step<T>::kDepth;
+    if (p.M <= 16) {
+        if (deep) k_rows<T, 1, 16><<<(int)blocks, 1024, 0, stream>>>(p.a, p.b, s, p.e);
+        else k_rows<T, 1, 4><<<(int)blocks, 256, 0, stream>>>(p.a, p.b, s, p.e);
+    } else {
+        if (deep) k_rows<T, 2, 16><<<(int)blocks, 1024, 0, stream>>>(p.a, p.b, s, p.e);
+        else k_rows<T, 2, 4><<<(int)blocks, 256, 0, stream>>>(p.a, p.b, s, p.e);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_rows(int dtype, const Product &p, hipStream_t s) { return dtype == AET_F32 ? run<float>(p, s) : run<bf16>(p, s); }
+
+}  // namespace aet_ops

@@ -17,6 +17,10 @@ struct Product {
     Epilogue e;
 };
 
+// Few rows (ops_rows.hip): both operands by rows, no scratch.
+bool rows_fit(const Product &p);
+hipError_t launch_rows(int dtype, const Product &p, hipStream_t s);
+
 // Bytes of scratch that the product wants (for sums that are split along k).
 size_t product_workspace(int dtype, const Product &p);
 hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStream_t s);

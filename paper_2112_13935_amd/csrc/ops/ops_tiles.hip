@@ -175,7 +175,7 @@ struct Tile {
 };
 
 template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT>
-__global__ __launch_bounds__(64 * WR * WC) void k_tiles(Operand oa, Operand ob, Shape s, Epilogue e) {
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand ob, Shape s, Epilogue e) {
     using L = Tile<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>;
     constexpr int FM = L::FM, FN = L::FN, P = L::kParts;
     using SA = typename L::SA;
@@ -385,6 +385,7 @@ static Choice choose(int dtype, const Product &p) {
 }
 
 size_t product_workspace(int dtype, const Product &p) {
+    if (rows_fit(p)) return 0;
     const Choice c = choose(dtype, p);
     return c.slices > 1 ? (size_t)c.slices * p.clients * p.M * p.N * sizeof(float) : 0;
 }
@@ -417,6 +418,7 @@ static hipError_t run_product(const Product &p, void *workspace, hipStream_t str
 }
 
 hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStream_t s) {
+    if (rows_fit(p)) return launch_rows(dtype, p, s);
     const bool f32 = dtype == AET_F32;
     if (!p.a.by_columns && !p.b.by_columns) return f32 ? run_product<float, false, false>(p, workspace, s) : run_product<bf16, false, false>(p, workspace, s);
     if (!p.a.by_columns) return f32 ? run_product<float, false, true>(p, workspace, s) : run_product<bf16, false, true>(p, workspace, s);

@@ -12,7 +12,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional, Sequence, Tuple
+from typing import Optional, Tuple
 
 import torch
 
@@ -96,65 +96,98 @@ def load_library():
     return lib
 
 
-def _check(lib, rc: int):
-    if rc != AET_OK:
-        raise AetError(rc, lib.aet_ops_last_error().decode())
+class _Call:
+    """The type, device and stream of a call, by its first tensor; marshals the others, which have to agree with it."""
 
+    __slots__ = ("dtype", "index", "code", "handle", "stream")
 
-def _same(first: torch.Tensor, *others: Tuple[str, Optional[torch.Tensor], Sequence[int]]):
-    """The other tensors' type and device are the first one's, their shapes as they are said to be."""
-    if first.dtype not in _DTYPES or not first.is_cuda:
-        raise ValueError(f"float32 or bfloat16 on a GPU is wanted, got {first.dtype} on {first.device}")
-    for name, t, shape in others:
-        if t is None:
-            continue
-        if t.dtype != first.dtype or t.device != first.device:
-            raise ValueError(f"{name} is {t.dtype} on {t.device}, the others are {first.dtype} on {first.device}")
-        if tuple(t.shape) != tuple(shape):
+    def __init__(self, x: torch.Tensor, stream: Optional[torch.cuda.Stream]):
+        self.dtype, self.index = x.dtype, x.get_device()
+        self.code = _DTYPES.get(x.dtype, -1)
+        if self.code < 0 or self.index < 0:
+            raise ValueError(f"float32 or bfloat16 on a GPU is wanted, got {x.dtype} on {x.device}")
+        self.stream = stream
+        self.handle = torch._C._cuda_getCurrentRawStream(self.index)
+        if stream is not None:
+            if stream.cuda_stream == self.handle:
+                self.stream = None
+            self.handle = stream.cuda_stream
+
+    def _ptr(self, name: str, t: torch.Tensor, shape) -> int:
+        if t.dtype is not self.dtype or t.get_device() != self.index:
+            raise ValueError(f"{name} is {t.dtype} on {t.device}, the others are {self.dtype} on GPU {self.index}")
+        if t.shape != shape:
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if self.stream is not None:   # its memory is not given out again before that stream is done with it
+            t.record_stream(self.stream)
+        return t.data_ptr()
+
+    def mat(self, name: str, t: Optional[torch.Tensor], shape):
+        """Pointer and strides of a matrix per client, or of one (two axes)."""
+        if t is None:
+            return None, 0, 0
+        ptr, st = self._ptr(name, t, shape), t.stride()
+        if st[-1] != 1 and shape[-1] > 1:
+            raise ValueError(f"{name}: the last axis has stride {st[-1]}, 1 is wanted")
+        return (ptr, st[0], st[1]) if len(st) == 3 else (ptr, shape[0] * st[0], st[0])
+
+    def weights(self, name: str, t: Optional[torch.Tensor], shape):
+        """The same, of one for all clients where there are two axes."""
+        ptr, client, row = self.mat(name, t, shape)
+        return (ptr, client, row) if len(shape) == 3 else (ptr, 0, row)
+
+    def vec(self, name: str, t: Optional[torch.Tensor], n: int, cols: int):
+        """Pointer and strides of a vector per client, or of one for all."""
+        if t is None:
+            return None, 0, 0
+        per = t.dim() == 2
+        ptr, st = self._ptr(name, t, (n, cols) if per else (cols,)), t.stride()
+        if st[-1] != 1 and cols > 1:
+            raise ValueError(f"{name}: the last axis has stride {st[-1]}, 1 is wanted")
+        return ptr, st[0] if per else 0, 0
+
+    def maps(self, name: str, t: Optional[torch.Tensor], shape):
+        if t is None:
+            return None, 0, 0, 0
+        ptr, st = self._ptr(name, t, shape), t.stride()
+        if st[-1] != 1 and shape[-1] > 1:
+            raise ValueError(f"{name}: the last axis has stride {st[-1]}, 1 is wanted")
+        return (ptr, st[0], st[1], st[2]) if len(st) == 4 else (ptr, shape[0] * st[0], st[0], st[1])
+
+    def stats(self, name: str, t: torch.Tensor, shape) -> int:
+        if t.dtype is not torch.float32 or t.get_device() != self.index or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} has to be as the forward call gave it: float32, contiguous, {tuple(shape)}")
+        if self.stream is not None:
+            t.record_stream(self.stream)
+        return t.data_ptr()
+
+    def run(self, fn, record, workspace_bytes=None):
+        """fn(record, workspace, its size, stream) on the tensors' device; its workspace from workspace_bytes(record)."""
+        if torch.cuda.current_device() != self.index:
+            with torch.cuda.device(self.index):
+                return self.run(fn, record, workspace_bytes)
+        at = C.addressof(record)
+        if workspace_bytes is None:
+            rc = fn(at, self.handle)
+        elif size := workspace_bytes(at):
+            ws = torch.empty(size, dtype=torch.uint8, device=torch.device("cuda", self.index))
+            if self.stream is not None:
+                ws.record_stream(self.stream)
+            rc = fn(at, ws.data_ptr(), size, self.handle)
+        else:
+            rc = fn(at, None, 0, self.handle)
+        if rc != AET_OK:
+            raise AetError(rc, _LIB.aet_ops_last_error().decode())
 
 
-def _dense_last(name: str, t: torch.Tensor):
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name}: the last axis has stride {t.stride(-1)}, 1 is wanted")
-
-
-def _m(name: str, t: Optional[torch.Tensor], clients: bool):
-    """Pointer and strides of a matrix per client."""
-    if t is None:
-        return None, 0, 0
-    _dense_last(name, t)
-    st = t.stride()
-    return (t.data_ptr(), st[0], st[1]) if clients else (t.data_ptr(), t.shape[0] * st[0], st[0])
-
-
-def _v(name: str, t: Optional[torch.Tensor]):
-    """Pointer and strides of a vector per client, or of one for all."""
-    if t is None:
-        return None, 0, 0
-    _dense_last(name, t)
-    return t.data_ptr(), t.stride(0) if t.dim() == 2 else 0, 0
-
-
-class _On:
-    """The call's device and stream; keeps the tensors' memory while the stream uses it."""
-
-    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream], tensors):
-        self.current = torch.cuda.current_stream(device)
-        self.handle = (self.current if stream is None else stream).cuda_stream
-        if self.handle != self.current.cuda_stream:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(stream)
-        self.device = device
-
-    def call(self, fn, record, nbytes: int):
-        ws = None
-        if nbytes:
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-            if self.handle != self.current.cuda_stream:
-                ws.record_stream(torch.cuda.ExternalStream(self.handle, device=self.device))
-        return fn(C.addressof(record), None if ws is None else ws.data_ptr(), nbytes, self.handle)
+def _axes(x: torch.Tensor, most: int):
+    """x's sizes with a leading axis of clients (1 where x has none)."""
+    shape = x.shape
+    if len(shape) == most:
+        return shape
+    if len(shape) != most - 1:
+        raise ValueError(f"a tensor of {most - 1} or {most} axes is wanted, got {tuple(shape)}")
+    return (1, *shape)
 
 
 def _act(act: str) -> int:
@@ -170,23 +203,17 @@ def aet_linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Te
     """residual + dropout(act(x w^T + bias)) and, with keep_pre, what act was given (else None).
     x: [n, rows, in] or [rows, in]; w: [n, out, in], or [out, in] for all clients; bias likewise
     [n, out] or [out]; residual and out (which may be the residual): as the result."""
-    lib = load_library()
-    clients = x.dim() == 3
-    n, rows, inp = x.shape if clients else (1, *x.shape)
-    outs = w.shape[-2]
-    shape = (n, rows, outs) if clients else (rows, outs)
-    per = w.dim() == 3
-    _same(x, ("w", w, (n, outs, inp) if per else (outs, inp)), ("residual", residual, shape), ("out", out, shape),
-          ("bias", bias, (n, outs) if bias is not None and bias.dim() == 2 else (outs,)))
+    lib = _LIB or load_library()
+    call = _Call(x, stream)
+    n, rows, inp = _axes(x, 3)
+    outs, per = w.shape[-2], w.dim() == 3
+    shape = (n, rows, outs) if x.dim() == 3 else (rows, outs)
     y = x.new_empty(shape) if out is None else out
     pre = x.new_empty(shape) if keep_pre else None
-    _dense_last("w", w)
-    a = aet_linear(_DTYPES[x.dtype], _act(act), n, rows, inp, outs, p, seed, first_row, *_m("x", x, clients),
-                   w.data_ptr(), w.stride(0) if per else 0, w.stride(-2), *_v("bias", bias),
-                   *_m("residual", residual, clients), *_m("out", y, clients), *_m("pre", pre, clients))
-    with torch.cuda.device(x.device):
-        on = _On(x.device, stream, (x, w, bias, residual, y, pre))
-        _check(lib, on.call(lib.aet_linear_forward, a, lib.aet_linear_workspace_bytes(C.addressof(a))))
+    a = aet_linear(call.code, _act(act), n, rows, inp, outs, p, seed, first_row, *call.mat("x", x, x.shape),
+                   *call.weights("w", w, (n, outs, inp) if per else (outs, inp)), *call.vec("bias", bias, n, outs),
+                   *call.mat("residual", residual, shape), *call.mat("out", y, shape), *call.mat("pre", pre, shape))
+    call.run(lib.aet_linear_forward, a, lib.aet_linear_workspace_bytes)
     return y, pre
 
 
@@ -196,36 +223,22 @@ def aet_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre:
                         stream: Optional[torch.cuda.Stream] = None):
     """(dx, dw, db) of aet_linear_forward, None where `need` says so; dw and db have w's clients: with
     w [out, in] for several clients they are sums over them."""
-    lib = load_library()
-    clients = x.dim() == 3
-    n, rows, inp = x.shape if clients else (1, *x.shape)
-    outs = w.shape[-2]
-    shape = (n, rows, outs) if clients else (rows, outs)
-    per = w.dim() == 3
-    _same(x, ("dy", dy, shape), ("w", w, (n, outs, inp) if per else (outs, inp)), ("pre", pre, shape))
+    lib = _LIB or load_library()
+    call = _Call(x, stream)
+    n, rows, inp = _axes(x, 3)
+    outs, per = w.shape[-2], w.dim() == 3
+    shape = (n, rows, outs) if x.dim() == 3 else (rows, outs)
+    wshape = (n, outs, inp) if per else (outs, inp)
     if pre is None and act != "none":
         raise ValueError("pre, as the forward call gave it, is wanted where there is an activation")
     dx = x.new_empty(x.shape) if need[0] else None
-    dw = x.new_empty(w.shape) if need[1] else None
-    db = x.new_empty(w.shape[:-1]) if need[2] else None
-    _dense_last("w", w)
-    a = aet_linear_grad(_DTYPES[x.dtype], _act(act), n, rows, inp, outs, p, seed, first_row, *_m("dy", dy, clients),
-                        *_m("x", x, clients), w.data_ptr(), w.stride(0) if per else 0, w.stride(-2),
-                        *_m("pre", pre, clients), *_m("dx", dx, clients),
-                        None if dw is None else dw.data_ptr(), dw.stride(0) if per and dw is not None else 0, inp,
-                        *_v("db", db))
-    with torch.cuda.device(x.device):
-        on = _On(x.device, stream, (dy, x, w, pre, dx, dw, db))
-        _check(lib, on.call(lib.aet_linear_backward, a, lib.aet_linear_backward_workspace_bytes(C.addressof(a))))
+    dw = x.new_empty(wshape) if need[1] else None
+    db = x.new_empty(wshape[:-1]) if need[2] else None
+    a = aet_linear_grad(call.code, _act(act), n, rows, inp, outs, p, seed, first_row, *call.mat("dy", dy, shape),
+                        *call.mat("x", x, x.shape), *call.weights("w", w, wshape), *call.mat("pre", pre, shape),
+                        *call.mat("dx", dx, x.shape), *call.weights("dw", dw, wshape), *call.vec("db", db, n, outs))
+    call.run(lib.aet_linear_backward, a, lib.aet_linear_backward_workspace_bytes)
     return dx, dw, db
-
-
-def _m3(name: str, t: Optional[torch.Tensor], clients: bool):
-    if t is None:
-        return None, 0, 0, 0
-    _dense_last(name, t)
-    st = t.stride()
-    return (t.data_ptr(), *st[:3]) if clients else (t.data_ptr(), t.shape[0] * st[0], st[0], st[1])
 
 
 def aet_group_norm_forward(x: torch.Tensor, groups: int, gamma: Optional[torch.Tensor] = None,
@@ -234,23 +247,18 @@ def aet_group_norm_forward(x: torch.Tensor, groups: int, gamma: Optional[torch.T
     """(y, mean, rstd): act of the normalised x * gamma + beta, and each group's statistics (float32).
     x: [n, batch, positions, channels] or [batch, positions, channels]; gamma, beta: [n, channels], or
     [channels] for all clients; out (which may be x): as x."""
-    lib = load_library()
-    clients = x.dim() == 4
-    n, batch, positions, ch = x.shape if clients else (1, *x.shape)
+    lib = _LIB or load_library()
+    n, batch, positions, ch = _axes(x, 4)
     if groups < 1 or ch % groups:
         raise ValueError(f"{ch} channels cannot be parted into {groups} groups")
-    _same(x, ("gamma", gamma, (n, ch) if gamma is not None and gamma.dim() == 2 else (ch,)),
-          ("beta", beta, (n, ch) if beta is not None and beta.dim() == 2 else (ch,)), ("out", out, x.shape))
+    call = _Call(x, stream)
     y = x.new_empty(x.shape) if out is None else out
-    stats = (n, batch, groups) if clients else (batch, groups)
-    mean = torch.empty(stats, dtype=torch.float32, device=x.device)
-    rstd = torch.empty(stats, dtype=torch.float32, device=x.device)
-    a = aet_group_norm(_DTYPES[x.dtype], _act(act), n, batch, positions, groups, ch // groups, eps,
-                       *_m3("x", x, clients), *_v("gamma", gamma), *_v("beta", beta), *_m3("out", y, clients),
-                       mean.data_ptr(), rstd.data_ptr())
-    with torch.cuda.device(x.device):
-        on = _On(x.device, stream, (x, gamma, beta, y, mean, rstd))
-        _check(lib, on.call(lib.aet_group_norm_forward, a, lib.aet_group_norm_workspace_bytes(C.addressof(a))))
+    stats = (n, batch, groups) if x.dim() == 4 else (batch, groups)
+    mean, rstd = x.new_empty(stats, dtype=torch.float32), x.new_empty(stats, dtype=torch.float32)
+    a = aet_group_norm(call.code, _act(act), n, batch, positions, groups, ch // groups, eps,
+                       *call.maps("x", x, x.shape), *call.vec("gamma", gamma, n, ch), *call.vec("beta", beta, n, ch),
+                       *call.maps("out", y, x.shape), call.stats("mean", mean, stats), call.stats("rstd", rstd, stats))
+    call.run(lib.aet_group_norm_forward, a, lib.aet_group_norm_workspace_bytes)
     return y, mean, rstd
 
 
@@ -260,47 +268,36 @@ def aet_group_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
                             stream: Optional[torch.cuda.Stream] = None):
     """(dx, dgamma, dbeta) of aet_group_norm_forward from its inputs and statistics.  `need`: dx; dgamma and dbeta (None
     where they are not wanted, or have no parameter).  A gamma or beta for all clients gets the sum over them."""
-    lib = load_library()
-    clients = x.dim() == 4
-    n, batch, positions, ch = x.shape if clients else (1, *x.shape)
+    lib = _LIB or load_library()
+    call = _Call(x, stream)
+    n, batch, positions, ch = _axes(x, 4)
     groups = mean.shape[-1]
-    stats = (n, batch, groups) if clients else (batch, groups)
+    stats = (n, batch, groups) if x.dim() == 4 else (batch, groups)
     if groups < 1 or ch % groups:
         raise ValueError(f"{ch} channels cannot be parted into {groups} groups")
-    _same(x, ("dy", dy, x.shape), ("gamma", gamma, (n, ch) if gamma is not None and gamma.dim() == 2 else (ch,)),
-          ("beta", beta, (n, ch) if beta is not None and beta.dim() == 2 else (ch,)))
     if gamma is not None and beta is not None and gamma.dim() != beta.dim():
         raise ValueError("gamma and beta: either both or none have an axis of clients")
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        if t.dtype != torch.float32 or t.device != x.device or tuple(t.shape) != stats or not t.is_contiguous():
-            raise ValueError(f"{name} has to be as the forward call gave it: float32, contiguous, {stats}")
     dx = x.new_empty(x.shape) if need[0] else None
     dgamma = x.new_empty(gamma.shape) if need[1] and gamma is not None else None
     dbeta = x.new_empty(beta.shape) if need[1] and beta is not None else None
-    a = aet_group_norm_grad(_DTYPES[x.dtype], _act(act), n, batch, positions, groups, ch // groups,
-                            *_m3("dy", dy, clients), *_m3("x", x, clients), mean.data_ptr(), rstd.data_ptr(),
-                            *_v("gamma", gamma), *_v("beta", beta), *_m3("dx", dx, clients), *_v("dgamma", dgamma),
-                            *_v("dbeta", dbeta))
-    with torch.cuda.device(x.device):
-        on = _On(x.device, stream, (dy, x, mean, rstd, gamma, beta, dx, dgamma, dbeta))
-        _check(lib, on.call(lib.aet_group_norm_backward, a,
-                            lib.aet_group_norm_backward_workspace_bytes(C.addressof(a))))
+    a = aet_group_norm_grad(call.code, _act(act), n, batch, positions, groups, ch // groups,
+                            *call.maps("dy", dy, x.shape), *call.maps("x", x, x.shape),
+                            call.stats("mean", mean, stats), call.stats("rstd", rstd, stats),
+                            *call.vec("gamma", gamma, n, ch), *call.vec("beta", beta, n, ch),
+                            *call.maps("dx", dx, x.shape), *call.vec("dgamma", dgamma, n, ch),
+                            *call.vec("dbeta", dbeta, n, ch))
+    call.run(lib.aet_group_norm_backward, a, lib.aet_group_norm_backward_workspace_bytes)
     return dx, dgamma, dbeta
 
 
 def _dropout(fn: str, x, p, seed, first_row, residual, out, stream):
-    lib = load_library()
-    if x.dim() not in (2, 3):
-        raise ValueError("[n, rows, cols] or [rows, cols] is wanted")
-    clients = x.dim() == 3
-    n, rows, cols = x.shape if clients else (1, *x.shape)
-    _same(x, ("residual", residual, x.shape), ("out", out, x.shape))
+    lib = _LIB or load_library()
+    call = _Call(x, stream)
+    n, rows, cols = _axes(x, 3)
     y = x.new_empty(x.shape) if out is None else out
-    a = aet_dropout(_DTYPES[x.dtype], n, rows, cols, p, seed, first_row, *_m("x", x, clients),
-                    *_m("residual", residual, clients), *_m("out", y, clients))
-    with torch.cuda.device(x.device):
-        on = _On(x.device, stream, (x, residual, y))
-        _check(lib, getattr(lib, fn)(C.addressof(a), on.handle))
+    a = aet_dropout(call.code, n, rows, cols, p, seed, first_row, *call.mat("x", x, x.shape),
+                    *call.mat("residual", residual, x.shape), *call.mat("out", y, x.shape))
+    call.run(getattr(lib, fn), a)
     return y
 
 
