@@ -11,6 +11,8 @@
 #include "ops_internal.h"
 #include "ops_tiles.h"
 
+#include <type_traits>
+
 #include "../split_bf16.h"
 
 namespace aet_ops {
@@ -43,7 +45,7 @@ struct Stage {
     static constexpr int kBytes = R * BK * 2;              // of a part
     static __device__ __forceinline__ int slot(int r, int c) {
         if constexpr (COLS) return r * kWidth + (c ^ ((r & 3 & (R / 32 - 1)) << 2));
-        else return r * kWidth + (c ^ (BK == 64 ? r & 7 : (r >> 1) & 3));
+        else return r * kWidth + (c ^ (BK == 64 ? (r >> 1) & 7 : (r >> 2) & 3));
     }
     // Lane addresses of fragment t (rows 32 t ..): 8 k of row 32 t + lane % 32 from k = 16 ks + 8 (lane / 32) on
     static __device__ __forceinline__ bf8 fragment(lds_ptr part, int t, int ks, int lane) {
@@ -68,13 +70,13 @@ template <typename T, int R, int BK, bool COLS, int THREADS>
 struct RegStage {
     using S = Stage<R, BK, COLS>;
     static constexpr int kCount = S::kPieces / THREADS;
-    static_assert(S::kPieces % THREADS == 0 && THREADS % S::kWidth == 0, "whole pieces a thread");
+    static_assert(kCount > 0 && S::kPieces % THREADS == 0 && THREADS % S::kWidth == 0, "whole pieces a thread");
     static constexpr int kStep = THREADS / S::kWidth;   // rows between a thread's pieces
     wide<T, 8> raw[kCount];
-    const T *p;          // the thread's first piece of the next stage
+    const T *p;          // of the thread's piece column in the next stage
     int64_t row;
-    int r, c, left;      // left: by rows, k until the end of the sum; by columns, likewise
-    int rows;            // rows of C there are from the tile's first on
+    int r, c, left;      // left: of the sum
+    int rows;            // of the operand, from the tile's first on
 
     __device__ __forceinline__ void begin(const Operand &o, int64_t client, int r0, int rows_all, int k0, int k1) {
         r = threadIdx.x / S::kWidth;
@@ -82,15 +84,22 @@ struct RegStage {
         row = o.row;
         rows = rows_all - r0;
         left = k1 - k0;
-        p = (const T *)o.p + client * o.client + (COLS ? (int64_t)(k0 + r) * row + r0 + 8 * c : (int64_t)(r0 + r) * row + k0 + 8 * c);
+        p = (const T *)o.p + client * o.client + (COLS ? (int64_t)k0 * row + r0 + 8 * c : (int64_t)r0 * row + k0 + 8 * c);
     }
+    // Whether whole stages can be read without looking where each piece ends.  By rows they always can: rows past the
+    // last are read from the last again, and become rows of C that are not stored.
+    __device__ __forceinline__ bool plain() const { return !COLS || rows >= R; }
+    template <bool PLAIN>
     __device__ __forceinline__ void load() {
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             const int ri = r + i * kStep;
-            const bool in = ri < (COLS ? left : rows);
-            const int count = in ? (COLS ? rows : left) - 8 * c : 0;
-            raw[i] = load_raw<T, 8>(p + (int64_t)(i * kStep) * row, count);
+            if (PLAIN) {
+                raw[i] = *(const wide<T, 8> *)(p + (int64_t)(COLS || ri < rows ? ri : rows - 1) * row);
+            } else {
+                const bool in = ri < (COLS ? left : rows);
+                raw[i] = load_raw<T, 8>(p + (int64_t)ri * row, in ? (COLS ? rows : left) - 8 * c : 0);
+            }
         }
         p += COLS ? BK * row : BK;
         left -= BK;
@@ -153,6 +162,18 @@ struct DirectStage {
     }
 };
 
+// Asks the compiler to put READS of LDS behind the first of PRODUCTS of the matrix unit, so that they have the others' time.
+template <int PRODUCTS, int READS>
+__device__ __forceinline__ void interleave() {
+    constexpr int first = PRODUCTS >= 8 ? 3 : 1, each = (READS + first - 1) / first;
+#pragma unroll
+    for (int i = 0; i < first; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, each, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - first, 0);
+}
+
 // ---- the kernel --------------------------------------------------------------------------
 
 template <typename T>
@@ -169,7 +190,7 @@ struct Tile {
     using SA = Stage<BM, BK, TA>;
     using SB = Stage<BN, BK, TB>;
     static constexpr int kStage = kParts * (SA::kBytes + SB::kBytes);
-    static constexpr int kBuffers = sizeof(T) == 2 ? 2 : 1;
+    static constexpr int kBuffers = DIRECT ? 2 : 1;
     static constexpr int kEpilogue = WR * WC * 32 * (FN * 32 + 4) * 4;
     static constexpr int kLds = kStage * kBuffers > kEpilogue ? kStage * kBuffers : kEpilogue;
 };
@@ -206,30 +227,31 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand o
             if constexpr (P == 3) corr[i][j] = f16v{};
         }
 
-    const auto compute = [&](lds_ptr a, lds_ptr b) {
+    struct Fragments {
+        bf8 a[FM][P], b[FN][P];
+    };
+    const auto read = [&](Fragments &f, lds_ptr stage, int ks) {
 #pragma unroll
-        for (int ks = 0; ks < BK / 16; ++ks) {
-            bf8 fa[FM][P], fb[FN][P];
+        for (int q = 0; q < P; ++q) {
 #pragma unroll
-            for (int q = 0; q < P; ++q) {
+            for (int i = 0; i < FN; ++i) f.b[i][q] = SB::fragment(stage + (P * SA::kBytes + q * SB::kBytes), wc * FN + i, ks, lane);
 #pragma unroll
-                for (int i = 0; i < FN; ++i) fb[i][q] = SB::fragment(b + q * SB::kBytes, wc * FN + i, ks, lane);
+            for (int j = 0; j < FM; ++j) f.a[j][q] = SA::fragment(stage + q * SA::kBytes, wr * FM + j, ks, lane);
+        }
+    };
+    const auto multiply = [&](const Fragments &f) {
+        if constexpr (P == 1) {
 #pragma unroll
-                for (int j = 0; j < FM; ++j) fa[j][q] = SA::fragment(a + q * SA::kBytes, wr * FM + j, ks, lane);
-            }
-            if constexpr (P == 1) {
+            for (int i = 0; i < FN; ++i)
+#pragma unroll
+                for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[i][0], f.a[j][0], acc[i][j], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 6; ++q)
 #pragma unroll
                 for (int i = 0; i < FN; ++i)
 #pragma unroll
-                    for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[i][0], fa[j][0], acc[i][j], 0, 0, 0);
-            } else {
-#pragma unroll
-                for (int q = 0; q < 6; ++q)
-#pragma unroll
-                    for (int i = 0; i < FN; ++i)
-#pragma unroll
-                        for (int j = 0; j < FM; ++j) aet::split_mfma(q, fb[i], fa[j], acc[i][j], corr[i][j]);
-            }
+                    for (int j = 0; j < FM; ++j) aet::split_mfma(q, f.b[i], f.a[j], acc[i][j], corr[i][j]);
         }
     };
 
@@ -240,40 +262,85 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand o
         DirectStage<BN, BK, TB, L::kThreads> lb;
         la.begin(oa, client, m0, s.M, k0, k1);
         lb.begin(ob, client, n0, s.N, k0, k1);
-        if (stages > 0) {
-            la.load(lds);
-            lb.load(lds + kPartA);
-        }
-        for (int i = 0; i < stages; ++i) {
-            const lds_ptr now = lds + (i & 1) * L::kStage, next = lds + ((i & 1) ^ 1) * L::kStage;
-            // this stage has arrived, and everybody is done with the one before
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // The fragments of the next 16 k are read while the matrix unit has the last ones, also across the barrier that
+        // says that the next stage has arrived everywhere and that this one's place may be written again: it comes
+        // ahead of the stage's last products, and right behind it the stage after the next is sent for.
+        constexpr int kBuffers = L::kBuffers, KS = BK / 16, kReads = (TA ? 2 : 1) * FM + (TB ? 2 : 1) * FN;
+        constexpr int kLoads = decltype(la)::kCount + decltype(lb)::kCount;
+        const auto fetch = [&](int i) {
+            const lds_ptr to = lds + i % kBuffers * L::kStage;
+            la.load(to);
+            lb.load(to + kPartA);
+        };
+        // s_waitcnt by its encoding (vmcnt low and high bits, lgkmcnt 0), which the compiler takes into account
+        const auto arrived = [&](auto still) {
+            __builtin_amdgcn_s_waitcnt(0x0070 | (still & 15) | (still >> 4) << 14);
             __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (i + 1 < stages) {
-                la.load(next);
-                lb.load(next + kPartA);
+        };
+        typedef std::integral_constant<int, (kBuffers - 2) * kLoads> Others;
+        typedef std::integral_constant<int, 0> None;
+        Fragments f[2];
+        for (int i = 0; i < kBuffers && i < stages; ++i) fetch(i);
+        if (stages >= kBuffers) arrived(std::integral_constant<int, (kBuffers - 1) * kLoads>());
+        else arrived(None());
+        if (stages > 0) read(f[0], lds, 0);
+        int i = 0;
+        for (; i + kBuffers < stages; ++i) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                if (ks + 1 == KS) {
+                    arrived(Others());
+                    fetch(i + kBuffers);
+                }
+                read(f[(ks + 1) % 2], lds + (i + (ks + 1) / KS) % kBuffers * L::kStage, (ks + 1) % KS);
+                multiply(f[ks % 2]);
+                interleave<FM * FN, kReads>();
             }
-            compute(now, now + kPartA);
+        }
+        for (; i < stages; ++i) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                if (ks + 1 == KS) arrived(None());
+                if (ks + 1 < KS || i + 1 < stages) read(f[(ks + 1) % 2], lds + (i + (ks + 1) / KS) % kBuffers * L::kStage, (ks + 1) % KS);
+                multiply(f[ks % 2]);
+            }
         }
     } else {
         RegStage<T, BM, BK, TA, L::kThreads> la;
         RegStage<T, BN, BK, TB, L::kThreads> lb;
         la.begin(oa, client, m0, s.M, k0, k1);
         lb.begin(ob, client, n0, s.N, k0, k1);
-        la.load();
-        lb.load();
-        for (int i = 0; i < stages; ++i) {
-            const lds_ptr now = lds + (L::kBuffers == 2 ? (i & 1) * L::kStage : 0);
-            if constexpr (L::kBuffers == 1) __syncthreads();
-            la.store(now);
-            lb.store(now + kPartA);
-            __syncthreads();
-            if (i + 1 < stages) {
-                la.load();
-                lb.load();
+        // A stage goes from memory to registers while the one before it is worked on.  One buffer: there is another
+        // workgroup on the compute unit whose products go on while this one splits and stores.
+        const auto work = [&]() {
+#pragma unroll
+            for (int ks = 0; ks < BK / 16; ++ks) {
+                Fragments f;
+                read(f, lds, ks);
+                multiply(f);
             }
-            compute(now, now + kPartA);
+        };
+        const auto put = [&]() {
+            __syncthreads();
+            la.store(lds);
+            lb.store(lds + kPartA);
+            __syncthreads();
+        };
+        const int whole = la.plain() && lb.plain() ? (k1 - k0) / BK : 0;
+        la.template load<false>();
+        lb.template load<false>();
+        int i = 0;
+        for (; i + 1 < whole; ++i) {
+            put();
+            la.template load<true>();
+            lb.template load<true>();
+            work();
+        }
+        for (; i < stages; ++i) {
+            put();
+            la.template load<false>();
+            lb.template load<false>();
+            work();
         }
     }
     __syncthreads();
@@ -368,20 +435,43 @@ static hipError_t run_tiles(const Product &p, Shape s, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// Kinds of tiles, and what they take: `alone` microseconds for a stage where a compute unit has one workgroup, `more` for
+// each further one that it has to do, `end` for each workgroup's epilogue.  Measured on products of 33 to 8192 rows, 100 to
+// 4096 columns and sums of 32 to 8192; a few examples, in microseconds, with the kinds as they are listed here:
+//   fp32  4096 x 4096 x 4096  690, 810, 900;   2048 x 2048 x 1024  72, 63, 67;   3 x (1001 x 771 x 1155)  85, 66, 58
+//   bf16  4096 x 4096 x 4096  124, 140, 166, 199;   2048 x 2048 x 1024  28, 13.8, 13.6, 15.8;   512 x 4096 x 4096  83, 41, 36, 32
+// A sum is split where its tiles leave compute units idle (fp32 512 x 4096 x 4096, 128 x 128: 238, two slices 138, four 109);
+// partial sums are written and read at about 2.5 TB/s, and the launch that adds them takes 4.
+struct Kind {
+    int bm, bn, bk;
+    float alone, more, end;
+};
+static const Kind kKinds32[] = {{128, 128, 32, 1.9f, 1.15f, 2.0f}, {64, 128, 32, 1.2f, 0.72f, 1.0f}, {64, 64, 32, 0.88f, 0.40f, 0.5f}};
+static const Kind kKinds16[] = {{256, 256, 64, 1.5f, 1.6f, 8.0f}, {128, 128, 64, 0.65f, 0.52f, 2.0f}, {64, 128, 64, 0.54f, 0.295f, 1.0f}, {64, 64, 64, 0.46f, 0.18f, 0.5f}};
+
 struct Choice {
-    int bm, bn, bk, slices;
+    const Kind *kind;
+    int slices;
 };
 static Choice choose(int dtype, const Product &p) {
-    Choice c;
-    if (dtype == AET_F32) {
-        c = {128, 128, 32, 1};
-    } else {
-        c = {128, 128, 64, 1};
-        if (p.M >= 256 && p.N >= 256 && p.clients * ceil_div(p.M, 256) * ceil_div(p.N, 256) >= 192) c.bm = c.bn = 256;
-    }
-    const int64_t tiles = p.clients * ceil_div(p.M, c.bm) * ceil_div(p.N, c.bn), stages = ceil_div(p.K, c.bk);
-    while (tiles * c.slices < 128 && stages / (c.slices * 2) >= 4) c.slices *= 2;
-    return c;
+    Choice best = {};
+    float least = 0;
+    const auto consider = [&](const Kind &k) {
+        const int64_t tiles = p.clients * ceil_div(p.M, k.bm) * ceil_div(p.N, k.bn), stages = ceil_div(p.K, k.bk);
+        const float sums = (float)p.clients * (float)p.M * (float)p.N * 4.0f;
+        for (int64_t slices = 1; slices == 1 || (slices <= 64 && stages / slices >= 2); slices *= 2) {
+            const float waves = (float)ceil_div(tiles * slices, 256);
+            float t = (float)ceil_div(stages, slices) * (k.alone + (waves - 1) * k.more) + waves * k.end;
+            if (slices > 1) t += 4.0f + (float)(slices + 1) * sums / 2.5e6f;
+            if (!best.kind || t < least) {
+                least = t;
+                best = {&k, (int)slices};
+            }
+        }
+    };
+    if (dtype == AET_F32) for (const Kind &k : kKinds32) consider(k);
+    else for (const Kind &k : kKinds16) consider(k);
+    return best;
 }
 
 size_t product_workspace(int dtype, const Product &p) {
@@ -395,22 +485,27 @@ static hipError_t run_product(const Product &p, void *workspace, hipStream_t str
     const Choice c = choose(sizeof(T) == 4 ? AET_F32 : AET_BF16, p);
     Shape s = {p.M, p.N, p.K};
     s.clients = p.clients;
-    s.tiles_n = (int)ceil_div(p.N, c.bn);
-    const int64_t tiles = ceil_div(p.M, c.bm) * s.tiles_n, blocks = tiles * p.clients * c.slices;
+    const Kind &k = *c.kind;
+    s.tiles_n = (int)ceil_div(p.N, k.bn);
+    const int64_t tiles = ceil_div(p.M, k.bm) * s.tiles_n, blocks = tiles * p.clients * c.slices;
     if (!blocks) return hipSuccess;
     if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
     s.tiles = (int)tiles;
     s.blocks = (int)blocks;
     s.slices = c.slices;
-    s.slice_k = (int)ceil_div(ceil_div(p.K, c.bk), c.slices) * c.bk;
+    s.slice_k = (int)ceil_div(ceil_div(p.K, k.bk), c.slices) * k.bk;
     s.partial = (float *)workspace;
     hipError_t e;
     if constexpr (sizeof(T) == 4) {
-        e = run_tiles<T, 128, 128, 32, 2, 2, TA, TB, false>(p, s, stream);
+        if (k.bm == 128) e = run_tiles<T, 128, 128, 32, 2, 2, TA, TB, false>(p, s, stream);
+        else if (k.bn == 128) e = run_tiles<T, 64, 128, 32, 2, 2, TA, TB, false>(p, s, stream);
+        else e = run_tiles<T, 64, 64, 32, 2, 2, TA, TB, false>(p, s, stream);
     } else {
-        const bool d = direct(p.a, p.M, p.K, c.bk) && direct(p.b, p.N, p.K, c.bk);
-        if (c.bm == 256) e = d ? run_tiles<T, 256, 256, 64, 2, 4, TA, TB, true>(p, s, stream) : run_tiles<T, 256, 256, 64, 2, 4, TA, TB, false>(p, s, stream);
-        else e = d ? run_tiles<T, 128, 128, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 128, 128, 64, 2, 2, TA, TB, false>(p, s, stream);
+        const bool d = direct(p.a, p.M, p.K, 64) && direct(p.b, p.N, p.K, 64);
+        if (k.bm == 256) e = d ? run_tiles<T, 256, 256, 64, 2, 4, TA, TB, true>(p, s, stream) : run_tiles<T, 256, 256, 64, 2, 4, TA, TB, false>(p, s, stream);
+        else if (k.bm == 128) e = d ? run_tiles<T, 128, 128, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 128, 128, 64, 2, 2, TA, TB, false>(p, s, stream);
+        else if (k.bn == 128) e = d ? run_tiles<T, 64, 128, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 64, 128, 64, 2, 2, TA, TB, false>(p, s, stream);
+        else e = d ? run_tiles<T, 64, 64, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 64, 64, 64, 2, 2, TA, TB, false>(p, s, stream);
     }
     if (e != hipSuccess || s.slices == 1) return e;
     k_join<T><<<(int)ceil_div((int64_t)p.clients * p.M * ceil_div(p.N, 8), 256), 256, 0, stream>>>(s, p.e);
