@@ -13,24 +13,24 @@ struct Epilogue {
     Drop d;
 };
 
-// Columns col .. col + count - 1 (col a multiple of 8, count 1 to 8) of a client's row; v: the sums plus bias.
-template <typename T>
-__device__ __forceinline__ void finish8(const Epilogue &e, int64_t client, int64_t row, int col, int count, float (&v)[8]) {
+// Columns col .. col + count - 1 (col a multiple of V, count 1 to V) of a client's row; v: the sums plus bias.
+template <typename T, int V>
+__device__ __forceinline__ void finish(const Epilogue &e, int64_t client, int64_t row, int col, int count, float (&v)[V]) {
     if (e.pre.p) store_some((T *)e.pre.p + client * e.pre.client + row * e.pre.row + col, count, v);
     act_each(e.act, v);
-    if (e.d.least) drop_apply<8>(e.d, drop_row(e.d, client * e.rows + row), col, v);
+    if (e.d.least) drop_apply(e.d, drop_row(e.d, client * e.rows + row), col, v);
     if (e.residual.p) {
-        float r[8];
+        float r[V];
         load_some((const T *)e.residual.p + client * e.residual.client + row * e.residual.row + col, count, r);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += r[i];
+        for (int i = 0; i < V; ++i) v[i] += r[i];
     }
     store_some((T *)e.y.p + client * e.y.client + row * e.y.row + col, count, v);
 }
-template <typename T>
-__device__ __forceinline__ void bias8(const Epilogue &e, int64_t client, int col, int count, float (&b)[8]) {
+template <typename T, int V>
+__device__ __forceinline__ void bias_of(const Epilogue &e, int64_t client, int col, int count, float (&b)[V]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = 0.0f;
+    for (int i = 0; i < V; ++i) b[i] = 0.0f;
     if (e.bias.p && count > 0) load_some((const T *)e.bias.p + client * e.bias.client + col, count, b);
 }
 

@@ -22,8 +22,9 @@ hipError_t launch_linear_forward(const aet_linear &a, void *workspace, hipStream
     return launch_product(a.dtype, forward_product(a), workspace, s);
 }
 
-// dz = dropout'(dy) * act'(z), and its sums over rows.  A workgroup has 32 pieces of 8 columns of a strip of a client's
-// rows, eight rows at a time; the sums of several strips go to `partial` and are added by k_db, in their order.
+// dz = dropout'(dy) * act'(z), and its sums over rows.  A workgroup has 32 pieces of 16 bytes of a strip of a client's rows,
+// eight rows at a time, and four times that on the way; the sums of several strips go to `partial` and are added by k_db,
+// in their order.
 struct DzShape {
     int across, strips, strip;   // workgroups: side by side, one below the other; rows of a strip
     int64_t dz_row;
@@ -32,37 +33,54 @@ struct DzShape {
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_dz(aet_linear_grad a, Drop d, DzShape s, T *dz) {
-    __shared__ float lds[8][256];
+    constexpr int V = 16 / sizeof(T), N = 4;
+    __shared__ float lds[8][32 * V];
     const int per = s.across * s.strips;
     const int64_t client = blockIdx.x / per;
     const int b = blockIdx.x % per, strip = b / s.across, tx = threadIdx.x % 32, ty = threadIdx.x / 32;
-    const int col = (b % s.across * 32 + tx) * 8, count = a.out - col;
+    const int col = (b % s.across * 32 + tx) * V;
     const int64_t first = (int64_t)strip * s.strip, end = first + s.strip < a.rows ? first + s.strip : a.rows;
     const T *dy = (const T *)a.dy.p + client * a.dy.client + col;
     const T *pre = a.act ? (const T *)a.pre.p + client * a.pre.client + col : nullptr;
-    float sum[8] = {};
-    if (count > 0) {
-#pragma unroll 4
-        for (int64_t r = first + ty; r < end; r += 8) {
-            float v[8];
-            load_some(dy + r * a.dy.row, count, v);
-            if (d.least) drop_apply(d, drop_row(d, client * a.rows + r), col, v);
-            if (pre) {
-                float z[8];
-                load_some(pre + r * a.pre.row, count, z);
-                slope_each(a.act, z, v);
-            }
-            if (dz) store_some(dz + (client * a.rows + r) * s.dz_row + col, count, v);
+    float sum[V] = {};
+    const auto rows = [&](int count) {   // with whole pieces a constant, and then nothing is between the loads
+        for (int64_t r0 = first + ty; r0 < end; r0 += 8 * N) {
+            wide<T, V> rd[N], rz[N];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += v[i];
+            for (int i = 0; i < N; ++i) {
+                const int64_t r = r0 + 8 * i < end ? r0 + 8 * i : end - 1;
+                rd[i] = load_raw<T, V>(dy + r * a.dy.row, count);
+                if (pre) rz[i] = load_raw<T, V>(pre + r * a.pre.row, count);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int64_t r = r0 + 8 * i;
+                if (r >= end) break;
+                float v[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = (float)rd[i][e];
+                if (d.least) drop_apply(d, drop_row(d, client * a.rows + r), col, v);
+                if (pre) {
+                    float z[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) z[e] = (float)rz[i][e];
+                    slope_each(a.act, z, v);
+                }
+                if (dz) store_some(dz + (client * a.rows + r) * s.dz_row + col, count, v);
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] += v[e];
+            }
         }
-    }
+    };
+    const int count = a.out - col;
+    if (count >= V) rows(V);
+    else if (count > 0) rows(count);
     if (!a.db.p) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) lds[ty][tx * 8 + i] = sum[i];
+    for (int e = 0; e < V; ++e) lds[ty][tx * V + e] = sum[e];
     __syncthreads();
-    const int mine = b % s.across * 256 + threadIdx.x;
-    if (mine >= a.out) return;
+    const int mine = b % s.across * (32 * V) + threadIdx.x;
+    if (threadIdx.x >= 32 * V || mine >= a.out) return;
     float total = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) total += lds[i][threadIdx.x];
@@ -91,7 +109,7 @@ static BackwardPlan plan(const aet_linear_grad &a, char *workspace) {
     const bool own = (a.p > 0 || a.act != AET_ACT_NONE) && (a.dx.p || a.dw.p);
     const int e = a.dtype == AET_F32 ? 4 : 2;
     b.dz.dz_row = ceil_div((int64_t)a.out * e, 16) * 16 / e;
-    b.dz.across = (int)ceil_div(a.out, 256);
+    b.dz.across = (int)ceil_div(a.out, 32 * 16 / e);
     // strips of at least 64 rows, as many as give every compute unit several workgroups
     const int64_t wanted = ceil_div(2048, (int64_t)a.n * b.dz.across + 1), most = ceil_div(a.rows, 64);
     b.dz.strip = (int)ceil_div(ceil_div(a.rows, wanted < most ? wanted : most > 0 ? most : 1), 8) * 8;

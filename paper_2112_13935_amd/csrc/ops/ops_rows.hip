@@ -81,7 +81,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_rows(Operand ox, Operand ow, Row
     const int row = threadIdx.x / 2, half = threadIdx.x % 2 * 8, count = s.N - n0 - half;
     if (row >= G * 16 || row >= s.M || count <= 0) return;
     float v[8];
-    bias8<T>(e, client, n0 + half, count, v);
+    bias_of<T>(e, client, n0 + half, count, v);
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
         const f4 lo = *(const f4 *)&lds[i][row][half], hi = *(const f4 *)&lds[i][row][half + 4];
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_rows(Operand ox, Operand ow, Row
             v[4 + y] += hi[y];
         }
     }
-    finish8<T>(e, client, row, n0 + half, count, v);
+    finish<T>(e, client, row, n0 + half, count, v);
 }
 
 bool rows_fit(const Product &p) { return !p.a.by_columns && !p.b.by_columns && p.M <= 32; }

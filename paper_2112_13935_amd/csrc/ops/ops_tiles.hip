@@ -346,13 +346,13 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand o
     __syncthreads();
 
     // A lane has, of row m0 + lane % 32 of a fragment, four columns at a time: through LDS, a wave for itself, to lanes
-    // with 8 columns each, in whole lines of memory.
-    constexpr int W = FN * 32, LINE = W + 4;
+    // with V columns (16 bytes) each, in whole lines of memory.
+    constexpr int V = 16 / sizeof(T), W = FN * 32, LINE = W + 4, ACROSS = W / V, DOWN = 64 / ACROSS;
     __attribute__((address_space(3))) float *mine = (__attribute__((address_space(3))) float *)lds + wave * (32 * LINE);
-    const int col = n0 + wc * W + lane % (W / 8) * 8;
+    const int col = n0 + wc * W + lane % ACROSS * V;
     const int count = s.N - col;
-    float bias[8];
-    bias8<T>(e, client, col, s.slices > 1 ? 0 : count, bias);
+    float bias[V];
+    bias_of<T>(e, client, col, s.slices > 1 ? 0 : count, bias);
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
 #pragma unroll
@@ -367,19 +367,19 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand o
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int r = 0; r < 32; r += 512 / W) {
-            const int line = r + lane / (W / 8);
+        for (int r = 0; r < 32; r += DOWN) {
+            const int line = r + lane / ACROSS;
             const int64_t row = m0 + (wr * FM + j) * 32 + line;
-            float v[8];
+            float v[V];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const f4 x = *(__attribute__((address_space(3))) f4 *)(mine + line * LINE + lane % (W / 8) * 8 + 4 * h);
+            for (int h = 0; h < V / 4; ++h) {
+                const f4 x = *(__attribute__((address_space(3))) f4 *)(mine + line * LINE + lane % ACROSS * V + 4 * h);
 #pragma unroll
                 for (int y = 0; y < 4; ++y) v[4 * h + y] = x[y] + bias[4 * h + y];
             }
             if (row < s.M && count > 0) {
                 if (s.slices > 1) store_some(s.partial + (((int64_t)slice * s.clients + client) * s.M + row) * s.N + col, count, v);
-                else finish8<T>(e, client, row, col, count, v);
+                else finish<T>(e, client, row, col, count, v);
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -387,24 +387,25 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand o
     }
 }
 
-// Adds the slices of a split sum, in their order, and ends it.  A thread has 8 columns.
+// Adds the slices of a split sum, in their order, and ends it.  A thread has 16 bytes of C.
 template <typename T>
 __global__ __launch_bounds__(256) void k_join(Shape s, Epilogue e) {
-    const int wide = (s.N + 7) / 8;
+    constexpr int V = 16 / sizeof(T);
+    const int wide = (s.N + V - 1) / V;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t line = i / wide;
     if (line >= (int64_t)s.clients * s.M) return;
-    const int col = (int)(i - line * wide) * 8, count = s.N - col;
+    const int col = (int)(i - line * wide) * V, count = s.N - col;
     const int64_t client = line / s.M, row = line - client * s.M;
-    float v[8];
-    bias8<T>(e, client, col, count, v);
+    float v[V];
+    bias_of<T>(e, client, col, count, v);
     for (int k = 0; k < s.slices; ++k) {
-        float x[8];
+        float x[V];
         load_some(s.partial + ((int64_t)k * s.clients * s.M + line) * s.N + col, count, x);
 #pragma unroll
-        for (int y = 0; y < 8; ++y) v[y] += x[y];
+        for (int y = 0; y < V; ++y) v[y] += x[y];
     }
-    finish8<T>(e, client, row, col, count, v);
+    finish<T>(e, client, row, col, count, v);
 }
 
 // ---- the choice --------------------------------------------------------------------------
@@ -446,14 +447,17 @@ struct Kind {
     int bm, bn, bk;
     float alone, more, end;
 };
-static const Kind kKinds32[] = {{128, 128, 32, 1.9f, 1.15f, 2.0f}, {64, 128, 32, 1.2f, 0.72f, 1.0f}, {64, 64, 32, 0.88f, 0.40f, 0.5f}};
+static const Kind kKinds32[] = {{128, 128, 32, 2.1f, 1.1f, 2.0f}, {64, 128, 32, 1.2f, 0.72f, 1.0f}, {64, 64, 32, 0.88f, 0.40f, 0.5f}};
 static const Kind kKinds16[] = {{256, 256, 64, 1.5f, 1.6f, 8.0f}, {128, 128, 64, 0.65f, 0.52f, 2.0f}, {64, 128, 64, 0.54f, 0.295f, 1.0f}, {64, 64, 64, 0.46f, 0.18f, 0.5f}};
+
+// bf16 through registers
+static const Kind kKinds16Any[] = {{256, 256, 64, 2.5f, 2.6f, 8.0f}, {128, 128, 64, 1.7f, 0.9f, 2.0f}, {64, 128, 64, 0.95f, 0.42f, 1.0f}, {64, 64, 64, 0.62f, 0.31f, 0.5f}};
 
 struct Choice {
     const Kind *kind;
     int slices;
 };
-static Choice choose(int dtype, const Product &p) {
+static Choice choose(int dtype, const Product &p, bool straight) {
     Choice best = {};
     float least = 0;
     const auto consider = [&](const Kind &k) {
@@ -470,19 +474,22 @@ static Choice choose(int dtype, const Product &p) {
         }
     };
     if (dtype == AET_F32) for (const Kind &k : kKinds32) consider(k);
-    else for (const Kind &k : kKinds16) consider(k);
+    else if (straight) for (const Kind &k : kKinds16) consider(k);
+    else for (const Kind &k : kKinds16Any) consider(k);
     return best;
 }
 
 size_t product_workspace(int dtype, const Product &p) {
     if (rows_fit(p)) return 0;
-    const Choice c = choose(dtype, p);
-    return c.slices > 1 ? (size_t)c.slices * p.clients * p.M * p.N * sizeof(float) : 0;
+    // enough for either way, so that it does not depend on where the tensors lie
+    const int a = choose(dtype, p, true).slices, b = choose(dtype, p, false).slices, slices = a > b ? a : b;
+    return slices > 1 ? (size_t)slices * p.clients * p.M * p.N * sizeof(float) : 0;
 }
 
 template <typename T, bool TA, bool TB>
 static hipError_t run_product(const Product &p, void *workspace, hipStream_t stream) {
-    const Choice c = choose(sizeof(T) == 4 ? AET_F32 : AET_BF16, p);
+    const bool d = sizeof(T) == 2 && direct(p.a, p.M, p.K, 64) && direct(p.b, p.N, p.K, 64);
+    const Choice c = choose(sizeof(T) == 4 ? AET_F32 : AET_BF16, p, d);
     Shape s = {p.M, p.N, p.K};
     s.clients = p.clients;
     const Kind &k = *c.kind;
@@ -501,14 +508,13 @@ static hipError_t run_product(const Product &p, void *workspace, hipStream_t str
         else if (k.bn == 128) e = run_tiles<T, 64, 128, 32, 2, 2, TA, TB, false>(p, s, stream);
         else e = run_tiles<T, 64, 64, 32, 2, 2, TA, TB, false>(p, s, stream);
     } else {
-        const bool d = direct(p.a, p.M, p.K, 64) && direct(p.b, p.N, p.K, 64);
         if (k.bm == 256) e = d ? run_tiles<T, 256, 256, 64, 2, 4, TA, TB, true>(p, s, stream) : run_tiles<T, 256, 256, 64, 2, 4, TA, TB, false>(p, s, stream);
         else if (k.bm == 128) e = d ? run_tiles<T, 128, 128, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 128, 128, 64, 2, 2, TA, TB, false>(p, s, stream);
         else if (k.bn == 128) e = d ? run_tiles<T, 64, 128, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 64, 128, 64, 2, 2, TA, TB, false>(p, s, stream);
         else e = d ? run_tiles<T, 64, 64, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 64, 64, 64, 2, 2, TA, TB, false>(p, s, stream);
     }
     if (e != hipSuccess || s.slices == 1) return e;
-    k_join<T><<<(int)ceil_div((int64_t)p.clients * p.M * ceil_div(p.N, 8), 256), 256, 0, stream>>>(s, p.e);
+    k_join<T><<<(int)ceil_div((int64_t)p.clients * p.M * ceil_div(p.N, 16 / sizeof(T)), 256), 256, 0, stream>>>(s, p.e);
     return hipGetLastError();
 }
 

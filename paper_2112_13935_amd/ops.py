@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -70,6 +71,23 @@ class aet_dropout(C.Structure):
     _fields_ = [(f, _i32) for f in ("dtype", "n", "rows", "cols")] + _DROP + _mat("x") + _mat("residual") + _mat("y")
 
 
+def _packer(record):
+    """The record's fields in its C layout, as bytes: several times faster than to fill the ctypes structure."""
+    code, end = "", 0
+    letters = {_i32: "i", _i64: "q", _vp: "Q", C.c_uint64: "Q", C.c_double: "d", C.c_float: "f"}
+    for name, kind in record._fields_:
+        field = getattr(record, name)
+        code += "x" * (field.offset - end) + letters[kind]
+        end = field.offset + field.size
+    packer = struct.Struct("=" + code + "x" * (C.sizeof(record) - end))
+    assert packer.size == C.sizeof(record)
+    return packer.pack
+
+
+_pack_linear, _pack_linear_grad = _packer(aet_linear), _packer(aet_linear_grad)
+_pack_norm, _pack_norm_grad, _pack_dropout = _packer(aet_group_norm), _packer(aet_group_norm_grad), _packer(aet_dropout)
+
+_U64 = (1 << 64) - 1
 _LIB = None
 
 
@@ -106,53 +124,59 @@ class _Call:
         self.code = _DTYPES.get(x.dtype, -1)
         if self.code < 0 or self.index < 0:
             raise ValueError(f"float32 or bfloat16 on a GPU is wanted, got {x.dtype} on {x.device}")
-        self.stream = stream
+        self.stream = None
         self.handle = torch._C._cuda_getCurrentRawStream(self.index)
-        if stream is not None:
-            if stream.cuda_stream == self.handle:
-                self.stream = None
-            self.handle = stream.cuda_stream
+        if stream is not None and stream.cuda_stream != self.handle:
+            self.stream, self.handle = stream, stream.cuda_stream
 
-    def _ptr(self, name: str, t: torch.Tensor, shape) -> int:
+    def _strides(self, name: str, t: torch.Tensor, shape):
         if t.dtype is not self.dtype or t.get_device() != self.index:
             raise ValueError(f"{name} is {t.dtype} on {t.device}, the others are {self.dtype} on GPU {self.index}")
         if t.shape != shape:
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        st = t.stride()
+        if st[-1] != 1 and shape[-1] > 1:
+            raise ValueError(f"{name}: the last axis has stride {st[-1]}, 1 is wanted")
         if self.stream is not None:   # its memory is not given out again before that stream is done with it
             t.record_stream(self.stream)
-        return t.data_ptr()
+        return st
 
     def mat(self, name: str, t: Optional[torch.Tensor], shape):
         """Pointer and strides of a matrix per client, or of one (two axes)."""
         if t is None:
-            return None, 0, 0
-        ptr, st = self._ptr(name, t, shape), t.stride()
-        if st[-1] != 1 and shape[-1] > 1:
-            raise ValueError(f"{name}: the last axis has stride {st[-1]}, 1 is wanted")
-        return (ptr, st[0], st[1]) if len(st) == 3 else (ptr, shape[0] * st[0], st[0])
+            return 0, 0, 0
+        st = self._strides(name, t, shape)
+        return (t.data_ptr(), st[0], st[1]) if len(st) == 3 else (t.data_ptr(), shape[0] * st[0], st[0])
 
     def weights(self, name: str, t: Optional[torch.Tensor], shape):
         """The same, of one for all clients where there are two axes."""
-        ptr, client, row = self.mat(name, t, shape)
-        return (ptr, client, row) if len(shape) == 3 else (ptr, 0, row)
+        if t is None:
+            return 0, 0, 0
+        st = self._strides(name, t, shape)
+        return (t.data_ptr(), st[0], st[1]) if len(st) == 3 else (t.data_ptr(), 0, st[0])
 
     def vec(self, name: str, t: Optional[torch.Tensor], n: int, cols: int):
         """Pointer and strides of a vector per client, or of one for all."""
         if t is None:
-            return None, 0, 0
+            return 0, 0, 0
         per = t.dim() == 2
-        ptr, st = self._ptr(name, t, (n, cols) if per else (cols,)), t.stride()
-        if st[-1] != 1 and cols > 1:
-            raise ValueError(f"{name}: the last axis has stride {st[-1]}, 1 is wanted")
-        return ptr, st[0] if per else 0, 0
+        st = self._strides(name, t, (n, cols) if per else (cols,))
+        return t.data_ptr(), st[0] if per else 0, 0
 
     def maps(self, name: str, t: Optional[torch.Tensor], shape):
         if t is None:
-            return None, 0, 0, 0
-        ptr, st = self._ptr(name, t, shape), t.stride()
-        if st[-1] != 1 and shape[-1] > 1:
-            raise ValueError(f"{name}: the last axis has stride {st[-1]}, 1 is wanted")
-        return (ptr, st[0], st[1], st[2]) if len(st) == 4 else (ptr, shape[0] * st[0], st[0], st[1])
+            return 0, 0, 0, 0
+        st = self._strides(name, t, shape)
+        return (t.data_ptr(), st[0], st[1], st[2]) if len(st) == 4 else (t.data_ptr(), shape[0] * st[0], st[0], st[1])
+
+    def new_mat(self, x: torch.Tensor, wanted: bool, shape):
+        """A new matrix per client (three axes) or one (two), without gaps: it, and as mat gives it."""
+        if not wanted:
+            return None, (0, 0, 0)
+        t = x.new_empty(shape)
+        if self.stream is not None:
+            t.record_stream(self.stream)
+        return t, (t.data_ptr(), shape[-2] * shape[-1], shape[-1])
 
     def stats(self, name: str, t: torch.Tensor, shape) -> int:
         if t.dtype is not torch.float32 or t.get_device() != self.index or t.shape != shape or not t.is_contiguous():
@@ -161,21 +185,20 @@ class _Call:
             t.record_stream(self.stream)
         return t.data_ptr()
 
-    def run(self, fn, record, workspace_bytes=None):
+    def run(self, fn, record: bytes, workspace_bytes=None):
         """fn(record, workspace, its size, stream) on the tensors' device; its workspace from workspace_bytes(record)."""
         if torch.cuda.current_device() != self.index:
             with torch.cuda.device(self.index):
                 return self.run(fn, record, workspace_bytes)
-        at = C.addressof(record)
         if workspace_bytes is None:
-            rc = fn(at, self.handle)
-        elif size := workspace_bytes(at):
+            rc = fn(record, self.handle)
+        elif size := workspace_bytes(record):
             ws = torch.empty(size, dtype=torch.uint8, device=torch.device("cuda", self.index))
             if self.stream is not None:
                 ws.record_stream(self.stream)
-            rc = fn(at, ws.data_ptr(), size, self.handle)
+            rc = fn(record, ws.data_ptr(), size, self.handle)
         else:
-            rc = fn(at, None, 0, self.handle)
+            rc = fn(record, None, 0, self.handle)
         if rc != AET_OK:
             raise AetError(rc, _LIB.aet_ops_last_error().decode())
 
@@ -208,11 +231,11 @@ def aet_linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Te
     n, rows, inp = _axes(x, 3)
     outs, per = w.shape[-2], w.dim() == 3
     shape = (n, rows, outs) if x.dim() == 3 else (rows, outs)
-    y = x.new_empty(shape) if out is None else out
-    pre = x.new_empty(shape) if keep_pre else None
-    a = aet_linear(call.code, _act(act), n, rows, inp, outs, p, seed, first_row, *call.mat("x", x, x.shape),
+    y, ym = (out, call.mat("out", out, shape)) if out is not None else call.new_mat(x, True, shape)
+    pre, prem = call.new_mat(x, keep_pre, shape)
+    a = _pack_linear(call.code, _act(act), n, rows, inp, outs, p, seed & _U64, first_row, *call.mat("x", x, x.shape),
                    *call.weights("w", w, (n, outs, inp) if per else (outs, inp)), *call.vec("bias", bias, n, outs),
-                   *call.mat("residual", residual, shape), *call.mat("out", y, shape), *call.mat("pre", pre, shape))
+                   *call.mat("residual", residual, shape), *ym, *prem)
     call.run(lib.aet_linear_forward, a, lib.aet_linear_workspace_bytes)
     return y, pre
 
@@ -231,12 +254,12 @@ def aet_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre:
     wshape = (n, outs, inp) if per else (outs, inp)
     if pre is None and act != "none":
         raise ValueError("pre, as the forward call gave it, is wanted where there is an activation")
-    dx = x.new_empty(x.shape) if need[0] else None
+    dx, dxm = call.new_mat(x, need[0], x.shape)
     dw = x.new_empty(wshape) if need[1] else None
     db = x.new_empty(wshape[:-1]) if need[2] else None
-    a = aet_linear_grad(call.code, _act(act), n, rows, inp, outs, p, seed, first_row, *call.mat("dy", dy, shape),
+    a = _pack_linear_grad(call.code, _act(act), n, rows, inp, outs, p, seed & _U64, first_row, *call.mat("dy", dy, shape),
                         *call.mat("x", x, x.shape), *call.weights("w", w, wshape), *call.mat("pre", pre, shape),
-                        *call.mat("dx", dx, x.shape), *call.weights("dw", dw, wshape), *call.vec("db", db, n, outs))
+                        *dxm, *call.weights("dw", dw, wshape), *call.vec("db", db, n, outs))
     call.run(lib.aet_linear_backward, a, lib.aet_linear_backward_workspace_bytes)
     return dx, dw, db
 
@@ -255,7 +278,7 @@ def aet_group_norm_forward(x: torch.Tensor, groups: int, gamma: Optional[torch.T
     y = x.new_empty(x.shape) if out is None else out
     stats = (n, batch, groups) if x.dim() == 4 else (batch, groups)
     mean, rstd = x.new_empty(stats, dtype=torch.float32), x.new_empty(stats, dtype=torch.float32)
-    a = aet_group_norm(call.code, _act(act), n, batch, positions, groups, ch // groups, eps,
+    a = _pack_norm(call.code, _act(act), n, batch, positions, groups, ch // groups, eps,
                        *call.maps("x", x, x.shape), *call.vec("gamma", gamma, n, ch), *call.vec("beta", beta, n, ch),
                        *call.maps("out", y, x.shape), call.stats("mean", mean, stats), call.stats("rstd", rstd, stats))
     call.run(lib.aet_group_norm_forward, a, lib.aet_group_norm_workspace_bytes)
@@ -280,7 +303,7 @@ def aet_group_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
     dx = x.new_empty(x.shape) if need[0] else None
     dgamma = x.new_empty(gamma.shape) if need[1] and gamma is not None else None
     dbeta = x.new_empty(beta.shape) if need[1] and beta is not None else None
-    a = aet_group_norm_grad(call.code, _act(act), n, batch, positions, groups, ch // groups,
+    a = _pack_norm_grad(call.code, _act(act), n, batch, positions, groups, ch // groups,
                             *call.maps("dy", dy, x.shape), *call.maps("x", x, x.shape),
                             call.stats("mean", mean, stats), call.stats("rstd", rstd, stats),
                             *call.vec("gamma", gamma, n, ch), *call.vec("beta", beta, n, ch),
@@ -294,9 +317,9 @@ def _dropout(fn: str, x, p, seed, first_row, residual, out, stream):
     lib = _LIB or load_library()
     call = _Call(x, stream)
     n, rows, cols = _axes(x, 3)
-    y = x.new_empty(x.shape) if out is None else out
-    a = aet_dropout(call.code, n, rows, cols, p, seed, first_row, *call.mat("x", x, x.shape),
-                    *call.mat("residual", residual, x.shape), *call.mat("out", y, x.shape))
+    y, ym = (out, call.mat("out", out, x.shape)) if out is not None else call.new_mat(x, True, x.shape)
+    a = _pack_dropout(call.code, n, rows, cols, p, seed & _U64, first_row, *call.mat("x", x, x.shape),
+                    *call.mat("residual", residual, x.shape), *ym)
     call.run(getattr(lib, fn), a)
     return y
 
