@@ -28,14 +28,15 @@ struct Where {
     int group[8];                             // of its channels
 };
 template <int V>
-__device__ __forceinline__ Where where(const NormShape &s, int batch, int width, int64_t block) {
+__device__ __forceinline__ Where where(const NormShape &s, int batch, int width, uint32_t block) {
     Where w;
-    w.sample = block / s.spans;
-    w.ch0 = (int)(block % s.spans) * s.span;
+    const uint32_t sample = block / (uint32_t)s.spans, client = sample / (uint32_t)batch;
+    w.sample = sample;
+    w.ch0 = (int)(block - sample * (uint32_t)s.spans) * s.span;
     w.chans = s.channels - w.ch0 < s.span ? s.channels - w.ch0 : s.span;
-    w.client = w.sample / batch;
-    w.in_batch = w.sample - w.client * batch;
-    w.lane = threadIdx.x / s.pieces;
+    w.client = client;
+    w.in_batch = sample - client * (uint32_t)batch;
+    w.lane = threadIdx.x / (uint32_t)s.pieces;
     w.piece = threadIdx.x - w.lane * s.pieces;
     w.ch = w.ch0 + w.piece * V;
     w.count = w.lane < s.lanes ? w.chans - w.piece * V : 0;
@@ -54,36 +55,43 @@ __device__ __forceinline__ Where where(const NormShape &s, int batch, int width,
     return w;
 }
 
-// Sums by channel over the workgroup's threads: tot[k], k < chans.  lds: threads * V floats.
-template <int V>
-__device__ __forceinline__ void channel_sums(const NormShape &s, const Where &w, const float (&v)[V], float *lds, float *tot) {
-    const int line = s.pieces * V;
-    __syncthreads();
-    if (w.lane < s.lanes) {
+// Sums by channel over the workgroup's threads, of N arrays at a time: tot[n * span + k], k < chans.  lds: N * threads * V
+// floats.  First within waves where a wave has whole rows of pieces, then by halving the rows until two are left.
+template <int V, int N>
+__device__ __forceinline__ void channel_sums(const NormShape &s, const Where &w, float (&v)[N][V], float *lds, float *tot) {
+    const int line = s.pieces * V, all = s.threads * V;
+    int rows = s.lanes, row = w.lane;
+    bool mine = w.lane < s.lanes;
+    if (s.pieces < 64 && !(s.pieces & (s.pieces - 1))) {   // (threads without a position have zeros)
+        for (int off = 32; off >= s.pieces; off >>= 1)
 #pragma unroll
-        for (int e = 0; e < V; ++e) lds[w.lane * line + w.piece * V + e] = v[e];
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[n][e] += __shfl_xor(v[n][e], off, 64);
+        rows = s.threads / 64;
+        row = threadIdx.x / 64;
+        mine = threadIdx.x % 64 < s.pieces;
     }
     __syncthreads();
-    // up to 16 threads a channel, then one
-    int parts = blockDim.x / line;
-    parts = parts > 16 ? 16 : parts < 1 ? 1 : parts;
-    if (parts > s.lanes) parts = s.lanes;
-    const int part = threadIdx.x / line;
-    if (parts > 1) {
-        float sum = 0;
-        if (part < parts)
-            for (int l = part; l < s.lanes; l += parts) sum += lds[l * line + threadIdx.x - part * line];
-        __syncthreads();
-        if (part < parts) lds[threadIdx.x] = sum;
-        __syncthreads();
-    } else {
-        parts = s.lanes;
+    if (mine) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < V; e += 4)
+                *(f4 *)(lds + n * all + row * line + w.piece * V + e) = f4{v[n][e], v[n][e + 1], v[n][e + 2], v[n][e + 3]};
     }
-    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
-        float sum = 0;
-        for (int l = 0; l < parts; ++l) sum += lds[l * line + k];
-        tot[k] = sum;
+    __syncthreads();
+    while (rows > 2) {
+        const int half = (rows + 1) / 2, count = (rows - half) * line;
+        for (int i = threadIdx.x; i < count; i += blockDim.x)
+#pragma unroll
+            for (int n = 0; n < N; ++n) lds[n * all + i] += lds[n * all + half * line + i];
+        __syncthreads();
+        rows = half;
     }
+    for (int k = threadIdx.x; k < w.chans; k += blockDim.x)
+#pragma unroll
+        for (int n = 0; n < N; ++n) tot[n * s.span + k] = lds[n * all + k] + (rows > 1 ? lds[n * all + line + k] : 0.0f);
     __syncthreads();
 }
 // Sums of a group's channels, a wave per group: out[g] = scale * sum of tot[k] (* by[k])
@@ -129,26 +137,32 @@ __global__ __launch_bounds__(kThreads) void k_norm_whole(aet_group_norm a, NormS
         const int pos = w.lane + i * s.lanes;
         raw[i] = load_raw<T, V>(x + pos * a.x.row, pos < a.positions ? w.count : 0);
     }
-    float acc[V] = {};
+    float gamma[V], beta[V];
+    const auto parameters = [&]() {
+        params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
+        params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+    };
+    if (N <= 4) parameters();   // early where there are registers for it (16 positions: 88 instead of 80, 124 -> 130 us)
+    float acc[1][V] = {};
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] += (float)raw[i][e];
+        for (int e = 0; e < V; ++e) acc[0][e] += (float)raw[i][e];
     const int groups = w.chans / a.width, g0 = w.ch0 / a.width;
     const float inv = 1.0f / ((float)a.positions * (float)a.width);
     channel_sums(s, w, acc, lds, tot);
     group_sums(tot, nullptr, groups, a.width, inv, stat);
-    float mean[V], scale[V], beta[V];
+    float mean[V], scale[V];
     by_channel(w, g0, stat, mean);
 #pragma unroll
-    for (int e = 0; e < V; ++e) acc[e] = 0;
+    for (int e = 0; e < V; ++e) acc[0][e] = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if (w.lane + i * s.lanes < a.positions) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float d = (float)raw[i][e] - mean[e];
-                acc[e] += d * d;
+                acc[0][e] += d * d;
             }
         }
     channel_sums(s, w, acc, lds, tot);
@@ -162,10 +176,9 @@ __global__ __launch_bounds__(kThreads) void k_norm_whole(aet_group_norm a, NormS
     }
     __syncthreads();
     by_channel(w, g0, stat, scale);
-    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, acc);
-    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+    if (N > 4) parameters();
 #pragma unroll
-    for (int e = 0; e < V; ++e) scale[e] *= acc[e];
+    for (int e = 0; e < V; ++e) scale[e] *= gamma[e];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int pos = w.lane + i * s.lanes;
@@ -195,7 +208,7 @@ __device__ __forceinline__ void slopes(int act, const wide<T, V> &x, const wide<
 template <typename T, int V, int N>
 __global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_grad a, NormShape s) {
     extern __shared__ float lds[];
-    float *const totA = lds + s.threads * V, *const totB = totA + s.span, *const gam = totB + s.span, *const stat = gam + s.span;
+    float *const totA = lds + 2 * s.threads * V, *const totB = totA + s.span, *const gam = totB + s.span, *const stat = gam + s.span;
     const Where w = where<V>(s, a.batch, a.width, blockIdx.x);
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
@@ -212,7 +225,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_gra
     by_channel(w, 0, a.rstd + w.sample * a.groups, rstd);
     params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
     params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
-    float A[V] = {}, B[V] = {};
+    float AB[2][V] = {};
     float d[N][V];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -220,12 +233,11 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_gra
         slopes<T, V>(a.act, rx[i], rd[i], mean, rstd, gamma, beta, d[i], xh);   // dy is 0 where there is no position
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            A[e] += d[i][e];
-            B[e] += d[i][e] * xh[e];
+            AB[0][e] += d[i][e];
+            AB[1][e] += d[i][e] * xh[e];
         }
     }
-    channel_sums(s, w, A, lds, totA);
-    channel_sums(s, w, B, lds, totB);
+    channel_sums(s, w, AB, lds, totA);
     for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
         float *to = s.sums + w.sample * 2 * s.channels + w.ch0 + k;
         to[0] = totA[k];
@@ -238,15 +250,16 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_gra
     group_sums(totA, gam, groups, a.width, inv, stat);
     group_sums(totB, gam, groups, a.width, inv, stat + groups);
     T *dx = (T *)a.dx.p + w.client * a.dx.client + w.in_batch * a.dx.sample + w.ch;
-    by_channel(w, g0, stat, A);
-    by_channel(w, g0, stat + groups, B);
+    float s1[V], s2[V];
+    by_channel(w, g0, stat, s1);
+    by_channel(w, g0, stat + groups, s2);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int pos = w.lane + i * s.lanes;
         if (pos >= a.positions || w.count <= 0) continue;
         float v[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = (d[i][e] * gamma[e] - A[e] - ((float)rx[i][e] - mean[e]) * rstd[e] * B[e]) * rstd[e];
+        for (int e = 0; e < V; ++e) v[e] = (d[i][e] * gamma[e] - s1[e] - ((float)rx[i][e] - mean[e]) * rstd[e] * s2[e]) * rstd[e];
         store_some(dx + pos * a.dx.row, w.count, v);
     }
 }
@@ -274,36 +287,31 @@ __device__ __forceinline__ void each_position(int pos, int end, int step, int co
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void k_norm_strips(aet_group_norm a, NormShape s) {
     extern __shared__ float lds[];
-    float *const tot = lds + s.threads * V;
-    const int strip = blockIdx.x % s.strips;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.strips);
+    float *const tot = lds + 2 * s.threads * V;
+    const int strip = blockIdx.x % (uint32_t)s.strips;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.strips);
     const int first = strip * s.strip, end = a.positions - first < s.strip ? a.positions : first + s.strip;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     // about the strip's first value, so that the squares do not cancel where the mean is far from 0
     const wide<T, V> about = load_raw<T, V>(x + first * a.x.row, w.count);
-    float S[V] = {}, Q[V] = {};
+    float SQ[2][V] = {};
     wide<T, V> raw[4];
     each_position(first + w.lane, end, s.lanes, w.count, V, [&](int pos, int i, int count) { raw[i] = load_raw<T, V>(x + pos * a.x.row, count); },
                   [&](int, int i, int) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float d = (float)raw[i][e] - (float)about[e];
-            S[e] += d;
-            Q[e] += d * d;
+            SQ[0][e] += d;
+            SQ[1][e] += d * d;
         }
     });
     float *to = s.sums + (w.sample * s.strips + strip) * 2 * s.channels + w.ch0;
     const float inv = 1.0f / (float)(end - first);
-    channel_sums(s, w, S, lds, tot);
+    channel_sums(s, w, SQ, lds, tot);
     const T *about0 = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + first * a.x.row + w.ch0;
     for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
-        const float off = tot[k];
-        to[k] = (float)about0[k] + off * inv;
-        to[s.channels + k] = off * off * inv;
-    }
-    channel_sums(s, w, Q, lds, tot);
-    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
-        const float m2 = tot[k] - to[s.channels + k];
+        const float off = tot[k] * inv, m2 = tot[s.span + k] - tot[k] * off;
+        to[k] = (float)about0[k] + off;
         to[s.channels + k] = m2 < 0 ? 0.0f : m2;
     }
 }
@@ -318,8 +326,8 @@ __device__ __forceinline__ float block_sum(float v, float *lds) {
 }
 __global__ __launch_bounds__(256) void k_norm_union(aet_group_norm a, NormShape s) {
     __shared__ float lds[4];
-    const int64_t sample = blockIdx.x / a.groups;
-    const int ch = (int)(blockIdx.x % a.groups) * a.width;
+    const int64_t sample = blockIdx.x / (uint32_t)a.groups;
+    const int ch = (int)(blockIdx.x % (uint32_t)a.groups) * a.width;
     const float *from = s.sums + sample * s.strips * 2 * s.channels + ch;
     const int64_t entries = (int64_t)s.strips * a.width;
     const float inv = 1.0f / ((float)a.positions * (float)a.width);
@@ -348,8 +356,8 @@ __global__ __launch_bounds__(256) void k_norm_union(aet_group_norm a, NormShape 
 
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void k_norm_apply(aet_group_norm a, NormShape s) {
-    const int part = blockIdx.x % s.parts;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.parts);
+    const int part = blockIdx.x % (uint32_t)s.parts;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.parts);
     if (w.count <= 0) return;
     const int first = part * s.part, end = a.positions - first < s.part ? a.positions : first + s.part;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
@@ -376,13 +384,13 @@ __global__ __launch_bounds__(kThreads) void k_norm_apply(aet_group_norm a, NormS
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void k_norm_back_strips(aet_group_norm_grad a, NormShape s) {
     extern __shared__ float lds[];
-    float *const tot = lds + s.threads * V;
-    const int strip = blockIdx.x % s.strips;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.strips);
+    float *const tot = lds + 2 * s.threads * V;
+    const int strip = blockIdx.x % (uint32_t)s.strips;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.strips);
     const int first = strip * s.strip, end = a.positions - first < s.strip ? a.positions : first + s.strip;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
-    float mean[V], rstd[V], gamma[V], beta[V], A[V] = {}, B[V] = {};
+    float mean[V], rstd[V], gamma[V], beta[V], AB[2][V] = {};
     by_channel(w, 0, a.mean + w.sample * a.groups, mean);
     by_channel(w, 0, a.rstd + w.sample * a.groups, rstd);
     params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
@@ -397,23 +405,24 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_strips(aet_group_norm_gr
         slopes<T, V>(a.act, rx[i], rd[i], mean, rstd, gamma, beta, d, xh);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            A[e] += d[e];
-            B[e] += d[e] * xh[e];
+            AB[0][e] += d[e];
+            AB[1][e] += d[e] * xh[e];
         }
     });
     float *to = s.sums + (w.sample * s.strips + strip) * 2 * s.channels + w.ch0;
-    channel_sums(s, w, A, lds, tot);
-    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) to[k] = tot[k];
-    channel_sums(s, w, B, lds, tot);
-    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) to[s.channels + k] = tot[k];
+    channel_sums(s, w, AB, lds, tot);
+    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
+        to[k] = tot[k];
+        to[s.channels + k] = tot[s.span + k];
+    }
 }
 
 // The strips' sums by channel go to the first strip's place; s1 and s2, divided by their number, to the group's.
 template <typename T>
 __global__ __launch_bounds__(256) void k_norm_back_union(aet_group_norm_grad a, NormShape s) {
     __shared__ float lds[4];
-    const int64_t sample = blockIdx.x / a.groups, client = sample / a.batch;
-    const int ch = (int)(blockIdx.x % a.groups) * a.width;
+    const int64_t sample = blockIdx.x / (uint32_t)a.groups, client = (uint32_t)sample / (uint32_t)a.batch;
+    const int ch = (int)(blockIdx.x % (uint32_t)a.groups) * a.width;
     float *from = s.sums + sample * s.strips * 2 * s.channels + ch;
     const float inv = 1.0f / ((float)a.positions * (float)a.width);
     float s1 = 0, s2 = 0;
@@ -440,8 +449,8 @@ __global__ __launch_bounds__(256) void k_norm_back_union(aet_group_norm_grad a, 
 
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void k_norm_back_apply(aet_group_norm_grad a, NormShape s) {
-    const int part = blockIdx.x % s.parts;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / s.parts);
+    const int part = blockIdx.x % (uint32_t)s.parts;
+    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.parts);
     if (w.count <= 0) return;
     const int first = part * s.part, end = a.positions - first < s.part ? a.positions : first + s.part;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
@@ -472,8 +481,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_apply(aet_group_norm_gra
 template <typename T>
 __global__ __launch_bounds__(256) void k_norm_params(aet_group_norm_grad a, const float *sums, int64_t apart, int channels, int across, int64_t samples) {
     __shared__ float lds[2][4][64];
-    const int64_t client = blockIdx.x / across;
-    const int k = threadIdx.x % 64, part = threadIdx.x / 64, ch = blockIdx.x % across * 64 + k;
+    const int64_t client = blockIdx.x / (uint32_t)across;
+    const int k = threadIdx.x % 64, part = threadIdx.x / 64, ch = (int)(blockIdx.x % (uint32_t)across) * 64 + k;
     float A = 0, B = 0;
     if (ch < channels) {
 #pragma unroll 8
@@ -543,7 +552,7 @@ static NormPlan make_plan(int64_t samples, int positions, int groups, int width,
         s.threads = (int)ceil_div(s.pieces * s.lanes, 64) * 64;
         s.strips = 1;
         s.strip = positions;
-        p.lds = sizeof(float) * ((size_t)s.threads * V + (back ? 3 : 1) * s.span + 2 * best);
+        p.lds = sizeof(float) * ((size_t)(back ? 2 : 1) * s.threads * V + (back ? 3 : 1) * s.span + 2 * best);
         p.sums_bytes = back ? up256((size_t)samples * 2 * s.channels * sizeof(float)) : 0;
         p.bytes = p.sums_bytes;
         return p;
@@ -560,7 +569,7 @@ static NormPlan make_plan(int64_t samples, int positions, int groups, int width,
     while (s.part < positions && samples * s.spans * ceil_div(positions, s.part) > 8192) s.part *= 2;
     s.parts = (int)ceil_div(positions, s.part);
     s.threads = (int)ceil_div(s.pieces * s.lanes, 64) * 64;
-    p.lds = sizeof(float) * ((size_t)s.threads * V + s.span);
+    p.lds = sizeof(float) * 2 * ((size_t)s.threads * V + s.span);
     p.sums_bytes = up256((size_t)samples * s.strips * 2 * s.channels * sizeof(float));
     p.bytes = p.sums_bytes + up256((size_t)samples * 2 * groups * sizeof(float));
     return p;
