@@ -19,7 +19,7 @@ struct NormShape {
     int strips, strip;      // positions' parts: for the sums (three kernels only)
     int parts, part;        // and for the second pass
     float *sums;            // whole: [sample][2][channels]; else [sample][strips][2][channels]
-    float *stats;           // [sample][2][groups], three kernels only: mean and rstd, or s1 and s2 (both by number)
+    float *stats;           // [sample][2][groups], three kernels only: mean and rstd; or s1 rstd and s2 rstd^2, s1 and s2 over the number of values
 };
 
 struct Where {
@@ -191,18 +191,35 @@ __global__ __launch_bounds__(kThreads) void k_norm_whole(aet_group_norm a, NormS
     }
 }
 
-// d = dy * act'(t) at one position, and x^
+// d = dy * act'(t) and xm = x - mean at one position; scale: rstd * gamma
 template <typename T, int V>
-__device__ __forceinline__ void slopes(int act, const wide<T, V> &x, const wide<T, V> &dy, const float (&mean)[V], const float (&rstd)[V],
-                                       const float (&gamma)[V], const float (&beta)[V], float (&d)[V], float (&xh)[V]) {
+__device__ __forceinline__ void slopes(int act, const wide<T, V> &x, const wide<T, V> &dy, const float (&mean)[V], const float (&scale)[V],
+                                       const float (&beta)[V], float (&d)[V], float (&xm)[V]) {
     float t[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        xh[e] = ((float)x[e] - mean[e]) * rstd[e];
-        t[e] = __builtin_fmaf(xh[e], gamma[e], beta[e]);
+        xm[e] = (float)x[e] - mean[e];
+        t[e] = __builtin_fmaf(xm[e], scale[e], beta[e]);
         d[e] = (float)dy[e];
     }
     slope_each(act, t, d);
+}
+// What a thread's channels need for it.
+template <typename T, int V>
+__device__ __forceinline__ void slope_params(const aet_group_norm_grad &a, const Where &w, float (&mean)[V], float (&scale)[V], float (&beta)[V]) {
+    float rstd[V];
+    by_channel(w, 0, a.mean + w.sample * a.groups, mean);
+    by_channel(w, 0, a.rstd + w.sample * a.groups, rstd);
+    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, scale);
+    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+#pragma unroll
+    for (int e = 0; e < V; ++e) scale[e] *= rstd[e];
+}
+// dx = (d gamma - s1 - x^ s2) rstd = d scale - (x - mean) (rstd^2 s2) - rstd s1
+template <int V>
+__device__ __forceinline__ void to_dx(const float (&scale)[V], const float (&c1)[V], const float (&c2)[V], const float (&xm)[V], float (&d)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) d[e] = __builtin_fmaf(d[e], scale[e], -__builtin_fmaf(xm[e], c2[e], c1[e]));
 }
 
 template <typename T, int V, int N>
@@ -220,26 +237,25 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_gra
         rd[i] = load_raw<T, V>(dy + pos * a.dy.row, count);
     }
     const int groups = w.chans / a.width, g0 = w.ch0 / a.width;
-    float mean[V], rstd[V], gamma[V], beta[V];
-    by_channel(w, 0, a.mean + w.sample * a.groups, mean);
-    by_channel(w, 0, a.rstd + w.sample * a.groups, rstd);
-    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
-    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+    float mean[V], scale[V], beta[V];
+    slope_params<T>(a, w, mean, scale, beta);
     float AB[2][V] = {};
     float d[N][V];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        float xh[V];
-        slopes<T, V>(a.act, rx[i], rd[i], mean, rstd, gamma, beta, d[i], xh);   // dy is 0 where there is no position
+        float xm[V];
+        slopes<T, V>(a.act, rx[i], rd[i], mean, scale, beta, d[i], xm);   // dy is 0 where there is no position
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             AB[0][e] += d[i][e];
-            AB[1][e] += d[i][e] * xh[e];
+            AB[1][e] += d[i][e] * xm[e];
         }
     }
     channel_sums(s, w, AB, lds, totA);
+    const float *const rstd_of = a.rstd + w.sample * a.groups + g0;
     for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
         float *to = s.sums + w.sample * 2 * s.channels + w.ch0 + k;
+        totB[k] *= rstd_of[k / a.width];
         to[0] = totA[k];
         to[s.channels] = totB[k];
         gam[k] = a.gamma.p ? (float)((const T *)a.gamma.p)[w.client * a.gamma.client + w.ch0 + k] : 1.0f;
@@ -249,18 +265,24 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_gra
     const float inv = 1.0f / ((float)a.positions * (float)a.width);
     group_sums(totA, gam, groups, a.width, inv, stat);
     group_sums(totB, gam, groups, a.width, inv, stat + groups);
+    for (int g = threadIdx.x; g < groups; g += blockDim.x) {
+        stat[g] *= rstd_of[g];
+        stat[groups + g] *= rstd_of[g] * rstd_of[g];
+    }
+    __syncthreads();
     T *dx = (T *)a.dx.p + w.client * a.dx.client + w.in_batch * a.dx.sample + w.ch;
-    float s1[V], s2[V];
-    by_channel(w, g0, stat, s1);
-    by_channel(w, g0, stat + groups, s2);
+    float c1[V], c2[V];
+    by_channel(w, g0, stat, c1);
+    by_channel(w, g0, stat + groups, c2);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int pos = w.lane + i * s.lanes;
         if (pos >= a.positions || w.count <= 0) continue;
-        float v[V];
+        float xm[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = (d[i][e] * gamma[e] - s1[e] - ((float)rx[i][e] - mean[e]) * rstd[e] * s2[e]) * rstd[e];
-        store_some(dx + pos * a.dx.row, w.count, v);
+        for (int e = 0; e < V; ++e) xm[e] = (float)rx[i][e] - mean[e];
+        to_dx(scale, c1, c2, xm, d[i]);
+        store_some(dx + pos * a.dx.row, w.count, d[i]);
     }
 }
 
@@ -390,34 +412,31 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_strips(aet_group_norm_gr
     const int first = strip * s.strip, end = a.positions - first < s.strip ? a.positions : first + s.strip;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
-    float mean[V], rstd[V], gamma[V], beta[V], AB[2][V] = {};
-    by_channel(w, 0, a.mean + w.sample * a.groups, mean);
-    by_channel(w, 0, a.rstd + w.sample * a.groups, rstd);
-    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
-    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+    float mean[V], scale[V], beta[V], AB[2][V] = {};
+    slope_params<T>(a, w, mean, scale, beta);
     wide<T, V> rx[4], rd[4];
     const auto load = [&](int pos, int i, int count) {
         rx[i] = load_raw<T, V>(x + pos * a.x.row, count);
         rd[i] = load_raw<T, V>(dy + pos * a.dy.row, count);
     };
-    each_position(first + w.lane, end, s.lanes, w.count, V, load, [&](int pos, int i, int count) {
-        float d[V], xh[V];
-        slopes<T, V>(a.act, rx[i], rd[i], mean, rstd, gamma, beta, d, xh);
+    each_position(first + w.lane, end, s.lanes, w.count, V, load, [&](int, int i, int) {
+        float d[V], xm[V];
+        slopes<T, V>(a.act, rx[i], rd[i], mean, scale, beta, d, xm);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             AB[0][e] += d[e];
-            AB[1][e] += d[e] * xh[e];
+            AB[1][e] += d[e] * xm[e];
         }
     });
     float *to = s.sums + (w.sample * s.strips + strip) * 2 * s.channels + w.ch0;
     channel_sums(s, w, AB, lds, tot);
     for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
         to[k] = tot[k];
-        to[s.channels + k] = tot[s.span + k];
+        to[s.channels + k] = tot[s.span + k] * a.rstd[w.sample * a.groups + (w.ch0 + k) / a.width];
     }
 }
 
-// The strips' sums by channel go to the first strip's place; s1 and s2, divided by their number, to the group's.
+// The strips' sums by channel go to the first strip's place; what to_dx wants, s1 rstd and s2 rstd^2, to the group's.
 template <typename T>
 __global__ __launch_bounds__(256) void k_norm_back_union(aet_group_norm_grad a, NormShape s) {
     __shared__ float lds[4];
@@ -443,8 +462,9 @@ __global__ __launch_bounds__(256) void k_norm_back_union(aet_group_norm_grad a, 
     s2 = block_sum(s2, lds) * inv;
     if (threadIdx.x) return;
     const int64_t at = sample * 2 * a.groups + ch / a.width;
-    s.stats[at] = s1;
-    s.stats[at + a.groups] = s2;
+    const float rstd = a.rstd[blockIdx.x];
+    s.stats[at] = s1 * rstd;
+    s.stats[at + a.groups] = s2 * rstd * rstd;
 }
 
 template <typename T, int V>
@@ -456,23 +476,19 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_apply(aet_group_norm_gra
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
     T *dx = (T *)a.dx.p + w.client * a.dx.client + w.in_batch * a.dx.sample + w.ch;
-    float mean[V], rstd[V], gamma[V], beta[V], s1[V], s2[V];
-    by_channel(w, 0, a.mean + w.sample * a.groups, mean);
-    by_channel(w, 0, a.rstd + w.sample * a.groups, rstd);
-    by_channel(w, 0, s.stats + w.sample * 2 * a.groups, s1);
-    by_channel(w, 0, s.stats + (w.sample * 2 + 1) * a.groups, s2);
-    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
-    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+    float mean[V], scale[V], beta[V], c1[V], c2[V];
+    slope_params<T>(a, w, mean, scale, beta);
+    by_channel(w, 0, s.stats + w.sample * 2 * a.groups, c1);
+    by_channel(w, 0, s.stats + (w.sample * 2 + 1) * a.groups, c2);
     wide<T, V> rx[4], rd[4];
     const auto load = [&](int pos, int i, int count) {
         rx[i] = load_raw<T, V>(x + pos * a.x.row, count);
         rd[i] = load_raw<T, V>(dy + pos * a.dy.row, count);
     };
     each_position(first + w.lane, end, s.lanes, w.count, V, load, [&](int pos, int i, int count) {
-        float d[V], xh[V];
-        slopes<T, V>(a.act, rx[i], rd[i], mean, rstd, gamma, beta, d, xh);
-#pragma unroll
-        for (int e = 0; e < V; ++e) d[e] = (d[e] * gamma[e] - s1[e] - xh[e] * s2[e]) * rstd[e];
+        float d[V], xm[V];
+        slopes<T, V>(a.act, rx[i], rd[i], mean, scale, beta, d, xm);
+        to_dx(scale, c1, c2, xm, d);
         store_some(dx + pos * a.dx.row, count, d);
     });
 }
