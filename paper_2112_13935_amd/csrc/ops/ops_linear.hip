@@ -59,13 +59,14 @@ __global__ __launch_bounds__(256) void k_dz(aet_linear_grad a, Drop d, DzShape s
                 float v[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) v[e] = (float)rd[i][e];
-                if (d.least) drop_apply(d, drop_row(d, client * a.rows + r), col, v);
                 if (pre) {
                     float z[V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) z[e] = (float)rz[i][e];
                     slope_each(a.act, z, v);
                 }
+                // last, so that what the forward pass took out has a gradient of 0 whatever z was
+                if (d.least) drop_apply(d, drop_row(d, client * a.rows + r), col, v);
                 if (dz) store_some(dz + (client * a.rows + r) * s.dz_row + col, count, v);
 #pragma unroll
                 for (int e = 0; e < V; ++e) sum[e] += v[e];

@@ -211,6 +211,42 @@ def test_values_that_are_not_finite(ops, dtype):
         assert bool((y[0].cpu()[gone] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+def test_what_dropout_took_out_has_no_gradient(ops, dtype, act):
+    """Infinities and NaN in z and dy, where the mask is 0, leave no trace."""
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(4)
+    n, rows, inp, out = 1, 70, 40, 72
+    x, w = rand(g, (n, rows, inp), dt), rand(g, (n, out, inp), dt)
+    dy, pre = rand(g, (n, rows, out), dt), rand(g, (n, rows, out), dt)
+    gone = (O.kept(9, 0, rows, out, 0.5) == 0).to(DEV)[None]
+    want = ops.aet_linear_backward(dy, x, w, pre, act=act, p=0.5, seed=9)
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        z, d = pre.clone(), dy.clone()
+        z[gone] = bad
+        d[gone] = bad
+        got = ops.aet_linear_backward(d, x, w, z, act=act, p=0.5, seed=9)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_into_given_places(ops, dtype):
+    """dw and db as parts of one row of parameters a client, dx with rows apart."""
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(6)
+    n, rows, inp, out = 3, 45, 56, 24
+    x, w, dy = rand(g, (n, rows, inp), dt), rand(g, (n, out, inp), dt), rand(g, (n, rows, out), dt)
+    want = ops.aet_linear_backward(dy, x, w)
+    flat = torch.full((n, out * inp + out + 9), 5.0, dtype=dt, device=DEV)
+    dw, db = flat[:, 3:3 + out * inp].view(n, out, inp), flat[:, 3 + out * inp:3 + out * inp + out]
+    wide = torch.full((n, rows, inp + 7), 5.0, dtype=dt, device=DEV)
+    got = ops.aet_linear_backward(dy, x, w, out=(wide[:, :, 2:2 + inp], dw, db))
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and got[1].data_ptr() == dw.data_ptr()
+    assert bool((flat[:, :3] == 5).all()) and bool((flat[:, 3 + out * inp + out:] == 5).all())
+    assert bool((wide[:, :, :2] == 5).all()) and bool((wide[:, :, 2 + inp:] == 5).all())
+
+
 def test_differences(ops):
     """The gradient of the whole operator against central differences of the forward call, in fp32: sum(y * c) along
     random directions.  Steps of 1/64 with values of order one: the third derivatives give 1e-4 of relative error at

@@ -74,6 +74,12 @@ def test_group_norm_parameters(ops, dtype):   # noqa: F811
     whole = torch.full((n, b, P, ch + 5), 3.0, dtype=dt, device=DEV)
     whole[..., 2:2 + ch] = x
     ops.aet_group_norm_forward(whole[..., 2:2 + ch], G, gamma, beta, act="gelu", out=whole[..., 2:2 + ch])
+    # dx in dy's place, dgamma and dbeta as parts of one row of parameters a client
+    onto, flat = dy.clone(), torch.full((n, 2 * ch + 3), 5.0, dtype=dt, device=DEV)
+    pg, pb = gamma.expand(n, ch).contiguous(), beta.expand(n, ch).contiguous()
+    want = ops.aet_group_norm_backward(dy, x, mean, rstd, pg, pb, act="gelu")
+    got = ops.aet_group_norm_backward(onto, x, mean, rstd, pg, pb, act="gelu", out=(onto, flat[:, 1:1 + ch], flat[:, 2 + ch:2 + 2 * ch]))
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(onto, want[0]) and bool((flat[:, 0] == 5).all())
     assert torch.equal(whole[..., 2:2 + ch], y) and bool((whole[..., :2] == 3).all()) and bool((whole[..., 2 + ch:] == 3).all())
 
 
