@@ -30,9 +30,13 @@ using wide = typename Wide<T, V>::type;
 template <typename T, int V>
 __device__ __forceinline__ wide<T, V> load_raw(const T *p, int count) {
     if (count >= V) return *(const wide<T, V> *)p;
-    wide<T, V> v;
+    wide<T, V> v = {};
+    if (count > 0) {   // all loads at once: what is past the end is the last one again, and then 0
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = i < count ? p[i] : (T)0.0f;
+        for (int i = 0; i < V; ++i) v[i] = p[i < count ? i : count - 1];
+#pragma unroll
+        for (int i = 1; i < V; ++i) v[i] = i < count ? v[i] : (T)0.0f;
+    }
     return v;
 }
 template <typename T, int V>
@@ -149,6 +153,24 @@ __device__ __forceinline__ void drop_apply(const Drop &d, uint64_t q, int col, f
         const uint64_t h = drop_hash(d, q, (col + i) >> 1);
         v[i] = (uint32_t)h >= d.least ? v[i] * d.scale : 0.0f;
         v[i + 1] = (uint32_t)(h >> 32) >= d.least ? v[i + 1] * d.scale : 0.0f;
+    }
+}
+
+// The same, col odd or even: a hash more.
+template <int V>
+__device__ __forceinline__ void drop_apply_any(const Drop &d, uint64_t q, int col, float (&v)[V]) {
+    const uint32_t odd = -(uint32_t)(col & 1);
+    uint32_t half[V + 2];
+#pragma unroll
+    for (int i = 0; i < V + 2; i += 2) {
+        const uint64_t h = drop_hash(d, q, (col + i) >> 1);
+        half[i] = (uint32_t)h;
+        half[i + 1] = (uint32_t)(h >> 32);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const uint32_t u = (odd & half[i + 1]) | (~odd & half[i]);   // (a choice of an array's element would put it in memory)
+        v[i] = u >= d.least ? v[i] * d.scale : 0.0f;
     }
 }
 

@@ -24,5 +24,7 @@ hipError_t launch_rows(int dtype, const Product &p, hipStream_t s);
 // Bytes of scratch that the product wants (for sums that are split along k).
 size_t product_workspace(int dtype, const Product &p);
 hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStream_t s);
+// Both gradients of a layer in one launch, where both are small (taken).
+hipError_t launch_pair(int dtype, const Product &x, const Product &w, hipStream_t s, bool *taken);
 
 }  // namespace aet_ops

@@ -196,15 +196,12 @@ struct Tile {
 };
 
 template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT>
-__global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand ob, Shape s, Epilogue e) {
+__device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, const Shape &s, const Epilogue &e, int block, lds_ptr lds) {
     using L = Tile<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>;
     constexpr int FM = L::FM, FN = L::FN, P = L::kParts;
     using SA = typename L::SA;
     using SB = typename L::SB;
-    extern __shared__ __attribute__((aligned(1024))) char lds_all[];
-    const lds_ptr lds = (lds_ptr)lds_all;
-
-    int id = xcd_order(blockIdx.x, s.blocks);
+    int id = xcd_order(block, s.blocks);
     const int tile = id % s.tiles;
     id /= s.tiles;
     const int slice = id % s.slices;
@@ -366,7 +363,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand o
             }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
-#pragma unroll
+#pragma unroll 1
         for (int r = 0; r < 32; r += DOWN) {
             const int line = r + lane / ACROSS;
             const int64_t row = m0 + (wr * FM + j) * 32 + line;
@@ -385,6 +382,21 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand o
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
     }
+}
+
+template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand ob, Shape s, Epilogue e) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    tile_of<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>(oa, ob, s, e, blockIdx.x, (lds_ptr)lds);
+}
+
+// Two small products in one launch: the gradients of a layer's inputs (B by columns) and of its weights (both by columns).
+template <typename T, int BM, int BN, int BK, int WR, int WC, bool DIRECT>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles_pair(Product x, Shape sx, Product w, Shape sw) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int block = blockIdx.x;
+    if (block < sx.blocks) tile_of<T, BM, BN, BK, WR, WC, false, true, DIRECT>(x.a, x.b, sx, x.e, block, (lds_ptr)lds);
+    else tile_of<T, BM, BN, BK, WR, WC, true, true, DIRECT>(w.a, w.b, sw, w.e, block - sx.blocks, (lds_ptr)lds);
 }
 
 // Adds the slices of a split sum, in their order, and ends it.  A thread has 16 bytes of C.
@@ -442,7 +454,7 @@ static hipError_t run_tiles(const Product &p, Shape s, hipStream_t stream) {
 //   fp32  4096 x 4096 x 4096  690, 810, 900;   2048 x 2048 x 1024  72, 63, 67;   3 x (1001 x 771 x 1155)  85, 66, 58
 //   bf16  4096 x 4096 x 4096  124, 140, 166, 199;   2048 x 2048 x 1024  28, 13.8, 13.6, 15.8;   512 x 4096 x 4096  83, 41, 36, 32
 // A sum is split where its tiles leave compute units idle (fp32 512 x 4096 x 4096, 128 x 128: 238, two slices 138, four 109);
-// partial sums are written and read at about 2.5 TB/s, and the launch that adds them takes 4.
+// partial sums are written and read at about 2.5 TB/s, and the launch that adds them takes 6 with the gap before it.
 struct Kind {
     int bm, bn, bk;
     float alone, more, end;
@@ -466,7 +478,7 @@ static Choice choose(int dtype, const Product &p, bool straight) {
         for (int64_t slices = 1; slices == 1 || (slices <= 64 && stages / slices >= 2); slices *= 2) {
             const float waves = (float)ceil_div(tiles * slices, 256);
             float t = (float)ceil_div(stages, slices) * (k.alone + (waves - 1) * k.more) + waves * k.end;
-            if (slices > 1) t += 4.0f + (float)(slices + 1) * sums / 2.5e6f;
+            if (slices > 1) t += 6.0f + (float)(slices + 1) * sums / 2.5e6f;
             if (!best.kind || t < least) {
                 least = t;
                 best = {&k, (int)slices};
@@ -486,22 +498,33 @@ size_t product_workspace(int dtype, const Product &p) {
     return slices > 1 ? (size_t)slices * p.clients * p.M * p.N * sizeof(float) : 0;
 }
 
+// The product's tiles of this kind.
+static bool shape_of(const Product &p, const Choice &c, void *workspace, Shape *s) {
+    const Kind &k = *c.kind;
+    *s = {p.M, p.N, p.K};
+    s->clients = p.clients;
+    s->tiles_n = (int)ceil_div(p.N, k.bn);
+    const int64_t tiles = ceil_div(p.M, k.bm) * s->tiles_n, blocks = tiles * p.clients * c.slices;
+    s->tiles = (int)tiles;
+    s->blocks = (int)blocks;
+    s->slices = c.slices;
+    s->slice_k = (int)ceil_div(ceil_div(p.K, k.bk), c.slices) * k.bk;
+    s->partial = (float *)workspace;
+    return blocks <= INT32_MAX;
+}
+template <typename T>
+static bool straight(const Product &p) {
+    return sizeof(T) == 2 && direct(p.a, p.M, p.K, 64) && direct(p.b, p.N, p.K, 64);
+}
+
 template <typename T, bool TA, bool TB>
 static hipError_t run_product(const Product &p, void *workspace, hipStream_t stream) {
-    const bool d = sizeof(T) == 2 && direct(p.a, p.M, p.K, 64) && direct(p.b, p.N, p.K, 64);
+    const bool d = straight<T>(p);
     const Choice c = choose(sizeof(T) == 4 ? AET_F32 : AET_BF16, p, d);
-    Shape s = {p.M, p.N, p.K};
-    s.clients = p.clients;
     const Kind &k = *c.kind;
-    s.tiles_n = (int)ceil_div(p.N, k.bn);
-    const int64_t tiles = ceil_div(p.M, k.bm) * s.tiles_n, blocks = tiles * p.clients * c.slices;
-    if (!blocks) return hipSuccess;
-    if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
-    s.tiles = (int)tiles;
-    s.blocks = (int)blocks;
-    s.slices = c.slices;
-    s.slice_k = (int)ceil_div(ceil_div(p.K, k.bk), c.slices) * k.bk;
-    s.partial = (float *)workspace;
+    Shape s;
+    if (!shape_of(p, c, workspace, &s)) return hipErrorInvalidConfiguration;
+    if (!s.blocks) return hipSuccess;
     hipError_t e;
     if constexpr (sizeof(T) == 4) {
         if (k.bm == 128) e = run_tiles<T, 128, 128, 32, 2, 2, TA, TB, false>(p, s, stream);
@@ -524,6 +547,35 @@ hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStrea
     if (!p.a.by_columns && !p.b.by_columns) return f32 ? run_product<float, false, false>(p, workspace, s) : run_product<bf16, false, false>(p, workspace, s);
     if (!p.a.by_columns) return f32 ? run_product<float, false, true>(p, workspace, s) : run_product<bf16, false, true>(p, workspace, s);
     return f32 ? run_product<float, true, true>(p, workspace, s) : run_product<bf16, true, true>(p, workspace, s);
+}
+
+template <typename T>
+static hipError_t run_pair(const Product &x, const Product &w, hipStream_t stream, bool *taken) {
+    const int dtype = sizeof(T) == 4 ? AET_F32 : AET_BF16;
+    const bool d = straight<T>(x);
+    const Choice cx = choose(dtype, x, d), cw = choose(dtype, w, d);
+    *taken = false;
+    Shape sx, sw;
+    if (d != straight<T>(w) || cx.slices > 1 || cw.slices > 1 || cx.kind->bm * cx.kind->bn != 64 * 64 || cw.kind->bm * cw.kind->bn != 64 * 64 ||
+        !shape_of(x, cx, nullptr, &sx) || !shape_of(w, cw, nullptr, &sw) || !sx.blocks || !sw.blocks || sx.blocks > INT32_MAX - sw.blocks)
+        return hipSuccess;
+    *taken = true;
+    constexpr int BK = sizeof(T) == 4 ? 32 : 64;
+    const int blocks = sx.blocks + sw.blocks;
+    if constexpr (sizeof(T) == 2) {
+        if (d) {
+            using L = Tile<T, 64, 64, BK, 2, 2, true, true, true>;
+            k_tiles_pair<T, 64, 64, BK, 2, 2, true><<<blocks, L::kThreads, L::kLds, stream>>>(x, sx, w, sw);
+            return hipGetLastError();
+        }
+    }
+    using L = Tile<T, 64, 64, BK, 2, 2, true, true, false>;
+    static_assert(L::kLds <= 64 * 1024, "no permission needed");
+    k_tiles_pair<T, 64, 64, BK, 2, 2, false><<<blocks, L::kThreads, L::kLds, stream>>>(x, sx, w, sw);
+    return hipGetLastError();
+}
+hipError_t launch_pair(int dtype, const Product &x, const Product &w, hipStream_t s, bool *taken) {
+    return dtype == AET_F32 ? run_pair<float>(x, w, s, taken) : run_pair<bf16>(x, w, s, taken);
 }
 
 }  // namespace aet_ops
