@@ -449,40 +449,42 @@ static hipError_t run_tiles(const Product &p, Shape s, hipStream_t stream) {
 }
 
 // Kinds of tiles, and what they take: `alone` microseconds for a stage where a compute unit has one workgroup, `more` for
-// each further one that it has to do, `end` for each workgroup's epilogue.  Measured on products of 33 to 8192 rows, 100 to
+// each further one up to the `fit` that it holds at a time (then it goes on as with all of them), `end` for each
+// workgroup's epilogue.  Measured on products of 33 to 8192 rows, 100 to
 // 4096 columns and sums of 32 to 8192; a few examples, in microseconds, with the kinds as they are listed here:
 //   fp32  4096 x 4096 x 4096  690, 810, 900;   2048 x 2048 x 1024  72, 63, 67;   3 x (1001 x 771 x 1155)  85, 66, 58
 //   bf16  4096 x 4096 x 4096  124, 140, 166, 199;   2048 x 2048 x 1024  28, 13.8, 13.6, 15.8;   512 x 4096 x 4096  83, 41, 36, 32
 // A sum is split where its tiles leave compute units idle (fp32 512 x 4096 x 4096, 128 x 128: 238, two slices 138, four 109);
-// partial sums are written and read at about 2.5 TB/s, and the launch that adds them takes 6 with the gap before it.
+// partial sums are written and read at about 6 TB/s (they stay in the caches), and the launch that adds them takes 4.
 struct Kind {
-    int bm, bn, bk;
+    int bm, bn, bk, fit;
     float alone, more, end;
 };
-static const Kind kKinds32[] = {{128, 128, 32, 2.1f, 1.1f, 2.0f}, {64, 128, 32, 1.2f, 0.72f, 1.0f}, {64, 64, 32, 0.88f, 0.40f, 0.5f}};
-static const Kind kKinds16[] = {{256, 256, 64, 1.5f, 1.6f, 8.0f}, {128, 128, 64, 0.65f, 0.52f, 2.0f}, {64, 128, 64, 0.54f, 0.295f, 1.0f}, {64, 64, 64, 0.46f, 0.18f, 0.5f}};
+static const Kind kKinds32[] = {{128, 128, 32, 2, 2.2f, 0.5f, 2.0f}, {64, 128, 32, 3, 1.35f, 0.60f, 1.0f}, {64, 64, 32, 5, 0.95f, 0.35f, 0.5f}};
+static const Kind kKinds16[] = {{256, 256, 64, 1, 1.6f, 0.0f, 8.0f}, {128, 128, 64, 2, 0.65f, 0.45f, 2.0f}, {64, 128, 64, 3, 0.54f, 0.22f, 1.0f}, {64, 64, 64, 5, 0.46f, 0.13f, 0.5f}};
 
 // bf16 through registers
-static const Kind kKinds16Any[] = {{256, 256, 64, 2.5f, 2.6f, 8.0f}, {128, 128, 64, 1.7f, 0.9f, 2.0f}, {64, 128, 64, 0.95f, 0.42f, 1.0f}, {64, 64, 64, 0.62f, 0.31f, 0.5f}};
+static const Kind kKinds16Any[] = {{256, 256, 64, 1, 2.6f, 0.0f, 8.0f}, {128, 128, 64, 2, 1.7f, 0.4f, 2.0f}, {64, 128, 64, 3, 0.95f, 0.42f, 1.0f}, {64, 64, 64, 5, 0.62f, 0.31f, 0.5f}};
 
 struct Choice {
     const Kind *kind;
     int slices;
+    float time;
 };
+static float time_of(const Kind &k, int64_t stages, int64_t blocks) {
+    const float waves = (float)ceil_div(blocks, 256);
+    const float stage = waves <= k.fit ? k.alone + (waves - 1) * k.more : (k.alone + (k.fit - 1) * k.more) * waves / k.fit;
+    return (float)stages * stage + waves * k.end;
+}
 static Choice choose(int dtype, const Product &p, bool straight) {
     Choice best = {};
-    float least = 0;
     const auto consider = [&](const Kind &k) {
         const int64_t tiles = p.clients * ceil_div(p.M, k.bm) * ceil_div(p.N, k.bn), stages = ceil_div(p.K, k.bk);
         const float sums = (float)p.clients * (float)p.M * (float)p.N * 4.0f;
         for (int64_t slices = 1; slices == 1 || (slices <= 64 && stages / slices >= 2); slices *= 2) {
-            const float waves = (float)ceil_div(tiles * slices, 256);
-            float t = (float)ceil_div(stages, slices) * (k.alone + (waves - 1) * k.more) + waves * k.end;
-            if (slices > 1) t += 6.0f + (float)(slices + 1) * sums / 2.5e6f;
-            if (!best.kind || t < least) {
-                least = t;
-                best = {&k, (int)slices};
-            }
+            float t = time_of(k, ceil_div(stages, slices), tiles * slices);
+            if (slices > 1) t += 4.0f + (float)(2 * slices + 1) * sums / 6e6f;
+            if (!best.kind || t < best.time) best = {&k, (int)slices, t};
         }
     };
     if (dtype == AET_F32) for (const Kind &k : kKinds32) consider(k);
@@ -552,12 +554,16 @@ hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStrea
 template <typename T>
 static hipError_t run_pair(const Product &x, const Product &w, hipStream_t stream, bool *taken) {
     const int dtype = sizeof(T) == 4 ? AET_F32 : AET_BF16;
+    // the smallest kind, sums in one piece; a launch less is worth 3
     const bool d = straight<T>(x);
-    const Choice cx = choose(dtype, x, d), cw = choose(dtype, w, d);
+    const Kind &k = dtype == AET_F32 ? kKinds32[2] : d ? kKinds16[3] : kKinds16Any[3];
+    const Choice one = {&k, 1};
     *taken = false;
     Shape sx, sw;
-    if (d != straight<T>(w) || cx.slices > 1 || cw.slices > 1 || cx.kind->bm * cx.kind->bn != 64 * 64 || cw.kind->bm * cw.kind->bn != 64 * 64 ||
-        !shape_of(x, cx, nullptr, &sx) || !shape_of(w, cw, nullptr, &sw) || !sx.blocks || !sw.blocks || sx.blocks > INT32_MAX - sw.blocks)
+    if (d != straight<T>(w) || !shape_of(x, one, nullptr, &sx) || !shape_of(w, one, nullptr, &sw) || !sx.blocks || !sw.blocks ||
+        sx.blocks > INT32_MAX - sw.blocks)
+        return hipSuccess;
+    if (time_of(k, ceil_div(x.K > w.K ? x.K : w.K, k.bk), (int64_t)sx.blocks + sw.blocks) > choose(dtype, x, d).time + choose(dtype, w, d).time + 3.0f)
         return hipSuccess;
     *taken = true;
     constexpr int BK = sizeof(T) == 4 ? 32 : 64;
