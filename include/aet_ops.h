@@ -89,7 +89,7 @@ aet_status aet_linear_forward(const aet_linear *a, void *workspace, size_t works
 /* The gradient:  dz = dropout'(dy) * act'(z),  dx = dz W,  dw = dz^T x,  db = sum of dz over
  * rows; that of the residual is dy itself.  Each output is left out where its p is NULL.
  *   pre       z as the forward call gave it; p = NULL where act is AET_ACT_NONE
- *   dw, db    client = 0 with n > 1: one W (bias) for all clients, whose gradient is the sum
+ *   dw, db    client = 0 with n other than 1: one W (bias) for all clients, whose gradient is the sum
  *             over them; x, dy, pre and dx then lie row after row, client after client
  *             (client = rows * row), and w.client, dw.client and db.client are all 0
  * bf16: dz is rounded to bf16 for the products (the matrix cores take bf16 only; its error
@@ -137,7 +137,7 @@ aet_status aet_group_norm_forward(const aet_group_norm *a, void *workspace, size
 
 /* Its gradient, from the inputs and the statistics that the forward call gave.
  *   dx            may be dy itself, with the same strides; or p = NULL
- *   dgamma, dbeta n x channels; client = 0 with n > 1: the sum over the clients; or p = NULL */
+ *   dgamma, dbeta n x channels; client = 0 with n other than 1: the sum over the clients; or p = NULL */
 typedef struct {
     int32_t dtype, act;
     int32_t n, batch, positions, groups, width;

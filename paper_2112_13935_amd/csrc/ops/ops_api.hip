@@ -138,7 +138,7 @@ static aet_status check(const aet_linear_grad *a, bool *shared) {
     if (bad_common(a->dtype, a->act, &why)) return fail(AET_EINVAL, "%s", why);
     if (bad_sizes({a->n, a->rows, a->in, a->out}, &why)) return fail(AET_EINVAL, "%s", why);
     if (bad_drop(a->p, a->first_row, (int64_t)a->n * a->rows, &why)) return fail(AET_EINVAL, "%s", why);
-    *shared = a->n > 1 && ((a->dw.p && !a->dw.client) || (a->db.p && !a->db.client));
+    *shared = a->n != 1 && ((a->dw.p && !a->dw.client) || (a->db.p && !a->db.client));
     const int64_t n = *shared ? 1 : a->n;   // gradients of parameters
     const int64_t nr[2] = {a->n, a->rows}, no[2] = {a->n, a->out}, go[2] = {n, a->out};
     auto in = [&](const aet_in &t, const int64_t *count) { const int64_t st[2] = {t.client, t.row}; return bad_in(t.p, a->dtype, 2, count, st); };
@@ -160,8 +160,8 @@ static aet_status check(const aet_linear_grad *a, bool *shared) {
         if (a->w.client || (a->dw.p && a->dw.client) || (a->db.p && a->db.client))
             return fail(AET_EINVAL, "w, dw and db: either all or none are the same for all clients (client = 0)");
         auto flat = [&](const void *p, int64_t client, int64_t row) { return !p || client == a->rows * row; };
-        if (!flat(a->dy.p, a->dy.client, a->dy.row) || !flat(a->x.p, a->x.client, a->x.row) ||
-            !flat(a->pre.p, a->pre.client, a->pre.row) || !flat(a->dx.p, a->dx.client, a->dx.row))
+        if (a->n && (!flat(a->dy.p, a->dy.client, a->dy.row) || !flat(a->x.p, a->x.client, a->x.row) ||
+                     !flat(a->pre.p, a->pre.client, a->pre.row) || !flat(a->dx.p, a->dx.client, a->dx.row)))
             return fail(AET_EINVAL, "one W for all clients: rows have to lie client after client (client = rows * row)");
         if ((int64_t)a->n * a->rows > kMostSize) return fail(AET_EINVAL, "one W for all clients: more than 2^30 rows");
     }
@@ -316,7 +316,6 @@ size_t aet_group_norm_backward_workspace_bytes(const aet_group_norm_grad *a) {
 }
 aet_status aet_group_norm_backward(const aet_group_norm_grad *a, void *workspace, size_t workspace_bytes, void *hip_stream) {
     if (const aet_status st = check(a)) return st;
-    if (!a->n) return AET_OK;
     const size_t need = group_norm_backward_workspace(*a);
     if (bad_workspace(workspace, workspace_bytes, need))
         return fail(AET_ENOMEM, "the workspace needs %zu bytes, 256-byte aligned; got %zu", need, workspace_bytes);

@@ -652,6 +652,7 @@ static hipError_t backward(const aet_group_norm_grad &a, char *workspace, hipStr
     if (a.dgamma.p || a.dbeta.p) {
         const bool shared = (a.dgamma.p && !a.dgamma.client) || (a.dbeta.p && !a.dbeta.client);
         const int clients = shared ? 1 : a.n, across = (int)ceil_div(channels, 64);
+        if (!clients) return hipSuccess;
         if ((int64_t)clients * across > INT32_MAX) return hipErrorInvalidConfiguration;
         k_norm_params<T><<<clients * across, 256, 0, s>>>(a, p.s.sums, (int64_t)p.s.strips * 2 * channels, (int)channels, across, samples / clients);
     }

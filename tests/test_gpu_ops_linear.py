@@ -299,3 +299,13 @@ def test_other_streams_and_graphs(ops):
             torch.cuda.synchronize()
             assert torch.equal(y, want_y) and torch.equal(pre, want_pre) and all(torch.equal(a, b) for a, b in zip(got, want))
             (x @ x.transpose(1, 2).contiguous()).sum().item()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_clients_of_a_shared_layer(ops, dtype):
+    """One W and bias of all clients, of whom there are none: their gradients are sums of nothing."""
+    dt = TYPES[dtype]
+    z = lambda *s: torch.ones(*s, dtype=dt, device=DEV)   # noqa: E731
+    out = (None, torch.full((6, 8), 5.0, dtype=dt, device=DEV), torch.full((6,), 5.0, dtype=dt, device=DEV))
+    dx, dw, db = ops.aet_linear_backward(z(0, 3, 6), z(0, 3, 8), z(6, 8), z(0, 3, 6), act="relu", out=out)
+    assert dx.shape == (0, 3, 8) and torch.equal(dw, z(6, 8) * 0) and torch.equal(db, z(6) * 0)

@@ -198,3 +198,13 @@ def test_other_streams_and_graphs(ops):   # noqa: F811
             torch.cuda.synchronize()
             assert all(torch.equal(a, w) for a, w in zip(got, want))
             x.float().sum().item()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_clients_of_shared_parameters(ops, dtype):   # noqa: F811
+    """gamma and beta of all clients, of whom there are none: the gradients are sums of nothing."""
+    dt = TYPES[dtype]
+    z = lambda *s: torch.ones(*s, dtype=dt, device=DEV)   # noqa: E731
+    out = (None, torch.full((8,), 5.0, dtype=dt, device=DEV), torch.full((8,), 5.0, dtype=dt, device=DEV))
+    dx, dgamma, dbeta = ops.aet_group_norm_backward(z(0, 3, 4, 8), z(0, 3, 4, 8), z(0, 3, 2).float(), z(0, 3, 2).float(), z(8), z(8), out=out)
+    assert dx.shape == (0, 3, 4, 8) and torch.equal(dgamma, z(8) * 0) and torch.equal(dbeta, z(8) * 0)
