@@ -549,6 +549,7 @@ static NormPlan make_plan(int64_t samples, int positions, int groups, int width,
     const int most = back ? 8 : 16;
     const int64_t lanes = ceil_div(positions, most), fit_pieces = lanes > kThreads ? 0 : kThreads / lanes;
     int64_t fit = (fit_pieces < 256 ? fit_pieces : 256) * V / width;
+    if (fit > 1024) fit = 1024;   // their statistics and their channels' sums have 64 KB of LDS with the threads' sums
     if (fit > groups) fit = groups;
     if (fit > 0) {
         const auto at_least_1 = [](int64_t v) { return v < 1 ? 1 : v; };

@@ -208,3 +208,20 @@ def test_no_clients_of_shared_parameters(ops, dtype):   # noqa: F811
     out = (None, torch.full((8,), 5.0, dtype=dt, device=DEV), torch.full((8,), 5.0, dtype=dt, device=DEV))
     dx, dgamma, dbeta = ops.aet_group_norm_backward(z(0, 3, 4, 8), z(0, 3, 4, 8), z(0, 3, 2).float(), z(0, 3, 2).float(), z(8), z(8), out=out)
     assert dx.shape == (0, 3, 4, 8) and torch.equal(dgamma, z(8) * 0) and torch.equal(dbeta, z(8) * 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_group_norm_of_many_groups(ops, dtype):   # noqa: F811
+    """Thousands of groups of a channel or two: what a workgroup keeps of each has to fit."""
+    dt = TYPES[dtype]
+    for n, b, P, G, width in ((1, 600, 3, 2048, 1), (2, 130, 16, 2500, 1), (1, 300, 5, 1030, 2)):
+        ch = G * width
+        g = torch.Generator().manual_seed(G)
+        x, dy, gamma, beta = (rand(g, s, dt) for s in ((n, b, P, ch), (n, b, P, ch), (n, ch), (n, ch)))
+        y, mean, rstd = ops.aet_group_norm_forward(x, G, gamma, beta, eps=1e-2, act="silu")
+        wy, _, _ = O.group_norm_forward(d64(x), G, d64(gamma), d64(beta), 1e-2, "silu", dt)
+        O.near(y, wy, f"y {dtype} {G}")
+        got = ops.aet_group_norm_backward(dy, x, mean, rstd, gamma, beta, act="silu")
+        want = O.group_norm_backward(d64(dy), d64(x), d64(mean), d64(rstd), d64(gamma), d64(beta), "silu", dt)
+        for what, a, w in zip(("dx", "dgamma", "dbeta"), got, want):
+            O.near(a, w, f"{what} {dtype} {G}")
