@@ -137,7 +137,7 @@ aet_status aet_group_norm_forward(const aet_group_norm *a, void *workspace, size
 
 /* Its gradient, from the inputs and the statistics that the forward call gave.
  *   dx            may be dy itself, with the same strides; or p = NULL
- *   dgamma, dbeta n x channels; client = 0 with n other than 1: the sum over the clients; or p = NULL */
+ *   dgamma, dbeta n x channels; client = 0 with n other than 1: the sum over the clients (then of both); or p = NULL */
 typedef struct {
     int32_t dtype, act;
     int32_t n, batch, positions, groups, width;

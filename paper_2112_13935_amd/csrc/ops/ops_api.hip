@@ -217,6 +217,8 @@ static aet_status check(const aet_group_norm_grad *a) {
     };
     if (a->dgamma.p) AET_CHECK("dgamma", param(a->dgamma));
     if (a->dbeta.p) AET_CHECK("dbeta", param(a->dbeta));
+    if (a->n != 1 && a->dgamma.p && a->dbeta.p && !a->dgamma.client != !a->dbeta.client)
+        return fail(AET_EINVAL, "dgamma and dbeta: either both or none are the same for all clients (client = 0)");
     if (!a->n || !a->batch || !a->positions) return AET_OK;
     AET_CHECK("dy", bad_maps(a->dy, a->dtype, a->n, a->batch, a->positions, C, false));
     AET_CHECK("x", bad_maps(a->x, a->dtype, a->n, a->batch, a->positions, C, false));

@@ -134,3 +134,11 @@ def test_binding_refuses():
         ops.aet_dropout_forward(x, p=0.1, seed=0)
     with pytest.raises(ValueError, match="groups"):
         ops.aet_group_norm_forward(torch.zeros(1, 4, 6), 4)
+
+
+def test_gradients_of_gamma_and_beta_agree(lib):
+    """One of them the sum over the clients, the other not."""
+    for wrong in (dict(dgamma_client=0), dict(dbeta_client=0)):
+        a = norm_grad(**wrong)
+        assert lib.aet_group_norm_backward(C.addressof(a), P, 1 << 40, None) == EINVAL
+        assert b"either both or none" in lib.aet_ops_last_error()
