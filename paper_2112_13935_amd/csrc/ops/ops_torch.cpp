@@ -1,6 +1,7 @@
 // Tensors to aet_ops.h: checks that the tensors of a call agree, allocates its outputs and its workspace with PyTorch and
 // hands pointers and strides over.  Marshalling only, compiled because it is most of a small call's time: a linear layer of
 // one row takes 4.9 us of the host this way, of which 3.6 are the C call with its launch, and took 8.9 in Python with ctypes.
+#include <c10/core/StreamGuard.h>
 #include <torch/extension.h>
 
 #include "aet_ops.h"
@@ -22,14 +23,18 @@ struct Call {
     const Tensor &x;
     int dtype;
     void *handle;
-    std::optional<c10::Stream> other;   // not the current stream: what is used on it is kept for it
     c10::DeviceGuard guard;
+    // Not the current stream: what is allocated belongs to it (memory that the current stream has given back may still
+    // be in use there) and is kept for the current one too; what is handed over is kept for it.
+    std::optional<c10::StreamGuard> other;
 
     Call(const Tensor &first, int64_t handle_, const std::optional<std::tuple<int64_t, int64_t, int64_t>> &stream)
         : x(first), dtype(AET_F32), handle((void *)handle_), guard(checked(first)) {
         if (first.scalar_type() == at::kBFloat16) dtype = AET_BF16;
-        if (stream)
-            other = c10::Stream::unpack3(std::get<0>(*stream), (c10::DeviceIndex)std::get<1>(*stream), (c10::DeviceType)std::get<2>(*stream));
+        if (!stream) return;
+        if (std::get<1>(*stream) != x.device().index())
+            value_error("the stream is one of device " + std::to_string(std::get<1>(*stream)) + ", the tensors are " + text(x));
+        other.emplace(c10::Stream::unpack3(std::get<0>(*stream), (c10::DeviceIndex)std::get<1>(*stream), (c10::DeviceType)std::get<2>(*stream)));
     }
     static c10::Device checked(const Tensor &t) {
         if ((t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) || !t.is_cuda())
@@ -37,7 +42,7 @@ struct Call {
         return t.device();
     }
     void *use(const Tensor &t) {
-        if (other) t.record_stream(*other);
+        if (other) t.record_stream(other->current_stream());
         return t.data_ptr();
     }
     // The tensor's type, device, shape and last stride are as they have to be.
@@ -81,9 +86,13 @@ struct Call {
         to.sample = st[d - 3];
         to.row = st[d - 2];
     }
-    Tensor made(at::IntArrayRef shape) { return at::empty(shape, x.options()); }
+    Tensor made(at::IntArrayRef shape, at::ScalarType type) {
+        const Tensor t = at::empty(shape, x.options().dtype(type));
+        if (other) t.record_stream(other->original_stream());
+        return t;
+    }
     OptTensor out(const OptTensor &given, bool wanted, at::IntArrayRef shape) {
-        return given ? given : wanted ? OptTensor(made(shape)) : std::nullopt;
+        return given ? given : wanted ? OptTensor(made(shape, x.scalar_type())) : std::nullopt;
     }
     template <class A>
     void run(aet_status (*fn)(const A *, void *, size_t, void *), size_t (*bytes)(const A *), const A &a) {
@@ -191,7 +200,7 @@ std::tuple<Tensor, Tensor, Tensor> group_norm_forward(const Tensor &x, int64_t g
     c.vec(a.beta, "beta", beta, s.n, x.size(-1));
     const OptTensor y = c.out(out, true, x.sizes());
     c.maps(a.y, "out", y, x.sizes());
-    const Tensor mean = at::empty(stats, x.options().dtype(at::kFloat)), rstd = at::empty(stats, x.options().dtype(at::kFloat));
+    const Tensor mean = c.made(stats, at::kFloat), rstd = c.made(stats, at::kFloat);
     a.mean = (float *)c.use(mean);
     a.rstd = (float *)c.use(rstd);
     c.run(aet_group_norm_forward, aet_group_norm_workspace_bytes, a);

@@ -6,8 +6,9 @@ Names follow the C entry points, whose records are here as ctypes structures too
 
 Tensors: one type a call, float32 or bfloat16, the last axis with stride 1, any other strides.  A
 leading axis of clients may be left out everywhere (one client).  Outputs are allocated unless they
-are given.  Calls enqueue on `stream`, the current stream where it is None; tensors used on another
-one are kept from being given out again before it is done with them (Tensor.record_stream).
+are given.  Calls enqueue on `stream`, the current stream where it is None.  Where it is another one,
+outputs and workspaces are allocated on it, and tensors are kept from being given out again before both
+are done with them (Tensor.record_stream); waiting for one another is the caller's (Stream.wait_stream).
 Seeds are taken modulo 2^64.
 """
 from __future__ import annotations

@@ -309,3 +309,16 @@ def test_no_clients_of_a_shared_layer(ops, dtype):
     out = (None, torch.full((6, 8), 5.0, dtype=dt, device=DEV), torch.full((6,), 5.0, dtype=dt, device=DEV))
     dx, dw, db = ops.aet_linear_backward(z(0, 3, 6), z(0, 3, 8), z(6, 8), z(0, 3, 6), act="relu", out=out)
     assert dx.shape == (0, 3, 8) and torch.equal(dw, z(6, 8) * 0) and torch.equal(db, z(6) * 0)
+
+
+def test_outputs_on_another_stream_are_its_own(ops):
+    """Memory given back on the current stream may still be in use there: a call on another stream gets its own."""
+    x, w = torch.randn(4, 64, device=DEV), torch.randn(96, 64, device=DEV)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    y, _ = ops.aet_linear_forward(x, w, stream=s)
+    at = y.data_ptr()
+    owner = [g["stream"] for g in torch.cuda.memory_snapshot() if g["address"] <= at < g["address"] + g["total_size"]]
+    assert owner == [s.cuda_stream]
+    s.synchronize()
+    assert torch.equal(y, ops.aet_linear_forward(x, w)[0])
