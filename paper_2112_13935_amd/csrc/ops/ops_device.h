@@ -60,6 +60,12 @@ __device__ __forceinline__ void store_some(T *p, int count, const float (&v)[V])
     }
 }
 
+// Workgroups go to the XCDs in turn: the order that gives each XCD consecutive ones, so that what they share meets in its L2.
+__device__ __forceinline__ int xcd_order(int id, int blocks) {
+    const int q = blocks / 8, r = blocks % 8, x = id % 8;
+    return x * q + (x < r ? x : r) + id / 8;
+}
+
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 // Phi(z) and exp(-z^2 / 2).  Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: erfc(u) =

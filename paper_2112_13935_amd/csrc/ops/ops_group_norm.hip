@@ -128,7 +128,7 @@ template <typename T, int V, int N>
 __global__ __launch_bounds__(kThreads) void k_norm_whole(aet_group_norm a, NormShape s) {
     extern __shared__ float lds[];   // threads * V, then by channel, then by group
     float *const tot = lds + s.threads * V, *const stat = tot + s.span;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x);
+    const Where w = where<V>(s, a.batch, a.width, xcd_order(blockIdx.x, gridDim.x));
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     T *y = (T *)a.y.p + w.client * a.y.client + w.in_batch * a.y.sample + w.ch;
     wide<T, V> raw[N];
@@ -226,7 +226,7 @@ template <typename T, int V, int N>
 __global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_grad a, NormShape s) {
     extern __shared__ float lds[];
     float *const totA = lds + 2 * s.threads * V, *const totB = totA + s.span, *const gam = totB + s.span, *const stat = gam + s.span;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x);
+    const Where w = where<V>(s, a.batch, a.width, xcd_order(blockIdx.x, gridDim.x));
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
     wide<T, V> rx[N], rd[N];
@@ -545,7 +545,11 @@ static NormPlan make_plan(int64_t samples, int positions, int groups, int width,
     NormShape &s = p.s;
     s.channels = groups * width;
     // Whole groups: as many as fit the registers, of those as give 512 workgroups, but 64 bytes of neighbouring channels
-    // unless that leaves fewer than 128.
+    // unless that leaves fewer than 128; and in whole pieces where half as many or more are (forward, 256 samples of
+    // 1024 x 320 in fp32, groups of 10 channels: two 220 us, three 258).  A sample's workgroups share lines of memory and
+    // run on one XCD (128 samples of 4096 x 128 in bf16, 16 channels each: 75 us, dealt over the XCDs 139).
+    // Less than 64 bytes, or pieces that are not whole: three kernels (the same samples 72 us; 256 samples of 1024 x 320
+    // in fp32, the gradient in groups of 10 channels: 344 us, in one kernel 500), unless the launches are what counts.
     const int most = back ? 8 : 16;
     const int64_t lanes = ceil_div(positions, most), fit_pieces = lanes > kThreads ? 0 : kThreads / lanes;
     int64_t fit = (fit_pieces < 256 ? fit_pieces : 256) * V / width;
@@ -557,10 +561,17 @@ static NormPlan make_plan(int64_t samples, int positions, int groups, int width,
         if (best < ceil_div(4 * V, width)) best = ceil_div(4 * V, width);
         if (best > at_least_1(samples * groups / 128)) best = at_least_1(samples * groups / 128);
         if (best > fit) best = fit;
-        s.span_groups = (int)ceil_div(groups, ceil_div(groups, best));
+        best = ceil_div(groups, ceil_div(groups, best));
+        if (best < groups)
+            for (int64_t b = best; b > best / 2; --b)
+                if (b * width % V == 0) {
+                    best = b;
+                    break;
+                }
+        s.span_groups = (int)best;
     }
     const int best = s.span_groups;
-    p.whole = best && (best == groups || best * width >= 2 * V || samples * positions * s.channels < (1 << 22));
+    p.whole = best && (best == groups || (best * width >= 4 * V && best * width % V == 0) || samples * positions * s.channels < (1 << 22));
     if (p.whole) {
         deal(s, V, best * width);
         s.lanes = kThreads / s.pieces;

@@ -29,12 +29,6 @@ struct Shape {
     int clients;
 };
 
-// Workgroups go to the XCDs in turn: each XCD gets consecutive tiles, whose operands meet in its L2.
-__device__ __forceinline__ int xcd_order(int id, int blocks) {
-    const int q = blocks / 8, r = blocks % 8, x = id % 8;
-    return x * q + (x < r ? x : r) + id / 8;
-}
-
 // ---- staging -----------------------------------------------------------------------------
 
 // Piece (r, c) of an operand's stage: by rows row r, values 8 c .. of the stage; by columns k = r, rows 8 c ..
