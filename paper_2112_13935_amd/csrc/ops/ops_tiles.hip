@@ -69,20 +69,25 @@ struct RegStage {
     wide<T, 8> raw[kCount];
     const T *p;          // of the thread's piece column in the next stage
     int64_t row;
-    int r, c, left;      // left: of the sum
+    int r, c, piece, left;   // left: of the sum
     int rows;            // of the operand, from the tile's first on
 
     __device__ __forceinline__ void begin(const Operand &o, int64_t client, int r0, int rows_all, int k0, int k1) {
         r = threadIdx.x / S::kWidth;
-        c = threadIdx.x % S::kWidth;
+        c = piece = threadIdx.x % S::kWidth;
         row = o.row;
         rows = rows_all - r0;
         left = k1 - k0;
+        if (COLS && 8 * c >= rows) c = (rows - 1) / 8;   // (the place in LDS is `piece`)
         p = (const T *)o.p + client * o.client + (COLS ? (int64_t)k0 * row + r0 + 8 * c : (int64_t)r0 * row + k0 + 8 * c);
     }
-    // Whether whole stages can be read without looking where each piece ends.  By rows they always can: rows past the
-    // last are read from the last again, and become rows of C that are not stored.
-    __device__ __forceinline__ bool plain() const { return !COLS || rows >= R; }
+    // Stages from the first that can be read without looking where each piece ends.  Rows past the last are read from
+    // the last again, and become rows of C that are not stored.  By columns so are pieces past the last; the last runs over
+    // the end of its line, which is in the operand's memory where lines of 8 and more values follow.
+    __device__ __forceinline__ int plain() const {
+        if (!COLS || rows >= R || rows % 8 == 0) return left / BK;
+        return row >= 8 ? (left - 1) / BK : 0;
+    }
     template <bool PLAIN>
     __device__ __forceinline__ void load() {
 #pragma unroll
@@ -102,7 +107,7 @@ struct RegStage {
     __device__ __forceinline__ void store(lds_ptr to) {
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const lds_ptr at = to + S::slot(r + i * kStep, c) * 16;
+            const lds_ptr at = to + S::slot(r + i * kStep, piece) * 16;
             if constexpr (sizeof(T) == 2) {
                 *(__attribute__((address_space(3))) bf8 *)at = raw[i];
             } else {
@@ -317,9 +322,14 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
             lb.store(lds + kPartA);
             __syncthreads();
         };
-        const int whole = la.plain() && lb.plain() ? (k1 - k0) / BK : 0;
-        la.template load<false>();
-        lb.template load<false>();
+        const int whole = la.plain() < lb.plain() ? la.plain() : lb.plain();
+        if (whole > 0) {
+            la.template load<true>();
+            lb.template load<true>();
+        } else {
+            la.template load<false>();
+            lb.template load<false>();
+        }
         int i = 0;
         for (; i + 1 < whole; ++i) {
             put();
