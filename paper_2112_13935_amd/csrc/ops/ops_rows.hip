@@ -7,6 +7,8 @@
 #include "ops_internal.h"
 #include "ops_tiles.h"
 
+#include <type_traits>
+
 namespace aet_ops {
 
 template <typename T>
@@ -33,8 +35,40 @@ struct RowsShape {
     int tiles_n;    // workgroups of a client
 };
 
+// bf16 whose rows do not all begin at multiples of 4 bytes: 16 bytes from another address take 3.6 times as long (9 TB/s
+// from the L2, not 33), so they are loaded from the multiple below.  What is missing is the first 4 bytes of the lane with
+// the next 8 k, 16 lanes on or in the next step; of the last step of those in a row it is loaded.
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+template <int N>
+struct OddRow {
+    const char *p;   // the multiple of 4 at or below the lane's first value
+    int shift;       // in bits: 0 or 16
+    wide<uint32_t, 4> v[N];
+    uint32_t after;
+    __device__ __forceinline__ void begin(const bf16 *at) {
+        p = (const char *)((uintptr_t)at & ~(uintptr_t)3);
+        shift = (int)((uintptr_t)at & 2) * 8;
+    }
+    __device__ __forceinline__ void load(int i, int64_t k) { v[i] = *(const wide<uint32_t, 4> *)(p + 2 * k); }
+    // k: of the last step
+    __device__ __forceinline__ void load_after(int64_t k) {
+        if (shift && threadIdx.x % 64 >= 48) after = *(const uint32_t *)(p + 2 * k + 16);
+    }
+    __device__ __forceinline__ bf8 step(int i, bool last) const {
+        const int lane = threadIdx.x % 64;
+        const uint32_t mine = lane < 16 && i + 1 < N ? v[i + 1 < N ? i + 1 : i][0] : v[i][0];
+        uint32_t next = __shfl(mine, (lane + 16) & 63, 64);
+        if (last && lane >= 48) next = after;
+        u4 r;
+#pragma unroll
+        for (int e = 0; e < 3; ++e) r[e] = __builtin_amdgcn_alignbit(v[i][e + 1], v[i][e], shift);
+        r[3] = __builtin_amdgcn_alignbit(next, v[i][3], shift);
+        return __builtin_bit_cast(bf8, r);
+    }
+};
+
 // G: groups of 16 rows.  AHEAD steps of a wave are on their way at a time.
-template <typename T, int G, int WAVES>
+template <typename T, int G, int WAVES, bool ODD>
 __global__ __launch_bounds__(64 * WAVES) void k_rows(Operand ox, Operand ow, RowsShape s, Epilogue e) {
     using S = Step<T>;
     constexpr int AHEAD = G == 1 ? 8 : 4;
@@ -52,20 +86,47 @@ __global__ __launch_bounds__(64 * WAVES) void k_rows(Operand ox, Operand ow, Row
     f4 acc[G] = {};
     const int whole = s.K / S::kDepth;   // steps
     // a wave's steps: AHEAD in a row, then those of the others
-    for (int i0 = wave * AHEAD; i0 < whole; i0 += WAVES * AHEAD) {
-        wide<T, S::kLane> a[AHEAD], b[AHEAD][G];
+    if constexpr (ODD) {
+        OddRow<AHEAD> a, b[G];
+        a.begin(w);
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int64_t k = (int64_t)(i0 + i < whole ? i0 + i : whole - 1) * S::kDepth;
-            a[i] = *(const wide<T, S::kLane> *)(w + k);
+        for (int g = 0; g < G; ++g) b[g].begin(x[g]);
+        for (int i0 = wave * AHEAD; i0 < whole; i0 += WAVES * AHEAD) {
+            const int last = i0 + AHEAD < whole ? i0 + AHEAD - 1 : whole - 1;
 #pragma unroll
-            for (int g = 0; g < G; ++g) b[i][g] = *(const wide<T, S::kLane> *)(x[g] + k);
+            for (int i = 0; i < AHEAD; ++i) {
+                const int64_t k = (int64_t)(i0 + i < last ? i0 + i : last) * S::kDepth;
+                a.load(i, k);
+#pragma unroll
+                for (int g = 0; g < G; ++g) b[g].load(i, k);
+            }
+            a.load_after((int64_t)last * S::kDepth);
+#pragma unroll
+            for (int g = 0; g < G; ++g) b[g].load_after((int64_t)last * S::kDepth);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (i0 + i <= last) {
+                    const bf8 va = a.step(i, i0 + i == last);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) acc[g] = S::product(va, b[g].step(i, i0 + i == last), acc[g]);
+                }
         }
+    } else {
+        for (int i0 = wave * AHEAD; i0 < whole; i0 += WAVES * AHEAD) {
+            wide<T, S::kLane> a[AHEAD], b[AHEAD][G];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (i0 + i < whole)
+            for (int i = 0; i < AHEAD; ++i) {
+                const int64_t k = (int64_t)(i0 + i < whole ? i0 + i : whole - 1) * S::kDepth;
+                a[i] = *(const wide<T, S::kLane> *)(w + k);
 #pragma unroll
-                for (int g = 0; g < G; ++g) acc[g] = S::product(a[i], b[i][g], acc[g]);
+                for (int g = 0; g < G; ++g) b[i][g] = *(const wide<T, S::kLane> *)(x[g] + k);
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (i0 + i < whole)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) acc[g] = S::product(a[i], b[i][g], acc[g]);
+        }
     }
     const int rest = s.K - whole * S::kDepth;   // the sum's end, less than a step
     if (rest && wave == WAVES - 1) {
@@ -104,13 +165,18 @@ static hipError_t run(const Product &p, hipStream_t stream) {
     if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
     // waves: what the sum keeps busy
     const bool deep = p.K >= 16 * 4 * Step<T>::kDepth;
-    if (p.M <= 16) {
-        if (deep) k_rows<T, 1, 16><<<(int)blocks, 1024, 0, stream>>>(p.a, p.b, s, p.e);
-        else k_rows<T, 1, 4><<<(int)blocks, 256, 0, stream>>>(p.a, p.b, s, p.e);
-    } else {
-        if (deep) k_rows<T, 2, 16><<<(int)blocks, 1024, 0, stream>>>(p.a, p.b, s, p.e);
-        else k_rows<T, 2, 4><<<(int)blocks, 256, 0, stream>>>(p.a, p.b, s, p.e);
-    }
+    const auto go = [&](auto odd) {
+        if (p.M <= 16) {
+            if (deep) k_rows<T, 1, 16, odd><<<(int)blocks, 1024, 0, stream>>>(p.a, p.b, s, p.e);
+            else k_rows<T, 1, 4, odd><<<(int)blocks, 256, 0, stream>>>(p.a, p.b, s, p.e);
+        } else {
+            if (deep) k_rows<T, 2, 16, odd><<<(int)blocks, 1024, 0, stream>>>(p.a, p.b, s, p.e);
+            else k_rows<T, 2, 4, odd><<<(int)blocks, 256, 0, stream>>>(p.a, p.b, s, p.e);
+        }
+    };
+    const auto odd = [](const Operand &o) { return ((o.row | o.client) & 1) || (uintptr_t)o.p % 4; };
+    if (sizeof(T) == 2 && (odd(p.a) || odd(p.b))) go(std::bool_constant<sizeof(T) == 2>());
+    else go(std::false_type());
     return hipGetLastError();
 }
 

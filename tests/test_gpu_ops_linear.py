@@ -322,3 +322,37 @@ def test_outputs_on_another_stream_are_its_own(ops):
     assert owner == [s.cuda_stream]
     s.synchronize()
     assert torch.equal(y, ops.aet_linear_forward(x, w)[0])
+
+
+def among_nan(g, shape, dtype, scale, pad, skip):
+    """rand(), with NaN in the places before, between and after the rows."""
+    t = rand(g, shape, dtype, scale)
+    flat = torch.full((skip + t.numel() // shape[-1] * (shape[-1] + pad) + 9,), float("nan"), dtype=dtype, device=DEV)
+    to = flat[skip:flat.numel() - 9].view(*shape[:-1], shape[-1] + pad)[..., :shape[-1]]
+    to.copy_(t)
+    return to
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,skip", [(0, 0), (1, 0), (0, 1), (1, 1), (3, 2), (8, 8)])
+@pytest.mark.parametrize("size", [(2, 27, 2101, 40), (1, 1, 4097, 33), (3, 16, 2080, 20), (2, 20, 300, 50), (1, 3, 64, 17), (3, 9, 31, 16),
+                                  (2, 150, 200, 77), (1, 70, 129, 131), (2, 65, 64, 9), (1, 260, 515, 261)], ids=str)
+def test_places_between_rows(ops, size, pad, skip, dtype):
+    """Rows that begin at odd places, and memory around them that must not count."""
+    n, rows, inp, out = size
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(rows + inp + pad)
+    x, w = among_nan(g, (n, rows, inp), dt, 1.0, pad, skip), among_nan(g, (n, out, inp), dt, inp ** -0.5, 2 * pad, skip)
+    dy, pre = among_nan(g, (n, rows, out), dt, 1.0, pad, skip), among_nan(g, (n, rows, out), dt, 1.0, 0, 1)
+    b = among_nan(g, (n, out), dt, 1.0, pad, skip)
+    for xx in (x, x.contiguous()):   # the operands' rows begin alike, or not
+        y, _ = ops.aet_linear_forward(xx, w, b, act="silu")
+        O.near(y, O.linear_forward(d64(x), d64(w), d64(b), None, "silu", 0.0, 0, 0, dt)[0], f"y {size} {dtype} {pad} {skip}")
+        got = ops.aet_linear_backward(dy, xx, w, pre, act="silu")
+        want = O.linear_backward(d64(dy), d64(x), d64(w), d64(pre), "silu", 0.0, 0, 0, dt)
+        for what, a, c in zip(("dx", "dw", "db"), got, want):
+            O.near(a, c, f"{what} {size} {dtype} {pad} {skip}")
+        got = ops.aet_linear_backward(dy, xx, w, need=(True, True, False))   # the products' operand is dy itself
+        want = O.linear_backward(d64(dy), d64(x), d64(w), None, "none", 0.0, 0, 0, dt)
+        for what, a, c in zip(("dx", "dw"), got, want):
+            O.near(a, c, f"{what} of dy {size} {dtype} {pad} {skip}")
