@@ -10,8 +10,8 @@ static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 static Product forward_product(const aet_linear &a) {
     Product p = {};
-    p.a = {a.x.p, a.x.client, a.x.row, false};
-    p.b = {a.w.p, a.w.client, a.w.row, false};
+    p.a = {a.x.p, a.x.client, a.x.row, false, false};
+    p.b = {a.w.p, a.w.client, a.w.row, false, false};
     p.clients = a.n;
     p.M = a.rows;
     p.N = a.out;
@@ -45,6 +45,7 @@ __global__ __launch_bounds__(256) void k_dz(aet_linear_grad a, Drop d, DzShape s
     // thread's own, from `own` on, is counted.  Rows of less than a piece have `rest`.
     const int place = (b % s.across * 32 + tx) * V, col = place + V <= a.out ? place : a.out > V ? a.out - V : 0, own = place - col;
     const int rest = a.out < V ? a.out : V;
+    const bool ends = sizeof(T) == 2 && place < a.out && place + V > a.out;
     const int64_t first = (int64_t)strip * s.strip, end = first + s.strip < a.rows ? first + s.strip : a.rows;
     const T *dy = (const T *)a.dy.p + client * a.dy.client + col;
     const T *pre = (const T *)a.pre.p + client * a.pre.client + col;
@@ -65,7 +66,11 @@ __global__ __launch_bounds__(256) void k_dz(aet_linear_grad a, Drop d, DzShape s
             if (a.out & 1) drop_apply_any(d, q, col, v);
             else drop_apply(d, q, col, v);
         }
-        if (dz) store_some(dz + (client * a.rows + r) * s.dz_row + col, count, v);
+        if (dz) {
+            T *const to = dz + (client * a.rows + r) * s.dz_row;
+            if (ends) *(wide<T, V> *)(to + s.dz_row - V) = wide<T, V>{};   // zeros up to the next row, for the products
+            store_some(to + col, count, v);
+        }
 #pragma unroll
         for (int e = 0; e < V; ++e) sum[e] += v[e];
     };
@@ -139,12 +144,12 @@ static BackwardPlan plan(const aet_linear_grad &a, char *workspace) {
     b.dz_bytes = own ? up256((size_t)a.n * a.rows * b.dz.dz_row * e) : 0;
     b.db_bytes = a.db.p && b.dz.strips > 1 ? up256((size_t)b.dz.strips * a.n * a.out * sizeof(float)) : 0;
     b.dz.partial = (float *)(workspace + b.dz_bytes);
-    Operand dz = {a.dy.p, a.dy.client, a.dy.row, false};
-    if (own) dz = {workspace, a.rows * b.dz.dz_row, b.dz.dz_row, false};
+    Operand dz = {a.dy.p, a.dy.client, a.dy.row, false, false};
+    if (own) dz = {workspace, a.rows * b.dz.dz_row, b.dz.dz_row, false, true};
     const Drop none = {};
     if (a.dx.p) {
         b.dx.a = dz;
-        b.dx.b = {a.w.p, a.w.client, a.w.row, true};
+        b.dx.b = {a.w.p, a.w.client, a.w.row, true, false};
         b.dx.clients = a.n;
         b.dx.M = a.rows;
         b.dx.N = a.in;
@@ -154,7 +159,7 @@ static BackwardPlan plan(const aet_linear_grad &a, char *workspace) {
     if (a.dw.p) {
         dz.by_columns = true;
         b.dw.a = dz;
-        b.dw.b = {a.x.p, a.x.client, a.x.row, true};
+        b.dw.b = {a.x.p, a.x.client, a.x.row, true, false};
         b.dw.clients = a.n;
         b.dw.M = a.out;
         b.dw.N = a.in;

@@ -4,11 +4,12 @@
 
 namespace aet_ops {
 
-// By rows: element (r, k) is at p + client * c + row * r + k.  By columns: at p + client * c + row * k + r.
+// By rows: element (r, k) is at p + client * c + row * r + k.  By columns: at p + client * c + row * k + r.  Padded: what
+// lies side by side goes on with zeros up to a multiple of 8.
 struct Operand {
     const void *p;
     int64_t client, row;
-    bool by_columns;
+    bool by_columns, padded;
 };
 
 struct Product {

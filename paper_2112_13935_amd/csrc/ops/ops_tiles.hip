@@ -125,8 +125,8 @@ struct RegStage {
     }
 };
 
-// From memory into LDS, without registers: 16-byte aligned pieces, sums of whole stages, whole pieces of rows.  Rows past
-// the last are read from the last again: they become rows of C that are not stored.
+// From memory into LDS, without registers: 16-byte aligned pieces, none of which an end of the rows or the sum parts.  Rows
+// past the last are read from the last again: they become rows of C that are not stored.
 template <int R, int BK, bool COLS, int THREADS>
 struct DirectStage {
     using S = Stage<R, BK, COLS>;
@@ -135,16 +135,21 @@ struct DirectStage {
     uint32_t at[kCount];
     int64_t step;
 
+    // The thread's piece i: its row and place in the row
+    static __device__ __forceinline__ int row_of(int i) { return (threadIdx.x + i * THREADS) / S::kWidth; }
+    static __device__ __forceinline__ int place_of(int i) {
+        const int r = row_of(i);
+        return S::slot(r, (threadIdx.x + i * THREADS) % S::kWidth) - r * S::kWidth;   // the permutation is its own inverse
+    }
     __device__ __forceinline__ void begin(const Operand &o, int64_t client, int r0, int rows_all, int k0, int) {
         const int rows = rows_all - r0;
         p = (const char *)((const bf16 *)o.p + client * o.client + (COLS ? (int64_t)k0 * o.row + r0 : (int64_t)r0 * o.row + k0));
         step = (COLS ? BK * o.row : BK) * 2;
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const int q = threadIdx.x + i * THREADS, r = q / S::kWidth, s = q % S::kWidth;
-            const int c = S::slot(r, s) - r * S::kWidth;   // the permutation is its own inverse
+            const int r = row_of(i), c = place_of(i);
             if (COLS) {
-                const int last = rows - 8;
+                const int last = (o.padded ? (rows + 7) & ~7 : rows) - 8;
                 at[i] = (uint32_t)r * (uint32_t)(o.row * 2) + (uint32_t)(8 * c < last ? 8 * c : last) * 2;
             } else {
                 at[i] = (uint32_t)(r < rows ? r : rows - 1) * (uint32_t)(o.row * 2) + c * 16;
@@ -158,6 +163,18 @@ struct DirectStage {
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p + at[i]),
                                              (__attribute__((address_space(3))) void *)(to + (i * THREADS + wave * 64) * 16), 16, 0, 0);
         p += step;
+    }
+    // The sum's last stage, of which `left` k are there: the rest are zeros.
+    __device__ __forceinline__ void load_end(lds_ptr to, int left) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            if ((COLS ? row_of(i) : 8 * place_of(i)) < left)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p + at[i]),
+                                                 (__attribute__((address_space(3))) void *)(to + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+            else
+                *(__attribute__((address_space(3))) bf8 *)(to + (i * THREADS + threadIdx.x) * 16) = bf8{};
+        }
     }
 };
 
@@ -263,10 +280,17 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
         // ahead of the stage's last products, and right behind it the stage after the next is sent for.
         constexpr int kBuffers = L::kBuffers, KS = BK / 16, kReads = (TA ? 2 : 1) * FM + (TB ? 2 : 1) * FN;
         constexpr int kLoads = decltype(la)::kCount + decltype(lb)::kCount;
+        static_assert(kBuffers == 2, "every wait in the loop is for all that is on its way");
+        const int whole = k1 > k0 ? (k1 - k0) / BK : 0;   // stages; there may be an end of another
         const auto fetch = [&](int i) {
             const lds_ptr to = lds + i % kBuffers * L::kStage;
             la.load(to);
             lb.load(to + kPartA);
+        };
+        const auto fetch_end = [&]() {
+            const lds_ptr to = lds + whole % kBuffers * L::kStage;
+            la.load_end(to, k1 - k0 - whole * BK);
+            lb.load_end(to + kPartA, k1 - k0 - whole * BK);
         };
         // s_waitcnt by its encoding (vmcnt low and high bits, lgkmcnt 0), which the compiler takes into account
         const auto arrived = [&](auto still) {
@@ -276,22 +300,28 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
         typedef std::integral_constant<int, (kBuffers - 2) * kLoads> Others;
         typedef std::integral_constant<int, 0> None;
         Fragments f[2];
-        for (int i = 0; i < kBuffers && i < stages; ++i) fetch(i);
-        if (stages >= kBuffers) arrived(std::integral_constant<int, (kBuffers - 1) * kLoads>());
+        for (int i = 0; i < kBuffers && i < whole; ++i) fetch(i);
+        if (whole < stages && whole < kBuffers) fetch_end();   // (whose loads cannot be counted)
+        if (whole >= kBuffers) arrived(std::integral_constant<int, (kBuffers - 1) * kLoads>());
         else arrived(None());
         if (stages > 0) read(f[0], lds, 0);
         int i = 0;
-        for (; i + kBuffers < stages; ++i) {
+        const auto stage = [&](auto get) {
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 if (ks + 1 == KS) {
                     arrived(Others());
-                    fetch(i + kBuffers);
+                    get();
                 }
                 read(f[(ks + 1) % 2], lds + (i + (ks + 1) / KS) % kBuffers * L::kStage, (ks + 1) % KS);
                 multiply(f[ks % 2]);
                 interleave<FM * FN, kReads>();
             }
+        };
+        for (; i + kBuffers < whole; ++i) stage([&]() { fetch(i + kBuffers); });
+        if (i + kBuffers < stages) {
+            stage(fetch_end);
+            ++i;
         }
         for (; i < stages; ++i) {
 #pragma unroll
@@ -429,8 +459,8 @@ __global__ __launch_bounds__(256) void k_join(Shape s, Epilogue e) {
 // Whether the operand's stages of BK can go straight into LDS.
 static bool direct(const Operand &o, int rows, int K, int BK) {
     const int64_t across = o.by_columns ? BK : 256;
-    return aligned16(o.p, 2, o.client, o.row) && o.row * 2 * across < (INT64_C(1) << 31) && K % BK == 0 && K > 0 &&
-           (!o.by_columns || rows % 8 == 0);
+    return aligned16(o.p, 2, o.client, o.row) && o.row * 2 * across < (INT64_C(1) << 31) && K > 0 &&
+           (o.padded || (o.by_columns ? rows : K) % 8 == 0);
 }
 
 template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT>
@@ -467,7 +497,7 @@ struct Kind {
 static const Kind kKinds32[] = {{128, 128, 32, 2, 2.2f, 0.5f, 2.0f}, {64, 128, 32, 3, 1.35f, 0.60f, 1.0f}, {64, 64, 32, 5, 0.95f, 0.35f, 0.5f}};
 static const Kind kKinds16[] = {{256, 256, 64, 1, 1.6f, 0.0f, 8.0f}, {128, 128, 64, 2, 0.65f, 0.45f, 2.0f}, {64, 128, 64, 3, 0.54f, 0.22f, 1.0f}, {64, 64, 64, 5, 0.46f, 0.13f, 0.5f}};
 
-// bf16 through registers
+// bf16 through registers (256 x 256 by rows only: 4095 x 4097 x 4093 by rows 160, 128 x 128 209, by columns 281 and 217)
 static const Kind kKinds16Any[] = {{256, 256, 64, 1, 2.6f, 0.0f, 8.0f}, {128, 128, 64, 2, 1.7f, 0.4f, 2.0f}, {64, 128, 64, 3, 0.95f, 0.42f, 1.0f}, {64, 64, 64, 5, 0.62f, 0.31f, 0.5f}};
 
 struct Choice {
@@ -493,7 +523,7 @@ static Choice choose(int dtype, const Product &p, bool straight) {
     };
     if (dtype == AET_F32) for (const Kind &k : kKinds32) consider(k);
     else if (straight) for (const Kind &k : kKinds16) consider(k);
-    else for (const Kind &k : kKinds16Any) consider(k);
+    else for (const Kind &k : kKinds16Any) if (k.bm < 256 || !p.b.by_columns) consider(k);
     return best;
 }
 
@@ -537,8 +567,10 @@ static hipError_t run_product(const Product &p, void *workspace, hipStream_t str
         else if (k.bn == 128) e = run_tiles<T, 64, 128, 32, 2, 2, TA, TB, false>(p, s, stream);
         else e = run_tiles<T, 64, 64, 32, 2, 2, TA, TB, false>(p, s, stream);
     } else {
-        if (k.bm == 256) e = d ? run_tiles<T, 256, 256, 64, 2, 4, TA, TB, true>(p, s, stream) : run_tiles<T, 256, 256, 64, 2, 4, TA, TB, false>(p, s, stream);
-        else if (k.bm == 128) e = d ? run_tiles<T, 128, 128, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 128, 128, 64, 2, 2, TA, TB, false>(p, s, stream);
+        if (k.bm == 256) {
+            if constexpr (TB) e = run_tiles<T, 256, 256, 64, 2, 4, TA, TB, true>(p, s, stream);
+            else e = d ? run_tiles<T, 256, 256, 64, 2, 4, TA, TB, true>(p, s, stream) : run_tiles<T, 256, 256, 64, 2, 4, TA, TB, false>(p, s, stream);
+        } else if (k.bm == 128) e = d ? run_tiles<T, 128, 128, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 128, 128, 64, 2, 2, TA, TB, false>(p, s, stream);
         else if (k.bn == 128) e = d ? run_tiles<T, 64, 128, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 64, 128, 64, 2, 2, TA, TB, false>(p, s, stream);
         else e = d ? run_tiles<T, 64, 64, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 64, 64, 64, 2, 2, TA, TB, false>(p, s, stream);
     }

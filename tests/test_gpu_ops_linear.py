@@ -356,3 +356,30 @@ def test_places_between_rows(ops, size, pad, skip, dtype):
         want = O.linear_backward(d64(dy), d64(x), d64(w), None, "none", 0.0, 0, 0, dt)
         for what, a, c in zip(("dx", "dw"), got, want):
             O.near(a, c, f"{what} of dy {size} {dtype} {pad} {skip}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(1, 200, 264, 333), (2, 300, 72, 70), (1, 520, 1000, 1000), (1, 40, 4104, 72), (1, 72, 8, 520), (3, 33, 136, 200),
+                                  (1, 300, 1992, 40), (1, 1992, 64, 328)], ids=str)
+def test_sums_that_end_inside_a_stage(ops, size, dtype):
+    """What lies behind the end of a sum, the next row's first values, must not count: they are infinite in every second row."""
+    n, rows, inp, out = size
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(rows + inp)
+    x, w, dy, pre = (rand(g, s, dt, c) for s, c in (((n, rows, inp), 1.0), ((n, out, inp), inp ** -0.5), ((n, rows, out), 1.0), ((n, rows, out), 1.0)))
+    y, _ = ops.aet_linear_forward(x, w)
+    O.near(y, O.linear_forward(d64(x), d64(w), None, None, "none", 0.0, 0, 0, dt)[0], f"y {size} {dtype}")
+    got = ops.aet_linear_backward(dy, x, w, pre, act="gelu", p=0.1, seed=9)
+    want = O.linear_backward(d64(dy), d64(x), d64(w), d64(pre), "gelu", 0.1, 9, 0, dt)
+    for what, a, c in zip(("dx", "dw", "db"), got, want):
+        O.near(a, c, f"{what} {size} {dtype}")
+    bad = x.clone()
+    bad[:, 1::2, 0] = float("inf")
+    assert torch.equal(ops.aet_linear_forward(bad, w)[0][:, ::2], y[:, ::2])
+    dx, dw, _ = ops.aet_linear_backward(dy, x, w)
+    bad = dy.clone()
+    bad[:, 1::2, 0] = float("inf")
+    assert torch.equal(ops.aet_linear_backward(bad, x, w)[0][:, ::2], dx[:, ::2])
+    bad = x.clone()
+    bad[..., 1::2] = float("nan")   # columns of the gradient of w
+    assert torch.equal(ops.aet_linear_backward(dy, bad, w)[1][..., ::2], dw[..., ::2])
