@@ -17,7 +17,8 @@
  *     are not negative (0: the same values for every row or client).  Outputs must not
  *     overlap themselves, nor an input, except where a call says so.  Any alignment that
  *     the type itself has is taken; 16-byte aligned pointers and strides of whole 16 bytes
- *     are faster.
+ *     are faster.  Memory between the rows of an input may be read; what it holds does not
+ *     count.
  *   - Work is enqueued on the given stream of the current device and is asynchronous; nothing
  *     synchronises, so that calls can be captured into a graph.  (The numbers in the
  *     argument record, the dropout's seed among them, are then part of the graph.)
@@ -137,7 +138,8 @@ aet_status aet_group_norm_forward(const aet_group_norm *a, void *workspace, size
 
 /* Its gradient, from the inputs and the statistics that the forward call gave.
  *   dx            may be dy itself, with the same strides; or p = NULL
- *   dgamma, dbeta n x channels; client = 0 with n other than 1: the sum over the clients (then of both); or p = NULL */
+ *   dgamma, dbeta n x channels; client = 0 with n other than 1: the sum over the clients
+ *                 (then of both); or p = NULL */
 typedef struct {
     int32_t dtype, act;
     int32_t n, batch, positions, groups, width;

@@ -9,14 +9,9 @@
 namespace aet_ops {
 
 typedef __bf16 bf16;
-typedef bf16 bf2 __attribute__((ext_vector_type(2)));
-typedef bf16 bf4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf8 __attribute__((ext_vector_type(8)));
-typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
-typedef float f8 __attribute__((ext_vector_type(8)));
 typedef float f16v __attribute__((ext_vector_type(16)));
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 // V values in memory, in one wide access whatever their alignment beyond the type's own.
 template <typename T, int V>

@@ -5,6 +5,9 @@
 // a group has few channels.  Where a sample's groups fit the registers of a workgroup, one kernel reads every value once
 // (k_norm_whole, k_norm_back_whole): mean first, then the squares of the differences from it.  Larger samples take
 // three: sums of strips of positions, their union by group, and a second pass over the values.
+//   2048 samples of 1024 x 32 in fp32, groups of 4 channels, silu: 123 us (537 MB, 4.4 TB/s; a copy of as much 107)
+//   gradient of 128 samples of 4096 x 320 in bf16, groups of 10: 343 us: sums 166 (671 MB read, 4.0 TB/s), union 8, second
+//   pass 197 (1.0 GB, 5.1 TB/s) under the profiler; reading the values once is 201, which no compute unit's registers hold
 #include "ops_internal.h"
 
 namespace aet_ops {
