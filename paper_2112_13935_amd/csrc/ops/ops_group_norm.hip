@@ -27,10 +27,15 @@ struct NormShape {
 
 struct Where {
     int64_t sample, client, in_batch;
-    int ch0, chans, piece, lane, ch, count;   // ch, count: the thread's first channel, and how many it has
-    int group[8];                             // of its channels
+    int ch0, chans, piece, lane, count;   // count: how many channels the thread has
+    // A thread reads V values from channel `ch` on, of which [lo, lo + count) are its own: where fewer are left it reads
+    // neighbours' too, or begins earlier, so that nobody has to look where pieces end.  (Samples of fewer channels than V
+    // have count values from ch on.)
+    int ch, lo;
+    int group[8];                         // of the channels read
 };
-template <int V>
+// ODD: some pieces are not whole.  (Compiled apart: 2 to 3 % where all are.)
+template <int V, bool ODD>
 __device__ __forceinline__ Where where(const NormShape &s, int batch, int width, uint32_t block) {
     Where w;
     const uint32_t sample = block / (uint32_t)s.spans, client = sample / (uint32_t)batch;
@@ -41,15 +46,17 @@ __device__ __forceinline__ Where where(const NormShape &s, int batch, int width,
     w.in_batch = sample - client * (uint32_t)batch;
     w.lane = threadIdx.x / (uint32_t)s.pieces;
     w.piece = threadIdx.x - w.lane * s.pieces;
-    w.ch = w.ch0 + w.piece * V;
+    const int own = w.ch0 + w.piece * V;
     w.count = w.lane < s.lanes ? w.chans - w.piece * V : 0;
     if (w.count > V) w.count = V;
-    // (channels that are not there have the group of one that is, so that nothing has to be tested to read what it has)
+    w.ch = !ODD || s.channels < V || own + V <= s.channels ? own : s.channels - V;
+    w.lo = own - w.ch;
+    // (channels of other workgroups have the group of one that is here, so that nothing has to be tested to read what it has)
     int g = w.ch / width, k = w.ch - g * width;
-    const int last = (w.ch0 + w.chans - 1) / width;
+    const int first = w.ch0 / width, last = (w.ch0 + w.chans - 1) / width;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        w.group[e] = g < last ? g : last;
+        w.group[e] = g < first ? first : g < last ? g : last;
         if (++k == width) {
             k = 0;
             ++g;
@@ -60,10 +67,17 @@ __device__ __forceinline__ Where where(const NormShape &s, int batch, int width,
 
 // Sums by channel over the workgroup's threads, of N arrays at a time: tot[n * span + k], k < chans.  lds: N * threads * V
 // floats.  First within waves where a wave has whole rows of pieces, then by halving the rows until two are left.
-template <int V, int N>
+template <bool ODD, int V, int N>
 __device__ __forceinline__ void channel_sums(const NormShape &s, const Where &w, float (&v)[N][V], float *lds, float *tot) {
     const int line = s.pieces * V, all = s.threads * V;
     int rows = s.lanes, row = w.lane;
+    if (ODD && w.count < V) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (e < w.lo || e >= w.lo + w.count) v[n][e] = 0.0f;
+    }
     bool mine = w.lane < s.lanes;
     if (s.pieces < 64 && !(s.pieces & (s.pieces - 1))) {   // (threads without a position have zeros)
         for (int off = 32; off >= s.pieces; off >>= 1)
@@ -76,12 +90,18 @@ __device__ __forceinline__ void channel_sums(const NormShape &s, const Where &w,
         mine = threadIdx.x % 64 < s.pieces;
     }
     __syncthreads();
-    if (mine) {
+    if (mine && (!ODD || w.lo == 0)) {
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int e = 0; e < V; e += 4)
                 *(f4 *)(lds + n * all + row * line + w.piece * V + e) = f4{v[n][e], v[n][e + 1], v[n][e + 2], v[n][e + 3]};
+    } else if (ODD && mine) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (e >= w.lo) lds[n * all + row * line + w.piece * V + e - w.lo] = v[n][e];
     }
     __syncthreads();
     while (rows > 2) {
@@ -109,6 +129,20 @@ __device__ __forceinline__ void group_sums(const float *tot, const float *by, in
     __syncthreads();
 }
 
+// The thread's V values of a row (count: V, or fewer in samples of fewer channels), and its own of them to their places.
+template <int V, bool ODD>
+__device__ __forceinline__ int to_read(const NormShape &s, const Where &w) { return w.count <= 0 ? 0 : ODD && s.channels < V ? w.count : V; }
+template <bool ODD, typename T, int V>
+__device__ __forceinline__ void store_own(T *p, const Where &w, const float (&v)[V]) {
+    if (!ODD || w.count == V) {
+        store_some(p, V, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (e >= w.lo && e < w.lo + w.count) p[e] = (T)v[e];
+    }
+}
+
 template <typename T, int V>
 __device__ __forceinline__ void params(const aet_in &p, int64_t client, int ch, int count, float none, float (&v)[V]) {
     if (p.p && count > 0) {
@@ -127,23 +161,23 @@ __device__ __forceinline__ void by_channel(const Where &w, int first, const floa
 
 // ---- a sample's groups in registers ------------------------------------------------------
 
-template <typename T, int V, int N>
+template <typename T, int V, int N, bool ODD>
 __global__ __launch_bounds__(kThreads) void k_norm_whole(aet_group_norm a, NormShape s) {
     extern __shared__ float lds[];   // threads * V, then by channel, then by group
     float *const tot = lds + s.threads * V, *const stat = tot + s.span;
-    const Where w = where<V>(s, a.batch, a.width, xcd_order(blockIdx.x, gridDim.x));
+    const Where w = where<V, ODD>(s, a.batch, a.width, xcd_order(blockIdx.x, gridDim.x));
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     T *y = (T *)a.y.p + w.client * a.y.client + w.in_batch * a.y.sample + w.ch;
     wide<T, V> raw[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int pos = w.lane + i * s.lanes;
-        raw[i] = load_raw<T, V>(x + pos * a.x.row, pos < a.positions ? w.count : 0);
+        raw[i] = load_raw<T, V>(x + pos * a.x.row, pos < a.positions ? to_read<V, ODD>(s, w) : 0);
     }
     float gamma[V], beta[V];
     const auto parameters = [&]() {
-        params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
-        params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+        params<T>(a.gamma, w.client, w.ch, to_read<V, ODD>(s, w), 1.0f, gamma);
+        params<T>(a.beta, w.client, w.ch, to_read<V, ODD>(s, w), 0.0f, beta);
     };
     if (N <= 4) parameters();   // early where there are registers for it (16 positions: 88 instead of 80, 124 -> 130 us)
     float acc[1][V] = {};
@@ -153,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_whole(aet_group_norm a, NormS
         for (int e = 0; e < V; ++e) acc[0][e] += (float)raw[i][e];
     const int groups = w.chans / a.width, g0 = w.ch0 / a.width;
     const float inv = 1.0f / ((float)a.positions * (float)a.width);
-    channel_sums(s, w, acc, lds, tot);
+    channel_sums<ODD>(s, w, acc, lds, tot);
     group_sums(tot, nullptr, groups, a.width, inv, stat);
     float mean[V], scale[V];
     by_channel(w, g0, stat, mean);
@@ -168,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_whole(aet_group_norm a, NormS
                 acc[0][e] += d * d;
             }
         }
-    channel_sums(s, w, acc, lds, tot);
+    channel_sums<ODD>(s, w, acc, lds, tot);
     if (a.mean)
         for (int g = threadIdx.x; g < groups; g += blockDim.x) a.mean[w.sample * a.groups + g0 + g] = stat[g];
     __syncthreads();
@@ -190,7 +224,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_whole(aet_group_norm a, NormS
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] = __builtin_fmaf((float)raw[i][e] - mean[e], scale[e], beta[e]);
         act_each(a.act, v);
-        store_some(y + pos * a.y.row, w.count, v);
+        store_own<ODD>(y + pos * a.y.row, w, v);
     }
 }
 
@@ -208,13 +242,13 @@ __device__ __forceinline__ void slopes(int act, const wide<T, V> &x, const wide<
     slope_each(act, t, d);
 }
 // What a thread's channels need for it.
-template <typename T, int V>
-__device__ __forceinline__ void slope_params(const aet_group_norm_grad &a, const Where &w, float (&mean)[V], float (&scale)[V], float (&beta)[V]) {
+template <bool ODD, typename T, int V>
+__device__ __forceinline__ void slope_params(const aet_group_norm_grad &a, const NormShape &s, const Where &w, float (&mean)[V], float (&scale)[V], float (&beta)[V]) {
     float rstd[V];
     by_channel(w, 0, a.mean + w.sample * a.groups, mean);
     by_channel(w, 0, a.rstd + w.sample * a.groups, rstd);
-    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, scale);
-    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+    params<T>(a.gamma, w.client, w.ch, to_read<V, ODD>(s, w), 1.0f, scale);
+    params<T>(a.beta, w.client, w.ch, to_read<V, ODD>(s, w), 0.0f, beta);
 #pragma unroll
     for (int e = 0; e < V; ++e) scale[e] *= rstd[e];
 }
@@ -225,23 +259,23 @@ __device__ __forceinline__ void to_dx(const float (&scale)[V], const float (&c1)
     for (int e = 0; e < V; ++e) d[e] = __builtin_fmaf(d[e], scale[e], -__builtin_fmaf(xm[e], c2[e], c1[e]));
 }
 
-template <typename T, int V, int N>
+template <typename T, int V, int N, bool ODD>
 __global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_grad a, NormShape s) {
     extern __shared__ float lds[];
     float *const totA = lds + 2 * s.threads * V, *const totB = totA + s.span, *const gam = totB + s.span, *const stat = gam + s.span;
-    const Where w = where<V>(s, a.batch, a.width, xcd_order(blockIdx.x, gridDim.x));
+    const Where w = where<V, ODD>(s, a.batch, a.width, xcd_order(blockIdx.x, gridDim.x));
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
     wide<T, V> rx[N], rd[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int pos = w.lane + i * s.lanes, count = pos < a.positions ? w.count : 0;
+        const int pos = w.lane + i * s.lanes, count = pos < a.positions ? to_read<V, ODD>(s, w) : 0;
         rx[i] = load_raw<T, V>(x + pos * a.x.row, count);
         rd[i] = load_raw<T, V>(dy + pos * a.dy.row, count);
     }
     const int groups = w.chans / a.width, g0 = w.ch0 / a.width;
     float mean[V], scale[V], beta[V];
-    slope_params<T>(a, w, mean, scale, beta);
+    slope_params<ODD, T>(a, s, w, mean, scale, beta);
     float AB[2][V] = {};
     float d[N][V];
 #pragma unroll
@@ -254,7 +288,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_gra
             AB[1][e] += d[i][e] * xm[e];
         }
     }
-    channel_sums(s, w, AB, lds, totA);
+    channel_sums<ODD>(s, w, AB, lds, totA);
     const float *const rstd_of = a.rstd + w.sample * a.groups + g0;
     for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
         float *to = s.sums + w.sample * 2 * s.channels + w.ch0 + k;
@@ -285,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_whole(aet_group_norm_gra
 #pragma unroll
         for (int e = 0; e < V; ++e) xm[e] = (float)rx[i][e] - mean[e];
         to_dx(scale, c1, c2, xm, d[i]);
-        store_some(dx + pos * a.dx.row, w.count, d[i]);
+        store_own<ODD>(dx + pos * a.dx.row, w, d[i]);
     }
 }
 
@@ -309,19 +343,19 @@ __device__ __forceinline__ void each_position(int pos, int end, int step, int co
 }
 
 // Of a strip's values of a channel: their mean, and the sum of squares of the differences from it.
-template <typename T, int V>
+template <typename T, int V, bool ODD>
 __global__ __launch_bounds__(kThreads) void k_norm_strips(aet_group_norm a, NormShape s) {
     extern __shared__ float lds[];
     float *const tot = lds + 2 * s.threads * V;
     const int strip = blockIdx.x % (uint32_t)s.strips;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.strips);
+    const Where w = where<V, ODD>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.strips);
     const int first = strip * s.strip, end = a.positions - first < s.strip ? a.positions : first + s.strip;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     // about the strip's first value, so that the squares do not cancel where the mean is far from 0
-    const wide<T, V> about = load_raw<T, V>(x + first * a.x.row, w.count);
+    const wide<T, V> about = load_raw<T, V>(x + first * a.x.row, to_read<V, ODD>(s, w));
     float SQ[2][V] = {};
     wide<T, V> raw[4];
-    each_position(first + w.lane, end, s.lanes, w.count, V, [&](int pos, int i, int count) { raw[i] = load_raw<T, V>(x + pos * a.x.row, count); },
+    each_position(first + w.lane, end, s.lanes, to_read<V, ODD>(s, w), V, [&](int pos, int i, int count) { raw[i] = load_raw<T, V>(x + pos * a.x.row, count); },
                   [&](int, int i, int) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -332,7 +366,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_strips(aet_group_norm a, Norm
     });
     float *to = s.sums + (w.sample * s.strips + strip) * 2 * s.channels + w.ch0;
     const float inv = 1.0f / (float)(end - first);
-    channel_sums(s, w, SQ, lds, tot);
+    channel_sums<ODD>(s, w, SQ, lds, tot);
     const T *about0 = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + first * a.x.row + w.ch0;
     for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
         const float off = tot[k] * inv, m2 = tot[s.span + k] - tot[k] * off;
@@ -379,10 +413,10 @@ __global__ __launch_bounds__(256) void k_norm_union(aet_group_norm a, NormShape 
     if (a.rstd) a.rstd[blockIdx.x] = rstd;
 }
 
-template <typename T, int V>
+template <typename T, int V, bool ODD>
 __global__ __launch_bounds__(kThreads) void k_norm_apply(aet_group_norm a, NormShape s) {
     const int part = blockIdx.x % (uint32_t)s.parts;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.parts);
+    const Where w = where<V, ODD>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.parts);
     if (w.count <= 0) return;
     const int first = part * s.part, end = a.positions - first < s.part ? a.positions : first + s.part;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
@@ -391,38 +425,38 @@ __global__ __launch_bounds__(kThreads) void k_norm_apply(aet_group_norm a, NormS
     const float *stat = s.stats + w.sample * 2 * a.groups;
     by_channel(w, 0, stat, mean);
     by_channel(w, 0, stat + a.groups, scale);
-    params<T>(a.gamma, w.client, w.ch, w.count, 1.0f, gamma);
-    params<T>(a.beta, w.client, w.ch, w.count, 0.0f, beta);
+    params<T>(a.gamma, w.client, w.ch, to_read<V, ODD>(s, w), 1.0f, gamma);
+    params<T>(a.beta, w.client, w.ch, to_read<V, ODD>(s, w), 0.0f, beta);
 #pragma unroll
     for (int e = 0; e < V; ++e) scale[e] *= gamma[e];
     wide<T, V> raw[4];
-    each_position(first + w.lane, end, s.lanes, w.count, V, [&](int pos, int i, int count) { raw[i] = load_raw<T, V>(x + pos * a.x.row, count); },
+    each_position(first + w.lane, end, s.lanes, to_read<V, ODD>(s, w), V, [&](int pos, int i, int count) { raw[i] = load_raw<T, V>(x + pos * a.x.row, count); },
                   [&](int pos, int i, int count) {
         float v[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] = __builtin_fmaf((float)raw[i][e] - mean[e], scale[e], beta[e]);
         act_each(a.act, v);
-        store_some(y + pos * a.y.row, count, v);
+        store_own<ODD>(y + pos * a.y.row, w, v);
     });
 }
 
-template <typename T, int V>
+template <typename T, int V, bool ODD>
 __global__ __launch_bounds__(kThreads) void k_norm_back_strips(aet_group_norm_grad a, NormShape s) {
     extern __shared__ float lds[];
     float *const tot = lds + 2 * s.threads * V;
     const int strip = blockIdx.x % (uint32_t)s.strips;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.strips);
+    const Where w = where<V, ODD>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.strips);
     const int first = strip * s.strip, end = a.positions - first < s.strip ? a.positions : first + s.strip;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
     float mean[V], scale[V], beta[V], AB[2][V] = {};
-    slope_params<T>(a, w, mean, scale, beta);
+    slope_params<ODD, T>(a, s, w, mean, scale, beta);
     wide<T, V> rx[4], rd[4];
     const auto load = [&](int pos, int i, int count) {
         rx[i] = load_raw<T, V>(x + pos * a.x.row, count);
         rd[i] = load_raw<T, V>(dy + pos * a.dy.row, count);
     };
-    each_position(first + w.lane, end, s.lanes, w.count, V, load, [&](int, int i, int) {
+    each_position(first + w.lane, end, s.lanes, to_read<V, ODD>(s, w), V, load, [&](int, int i, int) {
         float d[V], xm[V];
         slopes<T, V>(a.act, rx[i], rd[i], mean, scale, beta, d, xm);
 #pragma unroll
@@ -432,7 +466,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_strips(aet_group_norm_gr
         }
     });
     float *to = s.sums + (w.sample * s.strips + strip) * 2 * s.channels + w.ch0;
-    channel_sums(s, w, AB, lds, tot);
+    channel_sums<ODD>(s, w, AB, lds, tot);
     for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
         to[k] = tot[k];
         to[s.channels + k] = tot[s.span + k] * a.rstd[w.sample * a.groups + (w.ch0 + k) / a.width];
@@ -470,17 +504,17 @@ __global__ __launch_bounds__(256) void k_norm_back_union(aet_group_norm_grad a, 
     s.stats[at + a.groups] = s2 * rstd * rstd;
 }
 
-template <typename T, int V>
+template <typename T, int V, bool ODD>
 __global__ __launch_bounds__(kThreads) void k_norm_back_apply(aet_group_norm_grad a, NormShape s) {
     const int part = blockIdx.x % (uint32_t)s.parts;
-    const Where w = where<V>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.parts);
+    const Where w = where<V, ODD>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.parts);
     if (w.count <= 0) return;
     const int first = part * s.part, end = a.positions - first < s.part ? a.positions : first + s.part;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
     const T *dy = (const T *)a.dy.p + w.client * a.dy.client + w.in_batch * a.dy.sample + w.ch;
     T *dx = (T *)a.dx.p + w.client * a.dx.client + w.in_batch * a.dx.sample + w.ch;
     float mean[V], scale[V], beta[V], c1[V], c2[V];
-    slope_params<T>(a, w, mean, scale, beta);
+    slope_params<ODD, T>(a, s, w, mean, scale, beta);
     by_channel(w, 0, s.stats + w.sample * 2 * a.groups, c1);
     by_channel(w, 0, s.stats + (w.sample * 2 + 1) * a.groups, c2);
     wide<T, V> rx[4], rd[4];
@@ -488,11 +522,11 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_apply(aet_group_norm_gra
         rx[i] = load_raw<T, V>(x + pos * a.x.row, count);
         rd[i] = load_raw<T, V>(dy + pos * a.dy.row, count);
     };
-    each_position(first + w.lane, end, s.lanes, w.count, V, load, [&](int pos, int i, int count) {
+    each_position(first + w.lane, end, s.lanes, to_read<V, ODD>(s, w), V, load, [&](int pos, int i, int count) {
         float d[V], xm[V];
         slopes<T, V>(a.act, rx[i], rd[i], mean, scale, beta, d, xm);
         to_dx(scale, c1, c2, xm, d);
-        store_some(dx + pos * a.dx.row, count, d);
+        store_own<ODD>(dx + pos * a.dx.row, w, d);
     });
 }
 
@@ -548,11 +582,10 @@ static NormPlan make_plan(int64_t samples, int positions, int groups, int width,
     NormShape &s = p.s;
     s.channels = groups * width;
     // Whole groups: as many as fit the registers, of those as give 512 workgroups, but 64 bytes of neighbouring channels
-    // unless that leaves fewer than 128; and in whole pieces where half as many or more are (forward, 256 samples of
-    // 1024 x 320 in fp32, groups of 10 channels: two 220 us, three 258).  A sample's workgroups share lines of memory and
-    // run on one XCD (128 samples of 4096 x 128 in bf16, 16 channels each: 75 us, dealt over the XCDs 139).
-    // Less than 64 bytes, or pieces that are not whole: three kernels (the same samples 72 us; 256 samples of 1024 x 320
-    // in fp32, the gradient in groups of 10 channels: 344 us, in one kernel 500), unless the launches are what counts.
+    // unless that leaves fewer than 128.  A sample's workgroups share lines of memory and run on one XCD (128 samples of
+    // 4096 x 128 in bf16, 16 channels each: 75 us, dealt over the XCDs 139).  Less than 64 bytes: three kernels (the same
+    // samples 72 us; 256 samples of 1024 x 320 in fp32, the gradient in groups of 10 channels: 340 us, in one kernel 500),
+    // unless the launches are what counts.
     const int most = back ? 8 : 16;
     const int64_t lanes = ceil_div(positions, most), fit_pieces = lanes > kThreads ? 0 : kThreads / lanes;
     int64_t fit = (fit_pieces < 256 ? fit_pieces : 256) * V / width;
@@ -565,16 +598,10 @@ static NormPlan make_plan(int64_t samples, int positions, int groups, int width,
         if (best > at_least_1(samples * groups / 128)) best = at_least_1(samples * groups / 128);
         if (best > fit) best = fit;
         best = ceil_div(groups, ceil_div(groups, best));
-        if (best < groups)
-            for (int64_t b = best; b > best / 2; --b)
-                if (b * width % V == 0) {
-                    best = b;
-                    break;
-                }
         s.span_groups = (int)best;
     }
     const int best = s.span_groups;
-    p.whole = best && (best == groups || (best * width >= 4 * V && best * width % V == 0) || samples * positions * s.channels < (1 << 22));
+    p.whole = best && (best == groups || best * width >= 4 * V || samples * positions * s.channels < (1 << 22));
     if (p.whole) {
         deal(s, V, best * width);
         s.lanes = kThreads / s.pieces;
@@ -616,7 +643,14 @@ static NormPlan plan(const aet_group_norm_grad &a) {
 size_t group_norm_forward_workspace(const aet_group_norm &a) { return a.n && a.batch && a.positions ? plan(a).bytes : 0; }
 size_t group_norm_backward_workspace(const aet_group_norm_grad &a) { return a.n && a.batch && a.positions ? plan(a).bytes : 0; }
 
+// Whether a workgroup's channels are not whole pieces.
 template <typename T>
+static bool odd_pieces(const NormShape &s) {
+    constexpr int V = 16 / sizeof(T);
+    return s.channels % V || (s.spans > 1 && s.span % V);
+}
+
+template <typename T, bool ODD>
 static hipError_t forward(const aet_group_norm &a, char *workspace, hipStream_t s) {
     constexpr int V = 16 / sizeof(T);
     const int64_t samples = (int64_t)a.n * a.batch;
@@ -630,21 +664,25 @@ static hipError_t forward(const aet_group_norm &a, char *workspace, hipStream_t 
     const int64_t blocks = samples * p.s.spans * p.s.strips;
     if (blocks > INT32_MAX || samples * p.s.spans * p.s.parts > INT32_MAX || samples * a.groups > INT32_MAX) return hipErrorInvalidConfiguration;
     if (p.whole) {
-        if (p.n <= 4) k_norm_whole<T, V, 4><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
-        else if (p.n <= 8) k_norm_whole<T, V, 8><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
-        else k_norm_whole<T, V, 16><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+        if (p.n <= 4) k_norm_whole<T, V, 4, ODD><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+        else if (p.n <= 8) k_norm_whole<T, V, 8, ODD><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+        else k_norm_whole<T, V, 16, ODD><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
     } else {
-        k_norm_strips<T, V><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+        k_norm_strips<T, V, ODD><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
         k_norm_union<<<(int)(samples * a.groups), 256, 0, s>>>(a, p.s);
-        k_norm_apply<T, V><<<(int)(samples * p.s.spans * p.s.parts), p.s.threads, 0, s>>>(a, p.s);
+        k_norm_apply<T, V, ODD><<<(int)(samples * p.s.spans * p.s.parts), p.s.threads, 0, s>>>(a, p.s);
     }
     return hipGetLastError();
+}
+template <typename T>
+static hipError_t forward(const aet_group_norm &a, char *workspace, hipStream_t s) {
+    return odd_pieces<T>(a.positions ? plan(a).s : NormShape()) ? forward<T, true>(a, workspace, s) : forward<T, false>(a, workspace, s);
 }
 hipError_t launch_group_norm_forward(const aet_group_norm &a, void *workspace, hipStream_t s) {
     return a.dtype == AET_F32 ? forward<float>(a, (char *)workspace, s) : forward<bf16>(a, (char *)workspace, s);
 }
 
-template <typename T>
+template <typename T, bool ODD>
 static hipError_t backward(const aet_group_norm_grad &a, char *workspace, hipStream_t s) {
     constexpr int V = 16 / sizeof(T);
     const int64_t samples = a.positions ? (int64_t)a.n * a.batch : 0, channels = (int64_t)a.groups * a.width;
@@ -656,12 +694,12 @@ static hipError_t backward(const aet_group_norm_grad &a, char *workspace, hipStr
         const int64_t blocks = samples * p.s.spans * p.s.strips;
         if (blocks > INT32_MAX || samples * p.s.spans * p.s.parts > INT32_MAX || samples * a.groups > INT32_MAX) return hipErrorInvalidConfiguration;
         if (p.whole) {
-            if (p.n <= 4) k_norm_back_whole<T, V, 4><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
-            else k_norm_back_whole<T, V, 8><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+            if (p.n <= 4) k_norm_back_whole<T, V, 4, ODD><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+            else k_norm_back_whole<T, V, 8, ODD><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
         } else {
-            k_norm_back_strips<T, V><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
+            k_norm_back_strips<T, V, ODD><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
             k_norm_back_union<T><<<(int)(samples * a.groups), 256, 0, s>>>(a, p.s);
-            if (a.dx.p) k_norm_back_apply<T, V><<<(int)(samples * p.s.spans * p.s.parts), p.s.threads, 0, s>>>(a, p.s);
+            if (a.dx.p) k_norm_back_apply<T, V, ODD><<<(int)(samples * p.s.spans * p.s.parts), p.s.threads, 0, s>>>(a, p.s);
         }
     }
     if (a.dgamma.p || a.dbeta.p) {
@@ -672,6 +710,11 @@ static hipError_t backward(const aet_group_norm_grad &a, char *workspace, hipStr
         k_norm_params<T><<<clients * across, 256, 0, s>>>(a, p.s.sums, (int64_t)p.s.strips * 2 * channels, (int)channels, across, samples / clients);
     }
     return hipGetLastError();
+}
+template <typename T>
+static hipError_t backward(const aet_group_norm_grad &a, char *workspace, hipStream_t s) {
+    const bool some = a.n && a.batch && a.positions;
+    return odd_pieces<T>(some ? plan(a).s : NormShape()) ? backward<T, true>(a, workspace, s) : backward<T, false>(a, workspace, s);
 }
 hipError_t launch_group_norm_backward(const aet_group_norm_grad &a, void *workspace, hipStream_t s) {
     return a.dtype == AET_F32 ? backward<float>(a, (char *)workspace, s) : backward<bf16>(a, (char *)workspace, s);

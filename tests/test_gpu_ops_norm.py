@@ -225,3 +225,30 @@ def test_group_norm_of_many_groups(ops, dtype):   # noqa: F811
         want = O.group_norm_backward(d64(dy), d64(x), d64(mean), d64(rstd), d64(gamma), d64(beta), "silu", dt)
         for what, a, w in zip(("dx", "dgamma", "dbeta"), got, want):
             O.near(a, w, f"{what} {dtype} {G}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(2, 3, 50, 3, 5), (1, 2, 4096, 8, 3), (1, 40, 300, 6, 7), (1, 3, 20000, 3, 11), (1, 2, 9000, 1, 3), (2, 64, 1024, 9, 10),
+                                  (1, 700, 20, 300, 5)], ids=str)
+def test_pieces_in_place(ops, size, dtype):   # noqa: F811
+    """Channels that are not whole pieces of 16 bytes, results in the inputs' places, NaN between the rows: the same bits, and
+    nothing beside them is written."""
+    n, b, P, G, width = size
+    dt, ch = TYPES[dtype], G * width
+    g = torch.Generator().manual_seed(ch + P)
+    gamma, beta = rand(g, (n, ch), dt), rand(g, (n, ch), dt)
+    x, dy = rand(g, (n, b, P, ch), dt), rand(g, (n, b, P, ch), dt)
+    y, mean, rstd = ops.aet_group_norm_forward(x, G, gamma, beta, act="silu")
+    O.near(y, O.group_norm_forward(d64(x), G, d64(gamma), d64(beta), 1e-5, "silu", dt)[0], f"y {size} {dtype}")
+    want = ops.aet_group_norm_backward(dy, x, mean, rstd, gamma, beta, act="silu")
+    for what, a, w in zip(("dx", "dgamma", "dbeta"), want, O.group_norm_backward(d64(dy), d64(x), d64(mean), d64(rstd), d64(gamma), d64(beta), "silu", dt)):
+        O.near(a, w, f"{what} {size} {dtype}")
+    places = torch.full((2, n, b, P, ch + 3), float("nan"), dtype=dt, device=DEV)
+    px, pdy = places[0, ..., 1:1 + ch], places[1, ..., 1:1 + ch]
+    px.copy_(x)
+    pdy.copy_(dy)
+    got = ops.aet_group_norm_backward(pdy, px, mean, rstd, gamma, beta, act="silu", out=(pdy, None, None))
+    assert all(torch.equal(a, c) for a, c in zip(got, want)) and torch.equal(px, x)
+    out = ops.aet_group_norm_forward(px, G, gamma, beta, act="silu", out=px)
+    assert torch.equal(px, y) and torch.equal(out[1], mean) and torch.equal(out[2], rstd)
+    assert bool(torch.isnan(places[..., 0]).all()) and bool(torch.isnan(places[..., 1 + ch:]).all())
