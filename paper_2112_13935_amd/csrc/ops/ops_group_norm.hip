@@ -5,9 +5,9 @@
 // a group has few channels.  Where a sample's groups fit the registers of a workgroup, one kernel reads every value once
 // (k_norm_whole, k_norm_back_whole): mean first, then the squares of the differences from it.  Larger samples take
 // three: sums of strips of positions, their union by group, and a second pass over the values.
-//   2048 samples of 1024 x 32 in fp32, groups of 4 channels, silu: 123 us (537 MB, 4.4 TB/s; a copy of as much 107)
-//   gradient of 128 samples of 4096 x 320 in bf16, groups of 10: 343 us: sums 166 (671 MB read, 4.0 TB/s), union 8, second
-//   pass 197 (1.0 GB, 5.1 TB/s) under the profiler; reading the values once is 201, which no compute unit's registers hold
+//   2048 samples of 1024 x 32 in fp32, groups of 4 channels, silu: 122 us (537 MB, 4.4 TB/s; a copy of as much 107)
+//   gradient of 128 samples of 4096 x 320 in bf16, groups of 10: 328 us: sums 156 (671 MB read, 4.3 TB/s), union 9, second
+//   pass 175 (1.0 GB, 5.8 TB/s); reading the values once would be 201, but no compute unit's registers hold a sample
 #include "ops_internal.h"
 
 namespace aet_ops {
@@ -175,11 +175,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_whole(aet_group_norm a, NormS
         raw[i] = load_raw<T, V>(x + pos * a.x.row, pos < a.positions ? to_read<V, ODD>(s, w) : 0);
     }
     float gamma[V], beta[V];
-    const auto parameters = [&]() {
-        params<T>(a.gamma, w.client, w.ch, to_read<V, ODD>(s, w), 1.0f, gamma);
-        params<T>(a.beta, w.client, w.ch, to_read<V, ODD>(s, w), 0.0f, beta);
-    };
-    if (N <= 4) parameters();   // early where there are registers for it (16 positions: 88 instead of 80, 124 -> 130 us)
+    params<T>(a.gamma, w.client, w.ch, to_read<V, ODD>(s, w), 1.0f, gamma);
+    params<T>(a.beta, w.client, w.ch, to_read<V, ODD>(s, w), 0.0f, beta);
     float acc[1][V] = {};
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -213,7 +210,6 @@ __global__ __launch_bounds__(kThreads) void k_norm_whole(aet_group_norm a, NormS
     }
     __syncthreads();
     by_channel(w, g0, stat, scale);
-    if (N > 4) parameters();
 #pragma unroll
     for (int e = 0; e < V; ++e) scale[e] *= gamma[e];
 #pragma unroll
@@ -619,7 +615,7 @@ static NormPlan make_plan(int64_t samples, int positions, int groups, int width,
     s.lanes = kThreads / s.pieces;
     // Sums: as many strips as give every compute unit four workgroups, of 8 positions a thread or more (a workgroup's
     // own sums and their union cost as much as some 10 positions: gradient of 128 samples of 4096 x 320 in bf16, 1024 workgroups
-    // 170 us, 4096 220 us).  Second pass: short parts, 4 positions a thread (177 us; with 1024 workgroups 191 us).
+    // 156 us; forward, all three, 203 us, with 2048 209).  Second pass: short parts, 4 positions a thread (with 1024 workgroups 8 % more).
     const int64_t wanted = ceil_div(1024, samples * s.spans), most_strips = ceil_div(positions, (int64_t)s.lanes * 8);
     s.strip = (int)ceil_div(ceil_div(positions, wanted < most_strips ? wanted : most_strips), s.lanes) * s.lanes;
     s.strips = (int)ceil_div(positions, s.strip);
