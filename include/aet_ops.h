@@ -93,8 +93,9 @@ aet_status aet_linear_forward(const aet_linear *a, void *workspace, size_t works
  *   dw, db    client = 0 with n other than 1: one W (bias) for all clients, whose gradient is the sum
  *             over them; x, dy, pre and dx then lie row after row, client after client
  *             (client = rows * row), and w.client, dw.client and db.client are all 0
- * bf16: dz is rounded to bf16 for the products (the matrix cores take bf16 only; its error
- * is that of a bf16 input); db sums the values before that. */
+ * bf16: the matrix cores take bf16 only, so dz goes into the products as a sum of two bf16
+ * values, to within 2^-16 of it (and 2^-134 where it is tiny), a product with each; without
+ * activation and dropout it is dy as it is.  db sums dz in fp32. */
 typedef struct {
     int32_t dtype, act;
     int32_t n, rows, in, out;

@@ -10,8 +10,8 @@ static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 static Product forward_product(const aet_linear &a) {
     Product p = {};
-    p.a = {a.x.p, a.x.client, a.x.row, false, false};
-    p.b = {a.w.p, a.w.client, a.w.row, false, false};
+    p.a = {a.x.p, a.x.client, a.x.row};
+    p.b = {a.w.p, a.w.client, a.w.row};
     p.clients = a.n;
     p.M = a.rows;
     p.N = a.out;
@@ -29,9 +29,12 @@ hipError_t launch_linear_forward(const aet_linear &a, void *workspace, hipStream
 // in their order.  Bound by memory: 4 x 4096 rows of 8192 in bf16, two
 // values read and one written, 161 us, 5.0 TB/s.  Inside the products it would be worked out again for each column of
 // tiles, and for the second product.
+// bf16: dz is kept as the nearest bf16 value and the nearest to what that leaves, 16 bits, for two products of the matrix
+// unit each.  One value alone adds an error of the size of the outputs' own rounding to them (relative 2-norm of dx and dw 1.4 times
+// as large); a second leaves 2^-8 of that, which no output shows.
 struct DzShape {
     int across, strips, strip;   // workgroups: side by side, one below the other; rows of a strip
-    int64_t dz_row;
+    int64_t dz_row, low;         // low: bf16, where the second parts begin
     float *partial;              // [strip][client][out]
 };
 
@@ -72,6 +75,16 @@ __global__ __launch_bounds__(256) void k_dz(aet_linear_grad a, Drop d, DzShape s
             T *const to = dz + (client * a.rows + r) * s.dz_row;
             if (ends) *(wide<T, V> *)(to + s.dz_row - V) = wide<T, V>{};   // zeros up to the next row, for the products
             store_some(to + col, count, v);
+            if constexpr (sizeof(T) == 2) {
+                float low[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float high = (float)(T)v[e];
+                    low[e] = __builtin_fabsf(high) < __builtin_inff() ? v[e] - high : 0.0f;   // (NaN: 0 too; the first part has it)
+                }
+                if (ends) *(wide<T, V> *)(to + s.low + s.dz_row - V) = wide<T, V>{};
+                store_some(to + s.low + col, count, low);
+            }
         }
 #pragma unroll
         for (int e = 0; e < V; ++e) sum[e] += v[e];
@@ -143,15 +156,17 @@ static BackwardPlan plan(const aet_linear_grad &a, char *workspace) {
     const int64_t wanted = ceil_div(2048, (int64_t)a.n * b.dz.across + 1), most = a.rows <= 128 ? 1 : ceil_div(a.rows, 64);
     b.dz.strip = (int)ceil_div(ceil_div(a.rows, wanted < most ? wanted : most > 0 ? most : 1), 8) * 8;
     b.dz.strips = a.rows ? (int)ceil_div(a.rows, b.dz.strip) : 1;
-    b.dz_bytes = own ? up256((size_t)a.n * a.rows * b.dz.dz_row * e) : 0;
+    const size_t part = own ? up256((size_t)a.n * a.rows * b.dz.dz_row * e) : 0;
+    b.dz.low = e == 2 ? (int64_t)(part / e) : 0;
+    b.dz_bytes = part * (e == 2 ? 2 : 1);
     b.db_bytes = a.db.p && b.dz.strips > 1 ? up256((size_t)b.dz.strips * a.n * a.out * sizeof(float)) : 0;
     b.dz.partial = (float *)(workspace + b.dz_bytes);
-    Operand dz = {a.dy.p, a.dy.client, a.dy.row, false, false};
-    if (own) dz = {workspace, a.rows * b.dz.dz_row, b.dz.dz_row, false, true};
+    Operand dz = {a.dy.p, a.dy.client, a.dy.row};
+    if (own) dz = {workspace, a.rows * b.dz.dz_row, b.dz.dz_row, false, true, b.dz.low};
     const Drop none = {};
     if (a.dx.p) {
         b.dx.a = dz;
-        b.dx.b = {a.w.p, a.w.client, a.w.row, true, false};
+        b.dx.b = {a.w.p, a.w.client, a.w.row, true};
         b.dx.clients = a.n;
         b.dx.M = a.rows;
         b.dx.N = a.in;
@@ -161,7 +176,7 @@ static BackwardPlan plan(const aet_linear_grad &a, char *workspace) {
     if (a.dw.p) {
         dz.by_columns = true;
         b.dw.a = dz;
-        b.dw.b = {a.x.p, a.x.client, a.x.row, true, false};
+        b.dw.b = {a.x.p, a.x.client, a.x.row, true};
         b.dw.clients = a.n;
         b.dw.M = a.out;
         b.dw.N = a.in;

@@ -5,11 +5,13 @@
 namespace aet_ops {
 
 // By rows: element (r, k) is at p + client * c + row * r + k.  By columns: at p + client * c + row * k + r.  Padded: what
-// lies side by side goes on with zeros up to a multiple of 8.
+// lies side by side goes on with zeros up to a multiple of 8.  low: where not 0, the values are in two bf16 parts, whose second
+// lies that many elements behind the first (A of a product with B by columns only).
 struct Operand {
     const void *p;
     int64_t client, row;
     bool by_columns, padded;
+    int64_t low;
 };
 
 struct Product {

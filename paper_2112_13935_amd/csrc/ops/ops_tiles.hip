@@ -277,108 +277,119 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
 
     const int stages = (k1 - k0 + BK - 1) / BK;
     constexpr int kPartA = P * SA::kBytes;
-    if constexpr (DIRECT) {
-        DirectStage<BM, BK, TA, L::kThreads> la;
-        DirectStage<BN, BK, TB, L::kThreads> lb;
-        la.begin(oa, client, m0, s.M, k0, k1);
-        lb.begin(ob, client, n0, s.N, k0, k1);
-        // The fragments of the next 16 k are read while the matrix unit has the last ones, also across the barrier that
-        // says that the next stage has arrived everywhere and that this one's place may be written again: it comes
-        // ahead of the stage's last products, and right behind it the stage after the next is sent for.
-        constexpr int kBuffers = L::kBuffers, KS = BK / 16, kReads = (TA ? 2 : 1) * FM + (TB ? 2 : 1) * FN;
-        constexpr int kLoads = decltype(la)::kCount + decltype(lb)::kCount;
-        static_assert(kBuffers == 2, "every wait in the loop is for all that is on its way");
-        const int whole = k1 > k0 ? (k1 - k0) / BK : 0;   // stages; there may be an end of another
-        const auto fetch = [&](int i) {
-            const lds_ptr to = lds + i % kBuffers * L::kStage;
-            la.load(to);
-            lb.load(to + kPartA);
-        };
-        const auto fetch_end = [&]() {
-            const lds_ptr to = lds + whole % kBuffers * L::kStage;
-            la.load_end(to, k1 - k0 - whole * BK);
-            lb.load_end(to + kPartA, k1 - k0 - whole * BK);
-        };
-        // s_waitcnt by its encoding (vmcnt low and high bits, lgkmcnt 0), which the compiler takes into account
-        const auto arrived = [&](auto still) {
-            __builtin_amdgcn_s_waitcnt(0x0070 | (still & 15) | (still >> 4) << 14);
-            __builtin_amdgcn_s_barrier();
-        };
-        typedef std::integral_constant<int, (kBuffers - 2) * kLoads> Others;
-        typedef std::integral_constant<int, 0> None;
-        Fragments f[2];
-        for (int i = 0; i < kBuffers && i < whole; ++i) fetch(i);
-        if (whole < stages && whole < kBuffers) fetch_end();   // (whose loads cannot be counted)
-        if (whole >= kBuffers) arrived(std::integral_constant<int, (kBuffers - 1) * kLoads>());
-        else arrived(None());
-        if (stages > 0) read(f[0], lds, 0);
-        int i = 0;
-        const auto stage = [&](auto get) {
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                if (ks + 1 == KS) {
-                    arrived(Others());
-                    get();
+    const auto sum = [&](const Operand &oa) {
+        if constexpr (DIRECT) {
+            DirectStage<BM, BK, TA, L::kThreads> la;
+            DirectStage<BN, BK, TB, L::kThreads> lb;
+            la.begin(oa, client, m0, s.M, k0, k1);
+            lb.begin(ob, client, n0, s.N, k0, k1);
+            // The fragments of the next 16 k are read while the matrix unit has the last ones, also across the barrier that
+            // says that the next stage has arrived everywhere and that this one's place may be written again: it comes
+            // ahead of the stage's last products, and right behind it the stage after the next is sent for.
+            constexpr int kBuffers = L::kBuffers, KS = BK / 16, kReads = (TA ? 2 : 1) * FM + (TB ? 2 : 1) * FN;
+            constexpr int kLoads = decltype(la)::kCount + decltype(lb)::kCount;
+            static_assert(kBuffers == 2, "every wait in the loop is for all that is on its way");
+            const int whole = k1 > k0 ? (k1 - k0) / BK : 0;   // stages; there may be an end of another
+            const auto fetch = [&](int i) {
+                const lds_ptr to = lds + i % kBuffers * L::kStage;
+                la.load(to);
+                lb.load(to + kPartA);
+            };
+            const auto fetch_end = [&]() {
+                const lds_ptr to = lds + whole % kBuffers * L::kStage;
+                la.load_end(to, k1 - k0 - whole * BK);
+                lb.load_end(to + kPartA, k1 - k0 - whole * BK);
+            };
+            // s_waitcnt by its encoding (vmcnt low and high bits, lgkmcnt 0), which the compiler takes into account
+            const auto arrived = [&](auto still) {
+                __builtin_amdgcn_s_waitcnt(0x0070 | (still & 15) | (still >> 4) << 14);
+                __builtin_amdgcn_s_barrier();
+            };
+            typedef std::integral_constant<int, (kBuffers - 2) * kLoads> Others;
+            typedef std::integral_constant<int, 0> None;
+            Fragments f[2];
+            for (int i = 0; i < kBuffers && i < whole; ++i) fetch(i);
+            if (whole < stages && whole < kBuffers) fetch_end();   // (whose loads cannot be counted)
+            if (whole >= kBuffers) arrived(std::integral_constant<int, (kBuffers - 1) * kLoads>());
+            else arrived(None());
+            if (stages > 0) read(f[0], lds, 0);
+            int i = 0;
+            const auto stage = [&](auto get) {
+    #pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    if (ks + 1 == KS) {
+                        arrived(Others());
+                        get();
+                    }
+                    read(f[(ks + 1) % 2], lds + (i + (ks + 1) / KS) % kBuffers * L::kStage, (ks + 1) % KS);
+                    multiply(f[ks % 2]);
+                    interleave<FM * FN, kReads>();
                 }
-                read(f[(ks + 1) % 2], lds + (i + (ks + 1) / KS) % kBuffers * L::kStage, (ks + 1) % KS);
-                multiply(f[ks % 2]);
-                interleave<FM * FN, kReads>();
+            };
+            for (; i + kBuffers < whole; ++i) stage([&]() { fetch(i + kBuffers); });
+            if (i + kBuffers < stages) {
+                stage(fetch_end);
+                ++i;
             }
-        };
-        for (; i + kBuffers < whole; ++i) stage([&]() { fetch(i + kBuffers); });
-        if (i + kBuffers < stages) {
-            stage(fetch_end);
-            ++i;
-        }
-        for (; i < stages; ++i) {
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                if (ks + 1 == KS) arrived(None());
-                if (ks + 1 < KS || i + 1 < stages) read(f[(ks + 1) % 2], lds + (i + (ks + 1) / KS) % kBuffers * L::kStage, (ks + 1) % KS);
-                multiply(f[ks % 2]);
+            for (; i < stages; ++i) {
+    #pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    if (ks + 1 == KS) arrived(None());
+                    if (ks + 1 < KS || i + 1 < stages) read(f[(ks + 1) % 2], lds + (i + (ks + 1) / KS) % kBuffers * L::kStage, (ks + 1) % KS);
+                    multiply(f[ks % 2]);
+                }
             }
-        }
-    } else {
-        RegStage<T, BM, BK, TA, L::kThreads> la;
-        RegStage<T, BN, BK, TB, L::kThreads> lb;
-        la.begin(oa, client, m0, s.M, k0, k1);
-        lb.begin(ob, client, n0, s.N, k0, k1);
-        // A stage goes from memory to registers while the one before it is worked on.  One buffer: there is another
-        // workgroup on the compute unit whose products go on while this one splits and stores.
-        const auto work = [&]() {
-#pragma unroll
-            for (int ks = 0; ks < BK / 16; ++ks) {
-                Fragments f;
-                read(f, lds, ks);
-                multiply(f);
-            }
-        };
-        const auto put = [&]() {
-            __syncthreads();
-            la.store(lds);
-            lb.store(lds + kPartA);
-            __syncthreads();
-        };
-        const int whole = la.plain() < lb.plain() ? la.plain() : lb.plain();
-        if (whole > 0) {
-            la.template load<true>();
-            lb.template load<true>();
         } else {
-            la.template load<false>();
-            lb.template load<false>();
+            RegStage<T, BM, BK, TA, L::kThreads> la;
+            RegStage<T, BN, BK, TB, L::kThreads> lb;
+            la.begin(oa, client, m0, s.M, k0, k1);
+            lb.begin(ob, client, n0, s.N, k0, k1);
+            // A stage goes from memory to registers while the one before it is worked on.  One buffer: there is another
+            // workgroup on the compute unit whose products go on while this one splits and stores.
+            const auto work = [&]() {
+    #pragma unroll
+                for (int ks = 0; ks < BK / 16; ++ks) {
+                    Fragments f;
+                    read(f, lds, ks);
+                    multiply(f);
+                }
+            };
+            const auto put = [&]() {
+                __syncthreads();
+                la.store(lds);
+                lb.store(lds + kPartA);
+                __syncthreads();
+            };
+            const int whole = la.plain() < lb.plain() ? la.plain() : lb.plain();
+            if (whole > 0) {
+                la.template load<true>();
+                lb.template load<true>();
+            } else {
+                la.template load<false>();
+                lb.template load<false>();
+            }
+            int i = 0;
+            for (; i + 1 < whole; ++i) {
+                put();
+                la.template load<true>();
+                lb.template load<true>();
+                work();
+            }
+            for (; i < stages; ++i) {
+                put();
+                la.template load<false>();
+                lb.template load<false>();
+                work();
+            }
         }
-        int i = 0;
-        for (; i + 1 < whole; ++i) {
-            put();
-            la.template load<true>();
-            lb.template load<true>();
-            work();
-        }
-        for (; i < stages; ++i) {
-            put();
-            la.template load<false>();
-            lb.template load<false>();
-            work();
+    };
+    sum(oa);
+    if constexpr (TB && sizeof(T) == 2) {   // A in two parts: the sum over the second on top
+        if (oa.low) {
+            Operand low = oa;
+            low.p = (const T *)oa.p + oa.low;
+            __syncthreads();   // the last stage has been read
+            sum(low);
         }
     }
     __syncthreads();
@@ -523,8 +534,9 @@ static Choice choose(int dtype, const Product &p, bool straight) {
     const auto consider = [&](const Kind &k) {
         const int64_t tiles = p.clients * ceil_div(p.M, k.bm) * ceil_div(p.N, k.bn), stages = ceil_div(p.K, k.bk);
         const float sums = (float)p.clients * (float)p.M * (float)p.N * 4.0f;
+        const int parts = p.a.low ? 2 : 1;
         for (int64_t slices = 1; slices == 1 || (slices <= 64 && stages / slices >= 2); slices *= 2) {
-            float t = time_of(k, ceil_div(stages, slices), tiles * slices);
+            float t = time_of(k, ceil_div(stages, slices) * parts, tiles * slices);
             if (slices > 1) t += 4.0f + (float)(2 * slices + 1) * sums / 6e6f;
             if (!best.kind || t < best.time) best = {&k, (int)slices, t};
         }
@@ -607,7 +619,7 @@ static hipError_t run_pair(const Product &x, const Product &w, hipStream_t strea
     if (d != straight<T>(w) || !shape_of(x, one, nullptr, &sx) || !shape_of(w, one, nullptr, &sw) || !sx.blocks || !sw.blocks ||
         sx.blocks > INT32_MAX - sw.blocks)
         return hipSuccess;
-    if (time_of(k, ceil_div(x.K > w.K ? x.K : w.K, k.bk), (int64_t)sx.blocks + sw.blocks) > choose(dtype, x, d).time + choose(dtype, w, d).time + 3.0f)
+    if (time_of(k, ceil_div(x.K > w.K ? x.K : w.K, k.bk) * (x.a.low ? 2 : 1), (int64_t)sx.blocks + sw.blocks) > choose(dtype, x, d).time + choose(dtype, w, d).time + 3.0f)
         return hipSuccess;
     *taken = true;
     constexpr int BK = sizeof(T) == 4 ? 32 : 64;
