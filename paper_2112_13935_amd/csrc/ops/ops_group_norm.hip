@@ -10,6 +10,8 @@
 //   pass 175 (1.0 GB, 5.8 TB/s); reading the values once would be 201, but no compute unit's registers hold a sample
 #include "ops_internal.h"
 
+#include <type_traits>
+
 namespace aet_ops {
 
 constexpr int kThreads = 512;
@@ -338,7 +340,10 @@ __device__ __forceinline__ void each_position(int pos, int end, int step, int co
     else if (count > 0) some(count);
 }
 
-// Of a strip's values of a channel: their mean, and the sum of squares of the differences from it.
+// Of a strip's values of a channel: their mean, and the sum of squares of the differences from it.  No value is more than
+// any other: a thread takes its positions by four, their mean and then the squares of the differences from it in registers,
+// and joins them to what it has (Chan, Golub and LeVeque 1983); the threads' are joined about the strip's mean.  (Squares
+// about the first value cancel where that is unlike the others, a corner or a border of zeros: rstd of 4096 values was 2^-13 off.)
 template <typename T, int V, bool ODD>
 __global__ __launch_bounds__(kThreads) void k_norm_strips(aet_group_norm a, NormShape s) {
     extern __shared__ float lds[];
@@ -346,28 +351,68 @@ __global__ __launch_bounds__(kThreads) void k_norm_strips(aet_group_norm a, Norm
     const int strip = blockIdx.x % (uint32_t)s.strips;
     const Where w = where<V, ODD>(s, a.batch, a.width, blockIdx.x / (uint32_t)s.strips);
     const int first = strip * s.strip, end = a.positions - first < s.strip ? a.positions : first + s.strip;
+    const int start = first + w.lane, count = start < end ? to_read<V, ODD>(s, w) : 0;
     const T *x = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + w.ch;
-    // about the strip's first value, so that the squares do not cancel where the mean is far from 0
-    const wide<T, V> about = load_raw<T, V>(x + first * a.x.row, to_read<V, ODD>(s, w));
-    float SQ[2][V] = {};
+    // All differences are from the thread's first value, and in the end from the strip's, so that means far from 0 lose no bits.
+    const wide<T, V> own = load_raw<T, V>(x + (start < end ? start : first) * a.x.row, count);
+    const wide<T, V> about = load_raw<T, V>(x + first * a.x.row, count);
+    float n = 0, mean[V] = {}, m2[V] = {};
     wide<T, V> raw[4];
-    each_position(first + w.lane, end, s.lanes, to_read<V, ODD>(s, w), V, [&](int pos, int i, int count) { raw[i] = load_raw<T, V>(x + pos * a.x.row, count); },
-                  [&](int, int i, int) {
+    // FOUR: all four have a value, not the first `here` of them only
+    const auto join = [&](auto four, int here) {
+        constexpr bool FOUR = four;
+        const float k = (float)here, share = k / (n + k), inv = FOUR ? 0.25f : 1.0f / k;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float d = (float)raw[i][e] - (float)about[e];
-            SQ[0][e] += d;
-            SQ[1][e] += d * d;
+            float d[4], q = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[i] = FOUR || i < here ? (float)raw[i][e] - (float)own[e] : 0.0f;
+            const float m = (d[0] + d[1] + (d[2] + d[3])) * inv, off = m - mean[e];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float r = FOUR || i < here ? d[i] - m : 0.0f;
+                q = __builtin_fmaf(r, r, q);
+            }
+            m2[e] += __builtin_fmaf(off * share, off * n, q);
+            mean[e] = __builtin_fmaf(off, share, mean[e]);
         }
-    });
+        n += k;
+    };
+    const auto some = [&](int have) {
+        for (int pos = start; pos < end; pos += 4 * s.lanes) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw[i] = load_raw<T, V>(x + (pos + i * s.lanes < end ? pos + i * s.lanes : end - 1) * a.x.row, have);
+            if (pos + 3 * s.lanes < end) join(std::true_type(), 4);
+            else join(std::false_type(), (end - pos + s.lanes - 1) / s.lanes);
+        }
+    };
+    if (count >= V) some(V);
+    else if (count > 0) some(count);
+    float sum[1][V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        mean[e] += (float)own[e] - (float)about[e];
+        sum[0][e] = n * mean[e];
+    }
     float *to = s.sums + (w.sample * s.strips + strip) * 2 * s.channels + w.ch0;
     const float inv = 1.0f / (float)(end - first);
-    channel_sums<ODD>(s, w, SQ, lds, tot);
+    channel_sums<ODD>(s, w, sum, lds, tot);
+    // what the sum's roundings have left of the mean, and the squares about it
+    float DQ[2][V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const int k = w.ch + e - w.ch0;   // (one of another workgroup's channels, or none: not counted)
+        const float off = mean[e] - tot[k < 0 ? 0 : k < w.chans ? k : w.chans - 1] * inv;
+        DQ[0][e] = n * off;
+        DQ[1][e] = __builtin_fmaf(n * off, off, m2[e]);
+    }
     const T *about0 = (const T *)a.x.p + w.client * a.x.client + w.in_batch * a.x.sample + first * a.x.row + w.ch0;
+    for (int k = threadIdx.x; k < w.chans; k += blockDim.x) to[k] = (float)about0[k] + tot[k] * inv;
+    channel_sums<ODD>(s, w, DQ, lds, tot);
     for (int k = threadIdx.x; k < w.chans; k += blockDim.x) {
-        const float off = tot[k] * inv, m2 = tot[s.span + k] - tot[k] * off;
-        to[k] = (float)about0[k] + off;
-        to[s.channels + k] = m2 < 0 ? 0.0f : m2;
+        const float more = tot[k] * inv, squares = tot[s.span + k] - tot[k] * more;
+        to[k] += more;
+        to[s.channels + k] = squares < 0 ? 0.0f : squares;
     }
 }
 
@@ -615,7 +660,7 @@ static NormPlan make_plan(int64_t samples, int positions, int groups, int width,
     s.lanes = kThreads / s.pieces;
     // Sums: as many strips as give every compute unit four workgroups, of 8 positions a thread or more (a workgroup's
     // own sums and their union cost as much as some 10 positions: gradient of 128 samples of 4096 x 320 in bf16, 1024 workgroups
-    // 156 us; forward, all three, 203 us, with 2048 209).  Second pass: short parts, 4 positions a thread (with 1024 workgroups 8 % more).
+    // 156 us; forward, all three, 209).  Second pass: short parts, 4 positions a thread (with 1024 workgroups 8 % more).
     const int64_t wanted = ceil_div(1024, samples * s.spans), most_strips = ceil_div(positions, (int64_t)s.lanes * 8);
     s.strip = (int)ceil_div(ceil_div(positions, wanted < most_strips ? wanted : most_strips), s.lanes) * s.lanes;
     s.strips = (int)ceil_div(positions, s.strip);

@@ -55,3 +55,52 @@ def test_gradients_in_bf16_of_values_at_the_ends_of_the_range(ops):   # noqa: F8
     dx, _, db = ops.aet_linear_backward(dy, x, w, p=0.5, seed=9)
     assert bool((dx[0, 0] == float("inf")).all()) and bool((dx[0, 1] == -float("inf")).all()) and bool((dx[0, 2] == float("inf")).all())
     assert bool(torch.isnan(dx[0, 3]).all()) and bool(torch.isfinite(dx[0, 4:]).all())
+
+
+def one_first(x, others):
+    """x of N(0, 1): the first position is unlike the others, which are about `others`."""
+    x += others
+    x[:, :, 0] = 1000.0 if others == 0 else 0.0
+    return x
+
+
+def border(x):
+    """Zeros around values about 100."""
+    x += 100
+    x[:, :, :64] = 0
+    x[:, :, -64:] = 0
+    return x
+
+
+def trend(x):
+    """A mean that moves through the sample by a hundred times what values differ by next to each other."""
+    return x + torch.linspace(-50, 50, x.shape[2], device=x.device)[:, None]
+
+
+VALUES = {"first_0_others_100": lambda x: one_first(x, 100.0), "first_1000_others_0": lambda x: one_first(x, 0.0), "border": border, "trend": trend,
+          "one_value_last": lambda x: one_first(x, 100.0).flip(2), "far": lambda x: x + 1000.0}
+
+
+@pytest.mark.parametrize("values", VALUES)
+# n, batch, positions, groups, width: strips as long as the sample, and parts of it; samples that are no whole pieces; one that a
+# workgroup holds
+@pytest.mark.parametrize("size", [(4, 256, 4096, 8, 4), (1, 256, 16384, 2, 4), (1, 2, 65536, 3, 5), (2, 550, 9003, 1, 3), (1, 3, 9001, 2, 40),
+                                  (2, 3, 300, 4, 8)], ids=str)
+def test_group_norm_of_values_unlike_each_other(ops, size, values):   # noqa: F811
+    """Statistics and results in fp32, whichever value comes first: mean and rstd within 64 units of 2^-24 (the mean, of its
+    magnitude and the spread; rstd, also by the mean's error squared), y as much of the largest value's."""
+    n, b, P, G, width = size
+    g = torch.Generator(device=DEV).manual_seed(P + width)
+    x = VALUES[values](torch.randn(n * b, 1, P, G * width, generator=g, device=DEV)).view(n, b, P, G * width).contiguous()
+    y, mean, rstd = ops.aet_group_norm_forward(x, G, eps=1e-5)
+    for c in range(n):
+        for b0 in range(0, b, 64):
+            at = (slice(c, c + 1), slice(b0, b0 + 64))
+            v = x[at].double().view(1, -1, P, G, width)
+            m = v.mean((2, 4), keepdim=True)
+            r = 1 / torch.sqrt((v - m).square().mean((2, 4), keepdim=True) + 1e-5)
+            xh, big = (v - m) * r, v.abs().amax((2, 4), keepdim=True) * r
+            O.near(mean[at], (m[:, :, 0, :, 0].cpu(), 64 * O.U32 * (m.abs() + 1 / r)[:, :, 0, :, 0].cpu()), "mean")
+            O.near(rstd[at], (r[:, :, 0, :, 0].cpu(), (64 * O.U32 * r * (1 + O.U32 * (m * r).square()))[:, :, 0, :, 0].cpu()), "rstd")
+            off = (y[at].double().view(xh.shape) - xh).abs() - 64 * O.U32 * (big + xh.abs())
+            assert float(off.max()) <= 0, ("y", float(off.max()))
