@@ -63,18 +63,22 @@ __device__ __forceinline__ int xcd_order(int id, int blocks) {
 
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
-// Phi(z) and exp(-z^2 / 2).  Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: erfc(u) =
-// (a1 t + ... + a5 t^5) exp(-u^2), t = 1 / (1 + p u), u >= 0, with an error of at most 1.5e-7; Phi has half of
-// it, which is about the rounding of 1 + erf.
+// Phi(z) and exp(-z^2 / 2).  With u = |z| / sqrt(2) the tail is erfc(u) / 2 = (b1 t + ... + b8 t^8) exp(-u^2), t = 1 / (1 + 0.6 u),
+// which is the form of Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26, three terms longer; the b are a
+// least-squares fit to exp(u^2) erfc(u) / 2 over u = 0 to 10, weighted towards an even error.  It is within 1e-8, and 8e-6
+// of itself down to z = -5.  GELU of N(0, 1) in fp32: relative 2-norm 3.6e-8, its slope 5.0e-8; with an exact erf in fp32 3.8e-8 and 3.9e-8,
+// with that formula's five terms 8.5e-8 and 1.0e-7.
 __device__ __forceinline__ float normal_cdf(float z, float &e) {
-    const float u = __builtin_fabsf(z) * 0.70710678f;
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, u, 1.0f));
-    float s = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
-    s = __builtin_fmaf(t, s, 1.421413741f);
-    s = __builtin_fmaf(t, s, -0.284496736f);
-    s = __builtin_fmaf(t, s, 0.254829592f);
-    e = exp_fast(-u * u);
-    const float tail = 0.5f * t * s * e;
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.42426407f, __builtin_fabsf(z), 1.0f));
+    float s = __builtin_fmaf(t, -0.0266033318f, 0.115691967f);
+    s = __builtin_fmaf(t, s, -0.146613598f);
+    s = __builtin_fmaf(t, s, -0.0431476533f);
+    s = __builtin_fmaf(t, s, 0.150449857f);
+    s = __builtin_fmaf(t, s, 0.105136529f);
+    s = __builtin_fmaf(t, s, 0.17642127f);
+    s = __builtin_fmaf(t, s, 0.168664962f);
+    e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+    const float tail = t * s * e;
     return z < 0 ? tail : 1.0f - tail;
 }
 

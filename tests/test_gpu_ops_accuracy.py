@@ -104,3 +104,38 @@ def test_group_norm_of_values_unlike_each_other(ops, size, values):   # noqa: F8
             O.near(rstd[at], (r[:, :, 0, :, 0].cpu(), (64 * O.U32 * r * (1 + O.U32 * (m * r).square()))[:, :, 0, :, 0].cpu()), "rstd")
             off = (y[at].double().view(xh.shape) - xh).abs() - 64 * O.U32 * (big + xh.abs())
             assert float(off.max()) <= 0, ("y", float(off.max()))
+
+
+@pytest.mark.parametrize("rows", [1, 4096])
+def test_gelu_in_fp32(ops, rows):   # noqa: F811
+    """Through a layer of one input and w = 1, where z is x.  The definition's factors rounded once each, and their product, give a
+    relative 2-norm of about 2/3 of a unit of 2^-24 (with erf 0.64; the slope's two terms 0.66): one unit is allowed for the value, and
+    for the slope, a sum, one and a half.  The tail is itself to 2^-15 as far as z = -5."""
+    out = 1 << 16 if rows == 1 else 16
+    g = torch.Generator().manual_seed(1)
+    x = rand(g, (rows, 1), torch.float32)
+    w = torch.ones(out, 1, device=DEV) if rows > 1 else rand(g, (out, 1), torch.float32)   # one row: z is w instead
+    if rows == 1:
+        x.fill_(1.0)
+    y, z = ops.aet_linear_forward(x, w, act="gelu", keep_pre=True)
+    assert torch.equal(z, x * w.t())
+    want = O.act(d64(z), "gelu")
+    assert float((d64(y) - want).norm() / want.norm()) <= 2.0 ** -24
+    low = (d64(z) < -2) & (d64(z) > -5)
+    assert int(low.sum()) > 10 and float(((d64(y) - want) / want)[low].abs().max()) <= 2.0 ** -15
+    # dy has one 1 a row, and db is the slope there; with rows of one value, dx is
+    one = torch.ones(1, z.numel(), device=DEV)
+    _, _, db = ops.aet_linear_backward(one, one[:, :1], torch.ones(z.numel(), 1, device=DEV), z.reshape(1, -1), act="gelu")
+    slope = O.slope(d64(z).reshape(-1), "gelu")
+    assert float((d64(db) - slope).norm() / slope.norm()) <= 1.5 * 2.0 ** -24
+
+
+def test_gelu_at_the_ends_of_the_range(ops):   # noqa: F811
+    z = torch.tensor([[0.0, -0.0, 1e-30, -1e-30, 6.0, 1e20, torch.finfo(torch.float32).max, float("inf"), -12.0, -1e20, -torch.finfo(torch.float32).max,
+                       float("nan")]], device=DEV)
+    y = ops.aet_linear_forward(torch.ones(1, 1, device=DEV), z.t().contiguous(), act="gelu")[0][0].cpu()
+    assert torch.equal(y[4:8], z[0, 4:8].cpu()) and bool((y[:2] == 0).all()) and bool((y[2:4].abs() < 1e-30).all())
+    assert bool((y[8:11].abs() < 1e-30).all()) and bool(torch.isnan(y[11]))
+    one = torch.ones_like(z)
+    _, _, db = ops.aet_linear_backward(one, one[:, :1], torch.ones(z.shape[1], 1, device=DEV), z, act="gelu")
+    assert torch.equal(db[4:7].cpu(), torch.ones(3)) and bool((db[8:11].abs() < 1e-28).all())
