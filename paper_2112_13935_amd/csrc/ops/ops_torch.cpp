@@ -45,8 +45,15 @@ struct Call {
         if (other) t.record_stream(other->current_stream());
         return t.data_ptr();
     }
+    // Nothing is recorded for automatic differentiation: its gradient would be lost without a word.
+    static void no_graph(const char *name, const Tensor &t) {
+        if (t.requires_grad() && at::GradMode::is_enabled())
+            value_error(std::string(name) + " requires a gradient, which the operators do not record: call them under torch.no_grad() or with "
+                                            "detached tensors, and the _backward calls for gradients");
+    }
     // The tensor's type, device, shape and last stride are as they have to be.
     void agree(const char *name, const Tensor &t, at::IntArrayRef shape) {
+        no_graph(name, t);
         if (t.scalar_type() != x.scalar_type() || t.device() != x.device())
             value_error(std::string(name) + " is " + text(t) + ", the others are " + text(x));
         if (t.sizes() != shape) {
@@ -214,9 +221,11 @@ Three group_norm_backward(const Tensor &dy, const Tensor &x, const Tensor &mean,
     if (gamma && beta && gamma->dim() != beta->dim()) value_error("gamma and beta: either both or none have an axis of clients");
     const auto all = s.stats();
     const at::IntArrayRef stats = at::IntArrayRef(all).slice(4 - x.dim());
-    for (const auto &[name, t] : {std::pair<const char *, const Tensor &>("mean", mean), {"rstd", rstd}})
+    for (const auto &[name, t] : {std::pair<const char *, const Tensor &>("mean", mean), {"rstd", rstd}}) {
+        c.no_graph(name, t);
         if (t.scalar_type() != at::kFloat || t.device() != x.device() || t.sizes() != stats || !t.is_contiguous())
             value_error(std::string(name) + " has to be as the forward call gave it: float32, contiguous, [n, batch, groups]");
+    }
     aet_group_norm_grad a = {c.dtype, act, s.n, s.batch, s.positions, s.groups, s.width};
     const int64_t channels = x.size(-1);
     c.maps(a.dy, "dy", dy, x.sizes());

@@ -9,7 +9,8 @@ leading axis of clients may be left out everywhere (one client).  Outputs are al
 are given.  Calls enqueue on `stream`, the current stream where it is None.  Where it is another one,
 outputs and workspaces are allocated on it, and tensors are kept from being given out again before both
 are done with them (Tensor.record_stream); waiting for one another is the caller's (Stream.wait_stream).
-Seeds are taken modulo 2^64.
+Seeds are taken modulo 2^64.  Automatic differentiation does not know the calls: tensors that require a
+gradient are refused while gradients are on (torch.no_grad, or detach, says that it is meant).
 """
 from __future__ import annotations
 

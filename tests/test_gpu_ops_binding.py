@@ -1,0 +1,47 @@
+"""What the binding makes of tensors: those that it refuses, and what automatic differentiation is told."""
+import pytest
+import torch
+
+from test_gpu_ops_linear import DEV, ops  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def calls(ops):   # noqa: F811
+    """name: the call and its tensors, small and right."""
+    z = lambda *s: torch.ones(*s, device=DEV)   # noqa: E731
+    return {
+        "linear_forward": (lambda x, w, bias, residual, out: ops.aet_linear_forward(x, w, bias, residual=residual, out=out),
+                           dict(x=z(2, 3, 4), w=z(2, 5, 4), bias=z(2, 5), residual=z(2, 3, 5), out=z(2, 3, 5))),
+        "linear_backward": (lambda dy, x, w, pre, dx, dw, db: ops.aet_linear_backward(dy, x, w, pre, act="silu", out=(dx, dw, db)),
+                            dict(dy=z(2, 3, 5), x=z(2, 3, 4), w=z(2, 5, 4), pre=z(2, 3, 5), dx=z(2, 3, 4), dw=z(2, 5, 4), db=z(2, 5))),
+        "group_norm_forward": (lambda x, gamma, beta, out: ops.aet_group_norm_forward(x, 2, gamma, beta, out=out),
+                               dict(x=z(2, 3, 4, 6), gamma=z(2, 6), beta=z(2, 6), out=z(2, 3, 4, 6))),
+        "group_norm_backward": (lambda dy, x, mean, rstd, gamma, beta, dx, dgamma, dbeta: ops.aet_group_norm_backward(
+            dy, x, mean, rstd, gamma, beta, out=(dx, dgamma, dbeta)),
+            dict(dy=z(2, 3, 4, 6), x=z(2, 3, 4, 6), mean=z(2, 3, 2), rstd=z(2, 3, 2), gamma=z(2, 6), beta=z(2, 6), dx=z(2, 3, 4, 6),
+                 dgamma=z(2, 6), dbeta=z(2, 6))),
+        "dropout_forward": (lambda x, residual, out: ops.aet_dropout_forward(x, p=0.5, seed=1, residual=residual, out=out),
+                            dict(x=z(2, 3, 4), residual=z(2, 3, 4), out=z(2, 3, 4))),
+        "dropout_backward": (lambda dy, out: ops.aet_dropout_backward(dy, p=0.5, seed=1, out=out), dict(dy=z(2, 3, 4), out=z(2, 3, 4))),
+    }
+
+
+NAMES = ["linear_forward", "linear_backward", "group_norm_forward", "group_norm_backward", "dropout_forward", "dropout_backward"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_tensors_that_require_a_gradient(ops, name):   # noqa: F811
+    """Refused while gradients are on, whichever it is; taken where they are off, or of a detached tensor."""
+    call, tensors = calls(ops)[name]
+    call(**tensors)
+    for k in tensors:
+        some = dict(tensors, **{k: tensors[k].clone().requires_grad_()})
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call(**some)
+        with torch.no_grad():
+            call(**some)
+        with torch.inference_mode():
+            call(**some)
+        call(**dict(some, **{k: some[k].detach()}))
+    torch.cuda.synchronize()
