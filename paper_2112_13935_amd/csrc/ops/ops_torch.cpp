@@ -27,6 +27,8 @@ struct Call {
     // Not the current stream: what is allocated belongs to it (memory that the current stream has given back may still
     // be in use there) and is kept for the current one too; what is handed over is kept for it.
     std::optional<c10::StreamGuard> other;
+    const Tensor *places[3];   // outputs' that the caller gave
+    int count = 0;
 
     Call(const Tensor &first, int64_t handle_, const std::optional<std::tuple<int64_t, int64_t, int64_t>> &stream)
         : x(first), dtype(AET_F32), handle((void *)handle_), guard(checked(first)) {
@@ -99,6 +101,7 @@ struct Call {
         return t;
     }
     OptTensor out(const OptTensor &given, bool wanted, at::IntArrayRef shape) {
+        if (given) places[count++] = &*given;
         return given ? given : wanted ? OptTensor(made(shape, x.scalar_type())) : std::nullopt;
     }
     template <class A>
@@ -106,9 +109,12 @@ struct Call {
         const size_t need = bytes(&a);
         Tensor ws;
         if (need) ws = at::empty({(int64_t)need}, x.options().dtype(at::kByte));
-        check(fn(&a, need ? use(ws) : nullptr, need, handle));
+        done(fn(&a, need ? use(ws) : nullptr, need, handle));
     }
-    static void check(aet_status rc) {
+    // Written to, a tensor has another version: automatic differentiation that has kept it for a gradient finds out.
+    void done(aet_status rc) {
+        for (int i = 0; i < count; ++i)
+            if (!places[i]->is_inference()) places[i]->unsafeGetTensorImpl()->bump_version();
         if (rc == AET_OK) return;
         const py::object type = py::module_::import("paper_2112_13935_amd.binding").attr("AetError");
         PyErr_SetObject(type.ptr(), type((int)rc, std::string(aet_ops_last_error())).ptr());
@@ -252,7 +258,7 @@ Tensor dropout(bool back, const Tensor &x, double p, uint64_t seed, int64_t firs
     c.mat(a.x, "x", x, x.sizes());
     c.mat(a.residual, "residual", residual, x.sizes());
     c.mat(a.y, "out", y, x.sizes());
-    c.check(back ? aet_dropout_backward(&a, c.handle) : aet_dropout_forward(&a, c.handle));
+    c.done(back ? aet_dropout_backward(&a, c.handle) : aet_dropout_forward(&a, c.handle));
     return *y;
 }
 

@@ -45,3 +45,29 @@ def test_tensors_that_require_a_gradient(ops, name):   # noqa: F811
             call(**some)
         call(**dict(some, **{k: some[k].detach()}))
     torch.cuda.synchronize()
+
+
+# name: the places that a call writes to
+PLACES = {"linear_forward": ["out"], "linear_backward": ["dx", "dw", "db"], "group_norm_forward": ["out"],
+          "group_norm_backward": ["dx", "dgamma", "dbeta"], "dropout_forward": ["out"], "dropout_backward": ["out"]}
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_places_that_are_written_have_another_version(ops, name):   # noqa: F811
+    """As PyTorch's own operations on a tensor in place; inputs keep theirs."""
+    call, tensors = calls(ops)[name]
+    before = {k: t._version for k, t in tensors.items()}
+    call(**tensors)
+    for k, t in tensors.items():
+        assert (t._version > before[k]) == (k in PLACES[name]), k
+    with torch.inference_mode():
+        call(**{k: t.clone() for k, t in tensors.items()})
+
+
+def test_a_kept_tensor_that_is_overwritten_is_found(ops):   # noqa: F811
+    x = torch.ones(3, 4, device=DEV)
+    w = torch.ones(4, device=DEV, requires_grad=True)
+    y = (x * w).sum()   # keeps x for the gradient of w
+    ops.aet_dropout_forward(x, p=0.5, seed=1, out=x)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
