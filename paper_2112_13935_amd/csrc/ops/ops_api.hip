@@ -157,11 +157,12 @@ static aet_status check(const aet_linear_grad *a, bool *shared) {
         AET_CHECK("db", bad_out(a->db.p, a->dtype, 1, go, st, a->out));
     }
     if (*shared) {
-        if (a->w.client || (a->dw.p && a->dw.client) || (a->db.p && a->db.client))
+        if ((a->dx.p && a->w.client) || (a->dw.p && a->dw.client) || (a->db.p && a->db.client))
             return fail(AET_EINVAL, "w, dw and db: either all or none are the same for all clients (client = 0)");
         auto flat = [&](const void *p, int64_t client, int64_t row) { return !p || client == a->rows * row; };
-        if (a->n && (!flat(a->dy.p, a->dy.client, a->dy.row) || !flat(a->x.p, a->x.client, a->x.row) ||
-                     !flat(a->pre.p, a->pre.client, a->pre.row) || !flat(a->dx.p, a->dx.client, a->dx.row)))
+        // (of those that are read or written)
+        if (a->n && (!flat(a->dy.p, a->dy.client, a->dy.row) || (a->dw.p && !flat(a->x.p, a->x.client, a->x.row)) ||
+                     (a->act != AET_ACT_NONE && !flat(a->pre.p, a->pre.client, a->pre.row)) || !flat(a->dx.p, a->dx.client, a->dx.row)))
             return fail(AET_EINVAL, "one W for all clients: rows have to lie client after client (client = rows * row)");
         if ((int64_t)a->n * a->rows > kMostSize) return fail(AET_EINVAL, "one W for all clients: more than 2^30 rows");
     }

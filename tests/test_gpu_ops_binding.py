@@ -71,3 +71,15 @@ def test_a_kept_tensor_that_is_overwritten_is_found(ops):   # noqa: F811
     ops.aet_dropout_forward(x, p=0.5, seed=1, out=x)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradient_of_a_shared_bias_does_not_ask_for_x(ops, dtype):   # noqa: F811
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    g = torch.Generator().manual_seed(2)
+    dy, w = torch.randn(3, 70, 5, generator=g).to(dt).to(DEV), torch.randn(5, 8, generator=g).to(dt).to(DEV)
+    apart = torch.zeros(3, 90, 8, dtype=dt, device=DEV)[:, :70]   # clients' rows do not follow one another
+    want = ops.aet_linear_backward(dy, apart.contiguous(), w)
+    dx, none, db = ops.aet_linear_backward(dy, apart, w, need=(True, False, True))
+    assert none is None and torch.equal(dx, want[0]) and torch.equal(db, want[2])
+    assert torch.equal(ops.aet_linear_backward(dy, apart, w, need=(False, False, True))[2], want[2])
