@@ -92,8 +92,8 @@ aet_status aet_linear_forward(const aet_linear *a, void *workspace, size_t works
  *   pre       z as the forward call gave it; p = NULL where act is AET_ACT_NONE
  *   dw, db    client = 0 with n other than 1: one W (bias) for all clients, whose gradient is the sum
  *             over them; x, dy, pre and dx, those of them that the call wants, then lie row after
- *             row, client after client (client = rows * row), and w.client (for dx), dw.client and
- *             db.client are all 0
+ *             row, client after client (client = rows * row; with one row a client, any), and
+ *             w.client (for dx), dw.client and db.client are all 0
  * bf16: the matrix cores take bf16 only, so dz goes into the products as a sum of two bf16
  * values, to within 2^-16 of it (and 2^-134 where it is tiny), a product with each; without
  * activation and dropout it is dy as it is.  db sums dz in fp32. */

@@ -159,8 +159,8 @@ static aet_status check(const aet_linear_grad *a, bool *shared) {
     if (*shared) {
         if ((a->dx.p && a->w.client) || (a->dw.p && a->dw.client) || (a->db.p && a->db.client))
             return fail(AET_EINVAL, "w, dw and db: either all or none are the same for all clients (client = 0)");
-        auto flat = [&](const void *p, int64_t client, int64_t row) { return !p || client == a->rows * row; };
-        // (of those that are read or written)
+        // (of those that are read or written; up to one row a client, there is nothing that a row's stride would say)
+        auto flat = [&](const void *p, int64_t client, int64_t row) { return !p || a->rows <= 1 || client == a->rows * row; };
         if (a->n && (!flat(a->dy.p, a->dy.client, a->dy.row) || (a->dw.p && !flat(a->x.p, a->x.client, a->x.row)) ||
                      (a->act != AET_ACT_NONE && !flat(a->pre.p, a->pre.client, a->pre.row)) || !flat(a->dx.p, a->dx.client, a->dx.row)))
             return fail(AET_EINVAL, "one W for all clients: rows have to lie client after client (client = rows * row)");
@@ -171,6 +171,12 @@ static aet_status check(const aet_linear_grad *a, bool *shared) {
 
 static void fold(aet_linear_grad &a, bool shared) {
     if (!shared) return;
+    if (a.rows == 1) {
+        a.dy.row = a.dy.client;
+        a.x.row = a.x.client;
+        a.pre.row = a.pre.client;
+        a.dx.row = a.dx.client;
+    }
     a.rows *= a.n;
     a.n = 1;
 }

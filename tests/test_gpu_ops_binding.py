@@ -83,3 +83,22 @@ def test_gradient_of_a_shared_bias_does_not_ask_for_x(ops, dtype):   # noqa: F81
     dx, none, db = ops.aet_linear_backward(dy, apart, w, need=(True, False, True))
     assert none is None and torch.equal(dx, want[0]) and torch.equal(db, want[2])
     assert torch.equal(ops.aet_linear_backward(dy, apart, w, need=(False, False, True))[2], want[2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act,p", [("none", 0.0), ("gelu", 0.2)])
+def test_one_row_a_client_of_a_shared_layer(ops, dtype, act, p):   # noqa: F811
+    """Rows of a larger tensor, a client's first each, one W for all: as if they were copied together."""
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    g = torch.Generator().manual_seed(2)
+    rand = lambda *s: torch.randn(*s, generator=g).to(dt).to(DEV)   # noqa: E731
+    dy, x, pre, w = rand(37, 3, 24)[:, :1], rand(37, 2, 40)[:, 1:], rand(37, 4, 24)[:, 2:3], rand(24, 40)
+    if act == "none":
+        pre = None
+    more = dict(act=act, p=p, seed=3)
+    want = ops.aet_linear_backward(dy.contiguous(), x.contiguous(), w, pre if pre is None else pre.contiguous(), **more)
+    place = torch.full((37, 2, 40), 5.0, dtype=dt, device=DEV)
+    got = ops.aet_linear_backward(dy, x, w, pre, out=(place[:, :1], None, None), **more)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and bool((place[:, 1] == 5).all())
+    same = ops.aet_linear_backward(dy, x[:1].expand(37, 1, 40), w, pre, **more)   # one x for all
+    assert torch.equal(same[1], ops.aet_linear_backward(dy.contiguous(), x[:1].expand(37, 1, 40).contiguous(), w, pre if pre is None else pre.contiguous(), **more)[1])

@@ -39,3 +39,15 @@ def test_taken(what):
                                   dict(w_client=OUT * IN), dict(NO_DX, x_client=ROWS * IN + 8), dict(NO_DX, dw_client=OUT * IN)], ids=str)
 def test_refused(what):
     assert status(grad(**what)) == EINVAL
+
+
+def one_row(rows, **k):
+    """Clients' rows with gaps, and strides of rows that say nothing."""
+    big = 200   # enough clients for a workspace
+    return grad(n=big, rows=rows, dy_client=3 * OUT, dy_row=1, x_client=5 * IN, x_row=7, pre_client=0, pre_row=2, dx_client=IN + 1, dx_row=0, **k)
+
+
+def test_one_row_a_client():
+    assert status(one_row(1)) == ENOMEM
+    assert status(one_row(2)) == EINVAL
+
