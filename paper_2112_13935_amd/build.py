@@ -25,13 +25,21 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
 
 
-def needs_build() -> bool:
-    if not os.path.exists(LIB):
+def _older(libs, deps) -> bool:
+    if not all(os.path.exists(lib) for lib in libs):
         return True
-    t = os.path.getmtime(LIB)
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.h")) + [
-        os.path.join(os.path.dirname(HERE), "include", "aet_sgd.h")]
+    t = min(os.path.getmtime(lib) for lib in libs)
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def needs_build() -> bool:
+    return _older([LIB], sources() + glob.glob(os.path.join(CSRC, "*.h")) + [os.path.join(INCLUDE, "aet_sgd.h")])
+
+
+def needs_build_ops() -> bool:
+    """Whether the operators' library or its binding is missing or older than what it is made from."""
+    return _older([OPS_LIB, OPS_TORCH], [f for d in (CSRC, OPS_CSRC, INCLUDE) for f in glob.glob(os.path.join(d, "*.h"))]
+                  + glob.glob(os.path.join(OPS_CSRC, "*.hip")) + glob.glob(os.path.join(OPS_CSRC, "*.cpp")))
 
 
 def build(force: bool = True, verbose: bool = False) -> str:

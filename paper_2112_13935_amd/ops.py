@@ -17,6 +17,7 @@ from __future__ import annotations
 import ctypes as C
 import importlib.util
 import os
+import warnings
 from typing import Optional, Tuple
 
 import torch
@@ -79,12 +80,16 @@ _EXT = None
 
 
 def load_library():
-    """Load the in-tree library (building it only if it has never been built)."""
+    """Load the in-tree library (building it only if it has never been built; one that is older than its sources is
+    loaded with a warning)."""
     global _LIB
     if _LIB is not None:
         return _LIB
     if not (os.path.exists(_build.OPS_LIB) and os.path.exists(_build.OPS_TORCH)):
         _build.build_ops()
+    elif _build.needs_build_ops():
+        warnings.warn(f"{os.path.basename(_build.OPS_LIB)} or its binding is older than its sources: build.build_ops() makes them anew",
+                      RuntimeWarning, stacklevel=2)
     lib = C.CDLL(_build.OPS_LIB)
     for name in ("aet_linear", "aet_linear_backward", "aet_group_norm", "aet_group_norm_backward"):
         f = getattr(lib, name + "_workspace_bytes")
