@@ -139,3 +139,30 @@ def test_gelu_at_the_ends_of_the_range(ops):   # noqa: F811
     one = torch.ones_like(z)
     _, _, db = ops.aet_linear_backward(one, one[:, :1], torch.ones(z.shape[1], 1, device=DEV), z, act="gelu")
     assert torch.equal(db[4:7].cpu(), torch.ones(3)) and bool((db[8:11].abs() < 1e-28).all())
+
+
+# (n, batch, positions, groups, width) of the norm's tests, and larger ones of one launch and of three
+RELU = [(1, 1, 20, 1, 1), (2, 3, 1, 4, 8), (1, 2, 50, 16, 1), (2, 2, 35, 3, 5), (1, 1, 784, 4, 4), (3, 4, 64, 8, 4), (2, 2, 256, 2, 24), (1, 3, 100, 1, 33),
+        (1, 1, 4096, 8, 40), (1, 2, 3001, 5, 7), (1, 1, 20000, 2, 16), (4, 30, 9, 2, 6), (1, 2, 17, 32, 40), (1, 1, 1, 1, 2000), (1, 1, 900, 3, 96),
+        (2, 40, 300, 6, 7), (2, 64, 1024, 9, 10)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", RELU, ids=str)
+def test_group_norm_gradient_behind_relu(ops, size, dtype):   # noqa: F811
+    """Every size: where the value before the activation is so near 0 that its sign in fp32 is open, dy is 0."""
+    n, b, P, G, width = size
+    dt, ch = TYPES[dtype], G * width
+    g = torch.Generator().manual_seed(P + ch)
+    x, dy = rand(g, (n, b, P, ch), dt) + 0.5, rand(g, (n, b, P, ch), dt)
+    gamma, beta = rand(g, (n, ch), dt), rand(g, (n, ch), dt)
+    _, mean, rstd = ops.aet_group_norm_forward(x, G, gamma, beta, eps=1e-3, act="relu")
+    t = ((d64(x).view(n, b, P, G, width) - d64(mean)[:, :, None, :, None]) * d64(rstd)[:, :, None, :, None]).reshape(n, b, P, ch)
+    t = t * d64(gamma)[:, None, None] + d64(beta)[:, None, None]
+    near = t.abs() < 1e-5 * (t.abs().amax() + 1)
+    dy[near.to(DEV)] = 0
+    assert float(near.double().mean()) < 0.01 or near.numel() < 100
+    got = ops.aet_group_norm_backward(dy, x, mean, rstd, gamma, beta, act="relu")
+    want = O.group_norm_backward(d64(dy), d64(x), d64(mean), d64(rstd), d64(gamma), d64(beta), "relu", dt)
+    for what, a, c in zip(("dx", "dgamma", "dbeta"), got, want):
+        O.near(a, c, f"{what} {size} {dtype}")
