@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import ops_oracle as O
+from test_ops_bounds import product_norm
 from test_gpu_ops_linear import DEV, TYPES, d64, ops, rand  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -166,3 +167,25 @@ def test_group_norm_gradient_behind_relu(ops, size, dtype):   # noqa: F811
     want = O.group_norm_backward(d64(dy), d64(x), d64(mean), d64(rstd), d64(gamma), d64(beta), "relu", dt)
     for what, a, c in zip(("dx", "dgamma", "dbeta"), got, want):
         O.near(a, c, f"{what} {size} {dtype}")
+
+
+# n, rows, in, out: the products of a layer and of both its gradients in tiles of 128 x 128, 64 x 128 and 64 x 64, in one sum and in
+# slices, and the pair of small ones
+TILES = [(1, 2048, 1024, 2048), (1, 1024, 2048, 2048), (1, 3000, 700, 4104), (2, 2568, 2624, 2632), (64, 64, 1024, 512), (3, 1001, 1155, 771),
+         (1, 640, 640, 640), (1, 4096, 64, 40), (2, 40, 96, 64), (2, 257, 129, 255)]
+
+
+@pytest.mark.parametrize("size", TILES, ids=str)
+def test_products_in_fp32_hold_24_bits(ops, size):   # noqa: F811
+    """Relative 2-norms of normal deviates' products, more than 32 rows, within product_norm of their sums' lengths."""
+    n, rows, inp, out = size
+    f32 = torch.float32
+    g = torch.Generator().manual_seed(rows)
+    x, w, dy = rand(g, (n, rows, inp), f32), rand(g, (n, out, inp), f32), rand(g, (n, rows, out), f32)
+    y, _ = ops.aet_linear_forward(x, w)
+    dx, dw, _ = ops.aet_linear_backward(dy, x, w)
+    T = lambda t: t.transpose(1, 2).contiguous()   # noqa: E731
+    for what, got, a, b in (("y", y, x, T(w)), ("dx", dx, dy, w), ("dw", dw, T(dy), x)):
+        want = d64(a) @ d64(b)
+        off, most = float((d64(got) - want).norm() / want.norm()), product_norm(a.shape[-1])
+        assert off <= most, (what, size, off, most)
