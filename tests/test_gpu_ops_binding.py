@@ -102,3 +102,86 @@ def test_one_row_a_client_of_a_shared_layer(ops, dtype, act, p):   # noqa: F811
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and bool((place[:, 1] == 5).all())
     same = ops.aet_linear_backward(dy, x[:1].expand(37, 1, 40), w, pre, **more)   # one x for all
     assert torch.equal(same[1], ops.aet_linear_backward(dy.contiguous(), x[:1].expand(37, 1, 40).contiguous(), w, pre if pre is None else pre.contiguous(), **more)[1])
+
+
+# The first tensor says type, device and sizes; mean and rstd are fp32 always.
+FIRST = {"linear_forward": "x", "linear_backward": "x", "group_norm_forward": "x", "group_norm_backward": "x", "dropout_forward": "x",
+         "dropout_backward": "dy"}
+
+
+def another(t, how):
+    if how == "type":
+        return t.to(torch.bfloat16)
+    if how == "device":
+        return t.cpu()
+    if how == "last stride":
+        return t.new_zeros(*t.shape, 2)[..., 0]
+    if how == "longer":
+        return t.new_zeros(*t.shape[:-1], t.shape[-1] + 1)
+    if how == "shorter":
+        return t.new_zeros(t.shape[0], *t.shape[1:-1], t.shape[-1] - 1)
+    return t[None]   # another axis
+
+
+@pytest.mark.parametrize("how", ["type", "device", "last stride", "longer", "shorter", "axis"])
+@pytest.mark.parametrize("name", NAMES)
+def test_tensors_that_do_not_agree(ops, name, how):   # noqa: F811
+    """One tensor unlike what the others call for; nothing is written."""
+    call, tensors = calls(ops)[name]
+    for k in tensors:
+        if k == FIRST[name] and how != "last stride":
+            continue
+        places = {p: torch.full_like(tensors[p], 7.0) for p in PLACES[name]}
+        some = dict(tensors, **places)
+        some[k] = another(some[k], how)
+        with pytest.raises(ValueError) as e:
+            call(**some)
+        torch.cuda.synchronize()
+        assert all(bool((t == 7).all()) for p, t in places.items() if p != k), (k, how)
+        if how in ("type", "last stride") and name != "dropout_backward":
+            assert k in str(e.value), (k, how, str(e.value))
+
+
+def test_first_tensors_that_are_refused(ops):   # noqa: F811
+    z = lambda *s: torch.ones(*s, device=DEV)   # noqa: E731
+    for bad in (z(2, 3, 4).double(), z(2, 3, 4).half(), z(2, 3, 4).int(), torch.ones(2, 3, 4)):
+        with pytest.raises(ValueError, match="float32 or bfloat16 on a GPU"):
+            ops.aet_linear_forward(bad, z(2, 5, 4))
+        with pytest.raises(ValueError, match="float32 or bfloat16 on a GPU"):
+            ops.aet_dropout_forward(bad, p=0.5, seed=1)
+        with pytest.raises(ValueError, match="float32 or bfloat16 on a GPU"):
+            ops.aet_group_norm_forward(bad, 2)
+    for bad in (z(4), z(1, 2, 3, 4)):
+        with pytest.raises(ValueError, match="2 or 3 axes"):
+            ops.aet_linear_forward(bad, z(2, 5, 4))
+        with pytest.raises(ValueError, match="2 or 3 axes"):
+            ops.aet_dropout_forward(bad, p=0.5, seed=1)
+    for bad in (z(3, 4), z(1, 1, 2, 3, 4)):
+        with pytest.raises(ValueError, match="3 or 4 axes"):
+            ops.aet_group_norm_forward(bad, 2)
+
+
+def test_arguments_that_do_not_agree(ops):   # noqa: F811
+    from paper_2112_13935_amd import AetError
+    z = lambda *s: torch.ones(*s, device=DEV)   # noqa: E731
+    with pytest.raises(ValueError, match="pre"):
+        ops.aet_linear_backward(z(2, 3, 5), z(2, 3, 4), z(2, 5, 4), act="gelu")
+    with pytest.raises(ValueError, match="act is one of"):
+        ops.aet_linear_forward(z(2, 3, 4), z(2, 5, 4), act="tanh")
+    with pytest.raises(ValueError, match="groups"):
+        ops.aet_group_norm_forward(z(2, 3, 4, 6), 4)
+    with pytest.raises(ValueError, match="axis of clients"):
+        ops.aet_group_norm_backward(z(2, 3, 4, 6), z(2, 3, 4, 6), z(2, 3, 2), z(2, 3, 2), z(2, 6), z(6))
+    with pytest.raises(ValueError, match="rstd"):
+        ops.aet_group_norm_backward(z(2, 3, 4, 6), z(2, 3, 4, 6), z(2, 3, 2), z(2, 2, 3).transpose(1, 2), z(2, 6), z(2, 6))
+    for p in (1.0, -0.1, float("nan")):
+        with pytest.raises(AetError, match="p is not in"):
+            ops.aet_dropout_forward(z(3, 4), p=p, seed=1)
+    with pytest.raises(AetError, match="first_row"):
+        ops.aet_dropout_forward(z(3, 4), p=0.5, seed=1, first_row=-1)
+    with pytest.raises(AetError, match="overlaps itself"):
+        ops.aet_dropout_forward(z(3, 4), p=0.5, seed=1, out=z(1, 4).expand(3, 4))
+    with pytest.raises(AetError, match="eps"):
+        ops.aet_group_norm_forward(z(2, 3, 4, 6), 2, eps=-1.0)
+    with pytest.raises(AetError, match="client after client"):
+        ops.aet_linear_backward(z(2, 3, 5), z(2, 4, 4)[:, :3], z(5, 4))
