@@ -11,8 +11,10 @@
  *     256-byte aligned; NULL where that is 0).  It keeps nothing between calls.
  *   - All tensors of a call have the call's dtype, but for the statistics of a normalisation
  *     (fp32).  Products, sums, statistics and everything between a call's inputs and its
- *     outputs are fp32 or wider; an output is rounded once, to its type.  (One exception, in
- *     the gradient of a linear layer in bf16, is named there.)
+ *     outputs are fp32 or wider; an output is rounded once, to its type.  Two exceptions: dz in
+ *     the gradient of a linear layer in bf16 (named there); and fp32 products of more than 32
+ *     rows, and all of fp32 gradients, take their operands to within 2^-134, which is less
+ *     than 24 bits of one below 2^-110 (forward products of up to 32 rows take all of them).
  *   - Strides are in elements; the last axis has stride 1.  Inputs may have any strides that
  *     are not negative (0: the same values for every row or client).  Outputs must not
  *     overlap themselves, nor an input, except where a call says so.  Any alignment that

@@ -189,3 +189,28 @@ def test_products_in_fp32_hold_24_bits(ops, size):   # noqa: F811
         want = d64(a) @ d64(b)
         off, most = float((d64(got) - want).norm() / want.norm()), product_norm(a.shape[-1])
         assert off <= most, (what, size, off, most)
+
+
+@pytest.mark.parametrize("rows", [20, 48, 300])
+def test_tiny_operands_in_fp32(ops, rows):   # noqa: F811
+    """Operands of 2^-125 to 2^-105 beside others of 2^60: taken to within 2^-134 (those of a call of up to 32 rows whole), beside the
+    rounding of the sums."""
+    inp, out = 96, 80
+    f32 = torch.float32
+    g = torch.Generator().manual_seed(rows)
+
+    def tiny(*shape):
+        return (torch.randn(*shape, generator=g) * 2.0 ** (-105 - 20 * torch.rand(*shape, generator=g))).to(DEV)
+
+    def product(what, got, a, b, low):
+        want, S = d64(a) @ d64(b), d64(a).abs() @ d64(b).abs()
+        off = (a.shape[-1] + 4) * O.U32 * S + low * (torch.ones_like(d64(a)) @ d64(b).abs())
+        O.near(got * 2.0 ** 60, (want * 2.0 ** 60, (off + O.U32 * (want.abs() + off)) * 2.0 ** 60), what)
+
+    x, w, dy = tiny(1, rows, inp), rand(g, (1, out, inp), f32, 2.0 ** 60), tiny(1, rows, out)
+    big = rand(g, (1, rows, inp), f32, 2.0 ** 60)
+    T = lambda t: t.transpose(1, 2).contiguous()   # noqa: E731
+    product("y", ops.aet_linear_forward(x, w)[0], x, T(w), 0.0 if rows <= 32 else 2.0 ** -134)
+    dx, dw, _ = ops.aet_linear_backward(dy, big, w)
+    product("dx", dx, dy, w, 2.0 ** -134)
+    product("dw", dw, T(dy), big, 2.0 ** -134)
