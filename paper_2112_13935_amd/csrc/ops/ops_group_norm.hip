@@ -7,7 +7,8 @@
 // three: sums of strips of positions, their union by group, and a second pass over the values.
 //   2048 samples of 1024 x 32 in fp32, groups of 4 channels, silu: 122 us (537 MB, 4.4 TB/s; a copy of as much 107)
 //   gradient of 128 samples of 4096 x 320 in bf16, groups of 10: 328 us: sums 156 (671 MB read, 4.3 TB/s), union 9, second
-//   pass 175 (1.0 GB, 5.8 TB/s); reading the values once would be 201, but no compute unit's registers hold a sample
+//   pass 175 (1.0 GB, 5.8 TB/s); reading the values once would be 201, but four groups, the least of whole 64 bytes, are 655 KB of x
+//   and dy, and a compute unit's registers 512
 #include "ops_internal.h"
 
 #include <type_traits>

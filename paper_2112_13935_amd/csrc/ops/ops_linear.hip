@@ -27,7 +27,7 @@ hipError_t launch_linear_forward(const aet_linear &a, void *workspace, hipStream
 // dz = dropout'(dy) * act'(z), and its sums over rows.  A workgroup has 32 pieces of 16 bytes of a strip of a client's rows,
 // eight rows at a time, and four times that on the way; the sums of several strips go to `partial` and are added by k_db,
 // in their order.  Bound by memory: 4 x 4096 rows of 8192 in bf16, two
-// values read and one written, 161 us, 5.0 TB/s.  Inside the products it would be worked out again for each column of
+// values read and two written, 199 us, 5.4 TB/s.  Inside the products it would be worked out again for each column of
 // tiles, and for the second product.
 // bf16: dz is kept as the nearest bf16 value and the nearest to what that leaves, 16 bits, for two products of the matrix
 // unit each.  One value alone adds an error of the size of the outputs' own rounding to them (relative 2-norm of dx and dw 1.4 times

@@ -9,9 +9,10 @@
 // hand 16 lanes the transpose of 4 pieces of memory.  The pieces of a row are permuted by exclusive or with the row's number
 // (by columns: in groups of 4 with k), so that the lanes that read together find different banks.
 //
-// Bound by the matrix unit, whose clock falls under load, where there are tiles enough: 16384 x 4096 x 4096 in bf16 455 us
-// (1210 TF/s; with zeros 1376), 4 x (4096 x 2048 x 8192) with B by columns 530, with both 500; 4096 x 4096 x 4096 in fp32
-// 690 us (199 TF/s, which is as many bf16 products a second).  256 x 256 in bf16 is the tile whose operands the L2 brings in
+// Where there are tiles enough: 16384 x 4096 x 4096 in bf16 455 us (1210 TF/s; with zeros, at the full clock, 1376), 4 x
+// (4096 x 2048 x 8192) with B by columns 530, with both 500, with A in two parts twice that; 4096 x 4096 x 4096 in fp32 690 us (199
+// TF/s, which is as many bf16 products a second).  In the first the matrix unit is busy 54 % of the cycles; the waves, two a
+// SIMD, are at a wait or barrier 27 % of their time and ready but not chosen 47 %; LDS is busy 22 % (by columns 47, 53, 35 and 18 %).  256 x 256 in bf16 is the tile whose operands the L2 brings in
 // the time of its products (256 x 128, two workgroups a unit: 1037 TF/s).  fp32 has 128 x 128, whose parts and two
 // accumulators fill registers and LDS, two workgroups a unit: one splits and stores while the other multiplies.  Deeper
 // prefetch, more buffers and tiles that fetch the next tile's operands cost more than they gave.
