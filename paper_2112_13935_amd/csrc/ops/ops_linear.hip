@@ -74,16 +74,21 @@ __global__ __launch_bounds__(256) void k_dz(aet_linear_grad a, Drop d, DzShape s
         if (dz) {
             T *const to = dz + (client * a.rows + r) * s.dz_row;
             if (ends) *(wide<T, V> *)(to + s.dz_row - V) = wide<T, V>{};   // zeros up to the next row, for the products
-            store_some(to + col, count, v);
             if constexpr (sizeof(T) == 2) {
-                float low[V];
+                float high[V], low[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float high = (float)(T)v[e];
-                    low[e] = __builtin_fabsf(high) < __builtin_inff() ? v[e] - high : 0.0f;   // (NaN: 0 too; the first part has it)
+                    high[e] = (float)(T)v[e];
+                    // what would round to infinity has the largest value; infinities and NaN are in the first part alone
+                    const bool finite = __builtin_fabsf(v[e]) <= __FLT_MAX__;
+                    if (finite && __builtin_fabsf(high[e]) > __FLT_MAX__) high[e] = __builtin_copysignf(0x1.fep127f, v[e]);
+                    low[e] = finite ? v[e] - high[e] : 0.0f;
                 }
                 if (ends) *(wide<T, V> *)(to + s.low + s.dz_row - V) = wide<T, V>{};
+                store_some(to + col, count, high);
                 store_some(to + s.low + col, count, low);
+            } else {
+                store_some(to + col, count, v);
             }
         }
 #pragma unroll

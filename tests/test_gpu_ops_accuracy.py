@@ -214,3 +214,23 @@ def test_tiny_operands_in_fp32(ops, rows):   # noqa: F811
     dx, dw, _ = ops.aet_linear_backward(dy, big, w)
     product("dx", dx, dy, w, 2.0 ** -134)
     product("dw", dw, T(dy), big, 2.0 ** -134)
+
+
+def test_gradients_in_bf16_beyond_its_largest_value(ops):   # noqa: F811
+    """dz between bf16's largest value and fp32's is finite, and so is what it gives."""
+    bf16 = torch.bfloat16
+    big, p = torch.finfo(bf16).max, 0.0025
+    rows, inp, out = 70, 40, 72
+    g = torch.Generator().manual_seed(3)
+    w, x = rand(g, (1, out, inp), bf16, 2.0 ** -20), rand(g, (1, rows, inp), bf16, 2.0 ** -20)
+    dy = rand(g, (1, rows, out), bf16)
+    m = O.mask3((1, rows, out), 9, 0, p)
+    assert bool((m[0, 5:8, 3] > 0).all()) and big < big / (1 - p) < torch.finfo(torch.float32).max
+    dy[0, 5, 3], dy[0, 6, 3], dy[0, 7, 3] = big, -big, big
+    dx, dw, _ = ops.aet_linear_backward(dy, x, w, p=p, seed=9)
+    dz = d64(dy) * m
+    T = lambda t: t.transpose(1, 2).contiguous()   # noqa: E731
+    for what, got, a, b in (("dx", dx, dz, d64(w)), ("dw", dw, T(dz), d64(x))):
+        want, S = a @ b, a.abs() @ b.abs()
+        o = (2.0 ** -16 + (a.shape[-1] + 8) * O.U32) * S
+        O.near(got, (want, o + O.ROUND[bf16] * (want.abs() + o)), what)
