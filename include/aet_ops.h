@@ -1,8 +1,8 @@
 /*
  * aet_ops.h -- C ABI of the operators that residual blocks of clients' models are composed
  * from, on MI355X (gfx950): a linear layer with bias, activation, dropout and residual in its
- * epilogue, group normalisation with an activation on channels-last maps, and dropout from
- * the counter generator, each with its gradient.  All of them take many clients' models side
+ * epilogue, group normalisation with an activation on channels-last maps, layer normalisation
+ * of rows, and dropout from the counter generator, each with its gradient.  All of them take many clients' models side
  * by side in one call (`n`), each with parameters of its own or all with the same ones.
  *
  * Conventions
@@ -156,6 +156,42 @@ typedef struct {
 size_t aet_group_norm_backward_workspace_bytes(const aet_group_norm_grad *a);
 aet_status aet_group_norm_backward(const aet_group_norm_grad *a, void *workspace, size_t workspace_bytes,
                                    void *hip_stream);
+
+/* Layer normalisation of rows, the residual stream joined in:  h = x + residual; over the cols
+ * values of a row of h: mean m and variance v (divided by their number), rstd = 1 / sqrt(v + eps);
+ * y = (h - m) rstd gamma + beta, of h before it is rounded to its type.
+ *   x, residual  n x rows x cols; residual: or p = NULL
+ *   gamma, beta  n x cols (row is ignored; client = 0: the same for all), or p = NULL: 1, 0
+ *   y, h         n x rows x cols; h, the stream as it goes on: or p = NULL.  Either may be x or
+ *                residual itself, with the same strides (not both the same one).
+ *   mean, rstd   fp32, n x rows without gaps, for the gradient; NULL: not wanted.  With no
+ *                columns: 0 and 1 / sqrt(eps). */
+typedef struct {
+    int32_t dtype;
+    int32_t n, rows, cols;
+    float eps;
+    aet_in x, residual, gamma, beta;
+    aet_out y, h;
+    float *mean, *rstd;
+} aet_layer_norm;
+aet_status aet_layer_norm_forward(const aet_layer_norm *a, void *hip_stream);
+
+/* Its gradient.  x is what was normalised (the forward call's h, or its x where there was no
+ * residual), mean and rstd as that call gave them, dh what comes to h along the stream:
+ * dx = (gradient through the normalisation) + dh, which is that of x and of residual.
+ *   dh            n x rows x cols, or p = NULL
+ *   dx            n x rows x cols; may be dy or dh itself, with the same strides; or p = NULL
+ *   dgamma, dbeta n x cols; client = 0 with n other than 1: the sum over the clients (then of
+ *                 both); or p = NULL */
+typedef struct {
+    int32_t dtype;
+    int32_t n, rows, cols;
+    aet_in dy, x, dh, gamma;
+    const float *mean, *rstd;
+    aet_out dx, dgamma, dbeta;
+} aet_layer_norm_grad;
+size_t aet_layer_norm_backward_workspace_bytes(const aet_layer_norm_grad *a);
+aet_status aet_layer_norm_backward(const aet_layer_norm_grad *a, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* y = residual + dropout(x): n x rows x cols each; residual may have p = NULL, y may be x or
  * residual itself, with the same strides.  The gradient of x is the same mask and scale on

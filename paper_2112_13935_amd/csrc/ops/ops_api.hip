@@ -236,6 +236,60 @@ static aet_status check(const aet_group_norm_grad *a) {
     return AET_OK;
 }
 
+// ---- layer norm --------------------------------------------------------------------------
+
+static aet_status check(const aet_layer_norm *a) {
+    const char *why;
+    if (!a) return fail(AET_EINVAL, "the record is NULL");
+    if (bad_common(a->dtype, AET_ACT_NONE, &why)) return fail(AET_EINVAL, "%s", why);
+    if (bad_sizes({a->n, a->rows, a->cols}, &why)) return fail(AET_EINVAL, "%s", why);
+    if (!(a->eps >= 0)) return fail(AET_EINVAL, "eps is negative");
+    AET_CHECK("mean", bad_stats(a->mean));
+    AET_CHECK("rstd", bad_stats(a->rstd));
+    if (!a->n || !a->rows || !a->cols) return AET_OK;
+    const int64_t nr[2] = {a->n, a->rows}, one[1] = {a->n};
+    auto in = [&](const aet_in &t) { const int64_t st[2] = {t.client, t.row}; return bad_in(t.p, a->dtype, 2, nr, st); };
+    auto out = [&](const aet_out &t) { const int64_t st[2] = {t.client, t.row}; return bad_out(t.p, a->dtype, 2, nr, st, a->cols); };
+    AET_CHECK("x", in(a->x));
+    if (a->residual.p) AET_CHECK("residual", in(a->residual));
+    if (a->gamma.p) AET_CHECK("gamma", bad_in(a->gamma.p, a->dtype, 1, one, &a->gamma.client));
+    if (a->beta.p) AET_CHECK("beta", bad_in(a->beta.p, a->dtype, 1, one, &a->beta.client));
+    AET_CHECK("y", out(a->y));
+    if (a->h.p) AET_CHECK("h", out(a->h));
+    if (a->h.p == a->y.p) return fail(AET_EINVAL, "y and h are the same");
+    return AET_OK;
+}
+static aet_status check(const aet_layer_norm_grad *a) {
+    const char *why;
+    if (!a) return fail(AET_EINVAL, "the record is NULL");
+    if (bad_common(a->dtype, AET_ACT_NONE, &why)) return fail(AET_EINVAL, "%s", why);
+    if (bad_sizes({a->n, a->rows, a->cols}, &why)) return fail(AET_EINVAL, "%s", why);
+    if (!a->cols) return AET_OK;
+    auto param = [&](const aet_out &t) {
+        const int64_t count[1] = {t.client ? a->n : 1};
+        return bad_out(t.p, a->dtype, 1, count, &t.client, a->cols);
+    };
+    if (a->dgamma.p) AET_CHECK("dgamma", param(a->dgamma));
+    if (a->dbeta.p) AET_CHECK("dbeta", param(a->dbeta));
+    if (a->n != 1 && a->dgamma.p && a->dbeta.p && !a->dgamma.client != !a->dbeta.client)
+        return fail(AET_EINVAL, "dgamma and dbeta: either both or none are the same for all clients (client = 0)");
+    if (!a->n || !a->rows || !(a->dx.p || a->dgamma.p || a->dbeta.p)) return AET_OK;
+    const int64_t nr[2] = {a->n, a->rows}, one[1] = {a->n};
+    auto in = [&](const aet_in &t) { const int64_t st[2] = {t.client, t.row}; return bad_in(t.p, a->dtype, 2, nr, st); };
+    AET_CHECK("dy", in(a->dy));
+    AET_CHECK("x", in(a->x));
+    if (a->dh.p) AET_CHECK("dh", in(a->dh));
+    if (a->gamma.p) AET_CHECK("gamma", bad_in(a->gamma.p, a->dtype, 1, one, &a->gamma.client));
+    if (a->dx.p) {
+        const int64_t st[2] = {a->dx.client, a->dx.row};
+        AET_CHECK("dx", bad_out(a->dx.p, a->dtype, 2, nr, st, a->cols));
+    }
+    if (!a->mean || !a->rstd) return fail(AET_EINVAL, "mean or rstd is NULL");
+    AET_CHECK("mean", bad_stats(a->mean));
+    AET_CHECK("rstd", bad_stats(a->rstd));
+    return AET_OK;
+}
+
 // ---- dropout -----------------------------------------------------------------------------
 
 static aet_status run_dropout(const aet_dropout *a, bool residual, void *hip_stream) {
@@ -329,6 +383,23 @@ aet_status aet_group_norm_backward(const aet_group_norm_grad *a, void *workspace
     if (bad_workspace(workspace, workspace_bytes, need))
         return fail(AET_ENOMEM, "the workspace needs %zu bytes, 256-byte aligned; got %zu", need, workspace_bytes);
     return done(launch_group_norm_backward(*a, workspace, (hipStream_t)hip_stream));
+}
+
+aet_status aet_layer_norm_forward(const aet_layer_norm *a, void *hip_stream) {
+    if (const aet_status st = check(a)) return st;
+    if (!a->n || !a->rows) return AET_OK;
+    return done(launch_layer_norm_forward(*a, (hipStream_t)hip_stream));
+}
+
+size_t aet_layer_norm_backward_workspace_bytes(const aet_layer_norm_grad *a) {
+    return check(a) == AET_OK ? layer_norm_backward_workspace(*a) : 0;
+}
+aet_status aet_layer_norm_backward(const aet_layer_norm_grad *a, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (const aet_status st = check(a)) return st;
+    const size_t need = layer_norm_backward_workspace(*a);
+    if (bad_workspace(workspace, workspace_bytes, need))
+        return fail(AET_ENOMEM, "the workspace needs %zu bytes, 256-byte aligned; got %zu", need, workspace_bytes);
+    return done(launch_layer_norm_backward(*a, workspace, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

@@ -29,4 +29,8 @@ hipError_t launch_group_norm_forward(const aet_group_norm &a, void *workspace, h
 size_t group_norm_backward_workspace(const aet_group_norm_grad &a);
 hipError_t launch_group_norm_backward(const aet_group_norm_grad &a, void *workspace, hipStream_t s);
 
+hipError_t launch_layer_norm_forward(const aet_layer_norm &a, hipStream_t s);
+size_t layer_norm_backward_workspace(const aet_layer_norm_grad &a);
+hipError_t launch_layer_norm_backward(const aet_layer_norm_grad &a, void *workspace, hipStream_t s);
+
 }  // namespace aet_ops

@@ -27,7 +27,7 @@ struct Call {
     // Not the current stream: what is allocated belongs to it (memory that the current stream has given back may still
     // be in use there) and is kept for the current one too; what is handed over is kept for it.
     std::optional<c10::StreamGuard> other;
-    const Tensor *places[3];   // outputs' that the caller gave
+    const Tensor *places[4];   // outputs' that the caller gave
     int count = 0;
 
     Call(const Tensor &first, int64_t handle_, const std::optional<std::tuple<int64_t, int64_t, int64_t>> &stream)
@@ -201,6 +201,15 @@ struct MapAxes {
     std::array<int64_t, 3> stats() const { return {n, batch, groups}; }
 };
 
+// The statistics of a normalisation, as the forward call gave them
+void statistics(Call &c, const Tensor &mean, const Tensor &rstd, at::IntArrayRef shape, const char *axes) {
+    for (const auto &[name, t] : {std::pair<const char *, const Tensor &>("mean", mean), {"rstd", rstd}}) {
+        c.no_graph(name, t);
+        if (t.scalar_type() != at::kFloat || t.device() != c.x.device() || t.sizes() != shape || !t.is_contiguous())
+            value_error(std::string(name) + " has to be as the forward call gave it: float32, contiguous, " + axes);
+    }
+}
+
 std::tuple<Tensor, Tensor, Tensor> group_norm_forward(const Tensor &x, int64_t groups, const OptTensor &gamma, const OptTensor &beta, double eps, int act,
                                                       const OptTensor &out, int64_t handle, const Stream &stream) {
     const MapAxes s(x, groups);
@@ -227,11 +236,7 @@ Three group_norm_backward(const Tensor &dy, const Tensor &x, const Tensor &mean,
     if (gamma && beta && gamma->dim() != beta->dim()) value_error("gamma and beta: either both or none have an axis of clients");
     const auto all = s.stats();
     const at::IntArrayRef stats = at::IntArrayRef(all).slice(4 - x.dim());
-    for (const auto &[name, t] : {std::pair<const char *, const Tensor &>("mean", mean), {"rstd", rstd}}) {
-        c.no_graph(name, t);
-        if (t.scalar_type() != at::kFloat || t.device() != x.device() || t.sizes() != stats || !t.is_contiguous())
-            value_error(std::string(name) + " has to be as the forward call gave it: float32, contiguous, [n, batch, groups]");
-    }
+    statistics(c, mean, rstd, stats, "[n, batch, groups]");
     aet_group_norm_grad a = {c.dtype, act, s.n, s.batch, s.positions, s.groups, s.width};
     const int64_t channels = x.size(-1);
     c.maps(a.dy, "dy", dy, x.sizes());
@@ -262,6 +267,51 @@ Tensor dropout(bool back, const Tensor &x, double p, uint64_t seed, int64_t firs
     return *y;
 }
 
+std::tuple<Tensor, OptTensor, Tensor, Tensor> layer_norm_forward(const Tensor &x, const OptTensor &gamma, const OptTensor &beta, const OptTensor &residual,
+                                                                 double eps, const std::tuple<OptTensor, OptTensor> &out, int64_t handle, const Stream &stream) {
+    Call c(x, handle, stream);
+    const Axes s(x);
+    aet_layer_norm a = {c.dtype, s.n, s.rows, s.cols, (float)eps};
+    const at::IntArrayRef stats = x.sizes().slice(0, x.dim() - 1);
+    c.mat(a.x, "x", x, x.sizes());
+    c.mat(a.residual, "residual", residual, x.sizes());
+    c.vec(a.gamma, "gamma", gamma, s.n, s.cols);
+    c.vec(a.beta, "beta", beta, s.n, s.cols);
+    if (std::get<1>(out) && !residual) value_error("h is x where there is no residual: a place for it is not wanted");
+    const OptTensor y = c.out(std::get<0>(out), true, x.sizes()), h = c.out(std::get<1>(out), residual.has_value(), x.sizes());
+    c.mat(a.y, "out", y, x.sizes());
+    c.mat(a.h, "out", h, x.sizes());
+    const Tensor mean = c.made(stats, at::kFloat), rstd = c.made(stats, at::kFloat);
+    a.mean = (float *)c.use(mean);
+    a.rstd = (float *)c.use(rstd);
+    c.done(aet_layer_norm_forward(&a, c.handle));
+    return {*y, h, mean, rstd};
+}
+
+Three layer_norm_backward(const Tensor &dy, const Tensor &x, const Tensor &mean, const Tensor &rstd, const OptTensor &gamma, const OptTensor &dh,
+                          std::array<bool, 2> need, const Three &out, int64_t handle, const Stream &stream) {
+    Call c(x, handle, stream);
+    const Axes s(x);
+    statistics(c, mean, rstd, x.sizes().slice(0, x.dim() - 1), "[n, rows]");
+    aet_layer_norm_grad a = {c.dtype, s.n, s.rows, s.cols};
+    c.mat(a.dy, "dy", dy, x.sizes());
+    c.mat(a.x, "x", x, x.sizes());
+    c.mat(a.dh, "dh", dh, x.sizes());
+    c.vec(a.gamma, "gamma", gamma, s.n, s.cols);
+    a.mean = (const float *)c.use(mean);
+    a.rstd = (const float *)c.use(rstd);
+    const bool params = need[1] && gamma;
+    const Three made = {c.out(std::get<0>(out), need[0], x.sizes()), c.out(std::get<1>(out), params, gamma ? gamma->sizes() : at::IntArrayRef()),
+                        c.out(std::get<2>(out), params, gamma ? gamma->sizes() : at::IntArrayRef())};
+    const OptTensor &dgamma = std::get<1>(made), &dbeta = std::get<2>(made);
+    if (dgamma && dbeta && dgamma->dim() != dbeta->dim()) value_error("dgamma and dbeta: either both or none have an axis of clients");
+    c.mat(a.dx, "dx", std::get<0>(made), x.sizes());
+    c.vec(a.dgamma, "dgamma", dgamma, s.n, s.cols);
+    c.vec(a.dbeta, "dbeta", dbeta, s.n, s.cols);
+    c.run(aet_layer_norm_backward, aet_layer_norm_backward_workspace_bytes, a);
+    return made;
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_ops_torch, m) {
@@ -270,4 +320,6 @@ PYBIND11_MODULE(_ops_torch, m) {
     m.def("group_norm_forward", &group_norm_forward);
     m.def("group_norm_backward", &group_norm_backward);
     m.def("dropout", &dropout);
+    m.def("layer_norm_forward", &layer_norm_forward);
+    m.def("layer_norm_backward", &layer_norm_backward);
 }

@@ -1,6 +1,6 @@
 """Binding of libaet_ops.so (include/aet_ops.h): a linear layer with bias, activation, dropout and
-residual in its epilogue, group normalisation with an activation on channels-last maps, and dropout
-from the counter generator, each with its gradient.  Argument marshalling only, compiled
+residual in its epilogue, group normalisation with an activation on channels-last maps, layer
+normalisation of rows, and dropout from the counter generator, each with its gradient.  Argument marshalling only, compiled
 (csrc/ops/ops_torch.cpp); PyTorch supplies device memory and the stream, there is no CPU fallback.
 Names follow the C entry points, whose records are here as ctypes structures too.
 
@@ -31,7 +31,8 @@ _U64 = (1 << 64) - 1
 EXPORTS = [
     "aet_linear_workspace_bytes", "aet_linear_forward", "aet_linear_backward_workspace_bytes",
     "aet_linear_backward", "aet_group_norm_workspace_bytes", "aet_group_norm_forward",
-    "aet_group_norm_backward_workspace_bytes", "aet_group_norm_backward", "aet_dropout_forward",
+    "aet_group_norm_backward_workspace_bytes", "aet_group_norm_backward", "aet_layer_norm_forward",
+    "aet_layer_norm_backward_workspace_bytes", "aet_layer_norm_backward", "aet_dropout_forward",
     "aet_dropout_backward", "aet_ops_last_error",
 ]
 
@@ -71,6 +72,16 @@ class aet_group_norm_grad(C.Structure):
         "beta") + _maps("dx") + _mat("dgamma") + _mat("dbeta")
 
 
+class aet_layer_norm(C.Structure):
+    _fields_ = [(f, _i32) for f in ("dtype", "n", "rows", "cols")] + [("eps", C.c_float)] + _mat("x") + _mat("residual") + _mat(
+        "gamma") + _mat("beta") + _mat("y") + _mat("h") + [("mean", _vp), ("rstd", _vp)]
+
+
+class aet_layer_norm_grad(C.Structure):
+    _fields_ = [(f, _i32) for f in ("dtype", "n", "rows", "cols")] + _mat("dy") + _mat("x") + _mat("dh") + _mat("gamma") + [
+        ("mean", _vp), ("rstd", _vp)] + _mat("dx") + _mat("dgamma") + _mat("dbeta")
+
+
 class aet_dropout(C.Structure):
     _fields_ = [(f, _i32) for f in ("dtype", "n", "rows", "cols")] + _DROP + _mat("x") + _mat("residual") + _mat("y")
 
@@ -91,13 +102,14 @@ def load_library():
         warnings.warn(f"{os.path.basename(_build.OPS_LIB)} or its binding is older than its sources: build.build_ops() makes them anew",
                       RuntimeWarning, stacklevel=2)
     lib = C.CDLL(_build.OPS_LIB)
-    for name in ("aet_linear", "aet_linear_backward", "aet_group_norm", "aet_group_norm_backward"):
+    for name in ("aet_linear", "aet_linear_backward", "aet_group_norm", "aet_group_norm_backward", "aet_layer_norm_backward"):
         f = getattr(lib, name + "_workspace_bytes")
         f.restype, f.argtypes = C.c_size_t, [_vp]
-    for name in ("aet_linear_forward", "aet_linear_backward", "aet_group_norm_forward", "aet_group_norm_backward"):
+    for name in ("aet_linear_forward", "aet_linear_backward", "aet_group_norm_forward", "aet_group_norm_backward",
+                 "aet_layer_norm_backward"):
         f = getattr(lib, name)
         f.restype, f.argtypes = C.c_int, [_vp, _vp, C.c_size_t, _vp]
-    for name in ("aet_dropout_forward", "aet_dropout_backward"):
+    for name in ("aet_dropout_forward", "aet_dropout_backward", "aet_layer_norm_forward"):
         f = getattr(lib, name)
         f.restype, f.argtypes = C.c_int, [_vp, _vp]
     lib.aet_ops_last_error.restype = C.c_char_p
@@ -171,6 +183,26 @@ def aet_group_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
     where they are not wanted, or have no parameter).  A gamma or beta for all clients gets the sum over them.  out:
     places for the three, of any strides, or None; dx may be dy."""
     return (_EXT or _tensors()).group_norm_backward(dy, x, mean, rstd, gamma, beta, _act(act), need, out, *_on(x, stream))
+
+
+def aet_layer_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, *,
+                           residual: Optional[torch.Tensor] = None, eps: float = 1e-5, out=(None, None),
+                           stream: Optional[torch.cuda.Stream] = None):
+    """(y, h, mean, rstd): h = x + residual (None where there is no residual), its normalised rows * gamma + beta, and each
+    row's statistics (float32).  x: [n, rows, cols] or [rows, cols]; residual: as x; gamma, beta: [n, cols], or [cols] for all
+    clients.  out: places for y and h, or None; either may be x or the residual."""
+    return (_EXT or _tensors()).layer_norm_forward(x, gamma, beta, residual, eps, out, *_on(x, stream))
+
+
+def aet_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                            gamma: Optional[torch.Tensor] = None, *, dh: Optional[torch.Tensor] = None,
+                            need: Tuple[bool, bool] = (True, True), out=(None, None, None),
+                            stream: Optional[torch.cuda.Stream] = None):
+    """(dx, dgamma, dbeta) of aet_layer_norm_forward, x being what it normalised (its h where it had a residual), dh what
+    comes to h from behind, which is added to dx.  `need`: dx; dgamma and dbeta (made in gamma's shape: None without
+    gamma).  A gamma for all clients gets the sum over them.  out: places for the three, of any strides, or None; dx may be
+    dy or dh."""
+    return (_EXT or _tensors()).layer_norm_backward(dy, x, mean, rstd, gamma, dh, need, out, *_on(x, stream))
 
 
 def aet_dropout_forward(x: torch.Tensor, *, p: float, seed: int, first_row: int = 0,
