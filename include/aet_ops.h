@@ -2,7 +2,8 @@
  * aet_ops.h -- C ABI of the operators that residual blocks of clients' models are composed
  * from, on MI355X (gfx950): a linear layer with bias, activation, dropout and residual in its
  * epilogue, group normalisation with an activation on channels-last maps, layer normalisation
- * of rows, and dropout from the counter generator, each with its gradient.  All of them take many clients' models side
+ * of rows, and dropout from the counter generator, each with its gradient; values held in
+ * microscaled 4-bit floating point, and the linear layer of such values.  All of them take many clients' models side
  * by side in one call (`n`), each with parameters of its own or all with the same ones.
  *
  * Conventions
@@ -208,6 +209,70 @@ typedef struct {
 } aet_dropout;
 aet_status aet_dropout_forward(const aet_dropout *a, void *hip_stream);
 aet_status aet_dropout_backward(const aet_dropout *a, void *hip_stream);
+
+/* Microscaled 4-bit floating point, as messages and weights are held in.  The 32 neighbouring values
+ * of a row (the last ones of it may be fewer) that make up a block share an exponent x; a value is held
+ * as one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, times 2^x: the nearest to it, of two that are
+ * as near the one with the even code, and 6 for all beyond.  x = floor(log2(the largest magnitude)) - 2, at
+ * least -127, which is also that of a block of zeros.  A block with an infinity or NaN is NaN.
+ *   codes   a byte for two columns, the even one in its lower half: the sign's bit, and the place of the
+ *           magnitude in the list above.  ceil(cols / 2) bytes a row; a half that is left is 0, and not read.
+ *   scales  a byte for a block: x + 127, or 255 for NaN.  ceil(cols / 32) bytes a row.
+ * (The OCP Microscaling Formats specification's MXFP4.)  Their strides are in bytes, of any alignment; codes
+ * at multiples of 16 and scales at multiples of 4 bytes, rows too, are faster in products.  Any bytes are
+ * legal codes and scales. */
+
+/* x, n x rows x cols, to codes and scales. */
+typedef struct {
+    int32_t dtype;
+    int32_t n, rows, cols;
+    aet_in x;
+    aet_out codes, scales;
+} aet_mx4_values;
+aet_status aet_mx4_quantise(const aet_mx4_values *a, void *hip_stream);
+
+/* What codes and scales stand for: y, n x rows x cols.  (Exact, but for magnitudes of 2^128 and more, which the
+ * first call does not make.) */
+typedef struct {
+    int32_t dtype;
+    int32_t n, rows, cols;
+    aet_in codes, scales;
+    aet_out y;
+} aet_mx4_codes;
+aet_status aet_mx4_dequantise(const aet_mx4_codes *a, void *hip_stream);
+
+/* aet_linear_forward of held inputs and weights: y = residual + dropout(act(z)), z = x W^T + bias.
+ *   x, x_scales   n x rows x in, as codes and scales
+ *   w, w_scales   n x out x in; client = 0 (of both): one W for all
+ * dtype is that of bias, residual, y and pre; all else as in aet_linear.  Products are exact and sums fp32
+ * (a block's products that are below 2^-126 may be 0). */
+typedef struct {
+    int32_t dtype, act;
+    int32_t n, rows, in, out;
+    double p;
+    uint64_t seed;
+    int64_t first_row;
+    aet_in x, x_scales, w, w_scales, bias, residual;
+    aet_out y, pre;
+} aet_mx4_linear;
+size_t aet_mx4_linear_workspace_bytes(const aet_mx4_linear *a);
+aet_status aet_mx4_linear_forward(const aet_mx4_linear *a, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Its gradient with regard to what the codes stand for, from the codes: dx = dz W, dw = dz^T x, db = sum of dz over
+ * rows.  (That of the values that were quantised is the same where rounding is taken to have a slope of 1.)  dtype is that
+ * of dy, pre, dx, dw and db; all else as in aet_linear_grad, where x, if dw is wanted, and w, if dx is, stand for rows
+ * that lie one after another. */
+typedef struct {
+    int32_t dtype, act;
+    int32_t n, rows, in, out;
+    double p;
+    uint64_t seed;
+    int64_t first_row;
+    aet_in dy, x, x_scales, w, w_scales, pre;
+    aet_out dx, dw, db;
+} aet_mx4_linear_grad;
+size_t aet_mx4_linear_backward_workspace_bytes(const aet_mx4_linear_grad *a);
+aet_status aet_mx4_linear_backward(const aet_mx4_linear_grad *a, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Text of the calling thread's last failed call of this header, "" if there was none. */
 const char *aet_ops_last_error(void);

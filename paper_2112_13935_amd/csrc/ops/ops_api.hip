@@ -41,7 +41,8 @@ constexpr int64_t kMost = INT64_C(1) << 46;   // elements between the first and 
 static bool in_reach(int64_t count, int64_t stride) {
     return stride >= 0 && (count <= 1 || stride <= kMost / (count - 1));
 }
-static int64_t esize(int dtype) { return dtype == AET_F32 ? 4 : 2; }
+constexpr int kByte = -1;   // a type of our own: codes and scales
+static int64_t esize(int dtype) { return dtype == AET_F32 ? 4 : dtype == AET_BF16 ? 2 : 1; }
 
 static const char *bad_ptr(const void *p, int dtype) {
     if (!p) return "is NULL";
@@ -290,6 +291,91 @@ static aet_status check(const aet_layer_norm_grad *a) {
     return AET_OK;
 }
 
+// ---- microscaled 4-bit values ------------------------------------------------------------
+
+static const char *bad_held(const aet_in &t, int64_t n, int64_t rows) {
+    const int64_t count[2] = {n, rows}, st[2] = {t.client, t.row};
+    return bad_in(t.p, kByte, 2, count, st);
+}
+static aet_status check(const aet_mx4_values *a) {
+    const char *why;
+    if (!a) return fail(AET_EINVAL, "the record is NULL");
+    if (bad_common(a->dtype, AET_ACT_NONE, &why)) return fail(AET_EINVAL, "%s", why);
+    if (bad_sizes({a->n, a->rows, a->cols}, &why)) return fail(AET_EINVAL, "%s", why);
+    if (!a->n || !a->rows || !a->cols) return AET_OK;
+    const int64_t nr[2] = {a->n, a->rows}, xs[2] = {a->x.client, a->x.row}, cs[2] = {a->codes.client, a->codes.row},
+                  ss[2] = {a->scales.client, a->scales.row};
+    AET_CHECK("x", bad_in(a->x.p, a->dtype, 2, nr, xs));
+    AET_CHECK("codes", bad_out(a->codes.p, kByte, 2, nr, cs, ceil_div(a->cols, 2)));
+    AET_CHECK("scales", bad_out(a->scales.p, kByte, 2, nr, ss, ceil_div(a->cols, 32)));
+    return AET_OK;
+}
+static aet_status check(const aet_mx4_codes *a) {
+    const char *why;
+    if (!a) return fail(AET_EINVAL, "the record is NULL");
+    if (bad_common(a->dtype, AET_ACT_NONE, &why)) return fail(AET_EINVAL, "%s", why);
+    if (bad_sizes({a->n, a->rows, a->cols}, &why)) return fail(AET_EINVAL, "%s", why);
+    if (!a->n || !a->rows || !a->cols) return AET_OK;
+    const int64_t nr[2] = {a->n, a->rows}, ys[2] = {a->y.client, a->y.row};
+    AET_CHECK("codes", bad_held(a->codes, a->n, a->rows));
+    AET_CHECK("scales", bad_held(a->scales, a->n, a->rows));
+    AET_CHECK("y", bad_out(a->y.p, a->dtype, 2, nr, ys, a->cols));
+    return AET_OK;
+}
+
+static aet_status check(const aet_mx4_linear *a) {
+    const char *why;
+    if (!a) return fail(AET_EINVAL, "the record is NULL");
+    if (bad_sizes({a->n, a->rows, a->in, a->out}, &why)) return fail(AET_EINVAL, "%s", why);
+    if (a->n && a->rows && a->out && a->in) {
+        AET_CHECK("x", bad_held(a->x, a->n, a->rows));
+        AET_CHECK("x_scales", bad_held(a->x_scales, a->n, a->rows));
+        AET_CHECK("w", bad_held(a->w, a->n, a->out));
+        AET_CHECK("w_scales", bad_held(a->w_scales, a->n, a->out));
+        if (a->n > 1 && !a->w.client != !a->w_scales.client) return fail(AET_EINVAL, "w and w_scales: either both or none are the same for all clients (client = 0)");
+    }
+    // the rest as the linear layer has it
+    aet_linear b = {a->dtype, a->act, a->n, a->rows, a->in, a->out, a->p, a->seed, a->first_row};
+    b.x = {(void *)256, (int64_t)a->rows * a->in, a->in};
+    b.w = {(void *)256, (int64_t)a->out * a->in, a->in};
+    b.bias = a->bias;
+    b.residual = a->residual;
+    b.y = a->y;
+    b.pre = a->pre;
+    return check(&b);
+}
+static void fold(aet_mx4_linear &a) {
+    if (a.n <= 1) return;
+    auto flat = [&](const void *p, int64_t client, int64_t row) { return !p || client == a.rows * row; };
+    if (a.w.client || a.w_scales.client || (a.bias.p && a.bias.client) || (int64_t)a.n * a.rows > kMostSize) return;
+    if (!flat(a.x.p, a.x.client, a.x.row) || !flat(a.x_scales.p, a.x_scales.client, a.x_scales.row) ||
+        !flat(a.residual.p, a.residual.client, a.residual.row) || !flat(a.y.p, a.y.client, a.y.row) || !flat(a.pre.p, a.pre.client, a.pre.row))
+        return;
+    a.rows *= a.n;
+    a.n = 1;
+}
+
+static aet_status check(const aet_mx4_linear_grad *a, bool *shared) {
+    const char *why;
+    if (!a) return fail(AET_EINVAL, "the record is NULL");
+    if (bad_sizes({a->n, a->rows, a->in, a->out}, &why)) return fail(AET_EINVAL, "%s", why);
+    if (a->n && a->rows && a->out && a->in) {
+        if (a->dw.p) {
+            AET_CHECK("x", bad_held(a->x, a->n, a->rows));
+            AET_CHECK("x_scales", bad_held(a->x_scales, a->n, a->rows));
+        }
+        if (a->dx.p) {
+            AET_CHECK("w", bad_held(a->w, a->n, a->out));
+            AET_CHECK("w_scales", bad_held(a->w_scales, a->n, a->out));
+            if (a->n > 1 && !a->w.client != !a->w_scales.client)
+                return fail(AET_EINVAL, "w and w_scales: either both or none are the same for all clients (client = 0)");
+        }
+    }
+    size_t used;
+    const aet_linear_grad b = mx4_plain_gradient(*a, (void *)256, &used);
+    return check(&b, shared);
+}
+
 // ---- dropout -----------------------------------------------------------------------------
 
 static aet_status run_dropout(const aet_dropout *a, bool residual, void *hip_stream) {
@@ -400,6 +486,57 @@ aet_status aet_layer_norm_backward(const aet_layer_norm_grad *a, void *workspace
     if (bad_workspace(workspace, workspace_bytes, need))
         return fail(AET_ENOMEM, "the workspace needs %zu bytes, 256-byte aligned; got %zu", need, workspace_bytes);
     return done(launch_layer_norm_backward(*a, workspace, (hipStream_t)hip_stream));
+}
+
+aet_status aet_mx4_quantise(const aet_mx4_values *a, void *hip_stream) {
+    if (const aet_status st = check(a)) return st;
+    if (!a->n || !a->rows || !a->cols) return AET_OK;
+    return done(launch_mx4_quantise(*a, (hipStream_t)hip_stream));
+}
+aet_status aet_mx4_dequantise(const aet_mx4_codes *a, void *hip_stream) {
+    if (const aet_status st = check(a)) return st;
+    if (!a->n || !a->rows || !a->cols) return AET_OK;
+    return done(launch_mx4_dequantise(*a, (hipStream_t)hip_stream));
+}
+
+size_t aet_mx4_linear_workspace_bytes(const aet_mx4_linear *a) {
+    if (check(a) != AET_OK) return 0;
+    aet_mx4_linear b = *a;
+    fold(b);
+    return b.n && b.rows && b.out ? mx4_linear_forward_workspace(b) : 0;
+}
+aet_status aet_mx4_linear_forward(const aet_mx4_linear *a, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (const aet_status st = check(a)) return st;
+    aet_mx4_linear b = *a;
+    fold(b);
+    if (!b.n || !b.rows || !b.out) return AET_OK;
+    const size_t need = mx4_linear_forward_workspace(b);
+    if (bad_workspace(workspace, workspace_bytes, need))
+        return fail(AET_ENOMEM, "the workspace needs %zu bytes, 256-byte aligned; got %zu", need, workspace_bytes);
+    return done(launch_mx4_linear_forward(b, workspace, (hipStream_t)hip_stream));
+}
+
+size_t aet_mx4_linear_backward_workspace_bytes(const aet_mx4_linear_grad *a) {
+    bool shared;
+    if (check(a, &shared) != AET_OK || !a->n) return 0;
+    size_t used;
+    aet_linear_grad b = mx4_plain_gradient(*a, nullptr, &used);
+    fold(b, shared);
+    return used + linear_backward_workspace(b);
+}
+aet_status aet_mx4_linear_backward(const aet_mx4_linear_grad *a, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    bool shared;
+    if (const aet_status st = check(a, &shared)) return st;
+    if (!a->n) return AET_OK;
+    size_t used;
+    const aet_linear_grad plain = mx4_plain_gradient(*a, workspace, &used);
+    aet_linear_grad b = plain;
+    fold(b, shared);
+    const size_t need = used + linear_backward_workspace(b);
+    if (bad_workspace(workspace, workspace_bytes, need))
+        return fail(AET_ENOMEM, "the workspace needs %zu bytes, 256-byte aligned; got %zu", need, workspace_bytes);
+    const hipError_t e = launch_mx4_expand(*a, plain, (hipStream_t)hip_stream);
+    return done(e != hipSuccess ? e : launch_linear_backward(b, (char *)workspace + used, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

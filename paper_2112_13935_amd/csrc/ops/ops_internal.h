@@ -33,4 +33,13 @@ hipError_t launch_layer_norm_forward(const aet_layer_norm &a, hipStream_t s);
 size_t layer_norm_backward_workspace(const aet_layer_norm_grad &a);
 hipError_t launch_layer_norm_backward(const aet_layer_norm_grad &a, void *workspace, hipStream_t s);
 
+hipError_t launch_mx4_quantise(const aet_mx4_values &a, hipStream_t s);
+hipError_t launch_mx4_dequantise(const aet_mx4_codes &a, hipStream_t s);
+size_t mx4_linear_forward_workspace(const aet_mx4_linear &a);
+hipError_t launch_mx4_linear_forward(const aet_mx4_linear &a, void *workspace, hipStream_t s);
+// The gradient of the layer with the held values in `workspace` as they stand for (used: bytes of it), and the launches that
+// put them there.
+aet_linear_grad mx4_plain_gradient(const aet_mx4_linear_grad &a, void *workspace, size_t *used);
+hipError_t launch_mx4_expand(const aet_mx4_linear_grad &a, const aet_linear_grad &plain, hipStream_t s);
+
 }  // namespace aet_ops

@@ -1,0 +1,242 @@
+// Microscaled 4-bit floating point: values to codes and scales, and back.
+//
+// Bound by memory.  Four lanes have a block of 32 values, 8 each: their largest magnitude's exponent by two exchanges
+// between neighbours, then the hardware's conversions, which divide by the scale (given by its exponent alone; 0 is 2^-127,
+// 255 NaN), round to the nearest of the 16 values, ties to the even code, and end at 6.
+#include "ops_internal.h"
+
+#include <type_traits>
+
+namespace aet_ops {
+
+typedef bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+
+constexpr int kRows = 4;   // of a thread, all on their way at once
+
+struct Mx4Shape {
+    int pieces, wide;         // pieces of 8 columns in a row, whole blocks; threads side by side (a power of two, 4 and more)
+    int64_t across, down;     // workgroups: of a row of pieces, of a client
+};
+
+struct Mx4Place {
+    int64_t client, row0;
+    int col, high;
+};
+__device__ __forceinline__ bool place_of(const Mx4Shape &s, Mx4Place &p) {
+    const int64_t per = s.across * s.down, b = blockIdx.x % per;
+    p.client = blockIdx.x / per;
+    const int piece = (int)(b % s.across) * s.wide + (threadIdx.x & (s.wide - 1));
+    p.high = 256 / s.wide;
+    p.row0 = b / s.across * (p.high * kRows) + threadIdx.x / s.wide;
+    p.col = piece * 8;
+    return piece < s.pieces;   // (the same for the four lanes of a block)
+}
+
+// 8 values to codes; the block's scale
+template <typename T>
+__device__ __forceinline__ uint32_t quantise8(const wide<T, 8> &v, uint32_t &scale) {
+    uint32_t top = 0;   // the largest magnitude's bits: NaN is above infinity, which is above all others
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t m = __builtin_bit_cast(uint32_t, (float)v[e]) & 0x7fffffffu;
+        top = m > top ? m : top;
+    }
+#pragma unroll
+    for (int off = 1; off < 4; off *= 2) {
+        const uint32_t m = __shfl_xor(top, off, 64);
+        top = m > top ? m : top;
+    }
+    // floor(log2(top)) - 2 + 127 where that is 0 or more; subnormal values and 0 have 0 too
+    const uint32_t x = top >> 23;
+    scale = x == 255 ? 255 : x > 2 ? x - 2 : 0;
+    const float by = __builtin_bit_cast(float, scale << 23);
+    uint32_t code = 0;
+    if constexpr (sizeof(T) == 2) {
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, bf2{v[0], v[1]}, by, 0);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, bf2{v[2], v[3]}, by, 1);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, bf2{v[4], v[5]}, by, 2);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, bf2{v[6], v[7]}, by, 3);
+    } else {
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[0], v[1], by, 0);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[2], v[3], by, 1);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[4], v[5], by, 2);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[6], v[7], by, 3);
+    }
+    return scale == 255 ? 0 : code;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_mx4_quantise(aet_mx4_values a, Mx4Shape s) {
+    Mx4Place p;
+    if (!place_of(s, p)) return;
+    const T *x = (const T *)a.x.p + p.client * a.x.client + p.col;
+    uint8_t *codes = (uint8_t *)a.codes.p + p.client * a.codes.client + p.col / 2;
+    uint8_t *scales = (uint8_t *)a.scales.p + p.client * a.scales.client + p.col / 32;
+    const int count = a.cols - p.col, bytes = (count + 1) / 2;
+    wide<T, 8> v[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t row = p.row0 + i * p.high;
+        if (row < a.rows) v[i] = load_raw<T, 8>(x + row * a.x.row, count);
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t row = p.row0 + i * p.high;
+        if (row >= a.rows) continue;
+        uint32_t scale;
+        const wide<uint8_t, 4> code = __builtin_bit_cast(uint8_t __attribute__((ext_vector_type(4))), quantise8<T>(v[i], scale));
+        uint8_t *const to = codes + row * a.codes.row;
+        if (bytes >= 4) *(wide<uint8_t, 4> *)to = code;
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < bytes) to[e] = code[e];
+        if (p.col % 32 == 0) scales[row * a.scales.row] = (uint8_t)scale;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ wide<T, 8> expand8(uint32_t code, uint32_t scale) {
+    const float by = __builtin_bit_cast(float, scale << 23);
+    wide<T, 8> v;
+    if constexpr (sizeof(T) == 2) {
+        const bf2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, by, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, by, 1),
+                  c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, by, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, by, 3);
+        v = wide<T, 8>{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    } else {
+        const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, by, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, by, 1),
+                 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, by, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, by, 3);
+        v = wide<T, 8>{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+    return v;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_mx4_dequantise(aet_mx4_codes a, Mx4Shape s) {
+    Mx4Place p;
+    if (!place_of(s, p) || p.col >= a.cols) return;
+    const uint8_t *codes = (const uint8_t *)a.codes.p + p.client * a.codes.client + p.col / 2;
+    const uint8_t *scales = (const uint8_t *)a.scales.p + p.client * a.scales.client + p.col / 32;
+    T *y = (T *)a.y.p + p.client * a.y.client + p.col;
+    const int count = a.cols - p.col, bytes = (count + 1) / 2;
+    uint32_t code[kRows], scale[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t row = p.row0 + i * p.high;
+        if (row >= a.rows) continue;
+        const uint8_t *from = codes + row * a.codes.row;
+        if (bytes >= 4) {
+            code[i] = __builtin_bit_cast(uint32_t, (uint8_t __attribute__((ext_vector_type(4))))(*(const wide<uint8_t, 4> *)from));
+        } else {
+            code[i] = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) code[i] |= (uint32_t)from[e < bytes ? e : bytes - 1] << (8 * e);
+        }
+        scale[i] = scales[row * a.scales.row];
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t row = p.row0 + i * p.high;
+        if (row >= a.rows) continue;
+        const wide<T, 8> v = expand8<T>(code[i], scale[i]);
+        T *const to = y + row * a.y.row;
+        if (count >= 8) *(wide<T, 8> *)to = v;
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < count) to[e] = v[e];
+    }
+}
+
+static bool shape_of(int64_t n, int64_t rows, int64_t cols, Mx4Shape *s, int64_t *blocks) {
+    *s = {(int)ceil_div(cols, 32) * 4, 4, 0, 0};
+    while (s->wide < s->pieces && s->wide < 256) s->wide *= 2;
+    s->across = ceil_div(s->pieces, s->wide);
+    s->down = ceil_div(rows, 256 / s->wide * kRows);
+    *blocks = n * s->across * s->down;
+    return *blocks <= INT32_MAX;
+}
+hipError_t launch_mx4_quantise(const aet_mx4_values &a, hipStream_t s) {
+    Mx4Shape d;
+    int64_t blocks;
+    if (!shape_of(a.n, a.rows, a.cols, &d, &blocks)) return hipErrorInvalidConfiguration;
+    if (a.dtype == AET_F32) k_mx4_quantise<float><<<(int)blocks, 256, 0, s>>>(a, d);
+    else k_mx4_quantise<bf16><<<(int)blocks, 256, 0, s>>>(a, d);
+    return hipGetLastError();
+}
+hipError_t launch_mx4_dequantise(const aet_mx4_codes &a, hipStream_t s) {
+    Mx4Shape d;
+    int64_t blocks;
+    if (!shape_of(a.n, a.rows, a.cols, &d, &blocks)) return hipErrorInvalidConfiguration;
+    if (a.dtype == AET_F32) k_mx4_dequantise<float><<<(int)blocks, 256, 0, s>>>(a, d);
+    else k_mx4_dequantise<bf16><<<(int)blocks, 256, 0, s>>>(a, d);
+    return hipGetLastError();
+}
+
+// ---- the linear layer --------------------------------------------------------------------
+
+// The held values as they stand for: every one of them is a value of bf16 (2 bits of it, down to 2^-128), rows a multiple
+// of 16 bytes apart.
+static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+static int64_t line_of(int dtype, int64_t cols) { return ceil_div(cols, dtype == AET_F32 ? 4 : 8) * (dtype == AET_F32 ? 4 : 8); }
+static size_t expanded_bytes(int dtype, int64_t n, int64_t rows, int64_t cols) {
+    return up256((size_t)n * rows * line_of(dtype, cols) * (dtype == AET_F32 ? 4 : 2));
+}
+static hipError_t expand(int dtype, int64_t n, int64_t rows, int64_t cols, const aet_in &codes, const aet_in &scales, void *to, aet_in *out, hipStream_t s) {
+    const int64_t line = line_of(dtype, cols);
+    *out = {to, n > 1 ? rows * line : 0, line};
+    if (!n || !rows || !cols) return hipSuccess;
+    return launch_mx4_dequantise({dtype, (int32_t)n, (int32_t)rows, (int32_t)cols, codes, scales, {to, rows * line, line}}, s);
+}
+
+static aet_linear plain_of(const aet_mx4_linear &a, char *workspace, size_t *used) {
+    aet_linear b = {a.dtype, a.act, a.n, a.rows, a.in, a.out, a.p, a.seed, a.first_row};
+    b.bias = a.bias;
+    b.residual = a.residual;
+    b.y = a.y;
+    b.pre = a.pre;
+    const int64_t line = line_of(a.dtype, a.in), held = a.w.client ? a.n : 1;
+    const size_t x = expanded_bytes(a.dtype, a.n, a.rows, a.in);
+    b.x = {workspace, a.rows * line, line};
+    b.w = {workspace + x, held > 1 ? a.out * line : 0, line};
+    *used = x + expanded_bytes(a.dtype, held, a.out, a.in);
+    return b;
+}
+size_t mx4_linear_forward_workspace(const aet_mx4_linear &a) {
+    size_t used;
+    const aet_linear b = plain_of(a, nullptr, &used);
+    return used + linear_forward_workspace(b);
+}
+hipError_t launch_mx4_linear_forward(const aet_mx4_linear &a, void *workspace, hipStream_t s) {
+    size_t used;
+    aet_linear b = plain_of(a, (char *)workspace, &used);
+    aet_in out;
+    hipError_t e = expand(a.dtype, a.n, a.rows, a.in, a.x, a.x_scales, (void *)b.x.p, &out, s);
+    if (e == hipSuccess) e = expand(a.dtype, a.w.client ? a.n : 1, a.out, a.in, a.w, a.w_scales, (void *)b.w.p, &out, s);
+    return e == hipSuccess ? launch_linear_forward(b, (char *)workspace + used, s) : e;
+}
+
+aet_linear_grad mx4_plain_gradient(const aet_mx4_linear_grad &a, void *workspace, size_t *used) {
+    aet_linear_grad b = {a.dtype, a.act, a.n, a.rows, a.in, a.out, a.p, a.seed, a.first_row};
+    b.dy = a.dy;
+    b.pre = a.pre;
+    b.dx = a.dx;
+    b.dw = a.dw;
+    b.db = a.db;
+    const int64_t line = line_of(a.dtype, a.in), held = a.w.client ? a.n : 1;
+    const size_t x = a.dw.p ? expanded_bytes(a.dtype, a.n, a.rows, a.in) : 0;
+    b.x = {workspace, a.rows * line, line};
+    b.w = {(char *)workspace + x, held > 1 ? a.out * line : 0, line};
+    *used = x + (a.dx.p ? expanded_bytes(a.dtype, held, a.out, a.in) : 0);
+    return b;
+}
+hipError_t launch_mx4_expand(const aet_mx4_linear_grad &a, const aet_linear_grad &plain, hipStream_t s) {
+    aet_in out;
+    hipError_t e = hipSuccess;
+    if (a.dw.p) e = expand(a.dtype, a.n, a.rows, a.in, a.x, a.x_scales, (void *)plain.x.p, &out, s);
+    if (e == hipSuccess && a.dx.p) e = expand(a.dtype, a.w.client ? a.n : 1, a.out, a.in, a.w, a.w_scales, (void *)plain.w.p, &out, s);
+    return e;
+}
+
+}  // namespace aet_ops

@@ -14,13 +14,13 @@ namespace {
 
 [[noreturn]] void value_error(const std::string &what) { throw py::value_error(what); }
 
-std::string text(const Tensor &t) {
-    return std::string(c10::toString(t.scalar_type())) + " on " + t.device().str();
-}
+std::string text(at::ScalarType type, const Tensor &t) { return std::string(c10::toString(type)) + " on " + t.device().str(); }
+std::string text(const Tensor &t) { return text(t.scalar_type(), t); }
 
 // A call's type, device and stream, by its first tensor.
 struct Call {
     const Tensor &x;
+    at::ScalarType type;
     int dtype;
     void *handle;
     c10::DeviceGuard guard;
@@ -31,16 +31,18 @@ struct Call {
     int count = 0;
 
     Call(const Tensor &first, int64_t handle_, const std::optional<std::tuple<int64_t, int64_t, int64_t>> &stream)
-        : x(first), dtype(AET_F32), handle((void *)handle_), guard(checked(first)) {
-        if (first.scalar_type() == at::kBFloat16) dtype = AET_BF16;
+        : Call(first, first.scalar_type(), handle_, stream) {}
+    // The call's type is another than its first tensor's.
+    Call(const Tensor &first, at::ScalarType type_, int64_t handle_, const std::optional<std::tuple<int64_t, int64_t, int64_t>> &stream)
+        : x(first), type(type_), dtype(type_ == at::kBFloat16 ? AET_BF16 : AET_F32), handle((void *)handle_), guard(checked(first, type_)) {
         if (!stream) return;
         if (std::get<1>(*stream) != x.device().index())
             value_error("the stream is one of device " + std::to_string(std::get<1>(*stream)) + ", the tensors are " + text(x));
         other.emplace(c10::Stream::unpack3(std::get<0>(*stream), (c10::DeviceIndex)std::get<1>(*stream), (c10::DeviceType)std::get<2>(*stream)));
     }
-    static c10::Device checked(const Tensor &t) {
-        if ((t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) || !t.is_cuda())
-            value_error("float32 or bfloat16 on a GPU is wanted, got " + text(t));
+    static c10::Device checked(const Tensor &t, at::ScalarType type) {
+        if ((type != at::kFloat && type != at::kBFloat16) || !t.is_cuda())
+            value_error("float32 or bfloat16 on a GPU is wanted, got " + text(type, t));
         return t.device();
     }
     void *use(const Tensor &t) {
@@ -54,10 +56,11 @@ struct Call {
                                             "detached tensors, and the _backward calls for gradients");
     }
     // The tensor's type, device, shape and last stride are as they have to be.
-    void agree(const char *name, const Tensor &t, at::IntArrayRef shape) {
+    void agree(const char *name, const Tensor &t, at::IntArrayRef shape) { agree(name, t, shape, type); }
+    void agree(const char *name, const Tensor &t, at::IntArrayRef shape, at::ScalarType want) {
         no_graph(name, t);
-        if (t.scalar_type() != x.scalar_type() || t.device() != x.device())
-            value_error(std::string(name) + " is " + text(t) + ", the others are " + text(x));
+        if (t.scalar_type() != want || t.device() != x.device())
+            value_error(std::string(name) + " is " + text(t) + ", wanted is " + text(want, x));
         if (t.sizes() != shape) {
             std::ostringstream o;
             o << name << " has shape " << t.sizes() << ", expected " << shape;
@@ -68,9 +71,11 @@ struct Call {
     }
     // A matrix per client (three axes), or one (two); `shared`: two axes are one for all clients
     template <class M>
-    void mat(M &to, const char *name, const OptTensor &t, at::IntArrayRef shape, bool shared = false) {
+    void mat(M &to, const char *name, const OptTensor &t, at::IntArrayRef shape, bool shared = false) { mat(to, name, t, shape, shared, type); }
+    template <class M>
+    void mat(M &to, const char *name, const OptTensor &t, at::IntArrayRef shape, bool shared, at::ScalarType want) {
         if (!t) return;
-        agree(name, *t, shape);
+        agree(name, *t, shape, want);
         const auto st = t->strides();
         to.p = use(*t);
         to.client = st.size() == 3 ? st[0] : shared ? 0 : shape[0] * st[0];
@@ -102,7 +107,7 @@ struct Call {
     }
     OptTensor out(const OptTensor &given, bool wanted, at::IntArrayRef shape) {
         if (given) places[count++] = &*given;
-        return given ? given : wanted ? OptTensor(made(shape, x.scalar_type())) : std::nullopt;
+        return given ? given : wanted ? OptTensor(made(shape, type)) : std::nullopt;
     }
     template <class A>
     void run(aet_status (*fn)(const A *, void *, size_t, void *), size_t (*bytes)(const A *), const A &a) {
@@ -312,6 +317,112 @@ Three layer_norm_backward(const Tensor &dy, const Tensor &x, const Tensor &mean,
     return made;
 }
 
+// Codes and scales of a tensor of this shape (its last axis: cols)
+struct HeldShape {
+    std::vector<int64_t> codes, scales;
+    HeldShape(at::IntArrayRef shape) : codes(shape.vec()), scales(shape.vec()) {
+        codes.back() = (shape.back() + 1) / 2;
+        scales.back() = (shape.back() + 31) / 32;
+    }
+};
+
+std::tuple<Tensor, Tensor> mx4_quantise(const Tensor &x, const std::tuple<OptTensor, OptTensor> &out, int64_t handle, const Stream &stream) {
+    Call c(x, handle, stream);
+    const Axes s(x);
+    aet_mx4_values a = {c.dtype, s.n, s.rows, s.cols};
+    const HeldShape held(x.sizes());
+    c.mat(a.x, "x", x, x.sizes());
+    const auto place = [&](const OptTensor &given, at::IntArrayRef shape) {
+        if (given) c.places[c.count++] = &*given;
+        return given ? *given : c.made(shape, at::kByte);
+    };
+    const Tensor codes = place(std::get<0>(out), held.codes), scales = place(std::get<1>(out), held.scales);
+    c.mat(a.codes, "codes", codes, held.codes, false, at::kByte);
+    c.mat(a.scales, "scales", scales, held.scales, false, at::kByte);
+    c.done(aet_mx4_quantise(&a, c.handle));
+    return {codes, scales};
+}
+
+// The number of columns that codes stand for
+int64_t held_cols(const Tensor &codes, std::optional<int64_t> cols) {
+    if (codes.dim() != 2 && codes.dim() != 3) value_error("codes: a tensor of 2 or 3 axes is wanted");
+    const int64_t all = cols ? *cols : 2 * codes.size(-1);
+    if (all < 0 || (all + 1) / 2 != codes.size(-1))
+        value_error(std::to_string(codes.size(-1)) + " bytes of codes do not stand for " + std::to_string(all) + " columns");
+    return all;
+}
+std::vector<int64_t> held_shape(const Tensor &codes, int64_t cols) {
+    std::vector<int64_t> shape = codes.sizes().vec();
+    shape.back() = cols;
+    return shape;
+}
+
+Tensor mx4_dequantise(const Tensor &codes, const Tensor &scales, std::optional<int64_t> cols, bool bf16, const OptTensor &out, int64_t handle, const Stream &stream) {
+    const std::vector<int64_t> shape = held_shape(codes, held_cols(codes, cols));
+    const HeldShape held(shape);
+    Call c(codes, bf16 ? at::kBFloat16 : at::kFloat, handle, stream);
+    const Axes s(codes);
+    aet_mx4_codes a = {c.dtype, s.n, s.rows, size32(shape.back())};
+    c.mat(a.codes, "codes", codes, held.codes, false, at::kByte);
+    c.mat(a.scales, "scales", scales, held.scales, false, at::kByte);
+    const OptTensor y = c.out(out, true, shape);
+    c.mat(a.y, "out", y, shape);
+    c.done(aet_mx4_dequantise(&a, c.handle));
+    return *y;
+}
+
+std::tuple<Tensor, OptTensor> mx4_linear_forward(const Tensor &x, const Tensor &x_scales, const Tensor &w, const Tensor &w_scales, const OptTensor &bias,
+                                                 std::optional<int64_t> cols, const OptTensor &residual, int act, double p, uint64_t seed, int64_t first_row,
+                                                 bool keep_pre, bool bf16, const OptTensor &out, int64_t handle, const Stream &stream) {
+    const std::vector<int64_t> xs = held_shape(x, held_cols(x, cols));
+    Call c(x, bf16 ? at::kBFloat16 : at::kFloat, handle, stream);
+    const Axes s(x);
+    if (w.dim() != 2 && w.dim() != 3) value_error("w: [n, out, bytes] or [out, bytes] is wanted");
+    const int64_t outs = w.size(-2);
+    aet_mx4_linear a = {c.dtype, act, s.n, s.rows, size32(xs.back()), size32(outs), p, seed, first_row};
+    const std::array<int64_t, 3> ysh = {s.n, s.rows, outs}, wsh = {s.n, outs, xs.back()};
+    const at::IntArrayRef shape = at::IntArrayRef(ysh).slice(3 - x.dim());
+    const HeldShape hx(xs), hw(at::IntArrayRef(wsh).slice(3 - w.dim()));
+    c.mat(a.x, "x", x, hx.codes, false, at::kByte);
+    c.mat(a.x_scales, "x_scales", x_scales, hx.scales, false, at::kByte);
+    c.mat(a.w, "w", w, hw.codes, true, at::kByte);
+    c.mat(a.w_scales, "w_scales", w_scales, hw.scales, true, at::kByte);
+    c.vec(a.bias, "bias", bias, s.n, outs);
+    c.mat(a.residual, "residual", residual, shape);
+    const OptTensor y = c.out(out, true, shape), pre = c.out(std::nullopt, keep_pre, shape);
+    c.mat(a.y, "out", y, shape);
+    c.mat(a.pre, "pre", pre, shape);
+    c.run(aet_mx4_linear_forward, aet_mx4_linear_workspace_bytes, a);
+    return {*y, pre};
+}
+
+Three mx4_linear_backward(const Tensor &dy, const Tensor &x, const Tensor &x_scales, const Tensor &w, const Tensor &w_scales, const OptTensor &pre,
+                          std::optional<int64_t> cols, int act, double p, uint64_t seed, int64_t first_row, std::array<bool, 3> need, const Three &out,
+                          int64_t handle, const Stream &stream) {
+    const std::vector<int64_t> xsh = held_shape(x, held_cols(x, cols));
+    Call c(dy, handle, stream);
+    const Axes s(x);
+    if (w.dim() != 2 && w.dim() != 3) value_error("w: [n, out, bytes] or [out, bytes] is wanted");
+    if (act != AET_ACT_NONE && !pre) value_error("pre, as the forward call gave it, is wanted where there is an activation");
+    const int64_t outs = w.size(-2);
+    aet_mx4_linear_grad a = {c.dtype, act, s.n, s.rows, size32(xsh.back()), size32(outs), p, seed, first_row};
+    const std::array<int64_t, 3> ysh = {s.n, s.rows, outs}, wsh = {s.n, outs, xsh.back()};
+    const at::IntArrayRef xs = xsh, ys = at::IntArrayRef(ysh).slice(3 - x.dim()), ws = at::IntArrayRef(wsh).slice(3 - w.dim());
+    const HeldShape hx(xs), hw(ws);
+    c.mat(a.dy, "dy", dy, ys);
+    c.mat(a.x, "x", x, hx.codes, false, at::kByte);
+    c.mat(a.x_scales, "x_scales", x_scales, hx.scales, false, at::kByte);
+    c.mat(a.w, "w", w, hw.codes, true, at::kByte);
+    c.mat(a.w_scales, "w_scales", w_scales, hw.scales, true, at::kByte);
+    c.mat(a.pre, "pre", pre, ys);
+    const Three made = {c.out(std::get<0>(out), need[0], xs), c.out(std::get<1>(out), need[1], ws), c.out(std::get<2>(out), need[2], ws.slice(0, ws.size() - 1))};
+    c.mat(a.dx, "dx", std::get<0>(made), xs);
+    c.mat(a.dw, "dw", std::get<1>(made), ws, true);
+    c.vec(a.db, "db", std::get<2>(made), s.n, outs);
+    c.run(aet_mx4_linear_backward, aet_mx4_linear_backward_workspace_bytes, a);
+    return made;
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_ops_torch, m) {
@@ -322,4 +433,8 @@ PYBIND11_MODULE(_ops_torch, m) {
     m.def("dropout", &dropout);
     m.def("layer_norm_forward", &layer_norm_forward);
     m.def("layer_norm_backward", &layer_norm_backward);
+    m.def("mx4_quantise", &mx4_quantise);
+    m.def("mx4_dequantise", &mx4_dequantise);
+    m.def("mx4_linear_forward", &mx4_linear_forward);
+    m.def("mx4_linear_backward", &mx4_linear_backward);
 }

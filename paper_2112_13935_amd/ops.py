@@ -1,6 +1,7 @@
 """Binding of libaet_ops.so (include/aet_ops.h): a linear layer with bias, activation, dropout and
 residual in its epilogue, group normalisation with an activation on channels-last maps, layer
-normalisation of rows, and dropout from the counter generator, each with its gradient.  Argument marshalling only, compiled
+normalisation of rows, and dropout from the counter generator, each with its gradient; values held in
+microscaled 4-bit floating point, and the linear layer of such values.  Argument marshalling only, compiled
 (csrc/ops/ops_torch.cpp); PyTorch supplies device memory and the stream, there is no CPU fallback.
 Names follow the C entry points, whose records are here as ctypes structures too.
 
@@ -32,7 +33,9 @@ EXPORTS = [
     "aet_linear_workspace_bytes", "aet_linear_forward", "aet_linear_backward_workspace_bytes",
     "aet_linear_backward", "aet_group_norm_workspace_bytes", "aet_group_norm_forward",
     "aet_group_norm_backward_workspace_bytes", "aet_group_norm_backward", "aet_layer_norm_forward",
-    "aet_layer_norm_backward_workspace_bytes", "aet_layer_norm_backward", "aet_dropout_forward",
+    "aet_layer_norm_backward_workspace_bytes", "aet_layer_norm_backward", "aet_mx4_quantise", "aet_mx4_dequantise",
+    "aet_mx4_linear_workspace_bytes", "aet_mx4_linear_forward", "aet_mx4_linear_backward_workspace_bytes",
+    "aet_mx4_linear_backward", "aet_dropout_forward",
     "aet_dropout_backward", "aet_ops_last_error",
 ]
 
@@ -82,6 +85,22 @@ class aet_layer_norm_grad(C.Structure):
         ("mean", _vp), ("rstd", _vp)] + _mat("dx") + _mat("dgamma") + _mat("dbeta")
 
 
+class aet_mx4_values(C.Structure):
+    _fields_ = [(f, _i32) for f in ("dtype", "n", "rows", "cols")] + _mat("x") + _mat("codes") + _mat("scales")
+
+
+class aet_mx4_codes(C.Structure):
+    _fields_ = [(f, _i32) for f in ("dtype", "n", "rows", "cols")] + _mat("codes") + _mat("scales") + _mat("y")
+
+
+class aet_mx4_linear(C.Structure):
+    _fields_ = _LINEAR + _mat("x") + _mat("x_scales") + _mat("w") + _mat("w_scales") + _mat("bias") + _mat("residual") + _mat("y") + _mat("pre")
+
+
+class aet_mx4_linear_grad(C.Structure):
+    _fields_ = _LINEAR + _mat("dy") + _mat("x") + _mat("x_scales") + _mat("w") + _mat("w_scales") + _mat("pre") + _mat("dx") + _mat("dw") + _mat("db")
+
+
 class aet_dropout(C.Structure):
     _fields_ = [(f, _i32) for f in ("dtype", "n", "rows", "cols")] + _DROP + _mat("x") + _mat("residual") + _mat("y")
 
@@ -102,14 +121,15 @@ def load_library():
         warnings.warn(f"{os.path.basename(_build.OPS_LIB)} or its binding is older than its sources: build.build_ops() makes them anew",
                       RuntimeWarning, stacklevel=2)
     lib = C.CDLL(_build.OPS_LIB)
-    for name in ("aet_linear", "aet_linear_backward", "aet_group_norm", "aet_group_norm_backward", "aet_layer_norm_backward"):
+    for name in ("aet_linear", "aet_linear_backward", "aet_group_norm", "aet_group_norm_backward", "aet_layer_norm_backward",
+                 "aet_mx4_linear", "aet_mx4_linear_backward"):
         f = getattr(lib, name + "_workspace_bytes")
         f.restype, f.argtypes = C.c_size_t, [_vp]
     for name in ("aet_linear_forward", "aet_linear_backward", "aet_group_norm_forward", "aet_group_norm_backward",
-                 "aet_layer_norm_backward"):
+                 "aet_layer_norm_backward", "aet_mx4_linear_forward", "aet_mx4_linear_backward"):
         f = getattr(lib, name)
         f.restype, f.argtypes = C.c_int, [_vp, _vp, C.c_size_t, _vp]
-    for name in ("aet_dropout_forward", "aet_dropout_backward", "aet_layer_norm_forward"):
+    for name in ("aet_dropout_forward", "aet_dropout_backward", "aet_layer_norm_forward", "aet_mx4_quantise", "aet_mx4_dequantise"):
         f = getattr(lib, name)
         f.restype, f.argtypes = C.c_int, [_vp, _vp]
     lib.aet_ops_last_error.restype = C.c_char_p
@@ -203,6 +223,45 @@ def aet_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
     gamma).  A gamma for all clients gets the sum over them.  out: places for the three, of any strides, or None; dx may be
     dy or dh."""
     return (_EXT or _tensors()).layer_norm_backward(dy, x, mean, rstd, gamma, dh, need, out, *_on(x, stream))
+
+
+def _bf16(dtype: torch.dtype) -> bool:
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"dtype is torch.float32 or torch.bfloat16: got {dtype}")
+    return dtype == torch.bfloat16
+
+
+def aet_mx4_quantise(x: torch.Tensor, *, out=(None, None), stream: Optional[torch.cuda.Stream] = None):
+    """(codes, scales), uint8, [..., ceil(cols / 2)] and [..., ceil(cols / 32)]: x, [n, rows, cols] or [rows, cols], in
+    microscaled 4-bit floating point, blocks along the last axis.  out: places for the two, or None."""
+    return (_EXT or _tensors()).mx4_quantise(x, out, *_on(x, stream))
+
+
+def aet_mx4_dequantise(codes: torch.Tensor, scales: torch.Tensor, *, cols: Optional[int] = None, dtype: torch.dtype = torch.bfloat16,
+                       out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """What codes and scales stand for.  cols: of the rows, where it is odd (else twice the bytes)."""
+    return (_EXT or _tensors()).mx4_dequantise(codes, scales, cols, _bf16(dtype), out, *_on(codes, stream))
+
+
+def aet_mx4_linear_forward(x: torch.Tensor, x_scales: torch.Tensor, w: torch.Tensor, w_scales: torch.Tensor,
+                           bias: Optional[torch.Tensor] = None, *, cols: Optional[int] = None, residual: Optional[torch.Tensor] = None,
+                           act: str = "none", p: float = 0.0, seed: int = 0, first_row: int = 0, keep_pre: bool = False,
+                           dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None):
+    """aet_linear_forward where x and w are held in 4 bits (aet_mx4_quantise's codes and scales).  cols: of x and w, where
+    it is odd; dtype: of bias, residual, and the result."""
+    return (_EXT or _tensors()).mx4_linear_forward(x, x_scales, w, w_scales, bias, cols, residual, _act(act), p, seed & _U64, first_row,
+                                                   keep_pre, _bf16(dtype), out, *_on(x, stream))
+
+
+def aet_mx4_linear_backward(dy: torch.Tensor, x: torch.Tensor, x_scales: torch.Tensor, w: torch.Tensor, w_scales: torch.Tensor,
+                            pre: Optional[torch.Tensor] = None, *, cols: Optional[int] = None, act: str = "none", p: float = 0.0,
+                            seed: int = 0, first_row: int = 0, need: Tuple[bool, bool, bool] = (True, True, True),
+                            out=(None, None, None), stream: Optional[torch.cuda.Stream] = None):
+    """(dx, dw, db) of aet_mx4_linear_forward with regard to what the codes stand for, in dy's type, as
+    aet_linear_backward has them."""
+    return (_EXT or _tensors()).mx4_linear_backward(dy, x, x_scales, w, w_scales, pre, cols, _act(act), p, seed & _U64, first_row, need, out,
+                                                    *_on(dy, stream))
 
 
 def aet_dropout_forward(x: torch.Tensor, *, p: float, seed: int, first_row: int = 0,

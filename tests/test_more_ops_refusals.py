@@ -1,4 +1,4 @@
-"""What the entry points of layer normalisation refuse, on the host: nothing is launched, so no GPU is needed."""
+"""What the entry points of layer normalisation and of microscaled 4-bit values refuse, on the host: nothing is launched, so no GPU is needed."""
 import ctypes as C
 
 import pytest
@@ -58,3 +58,68 @@ def test_layer_norm_edges(lib):   # noqa: F811
 def test_binding_refuses_host_tensors():
     with pytest.raises(ValueError, match="on a GPU"):
         ops.aet_layer_norm_forward(torch.zeros(2, 3))
+
+
+def values(**k):
+    return made(ops.aet_mx4_values(0, 2, 3, 70, P, 210, 70, P, 105, 35, P, 9, 3), k)
+
+
+def codes(**k):
+    return made(ops.aet_mx4_codes(0, 2, 3, 70, P, 105, 35, P, 9, 3, P, 210, 70), k)
+
+
+def linear(**k):
+    return made(ops.aet_mx4_linear(0, 1, 2, 3, 70, 4, 0.1, 1, 0, P, 105, 35, P, 9, 3, P, 140, 35, P, 12, 3, P, 4, 0, P, 12, 4, P, 12, 4, P, 12, 4), k)
+
+
+def linear_grad(**k):
+    return made(ops.aet_mx4_linear_grad(0, 1, 2, 3, 70, 4, 0.1, 1, 0, P, 12, 4, P, 105, 35, P, 9, 3, P, 140, 35, P, 12, 3, P, 12, 4, P, 210, 70, P, 280, 70,
+                                        P, 4, 0), k)
+
+
+DROP = [dict(p=1.0), dict(p=float("nan")), dict(first_row=-1), dict(first_row=2 ** 63 - 2)]
+SIZES = [dict(dtype=2), dict(n=-1), dict(rows=-1), dict(rows=(1 << 30) + 1)]
+HELD = [dict(codes_p=None), dict(scales_p=None), dict(codes_row=-1), dict(scales_client=-1)]
+WRONG = {
+    "aet_mx4_quantise": (values, SIZES + HELD + [dict(cols=-1), dict(x_p=None), dict(x_p=P + 2), dict(x_row=-1), dict(codes_row=34), dict(codes_client=104),
+                                                 dict(scales_row=2), dict(scales_client=8)]),
+    "aet_mx4_dequantise": (codes, SIZES + HELD + [dict(cols=-1), dict(y_p=None), dict(y_p=P + 2), dict(y_row=69), dict(y_client=209)]),
+    "aet_mx4_linear_forward": (linear, SIZES + DROP + [dict(act=4), dict(out=-1), {"in": -1}, dict(x_p=None), dict(x_scales_p=None), dict(w_p=None),
+                                                       dict(w_scales_p=None), dict(x_row=-1), dict(w_scales_row=-1), dict(w_client=0), dict(w_scales_client=0),
+                                                       dict(y_p=None), dict(y_p=P + 2), dict(y_row=3), dict(bias_p=P + 1), dict(residual_row=-1),
+                                                       dict(pre_client=8), dict(n=1 << 30, rows=1 << 30), dict(x_client=1 << 60)]),
+    "aet_mx4_linear_backward": (linear_grad, SIZES + DROP + [dict(act=4), dict(out=-1), {"in": -1}, dict(x_p=None), dict(x_scales_p=None), dict(w_p=None),
+                                                             dict(w_scales_p=None), dict(dy_p=None), dict(pre_p=None), dict(w_client=0), dict(dx_row=69),
+                                                             dict(dw_client=279), dict(db_client=3), dict(dw_client=0), dict(dy_p=P + 2),
+                                                             dict(dw_client=0, db_client=0)])}
+
+
+@pytest.mark.parametrize("fn,wrong", [(f, w) for f, (_, all_) in WRONG.items() for w in all_], ids=str)
+def test_mx4_refused(lib, fn, wrong):   # noqa: F811
+    a = WRONG[fn][0](**wrong)
+    space = (P, 1 << 60) if "linear" in fn else ()
+    assert getattr(lib, fn)(C.addressof(a), *space, None) == EINVAL and lib.aet_ops_last_error()
+    if space:
+        assert getattr(lib, fn.replace("_forward", "") + "_workspace_bytes")(C.addressof(a)) == 0
+
+
+def test_mx4_edges(lib):   # noqa: F811
+    for fn, (make, _) in WRONG.items():
+        space = (None, 0) if "linear" in fn else ()
+        assert getattr(lib, fn)(None, *space, None) == EINVAL
+        assert getattr(lib, fn)(C.addressof(make(n=0)), *space, None) == 0
+    assert lib.aet_mx4_quantise(C.addressof(values(cols=0)), None) == 0 and lib.aet_mx4_dequantise(C.addressof(codes(rows=0)), None) == 0
+    assert lib.aet_mx4_linear_forward(C.addressof(linear(rows=0)), None, 0, None) == 0
+    a = linear_grad(rows=300, dy_client=1200, x_client=10500, x_scales_client=900, pre_client=1200, dx_client=21000)
+    need = lib.aet_mx4_linear_backward_workspace_bytes(C.addressof(a))
+    assert need > 0
+    for ws, size in ((None, need), (P, need - 1), (P + 128, need)):
+        assert lib.aet_mx4_linear_backward(C.addressof(a), ws, size, None) == ENOMEM
+
+
+def test_mx4_binding_refuses_host_tensors():
+    u = torch.zeros(2, 4, dtype=torch.uint8)
+    for call in (lambda: ops.aet_mx4_quantise(torch.zeros(2, 8)), lambda: ops.aet_mx4_dequantise(u, u[:, :1]),
+                 lambda: ops.aet_mx4_linear_forward(u, u[:, :1], u, u[:, :1]), lambda: ops.aet_mx4_linear_backward(torch.zeros(2, 2), u, u[:, :1], u, u[:, :1])):
+        with pytest.raises(ValueError, match="on a GPU"):
+            call()
