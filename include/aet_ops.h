@@ -3,7 +3,8 @@
  * from, on MI355X (gfx950): a linear layer with bias, activation, dropout and residual in its
  * epilogue, group normalisation with an activation on channels-last maps, layer normalisation
  * of rows, and dropout from the counter generator, each with its gradient; values held in
- * microscaled 4-bit floating point, and the linear layer of such values.  All of them take many clients' models side
+ * microscaled 4-bit floating point, and the linear layer of such values; and the orthogonalised
+ * update of weight matrices.  All of them take many clients' models side
  * by side in one call (`n`), each with parameters of its own or all with the same ones.
  *
  * Conventions
@@ -209,6 +210,27 @@ typedef struct {
 } aet_dropout;
 aet_status aet_dropout_forward(const aet_dropout *a, void *hip_stream);
 aet_status aet_dropout_backward(const aet_dropout *a, void *hip_stream);
+
+/* The orthogonalised update of weight matrices (Newton-Schulz products, as the Muon optimiser makes them):
+ *   X = g / (|g| + eps), |g| the root of the sum of g's squares (0 where both are 0);
+ *   `steps` times  X = a X + (b A + c A A) X, A = X X^T, which takes a singular value s to a s + b s^3 + c s^5
+ *   and leaves the singular vectors;
+ *   y = keep w + scale X.
+ *   g   n x rows x cols: a gradient, a sum of them, or a momentum of each client
+ *   w   n x rows x cols, or p = NULL: y = scale X
+ *   y   n x rows x cols; may be w or g itself, with the same strides
+ * The sides are at most 2^20, the polynomial one under which singular values up to 1 stay below 2^30.  Everything
+ * between is to within 2^-22 of each value and 2^-39 of what the norm and the polynomial bound all values of that step by; products'
+ * sums are fp32, the norm's 64 bits.  A client whose g has an infinity or NaN has a y of NaN. */
+typedef struct {
+    int32_t dtype;
+    int32_t n, rows, cols, steps;
+    double a, b, c, eps, keep, scale;
+    aet_in g, w;
+    aet_out y;
+} aet_orthogonal;
+size_t aet_orthogonalise_workspace_bytes(const aet_orthogonal *a);
+aet_status aet_orthogonalise(const aet_orthogonal *a, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Microscaled 4-bit floating point, as messages and weights are held in.  The 32 neighbouring values
  * of a row (the last ones of it may be fewer) that make up a block share an exponent x; a value is held

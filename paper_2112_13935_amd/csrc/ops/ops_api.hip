@@ -291,6 +291,28 @@ static aet_status check(const aet_layer_norm_grad *a) {
     return AET_OK;
 }
 
+// ---- orthogonalised updates --------------------------------------------------------------
+
+constexpr int kMostSide = 1 << 20;
+static aet_status check(const aet_orthogonal *a) {
+    const char *why;
+    if (!a) return fail(AET_EINVAL, "the record is NULL");
+    if (bad_common(a->dtype, AET_ACT_NONE, &why)) return fail(AET_EINVAL, "%s", why);
+    if (bad_sizes({a->n, a->rows, a->cols}, &why)) return fail(AET_EINVAL, "%s", why);
+    if (a->rows > kMostSide || a->cols > kMostSide) return fail(AET_EINVAL, "a side of the matrices is over 2^20");
+    if (a->steps < 0 || a->steps > 100) return fail(AET_EINVAL, "steps is not in [0, 100]");
+    if (!(a->eps >= 0) || !isfinite(a->eps)) return fail(AET_EINVAL, "eps is negative or not finite");
+    if (!isfinite(a->a) || !isfinite(a->b) || !isfinite(a->c) || !isfinite(a->keep) || !isfinite(a->scale))
+        return fail(AET_EINVAL, "a, b, c, keep and scale have to be finite");
+    if (!orthogonal_bounded(*a)) return fail(AET_EINVAL, "singular values up to 1 grow beyond 2^30 under this polynomial");
+    if (!a->n || !a->rows || !a->cols) return AET_OK;
+    const int64_t nr[2] = {a->n, a->rows}, gs[2] = {a->g.client, a->g.row}, ws[2] = {a->w.client, a->w.row}, ys[2] = {a->y.client, a->y.row};
+    AET_CHECK("g", bad_in(a->g.p, a->dtype, 2, nr, gs));
+    if (a->w.p) AET_CHECK("w", bad_in(a->w.p, a->dtype, 2, nr, ws));
+    AET_CHECK("y", bad_out(a->y.p, a->dtype, 2, nr, ys, a->cols));
+    return AET_OK;
+}
+
 // ---- microscaled 4-bit values ------------------------------------------------------------
 
 static const char *bad_held(const aet_in &t, int64_t n, int64_t rows) {
@@ -486,6 +508,18 @@ aet_status aet_layer_norm_backward(const aet_layer_norm_grad *a, void *workspace
     if (bad_workspace(workspace, workspace_bytes, need))
         return fail(AET_ENOMEM, "the workspace needs %zu bytes, 256-byte aligned; got %zu", need, workspace_bytes);
     return done(launch_layer_norm_backward(*a, workspace, (hipStream_t)hip_stream));
+}
+
+size_t aet_orthogonalise_workspace_bytes(const aet_orthogonal *a) {
+    return check(a) == AET_OK && a->n && a->rows && a->cols ? orthogonal_workspace(*a) : 0;
+}
+aet_status aet_orthogonalise(const aet_orthogonal *a, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (const aet_status st = check(a)) return st;
+    if (!a->n || !a->rows || !a->cols) return AET_OK;
+    const size_t need = orthogonal_workspace(*a);
+    if (bad_workspace(workspace, workspace_bytes, need))
+        return fail(AET_ENOMEM, "the workspace needs %zu bytes, 256-byte aligned; got %zu", need, workspace_bytes);
+    return done(launch_orthogonalise(*a, workspace, (hipStream_t)hip_stream));
 }
 
 aet_status aet_mx4_quantise(const aet_mx4_values *a, void *hip_stream) {

@@ -33,6 +33,11 @@ hipError_t launch_layer_norm_forward(const aet_layer_norm &a, hipStream_t s);
 size_t layer_norm_backward_workspace(const aet_layer_norm_grad &a);
 hipError_t launch_layer_norm_backward(const aet_layer_norm_grad &a, void *workspace, hipStream_t s);
 
+// Whether the polynomial keeps X within what the kernels' scales can hold.
+bool orthogonal_bounded(const aet_orthogonal &o);
+size_t orthogonal_workspace(const aet_orthogonal &o);
+hipError_t launch_orthogonalise(const aet_orthogonal &o, void *workspace, hipStream_t s);
+
 hipError_t launch_mx4_quantise(const aet_mx4_values &a, hipStream_t s);
 hipError_t launch_mx4_dequantise(const aet_mx4_codes &a, hipStream_t s);
 size_t mx4_linear_forward_workspace(const aet_mx4_linear &a);

@@ -317,6 +317,19 @@ Three layer_norm_backward(const Tensor &dy, const Tensor &x, const Tensor &mean,
     return made;
 }
 
+Tensor orthogonalise(const Tensor &g, int64_t steps, std::tuple<double, double, double> polynomial, double eps, const OptTensor &w, double keep, double scale,
+                     const OptTensor &out, int64_t handle, const Stream &stream) {
+    Call c(g, handle, stream);
+    const Axes s(g);
+    aet_orthogonal a = {c.dtype, s.n, s.rows, s.cols, size32(steps), std::get<0>(polynomial), std::get<1>(polynomial), std::get<2>(polynomial), eps, keep, scale};
+    const OptTensor y = c.out(out, true, g.sizes());
+    c.mat(a.g, "g", g, g.sizes());
+    c.mat(a.w, "w", w, g.sizes());
+    c.mat(a.y, "out", y, g.sizes());
+    c.run(aet_orthogonalise, aet_orthogonalise_workspace_bytes, a);
+    return *y;
+}
+
 // Codes and scales of a tensor of this shape (its last axis: cols)
 struct HeldShape {
     std::vector<int64_t> codes, scales;
@@ -433,6 +446,7 @@ PYBIND11_MODULE(_ops_torch, m) {
     m.def("dropout", &dropout);
     m.def("layer_norm_forward", &layer_norm_forward);
     m.def("layer_norm_backward", &layer_norm_backward);
+    m.def("orthogonalise", &orthogonalise);
     m.def("mx4_quantise", &mx4_quantise);
     m.def("mx4_dequantise", &mx4_dequantise);
     m.def("mx4_linear_forward", &mx4_linear_forward);

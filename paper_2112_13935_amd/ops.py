@@ -1,7 +1,8 @@
 """Binding of libaet_ops.so (include/aet_ops.h): a linear layer with bias, activation, dropout and
 residual in its epilogue, group normalisation with an activation on channels-last maps, layer
 normalisation of rows, and dropout from the counter generator, each with its gradient; values held in
-microscaled 4-bit floating point, and the linear layer of such values.  Argument marshalling only, compiled
+microscaled 4-bit floating point, and the linear layer of such values; the orthogonalised update of
+weight matrices.  Argument marshalling only, compiled
 (csrc/ops/ops_torch.cpp); PyTorch supplies device memory and the stream, there is no CPU fallback.
 Names follow the C entry points, whose records are here as ctypes structures too.
 
@@ -33,7 +34,8 @@ EXPORTS = [
     "aet_linear_workspace_bytes", "aet_linear_forward", "aet_linear_backward_workspace_bytes",
     "aet_linear_backward", "aet_group_norm_workspace_bytes", "aet_group_norm_forward",
     "aet_group_norm_backward_workspace_bytes", "aet_group_norm_backward", "aet_layer_norm_forward",
-    "aet_layer_norm_backward_workspace_bytes", "aet_layer_norm_backward", "aet_mx4_quantise", "aet_mx4_dequantise",
+    "aet_layer_norm_backward_workspace_bytes", "aet_layer_norm_backward", "aet_orthogonalise_workspace_bytes",
+    "aet_orthogonalise", "aet_mx4_quantise", "aet_mx4_dequantise",
     "aet_mx4_linear_workspace_bytes", "aet_mx4_linear_forward", "aet_mx4_linear_backward_workspace_bytes",
     "aet_mx4_linear_backward", "aet_dropout_forward",
     "aet_dropout_backward", "aet_ops_last_error",
@@ -85,6 +87,11 @@ class aet_layer_norm_grad(C.Structure):
         ("mean", _vp), ("rstd", _vp)] + _mat("dx") + _mat("dgamma") + _mat("dbeta")
 
 
+class aet_orthogonal(C.Structure):
+    _fields_ = [(f, _i32) for f in ("dtype", "n", "rows", "cols", "steps")] + [(f, C.c_double) for f in ("a", "b", "c", "eps", "keep", "scale")] + _mat(
+        "g") + _mat("w") + _mat("y")
+
+
 class aet_mx4_values(C.Structure):
     _fields_ = [(f, _i32) for f in ("dtype", "n", "rows", "cols")] + _mat("x") + _mat("codes") + _mat("scales")
 
@@ -122,11 +129,11 @@ def load_library():
                       RuntimeWarning, stacklevel=2)
     lib = C.CDLL(_build.OPS_LIB)
     for name in ("aet_linear", "aet_linear_backward", "aet_group_norm", "aet_group_norm_backward", "aet_layer_norm_backward",
-                 "aet_mx4_linear", "aet_mx4_linear_backward"):
+                 "aet_mx4_linear", "aet_mx4_linear_backward", "aet_orthogonalise"):
         f = getattr(lib, name + "_workspace_bytes")
         f.restype, f.argtypes = C.c_size_t, [_vp]
     for name in ("aet_linear_forward", "aet_linear_backward", "aet_group_norm_forward", "aet_group_norm_backward",
-                 "aet_layer_norm_backward", "aet_mx4_linear_forward", "aet_mx4_linear_backward"):
+                 "aet_layer_norm_backward", "aet_mx4_linear_forward", "aet_mx4_linear_backward", "aet_orthogonalise"):
         f = getattr(lib, name)
         f.restype, f.argtypes = C.c_int, [_vp, _vp, C.c_size_t, _vp]
     for name in ("aet_dropout_forward", "aet_dropout_backward", "aet_layer_norm_forward", "aet_mx4_quantise", "aet_mx4_dequantise"):
@@ -223,6 +230,15 @@ def aet_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
     gamma).  A gamma for all clients gets the sum over them.  out: places for the three, of any strides, or None; dx may be
     dy or dh."""
     return (_EXT or _tensors()).layer_norm_backward(dy, x, mean, rstd, gamma, dh, need, out, *_on(x, stream))
+
+
+def aet_orthogonalise(g: torch.Tensor, *, steps: int = 5, polynomial: Tuple[float, float, float] = (3.4445, -4.7750, 2.0315),
+                      eps: float = 1e-7, w: Optional[torch.Tensor] = None, keep: float = 1.0, scale: float = 1.0,
+                      out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """keep * w + scale * X (scale * X without w), X being g / (|g| + eps) after `steps` times X = a X + (b A + c A A) X, A = X X^T,
+    (a, b, c) the polynomial, which takes each singular value s to a s + b s^3 + c s^5.  g: [n, rows, cols] or [rows, cols]; w and
+    out, which may be w or g: as g."""
+    return (_EXT or _tensors()).orthogonalise(g, steps, polynomial, eps, w, keep, scale, out, *_on(g, stream))
 
 
 def _bf16(dtype: torch.dtype) -> bool:

@@ -1,4 +1,5 @@
-"""What the entry points of layer normalisation and of microscaled 4-bit values refuse, on the host: nothing is launched, so no GPU is needed."""
+"""What the entry points of layer normalisation, orthogonalised updates and microscaled 4-bit values refuse, on the host: nothing is launched, so no
+GPU is needed."""
 import ctypes as C
 
 import pytest
@@ -123,3 +124,29 @@ def test_mx4_binding_refuses_host_tensors():
                  lambda: ops.aet_mx4_linear_forward(u, u[:, :1], u, u[:, :1]), lambda: ops.aet_mx4_linear_backward(torch.zeros(2, 2), u, u[:, :1], u, u[:, :1])):
         with pytest.raises(ValueError, match="on a GPU"):
             call()
+
+
+def orthogonal(**k):
+    return made(ops.aet_orthogonal(0, 2, 3, 8, 5, 3.4445, -4.775, 2.0315, 1e-7, 1.0, 1.0, P, 24, 8, P, 24, 8, P, 24, 8), k)
+
+
+@pytest.mark.parametrize("wrong", SIZES + [dict(cols=-1), dict(cols=(1 << 20) + 1), dict(rows=(1 << 20) + 1), dict(steps=-1), dict(steps=101), dict(eps=-1.0),
+                                           dict(eps=float("nan")), dict(eps=float("inf")), dict(a=float("nan")), dict(b=float("inf")), dict(c=float("nan")),
+                                           dict(keep=float("inf")), dict(scale=float("nan")), dict(a=1e7), dict(c=1e30), dict(b=-1e30), dict(g_p=None),
+                                           dict(y_p=None), dict(g_p=P + 2), dict(w_p=P + 1), dict(g_row=-1), dict(w_client=-1), dict(y_row=7), dict(y_client=23)],
+                         ids=str)
+def test_orthogonalise_refused(lib, wrong):   # noqa: F811
+    a = orthogonal(**wrong)
+    assert lib.aet_orthogonalise(C.addressof(a), P, 1 << 60, None) == EINVAL and lib.aet_ops_last_error()
+    assert lib.aet_orthogonalise_workspace_bytes(C.addressof(a)) == 0
+
+
+def test_orthogonalise_edges(lib):   # noqa: F811
+    assert lib.aet_orthogonalise(None, None, 0, None) == EINVAL
+    for nothing in (dict(n=0), dict(rows=0), dict(cols=0)):
+        assert lib.aet_orthogonalise(C.addressof(orthogonal(**nothing)), None, 0, None) == 0
+    a = orthogonal()
+    need = lib.aet_orthogonalise_workspace_bytes(C.addressof(a))
+    assert need > 0
+    for ws, size in ((None, need), (P, need - 1), (P + 128, need)):
+        assert lib.aet_orthogonalise(C.addressof(a), ws, size, None) == ENOMEM
