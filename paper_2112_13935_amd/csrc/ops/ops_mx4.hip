@@ -4,6 +4,7 @@
 // between neighbours, then the hardware's conversions, which divide by the scale (given by its exponent alone; 0 is 2^-127,
 // 255 NaN), round to the nearest of the 16 values, ties to the even code, and end at 6.
 #include "ops_internal.h"
+#include "ops_mx4.h"
 
 #include <type_traits>
 
@@ -190,31 +191,14 @@ static hipError_t expand(int dtype, int64_t n, int64_t rows, int64_t cols, const
     return launch_mx4_dequantise({dtype, (int32_t)n, (int32_t)rows, (int32_t)cols, codes, scales, {to, rows * line, line}}, s);
 }
 
-static aet_linear plain_of(const aet_mx4_linear &a, char *workspace, size_t *used) {
-    aet_linear b = {a.dtype, a.act, a.n, a.rows, a.in, a.out, a.p, a.seed, a.first_row};
-    b.bias = a.bias;
-    b.residual = a.residual;
-    b.y = a.y;
-    b.pre = a.pre;
-    const int64_t line = line_of(a.dtype, a.in), held = a.w.client ? a.n : 1;
-    const size_t x = expanded_bytes(a.dtype, a.n, a.rows, a.in);
-    b.x = {workspace, a.rows * line, line};
-    b.w = {workspace + x, held > 1 ? a.out * line : 0, line};
-    *used = x + expanded_bytes(a.dtype, held, a.out, a.in);
-    return b;
+static HeldProduct forward_product(const aet_mx4_linear &a) {
+    HeldProduct p = {{a.x, a.x_scales}, {a.w, a.w_scales}, a.n, a.rows, a.out, a.in};
+    p.e = {a.bias, a.residual, a.y, a.pre, a.rows, a.act, make_drop(a.p, a.seed, a.first_row, a.out)};
+    return p;
 }
-size_t mx4_linear_forward_workspace(const aet_mx4_linear &a) {
-    size_t used;
-    const aet_linear b = plain_of(a, nullptr, &used);
-    return used + linear_forward_workspace(b);
-}
+size_t mx4_linear_forward_workspace(const aet_mx4_linear &a) { return mx4_product_workspace(forward_product(a)); }
 hipError_t launch_mx4_linear_forward(const aet_mx4_linear &a, void *workspace, hipStream_t s) {
-    size_t used;
-    aet_linear b = plain_of(a, (char *)workspace, &used);
-    aet_in out;
-    hipError_t e = expand(a.dtype, a.n, a.rows, a.in, a.x, a.x_scales, (void *)b.x.p, &out, s);
-    if (e == hipSuccess) e = expand(a.dtype, a.w.client ? a.n : 1, a.out, a.in, a.w, a.w_scales, (void *)b.w.p, &out, s);
-    return e == hipSuccess ? launch_linear_forward(b, (char *)workspace + used, s) : e;
+    return launch_mx4_product(a.dtype, forward_product(a), workspace, s);
 }
 
 aet_linear_grad mx4_plain_gradient(const aet_mx4_linear_grad &a, void *workspace, size_t *used) {

@@ -20,6 +20,19 @@ struct Product {
     Epilogue e;
 };
 
+// A product's tiles.
+struct Shape {
+    int M, N, K;
+    int tiles_n, tiles;       // tiles of C: in a row, of a client
+    int slices, slice_k;      // parts of the sum (slice_k a multiple of BK); partial sums go to `partial` where there are several
+    int blocks;
+    float *partial;           // [slice][client][M][N]
+    int clients;
+};
+
+// Adds the slices of a split sum, in their order, and ends it.
+hipError_t launch_join(int dtype, const Shape &s, const Epilogue &e, hipStream_t stream);
+
 // Few rows (ops_rows.hip): both operands by rows, no scratch.
 bool rows_fit(const Product &p);
 hipError_t launch_rows(int dtype, const Product &p, hipStream_t s);

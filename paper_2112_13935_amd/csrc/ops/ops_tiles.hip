@@ -26,15 +26,6 @@
 
 namespace aet_ops {
 
-struct Shape {
-    int M, N, K;
-    int tiles_n, tiles;       // tiles of C: in a row, of a client
-    int slices, slice_k;      // parts of the sum (slice_k a multiple of BK); partial sums go to `partial` where there are several
-    int blocks;
-    float *partial;           // [slice][client][M][N]
-    int clients;
-};
-
 // ---- staging -----------------------------------------------------------------------------
 
 // Through registers: any alignment, any end of rows and sums.
@@ -379,6 +370,15 @@ __global__ __launch_bounds__(256) void k_join(Shape s, Epilogue e) {
     finish<T>(e, client, row, col, count, v);
 }
 
+template <typename T>
+static hipError_t run_join(const Shape &s, const Epilogue &e, hipStream_t stream) {
+    k_join<T><<<(int)ceil_div((int64_t)s.clients * s.M * ceil_div(s.N, 16 / sizeof(T)), 256), 256, 0, stream>>>(s, e);
+    return hipGetLastError();
+}
+hipError_t launch_join(int dtype, const Shape &s, const Epilogue &e, hipStream_t stream) {
+    return dtype == AET_F32 ? run_join<float>(s, e, stream) : run_join<bf16>(s, e, stream);
+}
+
 // ---- the choice --------------------------------------------------------------------------
 
 // Whether the operand's stages of BK can go straight into LDS.
@@ -501,8 +501,7 @@ static hipError_t run_product(const Product &p, void *workspace, hipStream_t str
         else e = d ? run_tiles<T, 64, 64, 64, 2, 2, TA, TB, true>(p, s, stream) : run_tiles<T, 64, 64, 64, 2, 2, TA, TB, false>(p, s, stream);
     }
     if (e != hipSuccess || s.slices == 1) return e;
-    k_join<T><<<(int)ceil_div((int64_t)p.clients * p.M * ceil_div(p.N, 16 / sizeof(T)), 256), 256, 0, stream>>>(s, p.e);
-    return hipGetLastError();
+    return launch_join(sizeof(T) == 4 ? AET_F32 : AET_BF16, s, p.e, stream);
 }
 
 hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStream_t s) {
