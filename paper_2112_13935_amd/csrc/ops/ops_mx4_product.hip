@@ -19,67 +19,56 @@ __device__ __forceinline__ i8v widen(i4 v) { return __builtin_shufflevector(v, v
 
 // ---- tiles -------------------------------------------------------------------------------
 
-constexpr int kDeep = 256;           // k of a stage: 128 bytes of codes and 8 scales a row
-constexpr int kStageK = kDeep / 4;   // in values of bf16, which stages of codes are moved as
+constexpr int kDeep = 256, kGroup = 4;   // k of a stage, 128 bytes of codes a row; stages whose scales come together, 32 bytes a row
+constexpr int kUnit = 512;               // sums are whole ones of these: 16 bytes of scales a row
 
-// Scales of R rows in LDS, 8 bytes a row.  A thread moves 4 of them at a time.
-template <int R, int THREADS>
-struct ScaleStage {
-    static constexpr int kBytes = R * 8;
-    static constexpr bool kAll = R * 2 >= THREADS;   // else the first threads alone
-    static constexpr int kCount = kAll ? R * 2 / THREADS : 1;
+// Scales of BM rows of A and BN of B, a group of stages at a time.  (8 bytes a row and stage would be a line of memory for each.)
+template <int BM, int BN, int THREADS>
+struct ScaleGroup {
+    static constexpr int kBytes = (BM + BN) * 32, kCount = (BM + BN) * 2 / THREADS;
+    static_assert(kCount * THREADS == (BM + BN) * 2, "whole pieces a thread");
     const uint8_t *p[kCount];
-    __device__ __forceinline__ bool mine() const { return kAll || threadIdx.x < R * 2; }   // (whole waves)
-    __device__ __forceinline__ void begin(const Held &o, int64_t client, int r0, int rows_all, int k0) {
-        const int rows = rows_all - r0;
+    int piece, last;   // of 16 bytes, from the row's first on
+    __device__ __forceinline__ void begin(const Held &a, const Held &b, int64_t client, int m0, int M, int n0, int N, int k0, int K) {
+        piece = k0 / kUnit + threadIdx.x % 2;
+        last = K / kUnit - 1;
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const int q = threadIdx.x + i * THREADS, r = q / 2 < rows ? q / 2 : rows - 1;
-            p[i] = (const uint8_t *)o.scales.p + client * o.scales.client + (int64_t)(r0 + r) * o.scales.row + k0 / 32 + q % 2 * 4;
+            const int r = (threadIdx.x + i * THREADS) / 2, row = r < BM ? m0 + r : n0 + r - BM;
+            const aet_in &o = r < BM ? a.scales : b.scales;
+            const int most = (r < BM ? M : N) - 1;
+            p[i] = (const uint8_t *)o.p + client * o.client + (int64_t)(row < most ? row : most) * o.row;
         }
     }
+    // (behind the sum's end: the last piece again, which nobody reads)
     __device__ __forceinline__ void load(lds_ptr to) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-        if (mine())
+        const int at = (piece < last ? piece : last) * 16;
 #pragma unroll
-            for (int i = 0; i < kCount; ++i)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)p[i],
-                                                 (__attribute__((address_space(3))) void *)(to + (i * THREADS + wave * 64) * 4), 4, 0, 0);
-        step();
-    }
-    __device__ __forceinline__ void step() {
-#pragma unroll
-        for (int i = 0; i < kCount; ++i) p[i] += kDeep / 32;
-    }
-    // The last stage, of which `left` blocks are there: the others' scales are 1, beside codes of 0.
-    __device__ __forceinline__ void load_end(lds_ptr to, int left) {
-        if (!mine()) return;
-#pragma unroll
-        for (int i = 0; i < kCount; ++i) {
-            const int q = threadIdx.x + i * THREADS, have = left - q % 2 * 4;
-            uint32_t v = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v |= (uint32_t)(e < have ? p[i][e] : 127) << (8 * e);
-            *(__attribute__((address_space(3))) uint32_t *)(to + q * 4) = v;
-        }
+        for (int i = 0; i < kCount; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p[i] + at),
+                                             (__attribute__((address_space(3))) void *)(to + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+        piece += 2;
     }
 };
 
-template <int BM, int BN>
+// In LDS: two stages of codes of A and B, two groups of scales of A and B.  (Codes are moved as values of bf16, of 4 k each.)
+template <int BM, int BN, int THREADS>
 struct HeldTile {
-    using SA = Stage<BM, kStageK, false>;
-    using SB = Stage<BN, kStageK, false>;
-    static constexpr int kCodes = SA::kBytes + SB::kBytes, kStage = kCodes + (BM + BN) * 8;
+    using SA = Stage<BM, kDeep / 4, false>;
+    using SB = Stage<BN, kDeep / 4, false>;
+    using Scales = ScaleGroup<BM, BN, THREADS>;
+    static constexpr int kStage = SA::kBytes + SB::kBytes, kScales = 2 * kStage, kLds = kScales + 2 * Scales::kBytes;
 };
 
-template <typename T, int BM, int BN, int WR, int WC, int OCC>
-__global__ __launch_bounds__(64 * WR * WC, OCC) void k_mx4_tiles(Held oa, Held ob, Shape s, Epilogue e) {
+template <typename T, int BM, int BN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC, BM == 64 ? 4 : 2) void k_mx4_tiles(Held oa, Held ob, Shape s, Epilogue e) {
     extern __shared__ __attribute__((aligned(1024))) char lds_[];
     const lds_ptr lds = (lds_ptr)lds_;
-    using L = HeldTile<BM, BN>;
+    constexpr int THREADS = 64 * WR * WC, FM = BM / WR / 32, FN = BN / WC / 32, KS = kDeep / 64;
+    using L = HeldTile<BM, BN, THREADS>;
     using SA = typename L::SA;
     using SB = typename L::SB;
-    constexpr int THREADS = 64 * WR * WC, FM = BM / WR / 32, FN = BN / WC / 32, KS = kDeep / 64;
     int id = xcd_order(blockIdx.x, s.blocks);
     const int tile = id % s.tiles;
     id /= s.tiles;
@@ -102,23 +91,25 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void k_mx4_tiles(Held oa, Held o
     struct Fragments {
         i4 a[FM], b[FN];
     };
-    struct Scaled {   // four blocks of a row, shifted so that bytes 0 and 2 are the lane's
+    struct Scaled {   // of 128 k, shifted so that bytes 0 and 2 are the lane's
         uint32_t a[FM], b[FN];
     };
-    const auto read = [&](Fragments &f, lds_ptr stage, int ks) {
+    const auto read = [&](Fragments &f, int stage, int ks) {
+        const lds_ptr at = lds + stage % 2 * L::kStage;
 #pragma unroll
-        for (int i = 0; i < FN; ++i) f.b[i] = __builtin_bit_cast(i4, SB::fragment(stage + SA::kBytes, wc * FN + i, ks, lane));
+        for (int i = 0; i < FN; ++i) f.b[i] = __builtin_bit_cast(i4, SB::fragment(at + SA::kBytes, wc * FN + i, ks, lane));
 #pragma unroll
-        for (int j = 0; j < FM; ++j) f.a[j] = __builtin_bit_cast(i4, SA::fragment(stage, wr * FM + j, ks, lane));
+        for (int j = 0; j < FM; ++j) f.a[j] = __builtin_bit_cast(i4, SA::fragment(at, wr * FM + j, ks, lane));
     };
-    const auto read_scales = [&](Scaled &f, lds_ptr stage, int half) {
+    const auto read_scales = [&](Scaled &f, int stage, int word) {
+        const lds_ptr at = lds + L::kScales + stage / kGroup % 2 * L::Scales::kBytes + stage % kGroup * 8 + word * 4;
         const auto one = [&](lds_ptr at, int t) {
-            return *(__attribute__((address_space(3))) uint32_t *)(at + (t * 32 + (lane & 31)) * 8 + half * 4) >> (lane >> 5) * 8;
+            return *(__attribute__((address_space(3))) uint32_t *)(at + (t * 32 + (lane & 31)) * 32) >> (lane >> 5) * 8;
         };
 #pragma unroll
-        for (int i = 0; i < FN; ++i) f.b[i] = one(stage + L::kCodes + BM * 8, wc * FN + i);
+        for (int i = 0; i < FN; ++i) f.b[i] = one(at + BM * 32, wc * FN + i);
 #pragma unroll
-        for (int j = 0; j < FM; ++j) f.a[j] = one(stage + L::kCodes, wr * FM + j);
+        for (int j = 0; j < FM; ++j) f.a[j] = one(at, wr * FM + j);
     };
     const auto multiply = [&](const Fragments &f, const Scaled &c, auto ks) {
         constexpr int byte = ks % 2 * 2;
@@ -129,31 +120,19 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void k_mx4_tiles(Held oa, Held o
                 acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(f.b[i]), widen(f.a[j]), acc[i][j], kFp4, kFp4, byte, (int)c.b[i], byte, (int)c.a[j]);
     };
 
-    DirectStage<BM, kStageK, false, THREADS> la;
-    DirectStage<BN, kStageK, false, THREADS> lb;
-    ScaleStage<BM, THREADS> sa;
-    ScaleStage<BN, THREADS> sb;
-    // (codes as values of bf16: 4 k each; strides are multiples of 16 bytes)
+    DirectStage<BM, kDeep / 4, false, THREADS> la;
+    DirectStage<BN, kDeep / 4, false, THREADS> lb;
+    typename L::Scales sc;
     la.begin({oa.codes.p, oa.codes.client / 2, oa.codes.row / 2, false, false, 0}, client, m0, s.M, k0 / 4, k1 / 4);
     lb.begin({ob.codes.p, ob.codes.client / 2, ob.codes.row / 2, false, false, 0}, client, n0, s.N, k0 / 4, k1 / 4);
-    sa.begin(oa, client, m0, s.M, k0);
-    sb.begin(ob, client, n0, s.N, k0);
-    const int stages = (k1 - k0 + kDeep - 1) / kDeep, whole = k1 > k0 ? (k1 - k0) / kDeep : 0;
+    sc.begin(oa, ob, client, m0, s.M, n0, s.N, k0, s.K);
+    const int stages = k1 > k0 ? (k1 - k0) / kDeep : 0;
     const auto fetch = [&](int i) {
         const lds_ptr to = lds + i % 2 * L::kStage;
         la.load(to);
         lb.load(to + SA::kBytes);
-        sa.load(to + L::kCodes);
-        sb.load(to + L::kCodes + BM * 8);
     };
-    const auto fetch_end = [&]() {
-        const lds_ptr to = lds + whole % 2 * L::kStage;
-        const int left = k1 - k0 - whole * kDeep;
-        la.load_end(to, left / 4);
-        lb.load_end(to + SA::kBytes, left / 4);
-        sa.load_end(to + L::kCodes, left / 32);
-        sb.load_end(to + L::kCodes + BM * 8, left / 32);
-    };
+    const auto fetch_scales = [&](int g) { sc.load(lds + L::kScales + g % 2 * L::Scales::kBytes); };
     const auto arrived = [&]() {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(0x0070);   // all that is on its way to LDS, and what was read of it
@@ -164,27 +143,29 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void k_mx4_tiles(Held oa, Held o
     // next stage has arrived everywhere and that this one's place may be written again.
     Fragments f[2];
     Scaled c[2];
-    for (int i = 0; i < 2 && i < whole; ++i) fetch(i);
-    if (whole < stages && whole < 2) fetch_end();
-    arrived();
     if (stages > 0) {
-        read(f[0], lds, 0);
-        read_scales(c[0], lds, 0);
+        fetch_scales(0);
+        fetch(0);
+        if (stages > 1) fetch(1);
+        if (stages > kGroup) fetch_scales(1);
+        arrived();
+        read(f[0], 0, 0);
+        read_scales(c[0], 0, 0);
     }
-    // more: there is a stage behind this one; get: sends for the one after that
-    const auto stage = [&](int i, bool more, auto get) {
-        const lds_ptr at = lds + i % 2 * L::kStage, behind = lds + (i + 1) % 2 * L::kStage;
+    // Stage i; more: there is another behind it; get: sends for those that take its place.  (No branch inside: the unit's
+    // instructions and the reads that they want stay mixed.)
+    const auto stage = [&](int i, auto more, auto get) {
         const auto part = [&](auto ks) {
             if constexpr (ks + 1 == KS) {
                 arrived();
-                get();
-                if (more) {
-                    read(f[0], behind, 0);
-                    read_scales(c[0], behind, 0);
+                get(i);
+                if constexpr (more) {
+                    read(f[0], i + 1, 0);
+                    read_scales(c[0], i + 1, 0);
                 }
             } else {
-                read(f[(ks + 1) % 2], at, ks + 1);
-                if constexpr (ks == 1) read_scales(c[1], at, 1);
+                read(f[(ks + 1) % 2], i, ks + 1);
+                if constexpr (ks == 1) read_scales(c[1], i, 1);
             }
             multiply(f[ks % 2], c[ks / 2], ks);
             interleave<FM * FN, FM + FN>();
@@ -194,13 +175,28 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void k_mx4_tiles(Held oa, Held o
         part(std::integral_constant<int, 2>());
         part(std::integral_constant<int, 3>());
     };
-    int i = 0;
-    for (; i + 2 < whole; ++i) stage(i, true, [&]() { fetch(i + 2); });
-    if (i + 2 < stages) {
-        stage(i, true, fetch_end);
-        ++i;
+    static_assert(kGroup == 4 && kUnit == 2 * kDeep, "stages come in twos, scales for four");
+    const auto next = [&](int i) { fetch(i + 2); };
+    const auto none = [](int) {};
+    const int groups = stages > 0 ? (stages - 2) / kGroup : 0;   // with another group or half of one behind them
+    for (int g = 0; g < groups; ++g) {
+        const int i = g * kGroup;
+        stage(i, std::true_type(), next);
+        stage(i + 1, std::true_type(), next);
+        stage(i + 2, std::true_type(), next);
+        stage(i + 3, std::true_type(), [&](int i) {
+            fetch(i + 2);
+            fetch_scales(g);   // the one after the next takes this one's place
+        });
     }
-    for (; i < stages; ++i) stage(i, i + 1 < stages, []() {});
+    if (stages - groups * kGroup == kGroup) {
+        stage(groups * kGroup, std::true_type(), next);
+        stage(groups * kGroup + 1, std::true_type(), next);
+    }
+    if (stages > 0) {
+        stage(stages - 2, std::true_type(), none);
+        stage(stages - 1, std::false_type(), none);
+    }
     __syncthreads();
 
     // A lane has, of row m0 + lane % 32 of a fragment, four columns at a time: through LDS, a wave for itself, to lanes
@@ -345,9 +341,9 @@ static Choice choose(const HeldProduct &p) {
     Choice best = {};
     float least = 0;
     for (const Kind &k : kKinds) {
-        const int64_t tiles = p.clients * ceil_div(p.M, k.bm) * ceil_div(p.N, k.bn), stages = ceil_div(p.K, kDeep);
+        const int64_t tiles = p.clients * ceil_div(p.M, k.bm) * ceil_div(p.N, k.bn), stages = ceil_div(p.K, kUnit) * (kUnit / kDeep);
         const float sums = (float)p.clients * (float)p.M * (float)p.N * 4.0f;
-        for (int64_t slices = 1; slices == 1 || (slices <= 16 && stages / slices >= 2); slices *= 2) {
+        for (int64_t slices = 1; slices == 1 || (slices <= 16 && stages / slices >= 4); slices *= 2) {
             const float waves = (float)ceil_div(tiles * slices, 256);
             const float stage = waves <= k.fit ? k.alone + (waves - 1) * k.more : (k.alone + (k.fit - 1) * k.more) * waves / k.fit;
             float t = (float)ceil_div(stages, slices) * stage + waves * k.end;
@@ -363,11 +359,11 @@ static Choice choose(const HeldProduct &p) {
 
 // Whether the tiles can read an operand as it lies.
 static bool aligned(const Held &o, int64_t K) {
-    return K % 32 == 0 && aligned16(o.codes.p, 1, o.codes.client, o.codes.row) && o.codes.row <= INT64_C(1) << 23 &&
-           ((uintptr_t)o.scales.p | (uintptr_t)o.scales.client | (uintptr_t)o.scales.row) % 4 == 0;
+    return K % kUnit == 0 && aligned16(o.codes.p, 1, o.codes.client, o.codes.row) && o.codes.row <= INT64_C(1) << 23 &&
+           aligned16(o.scales.p, 1, o.scales.client, o.scales.row);
 }
 
-// Copies codes and scales into rows of whole stages: zeros and scales of 1 behind the end.  A thread has 16 bytes of codes.
+// Copies codes and scales into rows of whole units: zeros and scales of 1 behind the end.  A thread has 16 bytes of codes.
 static __global__ __launch_bounds__(256) void k_mx4_lay(Held from, Held to, int64_t n, int rows, int K, int pieces) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, line = i / pieces, client = line / rows;
     if (client >= n) return;
@@ -391,15 +387,15 @@ static __global__ __launch_bounds__(256) void k_mx4_lay(Held from, Held to, int6
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 static int64_t lines_of(const Held &o, int64_t clients, int64_t rows) { return (o.codes.client || o.scales.client ? clients : 1) * rows; }
 static size_t lay_bytes(const Held &o, int64_t clients, int64_t rows, int64_t K) {
-    const int64_t deep = ceil_div(K, kDeep), lines = lines_of(o, clients, rows);
-    return up256((size_t)lines * deep * (kDeep / 2)) + up256((size_t)lines * deep * (kDeep / 32));
+    const int64_t units = ceil_div(K, kUnit), lines = lines_of(o, clients, rows);
+    return up256((size_t)lines * units * (kUnit / 2)) + up256((size_t)lines * units * (kUnit / 32));
 }
 static hipError_t lay(Held &o, int64_t clients, int64_t rows, int64_t K, char *to, hipStream_t s) {
-    const int64_t deep = ceil_div(K, kDeep), lines = lines_of(o, clients, rows), n = lines / rows, pieces = deep * (kDeep / 32), blocks = ceil_div(lines * pieces, 256);
+    const int64_t units = ceil_div(K, kUnit), lines = lines_of(o, clients, rows), n = lines / rows, pieces = units * (kUnit / 32), blocks = ceil_div(lines * pieces, 256);
     if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
     Held d;
-    d.codes = {to, n > 1 ? rows * deep * (kDeep / 2) : 0, deep * (kDeep / 2)};
-    d.scales = {to + up256((size_t)lines * deep * (kDeep / 2)), n > 1 ? rows * deep * (kDeep / 32) : 0, deep * (kDeep / 32)};
+    d.codes = {to, n > 1 ? rows * units * (kUnit / 2) : 0, units * (kUnit / 2)};
+    d.scales = {to + up256((size_t)lines * units * (kUnit / 2)), n > 1 ? rows * units * (kUnit / 32) : 0, units * (kUnit / 32)};
     k_mx4_lay<<<(int)blocks, 256, 0, s>>>(o, d, n, (int)rows, (int)K, (int)pieces);
     o = d;
     return hipGetLastError();
@@ -413,10 +409,10 @@ size_t mx4_product_workspace(const HeldProduct &p) {
            (slices > 1 ? (size_t)slices * p.clients * p.M * p.N * sizeof(float) : 0);
 }
 
-template <typename T, int BM, int BN, int WR, int WC, int OCC>
+template <typename T, int BM, int BN, int WR, int WC>
 static hipError_t run_tiles(const HeldProduct &p, const Shape &s, hipStream_t stream) {
-    const auto kernel = k_mx4_tiles<T, BM, BN, WR, WC, OCC>;
-    constexpr int stages = 2 * HeldTile<BM, BN>::kStage, ends = WR * WC * 32 * (BN / WC + 4) * 4, lds = stages > ends ? stages : ends;
+    const auto kernel = k_mx4_tiles<T, BM, BN, WR, WC>;
+    constexpr int stages = HeldTile<BM, BN, 64 * WR * WC>::kLds, ends = WR * WC * 32 * (BN / WC + 4) * 4, lds = stages > ends ? stages : ends;
     if constexpr (lds > 64 * 1024) {
         static aet::PerDevice allowed;
         int dev = 0, ok = 0;
@@ -458,18 +454,17 @@ static hipError_t run(HeldProduct p, char *workspace, hipStream_t stream) {
         workspace += bytes;
     }
     if (e != hipSuccess) return e;
-    // (what was laid out ends with whole stages, but only as far as both operands do, and the end of a block is zeros there)
-    Shape s = {p.M, p.N, (int)(ceil_div(p.K, 32) * 32)};
+    Shape s = {p.M, p.N, (int)(ceil_div(p.K, kUnit) * kUnit)};
     s.tiles_n = (int)tiles_n;
     s.tiles = (int)tiles;
     s.slices = c.slices;
-    s.slice_k = (int)(ceil_div(ceil_div(p.K, kDeep), c.slices) * kDeep);
+    s.slice_k = (int)(ceil_div(ceil_div(p.K, kUnit), c.slices) * kUnit);
     s.blocks = (int)blocks;
     s.partial = (float *)workspace;
     s.clients = p.clients;
-    if (k.bm == 256) e = run_tiles<T, 256, 256, 2, 4, 2>(p, s, stream);
-    else if (k.bm == 128) e = run_tiles<T, 128, 128, 2, 2, 2>(p, s, stream);
-    else e = run_tiles<T, 64, 64, 2, 2, 4>(p, s, stream);
+    if (k.bm == 256) e = run_tiles<T, 256, 256, 2, 4>(p, s, stream);
+    else if (k.bm == 128) e = run_tiles<T, 128, 128, 2, 2>(p, s, stream);
+    else e = run_tiles<T, 64, 64, 2, 2>(p, s, stream);
     if (e != hipSuccess || s.slices == 1) return e;
     return launch_join(sizeof(T) == 4 ? AET_F32 : AET_BF16, s, p.e, stream);
 }
