@@ -23,11 +23,14 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// A matrix per client in two parts: [client][high, low][rows][cols]
-struct Planes {
+// A matrix per client in two parts, 32 columns of the one next to those of the other, which makes a line of memory:
+// [client][rows][cols / 32][high, low][32].  line: values of a row, 2 cols.
+struct Parts {
     _Float16 *p;
-    int64_t client, low;   // low: from the first part to the second
-    int cols;
+    int64_t client;
+    int line;
+    // of 8 columns from col on; the second parts are 32 further
+    __device__ __forceinline__ _Float16 *at(int64_t c, int row, int col) const { return p + c * client + (int64_t)row * line + col / 32 * 64 + col % 32; }
 };
 
 // high + low = v to within 2^-23 of it
@@ -37,6 +40,20 @@ __device__ __forceinline__ void split_half(const float (&v)[8], half8 &high, hal
         high[e] = (_Float16)v[e];
         low[e] = (_Float16)(v[e] - (float)high[e]);
     }
+}
+
+__device__ __forceinline__ void put_parts(const Parts &x, int64_t client, int row, int col, const float (&v)[8]) {
+    half8 high, low;
+    split_half(v, high, low);
+    _Float16 *const to = x.at(client, row, col);
+    *(half8 *)to = high;
+    *(half8 *)(to + 32) = low;
+}
+__device__ __forceinline__ void get_parts(const Parts &x, int64_t client, int row, int col, float (&v)[8]) {
+    const _Float16 *from = x.at(client, row, col);
+    const half8 high = *(const half8 *)from, low = *(const half8 *)(from + 32);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)high[e] + (float)low[e];
 }
 
 // ---- bounds and scales -------------------------------------------------------------------
@@ -136,12 +153,12 @@ __global__ __launch_bounds__(256) void k_ortho_norm(aet_orthogonal a, Whole w) {
     if (threadIdx.x == 0) w.sums[blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// A tile of 64 x 64 of X per workgroup, from G by rows or columns, through LDS where X is the transpose.
+// A tile of 64 x 64 of G per workgroup, with zeros behind its ends: X or its transpose, and through LDS the other.
 template <typename T>
-__global__ __launch_bounds__(256) void k_ortho_first(aet_orthogonal a, Whole w, Planes x) {
+__global__ __launch_bounds__(256) void k_ortho_first(aet_orthogonal a, Whole w, Parts straight, Parts turned) {
     __shared__ double lds[4];
     __shared__ float tile[64][65];
-    const int across = w.kp / 64, tiles = across * (w.mp / 64);
+    const int rows = w.tall ? w.kp : w.mp, cols = w.tall ? w.mp : w.kp, across = cols / 64, tiles = across * (rows / 64);
     const int64_t client = blockIdx.x / tiles;
     const int t = blockIdx.x % tiles, r0 = t / across * 64, c0 = t % across * 64;
     double sum = threadIdx.x < w.parts ? w.sums[client * w.parts + threadIdx.x] : 0;
@@ -156,35 +173,31 @@ __global__ __launch_bounds__(256) void k_ortho_first(aet_orthogonal a, Whole w, 
     // (values that are not finite: all of X is NaN)
     const double by = own < INFINITY ? (top > 0 ? room_of(top) / norm : 0) : __builtin_nan("");
     const T *g = (const T *)a.g.p + client * a.g.client;
-    if (w.tall) {
-        for (int i = threadIdx.x; i < 64 * 64; i += 256) {
-            const int c = i / 64, r = i % 64;   // of X
-            tile[r][c] = r0 + r < w.m && c0 + c < w.k ? (float)((double)(float)g[(int64_t)(c0 + c) * a.g.row + r0 + r] * by) : 0.0f;
-        }
-        __syncthreads();
-    }
     for (int i = threadIdx.x; i < 64 * 8; i += 256) {
         const int r = i / 8, c = i % 8 * 8;
         float v[8];
-        if (w.tall) {
+        load_some(g + (int64_t)(r0 + r) * a.g.row + c0 + c, r0 + r < a.rows ? a.cols - c0 - c : 0, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = tile[r][c + e];
-        } else {
-            load_some(g + (int64_t)(r0 + r) * a.g.row + c0 + c, r0 + r < w.m ? w.k - c0 - c : 0, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = r0 + r < w.m && c0 + c + e < w.k ? (float)((double)v[e] * by) : 0.0f;
+        for (int e = 0; e < 8; ++e) {
+            v[e] = r0 + r < a.rows && c0 + c + e < a.cols ? (float)((double)v[e] * by) : 0.0f;
+            tile[r][c + e] = v[e];
         }
-        half8 high, low;
-        split_half(v, high, low);
-        _Float16 *const to = x.p + client * x.client + (int64_t)(r0 + r) * x.cols + c0 + c;
-        *(half8 *)to = high;
-        *(half8 *)(to + x.low) = low;
+        if (straight.p) put_parts(straight, client, r0 + r, c0 + c, v);
+    }
+    if (!turned.p) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+        const int c = i / 8, r = i % 8 * 8;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = tile[r + e][c];
+        put_parts(turned, client, c0 + c, r0 + r, v);
     }
 }
 
 // y = keep w + scale X
 template <typename T>
-__global__ __launch_bounds__(256) void k_ortho_last(aet_orthogonal a, Whole w, Planes x) {
+__global__ __launch_bounds__(256) void k_ortho_last(aet_orthogonal a, Whole w, Parts x) {
     __shared__ float tile[64][65];
     const int across = (w.k + 63) / 64, tiles = across * ((w.m + 63) / 64);
     const int64_t client = blockIdx.x / tiles;
@@ -194,10 +207,9 @@ __global__ __launch_bounds__(256) void k_ortho_last(aet_orthogonal a, Whole w, P
     const double by = w.y_by[client];
     const float keep = (float)a.keep;
     const auto value = [&](int r, int c, float (&v)[8]) {
-        const _Float16 *from = x.p + client * x.client + (int64_t)(r0 + r) * x.cols + c0 + c;
-        const half8 high = *(const half8 *)from, low = *(const half8 *)(from + x.low);
+        get_parts(x, client, r0 + r, c0 + c, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (float)(((float)high[e] + (float)low[e]) * by);
+        for (int e = 0; e < 8; ++e) v[e] = (float)(v[e] * by);
     };
     if (w.tall) {
         for (int i = threadIdx.x; i < 64 * 8; i += 256) {
@@ -234,13 +246,16 @@ __global__ __launch_bounds__(256) void k_ortho_last(aet_orthogonal a, Whole w, P
 
 // ---- products ----------------------------------------------------------------------------
 
-// C = by sum over k of A(m, k) B(n, k), plus `plus` times what lies in the same place of `add`, in two parts.
+// C = by sum over k of A(m, k) B(n, k), plus `plus` times what lies in the same place of `add`.
 struct HalfProduct {
-    Planes a, b, c, add;
-    int tiles_m, tiles_n, tiles;   // tiles: of a client; SYM: of the upper half
-    int k, blocks;
-    const float *by, *plus;        // of the first client; steps apart
+    Parts a, b, c, add;
+    Parts turned;             // where C's transpose goes to too; p = NULL: nowhere
+    const float *by, *plus;   // of the first client; `apart` between clients
     int apart;
+    int M, N, K, clients;
+    int tiles_m, tiles_n, tiles;   // tiles: of a client; SYM: of the upper half
+    int slices, slice_k, blocks;   // parts of the sum; partial sums go to `partial` where there are several
+    float *partial;                // [slice][client][M][N]
 };
 
 // The place of tile t of the upper half, row after row, of n x n tiles
@@ -253,20 +268,36 @@ __device__ __forceinline__ void upper_tile(int t, int n, int &i, int &j) {
     j = i + t - (i * n - i * (i - 1) / 2);
 }
 
-// T x T tiles of C, W x W' waves.  SYM: C is symmetric; TB: B by columns.
-template <int T, int BK, int WR, int WC, bool SYM>
+// 8 columns of C from their sums
+__device__ __forceinline__ void finish_half(const HalfProduct &p, int64_t client, int row, int col, float by, float plus, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= by;
+    if (p.add.p) {
+        float o[8];
+        get_parts(p.add, client, row, col, o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(o[e], plus, v[e]);
+    }
+    put_parts(p.c, client, row, col, v);
+}
+
+// T x T tiles of C, WR x WC waves, NB stages of 32 k in use or on their way.  SYM: C is symmetric: only tiles of the upper half are
+// worked out, and are C's other half's when turned.  TB: B by columns, which takes longer to read from LDS (B X of 1024 x 1024 x 1024 21
+// us, with X's transpose by rows 14) but saves making the transpose: for large tiles.
+template <int T, int WR, int WC, int NB, bool SYM, bool TB>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_half(HalfProduct p) {
-    constexpr bool TB = !SYM;
-    constexpr int THREADS = 64 * WR * WC, FM = T / WR / 32, FN = T / WC / 32, KS = BK / 16;
-    using SA = Stage<T, BK, false>;
-    using SB = Stage<T, BK, TB>;
-    constexpr int kPart = SA::kBytes, kStage = 4 * kPart;   // A high, A low, B high, B low
-    static_assert(SA::kBytes == SB::kBytes, "square tiles");
+    constexpr int THREADS = 64 * WR * WC, FM = T / WR / 32, FN = T / WC / 32;
+    // (as values of one part: a line has 32 k of both; by columns a row of the stage has T columns of both)
+    using SA = Stage<T, 64, false>;
+    using SB = std::conditional_t<TB, Stage<2 * T, 32, true>, Stage<T, 64, false>>;
+    constexpr int kStage = SA::kBytes + SB::kBytes;
     extern __shared__ __attribute__((aligned(1024))) char lds_[];
     const lds_ptr lds = (lds_ptr)lds_;
-    const int id = xcd_order(blockIdx.x, p.blocks);
-    const int64_t client = id / p.tiles;
+    int id = xcd_order(blockIdx.x, p.blocks);
     const int tile = id % p.tiles;
+    id /= p.tiles;
+    const int slice = id % p.slices;
+    const int64_t client = id / p.slices;
     int ti, tj;
     if constexpr (SYM) {
         upper_tile(tile, p.tiles_m, ti, tj);
@@ -275,73 +306,87 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_half(HalfProduct p) {
         ti = group + in % high;
         tj = in / high;
     }
-    const int m0 = ti * T, n0 = tj * T;
+    const int m0 = ti * T, n0 = tj * T, k0 = slice * p.slice_k, k1 = k0 + p.slice_k < p.K ? k0 + p.slice_k : p.K;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wr = wave / WC, wc = wave % WC;
 
-    DirectStage<T, BK, false, THREADS> la, la2;
-    DirectStage<T, BK, TB, THREADS> lb, lb2;
-    la.begin({p.a.p, p.a.client, p.a.cols, false, true, 0}, client, m0, 1 << 30, 0, 0);
-    lb.begin({p.b.p, p.b.client, p.b.cols, TB, true, 0}, client, n0, 1 << 30, 0, 0);
-    la2 = la;
-    lb2 = lb;
-    la2.p += p.a.low * 2;
-    lb2.p += p.b.low * 2;
+    DirectStage<T, 64, false, THREADS> la;
+    std::conditional_t<TB, DirectStage<2 * T, 32, true, THREADS>, DirectStage<T, 64, false, THREADS>> lb;
+    la.begin({p.a.p, p.a.client, p.a.line, false, true, 0}, client, m0, 1 << 30, 2 * k0, 0);
+    lb.begin({p.b.p, p.b.client, p.b.line, TB, true, 0}, client, TB ? 2 * n0 : n0, 1 << 30, TB ? k0 : 2 * k0, 0);
     const auto fetch = [&](int i) {
-        const lds_ptr to = lds + i % 2 * kStage;
+        const lds_ptr to = lds + i % NB * kStage;
         la.load(to);
-        la2.load(to + kPart);
-        lb.load(to + 2 * kPart);
-        lb2.load(to + 3 * kPart);
+        lb.load(to + SA::kBytes);
     };
-    const float by = p.by[client * p.apart], plus = p.plus ? p.plus[client * p.apart] : 0.0f;
+    struct Fragments {
+        half8 a[FM][2], b[FN][2];
+    };
+    const auto read = [&](Fragments &f, int stage, int ks) {
+        const lds_ptr at = lds + stage % NB * kStage;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+                f.b[i][q] = __builtin_bit_cast(half8, TB ? SB::fragment(at + SA::kBytes, 2 * (wc * FN + i) + q, ks, lane) : SB::fragment(at + SA::kBytes, wc * FN + i, ks + 2 * q, lane));
+#pragma unroll
+            for (int j = 0; j < FM; ++j) f.a[j][q] = __builtin_bit_cast(half8, SA::fragment(at, wr * FM + j, ks + 2 * q, lane));
+        }
+    };
     f16v acc[FN][FM];
 #pragma unroll
     for (int i = 0; i < FN; ++i)
 #pragma unroll
         for (int j = 0; j < FM; ++j) acc[i][j] = f16v{};
-    const int stages = p.k / BK;
-    fetch(0);
-    for (int s = 0; s < stages; ++s) {
+    const auto multiply = [&](const Fragments &f) {
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+#pragma unroll
+                for (int j = 0; j < FM; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.b[i][q == 0], f.a[j][q == 1], acc[i][j], 0, 0, 0);
+    };
+    // All but the last `still` of what is on its way to LDS has arrived, and what was read of it, everywhere.
+    const auto arrived = [&](auto still) {
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0070);   // all that is on its way to LDS, and what was read of it
+        __builtin_amdgcn_s_waitcnt(0x0070 | (still & 15) | (still >> 4) << 14);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (s + 1 < stages) fetch(s + 1);
-        const lds_ptr at = lds + s % 2 * kStage;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            half8 a[FM][2], b[FN][2];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-#pragma unroll
-                for (int i = 0; i < FN; ++i) b[i][q] = __builtin_bit_cast(half8, SB::fragment(at + (2 + q) * kPart, wc * FN + i, ks, lane));
-#pragma unroll
-                for (int j = 0; j < FM; ++j) a[j][q] = __builtin_bit_cast(half8, SA::fragment(at + q * kPart, wr * FM + j, ks, lane));
-            }
-#pragma unroll
-            for (int q = 0; q < 3; ++q)
-#pragma unroll
-                for (int i = 0; i < FN; ++i)
-#pragma unroll
-                    for (int j = 0; j < FM; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(b[i][q == 0], a[j][q == 1], acc[i][j], 0, 0, 0);
-        }
-    }
+    };
+    // The fragments of the next 16 k are read while the matrix unit has the last ones, also across the barrier that says that the
+    // next stage has arrived everywhere and that this one's place may be written again.
+    const int stages = (k1 - k0) / 32;
+    constexpr int kLoads = decltype(la)::kCount + decltype(lb)::kCount, kReads = 2 * ((TB ? 2 : 1) * FN + FM);
+    typedef std::integral_constant<int, 0> None;
+    Fragments f[2];
+    for (int i = 0; i < NB && i < stages; ++i) fetch(i);
+    if (stages >= NB) arrived(std::integral_constant<int, (NB - 1) * kLoads>());
+    else arrived(None());
+    read(f[0], 0, 0);
+    const auto stage = [&](int i, auto more, auto still, auto get) {
+        read(f[1], i, 1);
+        multiply(f[0]);
+        interleave<3 * FM * FN, kReads>();
+        arrived(still);
+        get(i);
+        if constexpr (more) read(f[0], i + 1, 0);
+        multiply(f[1]);
+        interleave<3 * FM * FN, kReads>();
+    };
+    int i = 0;
+    for (; i + NB < stages; ++i) stage(i, std::true_type(), std::integral_constant<int, (NB - 2) * kLoads>(), [&](int i) { fetch(i + NB); });
+    for (; i + 1 < stages; ++i) stage(i, std::true_type(), None(), [](int) {});
+    stage(i, std::false_type(), None(), [](int) {});
     __syncthreads();
 
     // A lane has, of row m0 + lane % 32 of a fragment, four columns at a time: through LDS, a wave for itself, to lanes with 8 columns.
     constexpr int W = FN * 32, LINE = W + 4, ACROSS = W / 8, DOWN = 64 / ACROSS;
     __attribute__((address_space(3))) float *mine = (__attribute__((address_space(3))) float *)lds + wave * (32 * LINE);
+    const float by = p.by[client * p.apart], plus = p.plus ? p.plus[client * p.apart] : 0.0f;
+    const bool turn = p.turned.p && !(SYM && ti == tj) && p.slices == 1;
     const auto settle = [&]() {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
-    };
-    const auto put = [&](const float (&v)[8], int row, int col) {
-        half8 high, low;
-        split_half(v, high, low);
-        _Float16 *const to = p.c.p + client * p.c.client + (int64_t)row * p.c.cols + col;
-        *(half8 *)to = high;
-        *(half8 *)(to + p.c.low) = low;
     };
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
@@ -351,7 +396,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_half(HalfProduct p) {
             for (int q = 0; q < 4; ++q) {
                 f4 v;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) v[x] = acc[i][j][4 * q + x] * by;
+                for (int x = 0; x < 4; ++x) v[x] = acc[i][j][4 * q + x];
                 *(__attribute__((address_space(3))) f4 *)(mine + (lane & 31) * LINE + i * 32 + 8 * q + 4 * (lane >> 5)) = v;
             }
         settle();
@@ -363,47 +408,115 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_half(HalfProduct p) {
             __attribute__((address_space(3))) f4 *const at = (__attribute__((address_space(3))) f4 *)(mine + line * LINE + c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = at[e / 4][e % 4];
-            if (p.add.p) {
-                const _Float16 *from = p.add.p + client * p.add.client + (int64_t)(row0 + line) * p.add.cols + col0 + c;
-                const half8 high = *(const half8 *)from, low = *(const half8 *)(from + p.add.low);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf((float)high[e] + (float)low[e], plus, v[e]);
-                if (SYM && ti != tj) {
-                    at[0] = f4{v[0], v[1], v[2], v[3]};
-                    at[1] = f4{v[4], v[5], v[6], v[7]};
-                }
+            if (p.slices > 1) {
+                float *const to = p.partial + (((int64_t)slice * p.clients + client) * p.M + row0 + line) * p.N + col0 + c;
+                *(f4 *)to = f4{v[0], v[1], v[2], v[3]};
+                *(f4 *)(to + 4) = f4{v[4], v[5], v[6], v[7]};
+                continue;
             }
-            put(v, row0 + line, col0 + c);
+            finish_half(p, client, row0 + line, col0 + c, by, plus, v);
+            if (turn) {
+                at[0] = f4{v[0], v[1], v[2], v[3]};
+                at[1] = f4{v[4], v[5], v[6], v[7]};
+            }
         }
-        if (SYM && ti != tj) {   // the same values on the other side
+        if (turn) {
             settle();
 #pragma unroll 1
             for (int c = lane / 4; c < W; c += 16) {
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = mine[(lane % 4 * 8 + e) * LINE + c];
-                put(v, col0 + c, row0 + lane % 4 * 8);
+                put_parts(p.turned, client, col0 + c, row0 + lane % 4 * 8, v);
             }
         }
         settle();
     }
 }
 
+// Adds the slices of a split sum, in their order, and ends it: 64 x 64 of C a workgroup.
+template <bool SYM>
+__global__ __launch_bounds__(256) void k_half_join(HalfProduct p, int tiles) {
+    __shared__ float turned[64][65];
+    const int64_t client = blockIdx.x / tiles;
+    const int tile = blockIdx.x % tiles, across = p.N / 64;
+    int ti = tile / across, tj = tile % across;
+    if constexpr (SYM) upper_tile(tile, across, ti, tj);
+    const float by = p.by[client * p.apart], plus = p.plus ? p.plus[client * p.apart] : 0.0f;
+#pragma unroll
+    for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+        const int r = i / 8, c = i % 8 * 8;
+        float v[8] = {};
+        const float *from = p.partial + (client * p.M + ti * 64 + r) * p.N + tj * 64 + c;
+        for (int k = 0; k < p.slices; ++k, from += (int64_t)p.clients * p.M * p.N) {
+            const f4 x = *(const f4 *)from, y = *(const f4 *)(from + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] += x[e];
+                v[4 + e] += y[e];
+            }
+        }
+        finish_half(p, client, ti * 64 + r, tj * 64 + c, by, plus, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) turned[c + e][r] = v[e];
+    }
+    if (!p.turned.p || (SYM && ti == tj)) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+        const int r = i / 8, c = i % 8 * 8;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = turned[r][c + e];
+        put_parts(p.turned, client, tj * 64 + r, ti * 64 + c, v);
+    }
+}
+
 // ---- the steps ---------------------------------------------------------------------------
 
+// Kinds of tiles: microseconds for 32 k where a compute unit has one workgroup (`busy`: more when all units have one), for each further
+// one up to the `fit` that it holds, and for a workgroup's beginning and end.  Measured on products of 64 to 4096.
 struct Kind {
-    int tile;
-    float stage, end;   // microseconds of 32 k of all workgroups that a compute unit holds, and of an epilogue
-    int fit;
+    int tile, deep, fit;
+    float alone, busy, more, end;
 };
-static const Kind kKinds[] = {{256, 1.9f, 8.0f, 1}, {128, 1.1f, 3.0f, 2}, {64, 0.8f, 2.0f, 4}};
+static const Kind kKinds[] = {{256, 2, 1, 1.7f, 0.8f, 0.0f, 8.0f}, {128, 2, 2, 0.58f, 0.2f, 0.62f, 5.0f}, {64, 4, 2, 0.22f, 0.0f, 0.13f, 3.5f}, {64, 2, 4, 0.42f, 0.0f, 0.11f, 3.5f}};
+struct Choice {
+    const Kind *kind;
+    int slices;
+    float time;
+};
+static Choice choose(int64_t clients, int64_t M, int64_t N, int64_t K, bool sym) {
+    Choice best = {};
+    for (const Kind &k : kKinds) {
+        if (M % k.tile || N % k.tile) continue;
+        const int64_t tm = M / k.tile, tiles = clients * (sym ? tm * (tm + 1) / 2 : tm * (N / k.tile)), stages = K / 32;
+        // what is read and written beside the operands, at 5 TB/s: 4 bytes of each place a value
+        const float ends = (float)clients * (float)M * (float)N * (sym ? 8 : k.tile == 256 ? 8 : 12) / 5e6f;
+        for (int64_t slices = 1; slices == 1 || (slices <= 32 && stages / slices >= 4); slices *= 2) {
+            const int64_t blocks = tiles * slices;
+            const float waves = blocks <= 256 ? 1.0f : (float)ceil_div(blocks, 128) * 0.5f, fit = (float)k.fit;
+            const float alone = k.alone + k.busy * (blocks < 256 ? (float)blocks / 256 : 1.0f);
+            const float stage = waves <= fit ? alone + (waves - 1) * k.more : (alone + (fit - 1) * k.more) * waves / fit;
+            float t = (float)ceil_div(stages, slices) * stage;
+            // the L2s bring operands at some 12.7 TB/s
+            const float bring = (float)blocks * (float)ceil_div(stages, slices) * (float)(256 * k.tile) / 12.7e6f;
+            t = (t > bring ? t : bring) + k.end + ends;
+            // partial sums are written and read at about 6 TB/s, and the launch that adds them takes 5
+            if (slices > 1) t += 5.0f + (float)blocks * (float)(8 * k.tile * k.tile) / 6e6f;
+            if (!best.kind || t < best.time) best = {&k, (int)slices, t};
+        }
+    }
+    return best;
+}
 
 static int64_t up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
 
 struct OrthoPlan {
     Whole w;
-    const Kind *kind;
-    Planes x[2], a, b;
+    Choice gram, square, times;   // X X^T, A A, B X
+    Parts x[2], xt[2], a, b;   // xt: X's transpose, where B X wants that
+    bool turned() const { return times.kind->tile < 256; }
+    float *partial;
     size_t bytes;
 };
 static OrthoPlan plan(const aet_orthogonal &o, char *workspace) {
@@ -411,50 +524,61 @@ static OrthoPlan plan(const aet_orthogonal &o, char *workspace) {
     p.w.tall = o.rows > o.cols;
     p.w.m = p.w.tall ? o.cols : o.rows;
     p.w.k = p.w.tall ? o.rows : o.cols;
+    // sides up to whole tiles of one kind, the one that is the fastest in all
     float best = 0;
     for (const Kind &k : kKinds) {
-        const int64_t tm = ceil_div(p.w.m, k.tile), tk = ceil_div(p.w.k, k.tile);
-        const auto time = [&](int64_t tiles, int64_t sum) { return (float)ceil_div(tiles * o.n, 256 * k.fit) * ((float)ceil_div(sum, 32) * k.stage + k.end); };
-        const int64_t half = tm * (tm + 1) / 2;
-        const float t = time(half, tk * k.tile) + time(half, tm * k.tile) + time(tm * tk, tm * k.tile);
-        if (!p.kind || t < best) {
-            best = t;
-            p.kind = &k;
-        }
+        const int64_t mp = up(p.w.m, k.tile), kp = up(p.w.k, k.tile);
+        const Choice g = choose(o.n, mp, mp, kp, true), q = choose(o.n, mp, mp, mp, true), t = choose(o.n, mp, kp, mp, false);
+        const float time = g.time + q.time + t.time;
+        if (p.gram.kind && time >= best) continue;
+        best = time;
+        p.w.mp = (int)mp;
+        p.w.kp = (int)kp;
+        p.gram = g;
+        p.square = q;
+        p.times = t;
     }
-    p.w.mp = (int)up(p.w.m, p.kind->tile);
-    p.w.kp = (int)up(p.w.k, p.kind->tile);
     // parts of the sum of squares: some 2048 workgroups, each with values for its threads
     const int64_t pieces = ceil_div(o.cols, o.dtype == AET_F32 ? 4 : 8) * o.rows, wanted = ceil_div(2048, o.n > 0 ? o.n : 1);
     p.w.parts = (int)(wanted < 256 ? wanted : 256);
     if (p.w.parts > ceil_div(pieces, 256)) p.w.parts = (int)ceil_div(pieces, 256);
     size_t at = 0;
-    const auto planes = [&](int64_t rows, int64_t cols) {
-        const Planes q = {(_Float16 *)(workspace + at), 2 * rows * cols, rows * cols, (int)cols};
-        at += up256((size_t)o.n * 2 * rows * cols * sizeof(_Float16));
+    const auto take = [&](size_t bytes) {
+        char *const q = workspace + at;
+        at += up256(bytes);
         return q;
     };
-    p.x[0] = planes(p.w.mp, p.w.kp);
+    const auto parts = [&](int64_t rows, int64_t cols) {
+        return Parts{(_Float16 *)take((size_t)o.n * 2 * rows * cols * sizeof(_Float16)), 2 * rows * cols, (int)(2 * cols)};
+    };
+    p.x[0] = parts(p.w.mp, p.w.kp);
     if (o.steps) {
-        p.x[1] = planes(p.w.mp, p.w.kp);
-        p.a = planes(p.w.mp, p.w.mp);
-        p.b = planes(p.w.mp, p.w.mp);
+        p.x[1] = parts(p.w.mp, p.w.kp);
+        if (p.turned()) for (Parts &t : p.xt) t = parts(p.w.kp, p.w.mp);
+        p.a = parts(p.w.mp, p.w.mp);
+        p.b = parts(p.w.mp, p.w.mp);
+        int64_t most = 0;
+        const auto split = [&](const Choice &c, int64_t cols) {
+            const int64_t values = c.slices > 1 ? c.slices * p.w.mp * cols : 0;
+            most = values > most ? values : most;
+        };
+        split(p.gram, p.w.mp);
+        split(p.square, p.w.mp);
+        split(p.times, p.w.kp);
+        p.partial = (float *)take((size_t)o.n * most * sizeof(float));
     }
-    p.w.sums = (double *)(workspace + at);
-    at += up256((size_t)o.n * p.w.parts * sizeof(double));
-    p.w.scales = (Scales *)(workspace + at);
-    at += up256((size_t)o.n * o.steps * sizeof(Scales));
-    p.w.y_by = (double *)(workspace + at);
-    at += up256((size_t)o.n * sizeof(double));
+    p.w.sums = (double *)take((size_t)o.n * p.w.parts * sizeof(double));
+    p.w.scales = (Scales *)take((size_t)o.n * o.steps * sizeof(Scales));
+    p.w.y_by = (double *)take((size_t)o.n * sizeof(double));
     p.bytes = at;
     return p;
 }
 size_t orthogonal_workspace(const aet_orthogonal &o) { return plan(o, nullptr).bytes; }
 
-template <int T, int BK, int WR, int WC, bool SYM>
+template <int T, int WR, int WC, int NB, bool SYM, bool TB>
 static hipError_t run_half(const HalfProduct &p, hipStream_t stream) {
-    const auto kernel = k_half<T, BK, WR, WC, SYM>;
-    constexpr int stages = 2 * 4 * T * BK * 2, FN = T / WC / 32, ends = WR * WC * 32 * (FN * 32 + 4) * 4, lds = stages > ends ? stages : ends;
+    const auto kernel = k_half<T, WR, WC, NB, SYM, TB>;
+    constexpr int stages = NB * 2 * T * 128, ends = WR * WC * 32 * (T / WC + 4) * 4, lds = stages > ends ? stages : ends;
     if constexpr (lds > 64 * 1024) {
         static aet::PerDevice allowed;
         int dev = 0, ok = 0;
@@ -469,19 +593,26 @@ static hipError_t run_half(const HalfProduct &p, hipStream_t stream) {
     kernel<<<p.blocks, 64 * WR * WC, lds, stream>>>(p);
     return hipGetLastError();
 }
-// sym: C and A = B are symmetric, or A = B and C = A A^T; else B is by columns
-static hipError_t product(const OrthoPlan &plan, int64_t n, HalfProduct p, int64_t M, int64_t N, int64_t K, bool sym, hipStream_t s) {
-    const int t = plan.kind->tile;
-    const int64_t tm = M / t, tn = N / t, tiles = sym ? tm * (tm + 1) / 2 : tm * tn;
-    if (tiles * n > INT32_MAX) return hipErrorInvalidConfiguration;
+template <bool SYM>   // SYM: A = B
+static hipError_t product(const Choice &c, HalfProduct p, hipStream_t s) {
+    const int t = c.kind->tile;
+    const int64_t tm = p.M / t, tn = p.N / t, tiles = SYM ? tm * (tm + 1) / 2 : tm * tn;
+    const int64_t am = p.M / 64, joins = SYM ? am * (am + 1) / 2 : am * (p.N / 64);
+    if (tiles * p.clients * c.slices > INT32_MAX || joins * p.clients > INT32_MAX) return hipErrorInvalidConfiguration;
     p.tiles_m = (int)tm;
     p.tiles_n = (int)tn;
     p.tiles = (int)tiles;
-    p.blocks = (int)(tiles * n);
-    p.k = (int)K;
-    if (t == 256) return sym ? run_half<256, 32, 2, 4, true>(p, s) : run_half<256, 32, 2, 4, false>(p, s);
-    if (t == 128) return sym ? run_half<128, 32, 2, 2, true>(p, s) : run_half<128, 32, 2, 2, false>(p, s);
-    return sym ? run_half<64, 32, 2, 2, true>(p, s) : run_half<64, 32, 2, 2, false>(p, s);
+    p.slices = c.slices;
+    p.slice_k = (int)ceil_div(p.K / 32, c.slices) * 32;
+    p.slices = (int)ceil_div(p.K, p.slice_k);
+    p.blocks = (int)(tiles * p.clients * p.slices);
+    hipError_t e;
+    if (t == 256) e = run_half<256, 2, 4, 2, SYM, !SYM>(p, s);
+    else if (t == 128) e = run_half<128, 2, 2, 2, SYM, false>(p, s);
+    else e = c.kind->deep == 2 ? run_half<64, 2, 2, 2, SYM, false>(p, s) : run_half<64, 2, 2, 4, SYM, false>(p, s);
+    if (e != hipSuccess || p.slices == 1) return e;
+    k_half_join<SYM><<<(int)(joins * p.clients), 256, 0, s>>>(p, (int)joins);
+    return hipGetLastError();
 }
 
 template <typename T>
@@ -491,15 +622,22 @@ static hipError_t run(const aet_orthogonal &o, char *workspace, hipStream_t s) {
                   lasts = (int64_t)o.n * ceil_div(p.w.m, 64) * ceil_div(p.w.k, 64);
     if (norms > INT32_MAX || firsts > INT32_MAX) return hipErrorInvalidConfiguration;
     k_ortho_norm<T><<<(int)norms, 256, 0, s>>>(o, p.w);
-    k_ortho_first<T><<<(int)firsts, 256, 0, s>>>(o, p.w, p.x[0]);
+    k_ortho_first<T><<<(int)firsts, 256, 0, s>>>(o, p.w, p.w.tall ? p.xt[0] : p.x[0], p.w.tall ? p.x[0] : p.xt[0]);
     hipError_t e = hipGetLastError();
     for (int i = 0; i < o.steps && e == hipSuccess; ++i) {
-        const Planes &x = p.x[i % 2], &y = p.x[(i + 1) % 2], none = {};
+        const int now = i % 2, next = now ^ 1, apart = o.steps * (int)(sizeof(Scales) / sizeof(float)), mp = p.w.mp, kp = p.w.kp;
+        const Parts &x = p.x[now], none = {};
         const Scales *by = p.w.scales + i;
-        const int apart = o.steps * (int)(sizeof(Scales) / sizeof(float));
-        e = product(p, o.n, {x, x, p.a, none, 0, 0, 0, 0, 0, &by->a_by, nullptr, apart}, p.w.mp, p.w.mp, p.w.kp, true, s);
-        if (e == hipSuccess) e = product(p, o.n, {p.a, p.a, p.b, p.a, 0, 0, 0, 0, 0, &by->b_by, &by->b_plus, apart}, p.w.mp, p.w.mp, p.w.mp, true, s);
-        if (e == hipSuccess) e = product(p, o.n, {p.b, x, y, x, 0, 0, 0, 0, 0, &by->x_by, &by->x_plus, apart}, p.w.mp, p.w.kp, p.w.mp, false, s);
+        const auto of = [&](const Parts &a, const Parts &b, const Parts &c, const Parts &add, const Parts &turned, const float *times, const float *plus, int N,
+                            int K) {
+            HalfProduct h = {a, b, c, add, turned, times, plus, apart, mp, N, K, o.n};
+            h.partial = p.partial;
+            return h;
+        };
+        e = product<true>(p.gram, of(x, x, p.a, none, p.a, &by->a_by, nullptr, mp, kp), s);
+        if (e == hipSuccess) e = product<true>(p.square, of(p.a, p.a, p.b, p.a, p.b, &by->b_by, &by->b_plus, mp, mp), s);
+        if (e == hipSuccess)
+            e = product<false>(p.times, of(p.b, p.turned() ? p.xt[now] : x, p.x[next], x, i + 1 < o.steps ? p.xt[next] : none, &by->x_by, &by->x_plus, kp, mp), s);
     }
     if (e != hipSuccess) return e;
     k_ortho_last<T><<<(int)lasts, 256, 0, s>>>(o, p.w, p.x[o.steps % 2]);
