@@ -9,6 +9,12 @@
 // 4e-7 to 3e-6 where products in fp32 give 1e-6 to 2e-5; with one fp16 value 1e-3 to 3e-3, with one bf16 value 5e-3 to 2e-2,
 // as much as or more than the rounding of a bf16 result (1.7e-3).
 //
+// Where X is wide and the result bf16, several steps go by the matrices of m x m alone: X X^T once, then with P = a + b A + c A A
+// of each step Q <- Q P and A <- (A P) P, all of them polynomials of the first A, which commute and are symmetric; at the end
+// X <- Q X.  What A is off by is not corrected there, and grows as the square of what small singular values do, so X is worked out in
+// between where that has come to 2e3.  Relative 2-norm against 64 bits before the result is rounded, gradients of rank 2 to 512 with bf16's
+// noise, five steps (two such runs): 1e-5 to 6e-5; step by step 4e-6 to 3e-5, with products in fp32 6e-6 to 5e-5 (a run of all five: 3e-2).
+//
 // All matrices of a call lie in the workspace with zeros up to whole tiles, so that no product has to look where they end.
 #include <math.h>
 
@@ -102,19 +108,69 @@ __device__ inline double room_of(double bound) {
     return ldexp(1.0, 15 - e);
 }
 
+// The largest |a + b q + c q^2| over q in [0, top^2]: how much a step makes of a singular value, at most
+__host__ __device__ inline double most_growth(double a, double b, double c, double top) {
+    const auto p = [&](double q) { return fabs(a + q * (b + q * c)); };
+    double most = fmax(p(0), p(top * top));
+    if (c != 0) {
+        const double q = -b / (2 * c);
+        if (q > 0 && q < top * top) most = fmax(most, p(q));
+    }
+    return kRoom * most;
+}
+
 // What the products of a step multiply by, with the scales of what they take and make.
 struct Scales {
-    float a_by, b_by, b_plus, x_by, x_plus;
+    float a_by;                                     // A = X X^T
+    float b_by, b_plus, x_plus;                     // a step by itself: B = b A + c A A, X = a X + B X
+    float p_by, p_plus, p_diagonal;                 // several by A alone: P
+    float q_by, t_by, n_by;                         // Q P, A P, (A P) P
+    float x_by;                                     // B X or Q X
+};
+// The steps in runs that go by A alone: where a run ends.  (A run of one step is a step by itself.)
+struct Runs {
+    uint64_t ends[2];
+    __host__ __device__ bool end(int i) const { return ends[i / 64] >> (i % 64) & 1; }
 };
 // Of a client whose X begins with singular values up to x; the last X's own scale is taken out of *y_by.
-__device__ inline void scales_of(const aet_orthogonal &o, double x, Scales *to, double *y_by) {
-    double sx = room_of(x);
+__device__ inline void scales_of(const aet_orthogonal &o, const Runs &runs, double x, Scales *to, double *y_by) {
+    double sx = room_of(x), sa = 0, q = 0, sq = 0;
+    bool first = true;   // of a run
     for (int i = 0; i < o.steps; ++i) {
         const Bounds b = bounds_of(o, x);
-        const double sa = room_of(b.a), sb = room_of(b.b), next = room_of(b.next);
-        to[i] = {(float)(sa / (sx * sx)), (float)(o.c * sb / (sa * sa)), (float)(o.b * sb / sa), (float)(next / (sb * sx)), (float)(o.a * next / sx)};
+        const double next = room_of(b.next);
+        Scales t = {};
+        if (first) {
+            sa = room_of(b.a);
+            t.a_by = (float)(sa / (sx * sx));
+        }
+        if (first && runs.end(i)) {
+            const double sb = room_of(b.b);
+            t.b_by = (float)(o.c * sb / (sa * sa));
+            t.b_plus = (float)(o.b * sb / sa);
+            t.x_by = (float)(next / (sb * sx));
+            t.x_plus = (float)(o.a * next / sx);
+            sx = next;
+        } else {
+            const double p = most_growth(o.a, o.b, o.c, x), sp = room_of(p), st = room_of(x * b.next), sn = room_of(b.next * b.next);
+            t.p_by = (float)(o.c * sp / (sa * sa));
+            t.p_plus = (float)(o.b * sp / sa);
+            t.p_diagonal = (float)(o.a * sp);
+            const double more = first ? p : kRoom * q * p, s = first ? sp : room_of(more);
+            t.q_by = first ? 0.0f : (float)(s / (sq * sp));
+            t.t_by = (float)(st / (sa * sp));
+            t.n_by = (float)(sn / (st * sp));
+            q = more;
+            sq = s;
+            sa = sn;
+            if (runs.end(i)) {
+                t.x_by = (float)(next / (sq * sx));
+                sx = next;
+            }
+        }
+        to[i] = t;
+        first = runs.end(i);
         x = b.next;
-        sx = next;
     }
     *y_by = o.scale / sx;
 }
@@ -126,6 +182,7 @@ struct Whole {
     int mp, kp;         // with the zeros
     bool tall;          // X is G's transpose
     int parts;          // of the sum of squares
+    Runs runs;
     double *sums;       // [client][parts]
     Scales *scales;     // [client][steps]
     double *y_by;       // [client]
@@ -169,7 +226,7 @@ __global__ __launch_bounds__(256) void k_ortho_first(aet_orthogonal a, Whole w, 
     const double own = __builtin_sqrt((lds[0] + lds[1]) + (lds[2] + lds[3])), norm = own + a.eps;
     // singular values are at most the norm's share of norm + eps, and the scales go by that: also a gradient far below eps keeps its bits
     const double top = own > 0 && norm < INFINITY ? kRoom * own / norm : 0;
-    if (t == 0 && threadIdx.x == 0) scales_of(a, top, w.scales + client * a.steps, w.y_by + client);
+    if (t == 0 && threadIdx.x == 0) scales_of(a, w.runs, top, w.scales + client * a.steps, w.y_by + client);
     // (values that are not finite: all of X is NaN)
     const double by = own < INFINITY ? (top > 0 ? room_of(top) / norm : 0) : __builtin_nan("");
     const T *g = (const T *)a.g.p + client * a.g.client;
@@ -246,13 +303,17 @@ __global__ __launch_bounds__(256) void k_ortho_last(aet_orthogonal a, Whole w, P
 
 // ---- products ----------------------------------------------------------------------------
 
-// C = by sum over k of A(m, k) B(n, k), plus `plus` times what lies in the same place of `add`.
-struct HalfProduct {
+// C = by sum over k of A(m, k) B(n, k), plus `plus` times what lies in the same place of `add`, plus `diagonal` where row and column
+// are the same; or two products of the same sizes in one launch.
+struct Side {
     Parts a, b, c, add;
-    Parts turned;             // where C's transpose goes to too; p = NULL: nowhere
-    const float *by, *plus;   // of the first client; `apart` between clients
-    int apart;
-    int M, N, K, clients;
+    Parts turned;                           // where C's transpose goes to too; p = NULL: nowhere
+    const float *by, *plus, *diagonal;      // of the first client; `apart` between clients; plus, diagonal: or NULL
+};
+struct HalfProduct {
+    Side side[2];
+    int each, apart;               // clients of a side
+    int M, N, K, clients;          // clients: of all sides
     int tiles_m, tiles_n, tiles;   // tiles: of a client; SYM: of the upper half
     int slices, slice_k, blocks;   // parts of the sum; partial sums go to `partial` where there are several
     float *partial;                // [slice][client][M][N]
@@ -268,17 +329,25 @@ __device__ __forceinline__ void upper_tile(int t, int n, int &i, int &j) {
     j = i + t - (i * n - i * (i - 1) / 2);
 }
 
+// What C's sums are multiplied with
+struct Factors {
+    float by, plus, diagonal;
+    __device__ __forceinline__ Factors(const Side &d, int64_t at) : by(d.by[at]), plus(d.plus ? d.plus[at] : 0.0f), diagonal(d.diagonal ? d.diagonal[at] : 0.0f) {}
+};
 // 8 columns of C from their sums
-__device__ __forceinline__ void finish_half(const HalfProduct &p, int64_t client, int row, int col, float by, float plus, float (&v)[8]) {
+__device__ __forceinline__ void finish_half(const Side &d, int64_t client, int row, int col, const Factors &f, float (&v)[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= by;
-    if (p.add.p) {
+    for (int e = 0; e < 8; ++e) v[e] *= f.by;
+    if (d.add.p) {
         float o[8];
-        get_parts(p.add, client, row, col, o);
+        get_parts(d.add, client, row, col, o);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(o[e], plus, v[e]);
+        for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(o[e], f.plus, v[e]);
     }
-    put_parts(p.c, client, row, col, v);
+    if (d.diagonal)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += row == col + e ? f.diagonal : 0.0f;
+    put_parts(d.c, client, row, col, v);
 }
 
 // T x T tiles of C, WR x WC waves, NB stages of 32 k in use or on their way.  SYM: C is symmetric: only tiles of the upper half are
@@ -296,8 +365,10 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_half(HalfProduct p) {
     int id = xcd_order(blockIdx.x, p.blocks);
     const int tile = id % p.tiles;
     id /= p.tiles;
-    const int slice = id % p.slices;
-    const int64_t client = id / p.slices;
+    const int slice = id % p.slices, all = id / p.slices;   // all: the client's number among those of all sides
+    const Side &d = p.side[all >= p.each];
+    const int64_t client = all >= p.each ? all - p.each : all;
+    const Factors factors(d, client * p.apart);
     int ti, tj;
     if constexpr (SYM) {
         upper_tile(tile, p.tiles_m, ti, tj);
@@ -311,8 +382,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_half(HalfProduct p) {
 
     DirectStage<T, 64, false, THREADS> la;
     std::conditional_t<TB, DirectStage<2 * T, 32, true, THREADS>, DirectStage<T, 64, false, THREADS>> lb;
-    la.begin({p.a.p, p.a.client, p.a.line, false, true, 0}, client, m0, 1 << 30, 2 * k0, 0);
-    lb.begin({p.b.p, p.b.client, p.b.line, TB, true, 0}, client, TB ? 2 * n0 : n0, 1 << 30, TB ? k0 : 2 * k0, 0);
+    la.begin({d.a.p, d.a.client, d.a.line, false, true, 0}, client, m0, 1 << 30, 2 * k0, 0);
+    lb.begin({d.b.p, d.b.client, d.b.line, TB, true, 0}, client, TB ? 2 * n0 : n0, 1 << 30, TB ? k0 : 2 * k0, 0);
     const auto fetch = [&](int i) {
         const lds_ptr to = lds + i % NB * kStage;
         la.load(to);
@@ -382,8 +453,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_half(HalfProduct p) {
     // A lane has, of row m0 + lane % 32 of a fragment, four columns at a time: through LDS, a wave for itself, to lanes with 8 columns.
     constexpr int W = FN * 32, LINE = W + 4, ACROSS = W / 8, DOWN = 64 / ACROSS;
     __attribute__((address_space(3))) float *mine = (__attribute__((address_space(3))) float *)lds + wave * (32 * LINE);
-    const float by = p.by[client * p.apart], plus = p.plus ? p.plus[client * p.apart] : 0.0f;
-    const bool turn = p.turned.p && !(SYM && ti == tj) && p.slices == 1;
+    const bool turn = d.turned.p && !(SYM && ti == tj) && p.slices == 1;
     const auto settle = [&]() {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
@@ -409,12 +479,12 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_half(HalfProduct p) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = at[e / 4][e % 4];
             if (p.slices > 1) {
-                float *const to = p.partial + (((int64_t)slice * p.clients + client) * p.M + row0 + line) * p.N + col0 + c;
+                float *const to = p.partial + (((int64_t)slice * p.clients + all) * p.M + row0 + line) * p.N + col0 + c;
                 *(f4 *)to = f4{v[0], v[1], v[2], v[3]};
                 *(f4 *)(to + 4) = f4{v[4], v[5], v[6], v[7]};
                 continue;
             }
-            finish_half(p, client, row0 + line, col0 + c, by, plus, v);
+            finish_half(d, client, row0 + line, col0 + c, factors, v);
             if (turn) {
                 at[0] = f4{v[0], v[1], v[2], v[3]};
                 at[1] = f4{v[4], v[5], v[6], v[7]};
@@ -427,7 +497,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_half(HalfProduct p) {
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = mine[(lane % 4 * 8 + e) * LINE + c];
-                put_parts(p.turned, client, col0 + c, row0 + lane % 4 * 8, v);
+                put_parts(d.turned, client, col0 + c, row0 + lane % 4 * 8, v);
             }
         }
         settle();
@@ -438,16 +508,17 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_half(HalfProduct p) {
 template <bool SYM>
 __global__ __launch_bounds__(256) void k_half_join(HalfProduct p, int tiles) {
     __shared__ float turned[64][65];
-    const int64_t client = blockIdx.x / tiles;
-    const int tile = blockIdx.x % tiles, across = p.N / 64;
+    const int all = blockIdx.x / tiles, tile = blockIdx.x % tiles, across = p.N / 64;
+    const Side &d = p.side[all >= p.each];
+    const int64_t client = all >= p.each ? all - p.each : all;
+    const Factors factors(d, client * p.apart);
     int ti = tile / across, tj = tile % across;
     if constexpr (SYM) upper_tile(tile, across, ti, tj);
-    const float by = p.by[client * p.apart], plus = p.plus ? p.plus[client * p.apart] : 0.0f;
 #pragma unroll
     for (int i = threadIdx.x; i < 64 * 8; i += 256) {
         const int r = i / 8, c = i % 8 * 8;
         float v[8] = {};
-        const float *from = p.partial + (client * p.M + ti * 64 + r) * p.N + tj * 64 + c;
+        const float *from = p.partial + ((int64_t)all * p.M + ti * 64 + r) * p.N + tj * 64 + c;
         for (int k = 0; k < p.slices; ++k, from += (int64_t)p.clients * p.M * p.N) {
             const f4 x = *(const f4 *)from, y = *(const f4 *)(from + 4);
 #pragma unroll
@@ -456,18 +527,18 @@ __global__ __launch_bounds__(256) void k_half_join(HalfProduct p, int tiles) {
                 v[4 + e] += y[e];
             }
         }
-        finish_half(p, client, ti * 64 + r, tj * 64 + c, by, plus, v);
+        finish_half(d, client, ti * 64 + r, tj * 64 + c, factors, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) turned[c + e][r] = v[e];
     }
-    if (!p.turned.p || (SYM && ti == tj)) return;
+    if (!d.turned.p || (SYM && ti == tj)) return;
     __syncthreads();
     for (int i = threadIdx.x; i < 64 * 8; i += 256) {
         const int r = i / 8, c = i % 8 * 8;
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = turned[r][c + e];
-        put_parts(p.turned, client, tj * 64 + r, ti * 64 + c, v);
+        put_parts(d.turned, client, tj * 64 + r, ti * 64 + c, v);
     }
 }
 
@@ -513,30 +584,66 @@ static int64_t up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
 
 struct OrthoPlan {
     Whole w;
-    Choice gram, square, times;   // X X^T, A A, B X
-    Parts x[2], xt[2], a, b;   // xt: X's transpose, where B X wants that
+    Choice gram, square, pair, times;   // X X^T, A A, two of those, B X
+    bool runs;                          // several steps by A alone
+    Parts x[2], xt[2], a[2], b, p[2], q[2], t;   // xt: X's transpose, where B X wants that
     bool turned() const { return times.kind->tile < 256; }
     float *partial;
     size_t bytes;
 };
+// Where runs end, if there are any.
+static Runs runs_of(const aet_orthogonal &o, bool any) {
+    Runs r = {};
+    double x = kRoom, grown = 1;
+    for (int i = 0; i < o.steps; ++i) {
+        const auto square = [](double v) { return v > 1 ? v * v : 1.0; };
+        grown *= square(most_growth(o.a, o.b, o.c, x));
+        x = bounds_of(o, x).next;
+        // (the last step is one, too)
+        const bool end = !any || i + 1 == o.steps || grown * square(most_growth(o.a, o.b, o.c, x)) > 2e3;
+        if (end) {
+            r.ends[i / 64] |= UINT64_C(1) << (i % 64);
+            grown = 1;
+        }
+    }
+    return r;
+}
+// The time of the products
+static float time_of(const OrthoPlan &p, int steps, const Runs &runs) {
+    float t = 0;
+    for (int i = 0, first = 0; i < steps; ++i) {
+        if (!runs.end(i)) continue;
+        const int len = i + 1 - first;
+        first = i + 1;
+        t += p.gram.time + p.times.time + (float)len * p.square.time;
+        // A P and (A P) P of all but the last; Q P of all but the first: with A P where a step has both
+        if (len > 1) t += (float)(len + 1) * p.square.time + (float)(len - 2) * p.pair.time;
+    }
+    return t;
+}
 static OrthoPlan plan(const aet_orthogonal &o, char *workspace) {
     OrthoPlan p = {};
     p.w.tall = o.rows > o.cols;
     p.w.m = p.w.tall ? o.cols : o.rows;
     p.w.k = p.w.tall ? o.rows : o.cols;
+    const Runs one = runs_of(o, false), several = runs_of(o, true);
     // sides up to whole tiles of one kind, the one that is the fastest in all
     float best = 0;
     for (const Kind &k : kKinds) {
         const int64_t mp = up(p.w.m, k.tile), kp = up(p.w.k, k.tile);
-        const Choice g = choose(o.n, mp, mp, kp, true), q = choose(o.n, mp, mp, mp, true), t = choose(o.n, mp, kp, mp, false);
-        const float time = g.time + q.time + t.time;
-        if (p.gram.kind && time >= best) continue;
-        best = time;
-        p.w.mp = (int)mp;
-        p.w.kp = (int)kp;
-        p.gram = g;
-        p.square = q;
-        p.times = t;
+        OrthoPlan q = p;
+        q.w.mp = (int)mp;
+        q.w.kp = (int)kp;
+        q.gram = choose(o.n, mp, mp, kp, true);
+        q.square = choose(o.n, mp, mp, mp, true);
+        q.pair = choose(2 * (int64_t)o.n, mp, mp, mp, true);
+        q.times = choose(o.n, mp, kp, mp, false);
+        const float a = time_of(q, o.steps, one), b = time_of(q, o.steps, several);
+        q.runs = o.dtype == AET_BF16 && b < a;
+        q.w.runs = q.runs ? several : one;
+        if (p.gram.kind && (q.runs ? b : a) >= best) continue;
+        best = q.runs ? b : a;
+        p = q;
     }
     // parts of the sum of squares: some 2048 workgroups, each with values for its threads
     const int64_t pieces = ceil_div(o.cols, o.dtype == AET_F32 ? 4 : 8) * o.rows, wanted = ceil_div(2048, o.n > 0 ? o.n : 1);
@@ -555,17 +662,24 @@ static OrthoPlan plan(const aet_orthogonal &o, char *workspace) {
     if (o.steps) {
         p.x[1] = parts(p.w.mp, p.w.kp);
         if (p.turned()) for (Parts &t : p.xt) t = parts(p.w.kp, p.w.mp);
-        p.a = parts(p.w.mp, p.w.mp);
-        p.b = parts(p.w.mp, p.w.mp);
-        int64_t most = 0;
-        const auto split = [&](const Choice &c, int64_t cols) {
-            const int64_t values = c.slices > 1 ? c.slices * p.w.mp * cols : 0;
+        const auto squares = [&](Parts &t) { t = parts(p.w.mp, p.w.mp); };
+        squares(p.a[0]);
+        squares(p.b);
+        if (p.runs) {
+            squares(p.a[1]);
+            for (int i = 0; i < 2; ++i) squares(p.p[i]), squares(p.q[i]);
+            squares(p.t);
+        }
+        size_t most = 0;
+        const auto split = [&](const Choice &c, int64_t clients, int64_t cols) {
+            const size_t values = c.slices > 1 ? (size_t)c.slices * clients * p.w.mp * cols : 0;
             most = values > most ? values : most;
         };
-        split(p.gram, p.w.mp);
-        split(p.square, p.w.mp);
-        split(p.times, p.w.kp);
-        p.partial = (float *)take((size_t)o.n * most * sizeof(float));
+        split(p.gram, o.n, p.w.mp);
+        split(p.square, o.n, p.w.mp);
+        if (p.runs) split(p.pair, 2 * (int64_t)o.n, p.w.mp);
+        split(p.times, o.n, p.w.kp);
+        p.partial = (float *)take(most * sizeof(float));
     }
     p.w.sums = (double *)take((size_t)o.n * p.w.parts * sizeof(double));
     p.w.scales = (Scales *)take((size_t)o.n * o.steps * sizeof(Scales));
@@ -624,23 +738,59 @@ static hipError_t run(const aet_orthogonal &o, char *workspace, hipStream_t s) {
     k_ortho_norm<T><<<(int)norms, 256, 0, s>>>(o, p.w);
     k_ortho_first<T><<<(int)firsts, 256, 0, s>>>(o, p.w, p.w.tall ? p.xt[0] : p.x[0], p.w.tall ? p.x[0] : p.xt[0]);
     hipError_t e = hipGetLastError();
-    for (int i = 0; i < o.steps && e == hipSuccess; ++i) {
-        const int now = i % 2, next = now ^ 1, apart = o.steps * (int)(sizeof(Scales) / sizeof(float)), mp = p.w.mp, kp = p.w.kp;
-        const Parts &x = p.x[now], none = {};
+    const Parts none = {};
+    const int apart = o.steps * (int)(sizeof(Scales) / sizeof(float)), mp = p.w.mp, kp = p.w.kp;
+    const auto one = [&](const Side &d, int N, int K) {
+        HalfProduct h = {{d, d}, o.n, apart, mp, N, K, o.n};
+        h.partial = p.partial;
+        return h;
+    };
+    const auto step = [&](hipError_t now) {
+        if (e == hipSuccess) e = now;
+        return e == hipSuccess;
+    };
+    int now = 0, at = 0;   // of x and xt, and of a: the one that has the present values
+    const Parts *q = nullptr;
+    for (int i = 0, first = 0; i < o.steps; ++i) {
         const Scales *by = p.w.scales + i;
-        const auto of = [&](const Parts &a, const Parts &b, const Parts &c, const Parts &add, const Parts &turned, const float *times, const float *plus, int N,
-                            int K) {
-            HalfProduct h = {a, b, c, add, turned, times, plus, apart, mp, N, K, o.n};
-            h.partial = p.partial;
-            return h;
-        };
-        e = product<true>(p.gram, of(x, x, p.a, none, p.a, &by->a_by, nullptr, mp, kp), s);
-        if (e == hipSuccess) e = product<true>(p.square, of(p.a, p.a, p.b, p.a, p.b, &by->b_by, &by->b_plus, mp, mp), s);
-        if (e == hipSuccess)
-            e = product<false>(p.times, of(p.b, p.turned() ? p.xt[now] : x, p.x[next], x, i + 1 < o.steps ? p.xt[next] : none, &by->x_by, &by->x_plus, kp, mp), s);
+        const Parts &x = p.x[now], &xt = p.turned() ? p.xt[now] : x, &y = p.x[now ^ 1], &yt = i + 1 < o.steps && p.turned() ? p.xt[now ^ 1] : none;
+        const bool end = p.w.runs.end(i);
+        if (i == first && !step(product<true>(p.gram, one({x, x, p.a[at], none, p.a[at], &by->a_by}, mp, kp), s))) return e;
+        const Parts &a = p.a[at];
+        if (i == first && end) {   // a step by itself
+            if (!step(product<true>(p.square, one({a, a, p.b, a, p.b, &by->b_by, &by->b_plus}, mp, mp), s))) return e;
+            if (!step(product<false>(p.times, one({p.b, xt, y, x, yt, &by->x_by, &by->x_plus}, kp, mp), s))) return e;
+        } else {
+            const Parts &pp = p.p[i % 2], &next = p.a[at ^ 1];
+            if (!step(product<true>(p.square, one({a, a, pp, a, pp, &by->p_by, &by->p_plus, &by->p_diagonal}, mp, mp), s))) return e;
+            const Side qs = {q ? *q : a, pp, p.q[i % 2], none, p.q[i % 2], &by->q_by}, ts = {a, pp, p.t, none, p.t, &by->t_by};
+            if (i == first) {
+                q = &pp;
+                if (!step(product<true>(p.square, one(ts, mp, mp), s))) return e;
+            } else {
+                q = &p.q[i % 2];
+                HalfProduct h = one(qs, mp, mp);
+                if (!end) {
+                    h.side[1] = ts;
+                    h.clients = 2 * o.n;
+                }
+                if (!step(product<true>(end ? p.square : p.pair, h, s))) return e;
+            }
+            if (!end) {
+                if (!step(product<true>(p.square, one({p.t, pp, next, none, next, &by->n_by}, mp, mp), s))) return e;
+                at ^= 1;
+            } else if (!step(product<false>(p.times, one({*q, xt, y, none, yt, &by->x_by}, kp, mp), s))) {
+                return e;
+            }
+        }
+        if (end) {
+            now ^= 1;
+            first = i + 1;
+            q = nullptr;
+        }
     }
     if (e != hipSuccess) return e;
-    k_ortho_last<T><<<(int)lasts, 256, 0, s>>>(o, p.w, p.x[o.steps % 2]);
+    k_ortho_last<T><<<(int)lasts, 256, 0, s>>>(o, p.w, p.x[now]);
     return hipGetLastError();
 }
 hipError_t launch_orthogonalise(const aet_orthogonal &o, void *workspace, hipStream_t s) {

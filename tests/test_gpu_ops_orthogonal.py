@@ -36,7 +36,8 @@ def close(got, want, scale, w, keep, steps, dt, what):
 
 # n, rows, cols: single values, rows and columns; wide, square and tall; odd sizes; sides that end inside tiles of every kind
 SIZES = [(1, 1, 1), (3, 1, 40), (2, 40, 1), (2, 7, 5), (1, 16, 16), (1, 64, 64), (3, 33, 130), (2, 130, 33), (16, 128, 784), (1, 127, 129), (1, 200, 200),
-         (2, 257, 771), (1, 1001, 515), (1, 320, 1024), (5, 250, 250), (1, 640, 640), (40, 10, 30), (1, 128, 5000)]
+         (2, 257, 771), (1, 1001, 515), (1, 320, 1024), (5, 250, 250), (1, 640, 640), (40, 10, 30), (1, 128, 5000), (2, 130, 2000),
+         (3, 1500, 70), (1, 520, 2600)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -45,7 +46,7 @@ def test_orthogonalise(ops, size, dtype):   # noqa: F811
     n, rows, cols = size
     dt = TYPES[dtype]
     for k, (polynomial, steps, with_w, pad, skip) in enumerate(((MUON, 5, False, 0, 0), (MUON, 5, True, 3, 1), (CUBIC, 8, False, 8, 0), (MUON, 1, True, 0, 0),
-                                                                (MUON, 0, False, 0, 0))):
+                                                                (MUON, 0, False, 0, 0), (MUON, 7, False, 0, 0), (CUBIC, 14, False, 0, 0))):
         gen = torch.Generator().manual_seed(rows + k)
         g = rand(gen, size, dt, 1e-3 if k else 30.0, pad, skip)
         w = rand(gen, size, dt, pad=pad, skip=skip) if with_w else None
@@ -54,7 +55,7 @@ def test_orthogonalise(ops, size, dtype):   # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("size", [(2, 64, 96), (1, 300, 200)], ids=str)
+@pytest.mark.parametrize("size", [(2, 64, 96), (1, 300, 200), (1, 1400, 130), (2, 256, 2048)], ids=str)
 def test_few_directions(ops, size, dtype):   # noqa: F811
     """Gradients of mini-batches: a rank below the sides, and singular values over five orders."""
     dt = TYPES[dtype]
