@@ -1,8 +1,10 @@
 // Layer normalisation of rows, the residual stream joined in, and its gradient.
 //
 // Bound by memory.  A row lies in the registers of 4, 16 or 64 lanes of a wave, or of 4 to 16 waves, in pieces of 16 bytes;
-// it is read once: mean first, then the squares of the differences from it.  Rows too long for that are read again for each
-// pass (k_ln_long).
+// it is read once: mean first, then the squares of the differences from it.  Rows too long for that (16384 values in fp32, 32768
+// in bf16; half as many in a gradient with sums by column) are read again for each pass (k_ln_long).
+//   16384 rows of 4096 in bf16: 46 us (5.8 TB/s), with the residual and h 97 (5.5); gradient with dh joined in 123 (4.4; without sums
+//   over rows 107: the rest are the sums of 512 strips, written and read).  A row of 784 in fp32: 6.1 us, the call.
 #include "ops_internal.h"
 
 #include <type_traits>
@@ -201,8 +203,9 @@ __global__ __launch_bounds__(kLong) void k_ln_long(aet_layer_norm a, double inv)
     }
 }
 
-// Calls f(L, WAVES, NP) for the smallest group that holds a row of so many pieces; false: none does.
-template <class F>
+// Calls f(L, WAVES, NP) for the smallest group that holds a row of so many pieces; false: none does.  (Sixteen waves have too few
+// registers for sums by column.)
+template <bool SUMS, class F>
 static bool for_width(int64_t pieces, F f) {
 #define AET_WIDTH(L, W, NP) \
     if (pieces <= (L) * (W) * (NP)) return f(std::integral_constant<int, L>(), std::integral_constant<int, W>(), std::integral_constant<int, NP>()), true
@@ -214,7 +217,7 @@ static bool for_width(int64_t pieces, F f) {
     AET_WIDTH(64, 4, 2);
     AET_WIDTH(64, 4, 4);
     AET_WIDTH(64, 8, 4);
-    AET_WIDTH(64, 16, 4);
+    if constexpr (!SUMS) AET_WIDTH(64, 16, 4);
 #undef AET_WIDTH
     return false;
 }
@@ -225,7 +228,7 @@ static hipError_t forward(const aet_layer_norm &a, hipStream_t s) {
     const int64_t rows = (int64_t)a.n * a.rows;
     const float inv = a.cols ? (float)(1.0 / a.cols) : 0.0f;
     hipError_t e = hipSuccess;
-    const bool held = a.cols > 0 && for_width(ceil_div(a.cols, V), [&](auto L, auto W, auto NP) {
+    const bool held = a.cols > 0 && for_width<false>(ceil_div(a.cols, V), [&](auto L, auto W, auto NP) {
         constexpr int threads = threads_of(W), R = threads / (L * W);
         const int64_t blocks = ceil_div(rows, R);
         if (blocks > INT32_MAX) {
@@ -279,32 +282,37 @@ __global__ __launch_bounds__(threads_of(WAVES)) void k_ln_back(aet_layer_norm_gr
     const int64_t first = (int64_t)strip * s.strip, end = first + s.strip < a.rows ? first + s.strip : a.rows;
     const T *dy = (const T *)a.dy.p + client * a.dy.client, *x = (const T *)a.x.p + client * a.x.client;
     const T *dh = a.dh.p ? (const T *)a.dh.p + client * a.dh.client : nullptr;
-    float gamma[NP][V], dg[PARAMS ? NP : 1][V] = {}, db[PARAMS ? NP : 1][V] = {};
+    float dg[PARAMS ? NP : 1][V] = {}, db[PARAMS ? NP : 1][V] = {};
+    wide<T, V> gamma[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-        const Piece<V> p(t + i * G, a.cols);
-        if (a.gamma.p) {
-            const wide<T, V> g = load_piece<T, V, ODD>((const T *)a.gamma.p + client * a.gamma.client, p, a.cols);
+        if (a.gamma.p) gamma[i] = load_piece<T, V, ODD>((const T *)a.gamma.p + client * a.gamma.client, Piece<V>(t + i * G, a.cols), a.cols);
+        else
 #pragma unroll
-            for (int e = 0; e < V; ++e) gamma[i][e] = (float)g[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) gamma[i][e] = 1.0f;
-        }
+            for (int e = 0; e < V; ++e) gamma[i][e] = (T)1.0f;
     }
-    int turn = 0;
-    for (int64_t r0 = first; r0 < end; r0 += R, turn ^= 1) {   // (all groups of a workgroup as often)
-        const bool in = r0 + group < end;
-        const int64_t row = in ? r0 + group : end - 1;
-        wide<T, V> rd[NP], rx[NP], rh[NP];
+    struct Row {
+        wide<T, V> d[NP], x[NP], h[NP];
+        float mean, rstd;
+        int64_t at;
+        bool in;
+    };
+    // the group's row of the turn from r0 on (its last one again behind the end)
+    const auto load = [&](Row &row, int64_t r0) {
+        row.in = r0 + group < end;
+        row.at = row.in ? r0 + group : end - 1;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const Piece<V> p(t + i * G, a.cols);
-            rd[i] = load_piece<T, V, ODD>(dy + row * a.dy.row, p, a.cols);
-            rx[i] = load_piece<T, V, ODD>(x + row * a.x.row, p, a.cols);
-            if (dh) rh[i] = load_piece<T, V, ODD>(dh + row * a.dh.row, p, a.cols);
+            row.d[i] = load_piece<T, V, ODD>(dy + row.at * a.dy.row, p, a.cols);
+            row.x[i] = load_piece<T, V, ODD>(x + row.at * a.x.row, p, a.cols);
+            if (dh) row.h[i] = load_piece<T, V, ODD>(dh + row.at * a.dh.row, p, a.cols);
         }
-        const float mean = a.mean[client * a.rows + row], rstd = a.rstd[client * a.rows + row];
+        row.mean = a.mean[client * a.rows + row.at];
+        row.rstd = a.rstd[client * a.rows + row.at];
+    };
+    int turn = 0;
+    const auto work = [&](Row &row) {
         float v[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
@@ -312,35 +320,60 @@ __global__ __launch_bounds__(threads_of(WAVES)) void k_ln_back(aet_layer_norm_gr
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const bool own = p.template has<ODD>(e);
-                const float d = own ? (float)rd[i][e] : 0.0f, xh = own ? ((float)rx[i][e] - mean) * rstd : 0.0f, g = d * gamma[i][e];
+                const float d = own ? (float)row.d[i][e] : 0.0f, xh = own ? ((float)row.x[i][e] - row.mean) * row.rstd : 0.0f, g = d * (float)gamma[i][e];
                 v[0] += own ? g : 0.0f;
                 v[1] = __builtin_fmaf(own ? g : 0.0f, xh, v[1]);
-                if (PARAMS && in) {
+                if (PARAMS && row.in) {
                     dg[i][e] = __builtin_fmaf(d, xh, dg[i][e]);
                     db[i][e] += d;
                 }
             }
         }
-        if (!a.dx.p) continue;
+        if (!a.dx.p) return;
         // dx may be dh, and a row's last two pieces share columns: what is loaded of dh has arrived before anybody stores
         if (dh)
 #pragma unroll
-            for (int i = 0; i < NP; ++i) asm volatile("" ::"v"(rh[i]));
+            for (int i = 0; i < NP; ++i) asm volatile("" ::"v"(row.h[i]));
         row_sums<L, WAVES, 2>(v, lds[turn]);
+        turn ^= 1;
+        if (NP > 2)   // kept as they were read, not as fp32
+#pragma unroll
+            for (int i = 0; i < NP; ++i) asm volatile("" : "+v"(row.d[i]), "+v"(row.x[i]));
         const float m1 = v[0] * inv, m2 = v[1] * inv;
-        T *dx = (T *)a.dx.p + client * a.dx.client + row * a.dx.row;
+        T *dx = (T *)a.dx.p + client * a.dx.client + row.at * a.dx.row;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const Piece<V> p(t + i * G, a.cols);
             float o[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float xh = ((float)rx[i][e] - mean) * rstd;
-                o[e] = ((float)rd[i][e] * gamma[i][e] - m1 - xh * m2) * rstd;
-                if (dh) o[e] += (float)rh[i][e];
+                const float xh = ((float)row.x[i][e] - row.mean) * row.rstd;
+                o[e] = ((float)row.d[i][e] * (float)gamma[i][e] - m1 - xh * m2) * row.rstd;
+                if (dh) o[e] += (float)row.h[i][e];
             }
-            if (in) store_piece<T, V, ODD>(dx, p, a.cols, o);
+            if (row.in) store_piece<T, V, ODD>(dx, p, a.cols, o);
         }
+    };
+    // The next turn's rows are on their way while this one's are worked on, where the registers hold them (all groups of a workgroup
+    // have as many turns).  dx may be dy or dh: a row is stored only where it is read, in its own turn.
+    Row row[2];
+    if constexpr (WAVES > 4) {
+        for (int64_t r0 = first; r0 < end; r0 += R) {
+            load(row[0], r0);
+            work(row[0]);
+        }
+    } else {
+        load(row[0], first);
+        int64_t r0 = first;
+        for (; r0 + 2 * R < end; r0 += 2 * R) {
+            load(row[1], r0 + R);
+            work(row[0]);
+            load(row[0], r0 + 2 * R);
+            work(row[1]);
+        }
+        if (r0 + R < end) load(row[1], r0 + R);
+        work(row[0]);
+        if (r0 + R < end) work(row[1]);
     }
     if constexpr (PARAMS) {
 #pragma unroll
@@ -480,16 +513,23 @@ __global__ __launch_bounds__(256) void k_ln_none(aet_layer_norm_grad a, int64_t 
 }
 
 static bool shared_of(const aet_layer_norm_grad &a) { return a.n != 1 && ((a.dgamma.p && !a.dgamma.client) || (a.dbeta.p && !a.dbeta.client)); }
-// Strips: some 1024 workgroups, each with 8 or more turns.
+// Strips: as many workgroups as the compute units hold (what a group of four waves with a piece a lane leaves room for is four a unit, with
+// two pieces two, else one), since every strip's sums are written and read again; each with four or more turns where there are
+// rows enough.  16384 rows of 4096 in bf16, dh joined in: 512 strips 123 us, 1024 133, 256 138.
 static StripShape strips_of(const aet_layer_norm_grad &a, void *workspace) {
     const int V = a.dtype == AET_F32 ? 4 : 8;
-    int at_once = 1;
-    const bool held = for_width(ceil_div(a.cols, V), [&](auto L, auto W, auto) { at_once = threads_of(W) / (L * W); });
-    StripShape s = {};
+    int at_once = 1, all = 512;
     const bool params = a.dgamma.p || a.dbeta.p;
+    const auto group = [&](auto L, auto W, auto NP) {
+        at_once = threads_of(W) / (L * W);
+        all = NP == 4 ? 256 : W == 4 && NP == 1 ? 1024 : 512;
+    };
+    const bool held = params ? for_width<true>(ceil_div(a.cols, V), group) : for_width<false>(ceil_div(a.cols, V), group);
+    StripShape s = {};
     const int64_t per = held ? a.n : a.n * ceil_div(a.cols, 256 * V);
-    const int64_t wanted = ceil_div(1024, per > 0 ? per : 1), most = ceil_div(a.rows, (int64_t)at_once * (params ? 8 : 1));
-    const int64_t strips = wanted < most ? wanted : most;
+    const int64_t wanted = ceil_div(all, per > 0 ? per : 1), most = ceil_div(a.rows, 4 * (int64_t)at_once);
+    int64_t strips = wanted < most ? wanted : most;
+    if (strips * per < 256) strips = wanted < ceil_div(a.rows, at_once) ? wanted : ceil_div(a.rows, at_once);
     s.strip = (int)(ceil_div(ceil_div(a.rows, strips > 0 ? strips : 1), at_once) * at_once);
     s.strips = s.strip ? (int)ceil_div(a.rows, s.strip) : 1;
     s.line = (int)(ceil_div(a.cols, 4) * 4);
@@ -520,11 +560,12 @@ static hipError_t backward(const aet_layer_norm_grad &a, void *workspace, hipStr
     const float inv = (float)(1.0 / a.cols);
     const int64_t blocks = (int64_t)a.n * s.strips;
     if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
-    const bool held = for_width(ceil_div(a.cols, V), [&](auto L, auto W, auto NP) {
-        const auto kernel = a.cols % V ? params ? k_ln_back<T, L, W, NP, true, true> : k_ln_back<T, L, W, NP, true, false>
-                                       : params ? k_ln_back<T, L, W, NP, false, true> : k_ln_back<T, L, W, NP, false, false>;
+    const auto go = [&](auto sums, auto L, auto W, auto NP) {
+        const auto kernel = a.cols % V ? k_ln_back<T, L, W, NP, true, sums> : k_ln_back<T, L, W, NP, false, sums>;
         kernel<<<(int)blocks, threads_of(W), 0, stream>>>(a, s, inv);
-    });
+    };
+    const bool held = params ? for_width<true>(ceil_div(a.cols, V), [&](auto... g) { go(std::true_type(), g...); })
+                             : for_width<false>(ceil_div(a.cols, V), [&](auto... g) { go(std::false_type(), g...); });
     if (!held) {
         const int64_t rows = (int64_t)a.n * a.rows, across = ceil_div(a.cols, 256 * V);
         if (rows > INT32_MAX || blocks * across > INT32_MAX) return hipErrorInvalidConfiguration;
