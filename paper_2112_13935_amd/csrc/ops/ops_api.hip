@@ -377,6 +377,23 @@ static void fold(aet_mx4_linear &a) {
     a.n = 1;
 }
 
+// One W for all clients: the clients are one, if the rows of held inputs lie one after another, too.
+static bool fold(aet_mx4_linear_grad &a, bool shared) {
+    if (!shared) return true;
+    if (a.rows == 1) {
+        a.dy.row = a.dy.client;
+        a.x.row = a.x.client;
+        a.x_scales.row = a.x_scales.client;
+        a.pre.row = a.pre.client;
+        a.dx.row = a.dx.client;
+    } else if (a.dw.p && (a.x.client != a.rows * a.x.row || a.x_scales.client != a.rows * a.x_scales.row)) {
+        return false;
+    }
+    a.rows *= a.n;
+    a.n = 1;
+    return true;
+}
+
 static aet_status check(const aet_mx4_linear_grad *a, bool *shared) {
     const char *why;
     if (!a) return fail(AET_EINVAL, "the record is NULL");
@@ -553,6 +570,8 @@ aet_status aet_mx4_linear_forward(const aet_mx4_linear *a, void *workspace, size
 size_t aet_mx4_linear_backward_workspace_bytes(const aet_mx4_linear_grad *a) {
     bool shared;
     if (check(a, &shared) != AET_OK || !a->n) return 0;
+    aet_mx4_linear_grad h = *a;
+    if (fold(h, shared) && mx4_half_pays(h)) return mx4_half_workspace(h);
     size_t used;
     aet_linear_grad b = mx4_plain_gradient(*a, nullptr, &used);
     fold(b, shared);
@@ -562,13 +581,16 @@ aet_status aet_mx4_linear_backward(const aet_mx4_linear_grad *a, void *workspace
     bool shared;
     if (const aet_status st = check(a, &shared)) return st;
     if (!a->n) return AET_OK;
-    size_t used;
+    aet_mx4_linear_grad h = *a;
+    const bool half = fold(h, shared) && mx4_half_pays(h);
+    size_t used = 0;
     const aet_linear_grad plain = mx4_plain_gradient(*a, workspace, &used);
     aet_linear_grad b = plain;
     fold(b, shared);
-    const size_t need = used + linear_backward_workspace(b);
+    const size_t need = half ? mx4_half_workspace(h) : used + linear_backward_workspace(b);
     if (bad_workspace(workspace, workspace_bytes, need))
         return fail(AET_ENOMEM, "the workspace needs %zu bytes, 256-byte aligned; got %zu", need, workspace_bytes);
+    if (half) return done(launch_mx4_half(h, workspace, (hipStream_t)hip_stream));
     const hipError_t e = launch_mx4_expand(*a, plain, (hipStream_t)hip_stream);
     return done(e != hipSuccess ? e : launch_linear_backward(b, (char *)workspace + used, (hipStream_t)hip_stream));
 }

@@ -25,8 +25,6 @@
 
 namespace aet_ops {
 
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // A matrix per client in two parts, 32 columns of the one next to those of the other, which makes a line of memory:
@@ -39,7 +37,7 @@ struct Parts {
     __device__ __forceinline__ _Float16 *at(int64_t c, int row, int col) const { return p + c * client + (int64_t)row * line + col / 32 * 64 + col % 32; }
 };
 
-// high + low = v to within 2^-23 of it
+// high + low = v to within 2^-22 of it
 __device__ __forceinline__ void split_half(const float (&v)[8], half8 &high, half8 &low) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {

@@ -5,6 +5,7 @@
 namespace aet_ops {
 
 typedef short s4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char *lds_ptr;
 
 // Piece (r, c) of an operand's stage: by rows row r, values 8 c .. of the stage; by columns k = r, rows 8 c ..

@@ -40,6 +40,18 @@ hipError_t launch_rows(int dtype, const Product &p, hipStream_t s);
 // Bytes of scratch that the product wants (for sums that are split along k).
 size_t product_workspace(int dtype, const Product &p);
 hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStream_t s);
+// C's rows times 2^exps[client * .client + row]
+struct RowExponents {
+    const int32_t *exps;
+    int64_t client;
+};
+// The same of fp16 operands (A in one part or two), B by columns, where both can go straight into LDS; dtype is C's.
+bool half_fits(const Product &p);
+size_t half_product_workspace(const Product &p);
+hipError_t launch_half_product(int dtype, const Product &p, const RowExponents &half, void *workspace, hipStream_t s);
+// Microseconds that the two are expected to take.
+float half_product_time(const Product &p);
+float product_time(int dtype, const Product &p);
 // Both gradients of a layer in one launch, where both are small (taken).
 hipError_t launch_pair(int dtype, const Product &x, const Product &w, hipStream_t s, bool *taken);
 

@@ -115,8 +115,11 @@ struct Tile {
     static constexpr int kLds = kStage * kBuffers > kEpilogue ? kStage * kBuffers : kEpilogue;
 };
 
-template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT>
-__device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, const Shape &s, const Epilogue &e, int block, lds_ptr lds) {
+// O: the type of C and what is beside it.  HALF: the operands are fp16 (T says bf16, which lies as they do), and C's rows are
+// multiplied by 2^half.exps[row].
+template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT, typename O = T, bool HALF = false>
+__device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, const Shape &s, const Epilogue &e, int block, lds_ptr lds,
+                                        const RowExponents &half = {}) {
     using L = Tile<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>;
     constexpr int FM = L::FM, FN = L::FN, P = L::kParts;
     using SA = typename L::SA;
@@ -161,7 +164,12 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
 #pragma unroll
             for (int i = 0; i < FN; ++i)
 #pragma unroll
-                for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[i][0], f.a[j][0], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < FM; ++j) {
+                    if constexpr (HALF)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, f.b[i][0]), __builtin_bit_cast(half8, f.a[j][0]), acc[i][j], 0, 0, 0);
+                    else
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[i][0], f.a[j][0], acc[i][j], 0, 0, 0);
+                }
         } else {
 #pragma unroll
             for (int q = 0; q < 6; ++q)
@@ -293,12 +301,12 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
 
     // A lane has, of row m0 + lane % 32 of a fragment, four columns at a time: through LDS, a wave for itself, to lanes
     // with V columns (16 bytes) each, in whole lines of memory.
-    constexpr int V = 16 / sizeof(T), W = FN * 32, LINE = W + 4, ACROSS = W / V, DOWN = 64 / ACROSS;
+    constexpr int V = 16 / sizeof(O), W = FN * 32, LINE = W + 4, ACROSS = W / V, DOWN = 64 / ACROSS;
     __attribute__((address_space(3))) float *mine = (__attribute__((address_space(3))) float *)lds + wave * (32 * LINE);
     const int col = n0 + wc * W + lane % ACROSS * V;
     const int count = s.N - col;
     float bias[V];
-    bias_of<T>(e, client, col, s.slices > 1 ? 0 : count, bias);
+    bias_of<O>(e, client, col, s.slices > 1 ? 0 : count, bias);
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
 #pragma unroll
@@ -323,9 +331,14 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
 #pragma unroll
                 for (int y = 0; y < 4; ++y) v[4 * h + y] = x[y] + bias[4 * h + y];
             }
+            if constexpr (HALF) {
+                const int by = row < s.M ? half.exps[client * half.client + row] : 0;
+#pragma unroll
+                for (int y = 0; y < V; ++y) v[y] = __builtin_ldexpf(v[y], by);
+            }
             if (row < s.M && count > 0) {
                 if (s.slices > 1) store_some(s.partial + (((int64_t)slice * s.clients + client) * s.M + row) * s.N + col, count, v);
-                else finish<T>(e, client, row, col, count, v);
+                else finish<O>(e, client, row, col, count, v);
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -337,6 +350,13 @@ template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, 
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand ob, Shape s, Epilogue e) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     tile_of<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>(oa, ob, s, e, blockIdx.x, (lds_ptr)lds);
+}
+
+// Operands in fp16, B by columns.
+template <typename O, int BM, int BN, int WR, int WC, bool TA>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles_half(Operand oa, Operand ob, Shape s, Epilogue e, RowExponents half) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    tile_of<bf16, BM, BN, 64, WR, WC, TA, true, true, O, true>(oa, ob, s, e, blockIdx.x, (lds_ptr)lds, half);
 }
 
 // Two small products in one launch: the gradients of a layer's inputs (B by columns) and of its weights (both by columns).
@@ -510,6 +530,52 @@ hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStrea
     if (!p.a.by_columns && !p.b.by_columns) return f32 ? run_product<float, false, false>(p, workspace, s) : run_product<bf16, false, false>(p, workspace, s);
     if (!p.a.by_columns) return f32 ? run_product<float, false, true>(p, workspace, s) : run_product<bf16, false, true>(p, workspace, s);
     return f32 ? run_product<float, true, true>(p, workspace, s) : run_product<bf16, true, true>(p, workspace, s);
+}
+
+// Products of fp16 operands, B by columns, both as stages go straight into LDS.
+bool half_fits(const Product &p) { return direct(p.a, p.M, p.K, 64) && direct(p.b, p.N, p.K, 64); }
+size_t half_product_workspace(const Product &p) {
+    const int slices = choose(AET_BF16, p, true).slices;
+    return slices > 1 ? (size_t)slices * p.clients * p.M * p.N * sizeof(float) : 0;
+}
+float half_product_time(const Product &p) { return choose(AET_BF16, p, true).time; }
+float product_time(int dtype, const Product &p) { return choose(dtype, p, dtype == AET_BF16).time; }
+
+template <typename O, int BM, int BN, int WR, int WC, bool TA>
+static hipError_t run_half(const Product &p, const Shape &s, const RowExponents &half, hipStream_t stream) {
+    using L = Tile<bf16, BM, BN, 64, WR, WC, TA, true, true>;
+    const auto kernel = k_tiles_half<O, BM, BN, WR, WC, TA>;
+    if constexpr (L::kLds > 64 * 1024) {
+        static aet::PerDevice allowed;
+        int dev = 0, ok = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        e = allowed.get(dev, &ok, [&](int *v) {
+            *v = 1;
+            return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kLds);
+        });
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<s.blocks, L::kThreads, L::kLds, stream>>>(p.a, p.b, s, p.e, half);
+    return hipGetLastError();
+}
+template <typename O, bool TA>
+static hipError_t run_half(const Product &p, const RowExponents &half, void *workspace, hipStream_t stream) {
+    const Choice c = choose(AET_BF16, p, true);
+    Shape s;
+    if (!shape_of(p, c, workspace, &s)) return hipErrorInvalidConfiguration;
+    if (!s.blocks) return hipSuccess;
+    hipError_t e;
+    if (c.kind->bm == 256) e = run_half<O, 256, 256, 2, 4, TA>(p, s, half, stream);
+    else if (c.kind->bm == 128) e = run_half<O, 128, 128, 2, 2, TA>(p, s, half, stream);
+    else if (c.kind->bn == 128) e = run_half<O, 64, 128, 2, 2, TA>(p, s, half, stream);
+    else e = run_half<O, 64, 64, 2, 2, TA>(p, s, half, stream);
+    if (e != hipSuccess || s.slices == 1) return e;
+    return launch_join(sizeof(O) == 4 ? AET_F32 : AET_BF16, s, p.e, stream);
+}
+hipError_t launch_half_product(int dtype, const Product &p, const RowExponents &half, void *workspace, hipStream_t s) {
+    if (dtype == AET_F32) return p.a.by_columns ? run_half<float, true>(p, half, workspace, s) : run_half<float, false>(p, half, workspace, s);
+    return p.a.by_columns ? run_half<bf16, true>(p, half, workspace, s) : run_half<bf16, false>(p, half, workspace, s);
 }
 
 template <typename T>

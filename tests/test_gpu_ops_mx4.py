@@ -129,6 +129,112 @@ def test_linear(ops, size, dtype):   # noqa: F811
             O.near(t, want, f"{part} {what}")
 
 
+# Sizes at which the gradient takes all operands in fp16: odd ones, several clients, rows and columns that end inside tiles and pieces
+LARGE = [(1, 2055, 1031, 1543), (3, 1030, 1030, 1030), (1, 4096, 520, 2048), (16, 257, 512, 1000)]
+
+
+def gradient(dy, vx, vw, pre, name, p, seed, dt):
+    """Like the oracle's, which multiplies in 64 bits: on the GPU, for the time that it takes."""
+    m = O.mask3(dy.shape, seed, 0, p) if p else 1.0
+    dz = dy * m * (O.slope(pre, name) if name != "none" else 1.0)
+    off = dz.abs() * ((4 * 1.13 + 10 * (pre.abs() + 1)) * O.U32 if name in ("silu", "gelu") else 4 * O.U32)
+    # dz as the products see it: in bf16 one fp16 value, which is off by half a step, torch.finfo(torch.float16).eps / 2 = 2^-11 (or two bf16
+    # ones), in fp32 two, the second of which is off by 2^-11 of the at most 2^-11 that the first leaves
+    dzr = off + dz.abs() * (2.0 ** -11 if dt == torch.bfloat16 else 2.0 ** -22)
+    r = O.ROUND[dt]
+
+    def product(a, aoff, b):
+        g = [t.to(DEV) for t in (a, aoff, b)]
+        v, S = torch.matmul(g[0], g[2]).cpu(), torch.matmul(g[0].abs(), g[2].abs()).cpu()
+        o = torch.matmul(g[1], g[2].abs()).cpu() + (a.shape[-1] + 4) * O.U32 * S
+        return v, o + r * (v.abs() + o)
+
+    t = lambda v: v.transpose(1, 2).contiguous()   # noqa: E731
+    db = dz.sum(1)
+    o = off.sum(1) + (dz.shape[1] + 4) * O.U32 * dz.abs().sum(1)
+    return product(dz, dzr, vw), product(t(dz), t(dzr), vx), (db, o + r * (db.abs() + o))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", LARGE, ids=str)
+def test_large_gradients(ops, size, dtype):   # noqa: F811
+    n, rows, inp, out = size
+    dt = TYPES[dtype]
+    for k, (name, p, pad, skip) in enumerate((("silu", 0.0, 0, 0), ("gelu", 0.3, 1, 1), ("none", 0.0, 0, 0))):
+        g = torch.Generator().manual_seed(k + rows)
+        (x, xs), (w, ws) = held(g, (n, rows, inp), pad, skip), held(g, (n, out, inp), pad, skip)
+        dy, pre = rand(g, (n, rows, out), dt, 1e-3, pad, skip), rand(g, (n, rows, out), dt, pad=pad, skip=skip)
+        want = gradient(d64(dy), M.values(x, xs, inp), M.values(w, ws, inp), d64(pre), name, p, 5, dt)
+        got = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, cols=inp, act=name, p=p, seed=5)
+        for t, q, part in zip(got, want, ("dx", "dw", "db")):
+            O.near(t, q, f"{part} {size} {dtype} {name}")
+        for need in ((True, False, False), (False, True, True)):
+            some = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, cols=inp, act=name, p=p, seed=5, need=need)
+            for t, q, yes in zip(some, want, need):
+                assert (t is None) != yes
+                if yes:
+                    O.near(t, q, f"{need} {size} {dtype} {name}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_gradients_of_rows_of_all_sizes(ops, dtype):   # noqa: F811
+    """Rows of dz, of x and of W whose sizes are 2^-50 to 2^50 of each other, a row of zeros each, and blocks of zeros with the largest scale."""
+    dt = TYPES[dtype]
+    n, rows, inp, out = 1, 1500, 1024, 1500
+    g = torch.Generator().manual_seed(3)
+    (x, xs), (w, ws) = held(g, (n, rows, inp)), held(g, (n, out, inp))
+    for t in (xs, ws):
+        t += torch.randint(-50, 50, (n, t.shape[1], 1), generator=g, dtype=torch.int8).to(torch.uint8).to(DEV)
+    for c, s in ((x, xs), (w, ws)):
+        c[0, 7] = 0
+        c[0, 9, 16:32] = 0x80   # a block of zeros
+        s[0, 9, 1] = 254
+    dy = rand(g, (n, rows, out), dt) * torch.exp2(torch.randint(-20, 20, (n, rows, 1), generator=g).float()).to(dt).to(DEV)
+    dy[0, 11] = 0
+    pre = rand(g, (n, rows, out), dt)
+    want = gradient(d64(dy), M.values(x, xs, inp), M.values(w, ws, inp), d64(pre), "silu", 0.0, 5, dt)
+    got = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act="silu")
+    for t, (v, bound), part in zip(got, want, ("dx", "dw", "db")):
+        # (beside the bound: 2^-39 of the largest term of the row of the contraction, for each)
+        room = 2.0 ** -39 * v.abs().amax(-1, keepdim=True) * 1500 if part != "db" else 0
+        O.near(t, (v, bound + room), part)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_gradients_that_are_not_finite(ops, dtype):   # noqa: F811
+    dt = TYPES[dtype]
+    n, rows, inp, out = 1, 1500, 1024, 1500
+    g = torch.Generator().manual_seed(3)
+    (x, xs), (w, ws) = held(g, (n, rows, inp)), held(g, (n, out, inp))
+    dy, pre = rand(g, (n, rows, out), dt), rand(g, (n, rows, out), dt)
+    want = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act="gelu")
+    dy[0, 3, 5] = float("nan")
+    xs[0, 10, 2], ws[0, 20, 4] = 255, 255
+    dx, dw, db = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act="gelu")
+    fine = torch.ones(rows, inp, dtype=torch.bool, device=DEV)
+    fine[3], fine[:, 128:160] = False, False
+    assert bool(dx[0][~fine].isnan().all()) and torch.equal(dx[0][fine], want[0][0][fine])
+    fine = torch.ones(out, inp, dtype=torch.bool, device=DEV)
+    fine[5], fine[:, 64:96] = False, False
+    assert bool(dw[0][~fine].isnan().all()) and torch.equal(dw[0][fine], want[1][0][fine])
+    assert bool(db[0, 5].isnan()) and int(db.isnan().sum()) == 1
+
+
+def test_large_gradient_of_one_w_for_all_clients(ops):   # noqa: F811
+    g = torch.Generator().manual_seed(4)
+    n, rows, inp, out = 5, 400, 512, 1024
+    (x, xs), (w, ws) = held(g, (n, rows, inp)), held(g, (out, inp))
+    dy, pre = rand(g, (n, rows, out), torch.bfloat16), rand(g, (n, rows, out), torch.bfloat16)
+    flat = lambda t: t.reshape(1, n * rows, t.shape[-1])   # noqa: E731
+    want = gradient(flat(d64(dy)), flat(M.values(x, xs, inp)), M.values(w, ws, inp)[None], flat(d64(pre)), "gelu", 0.0, 0, torch.bfloat16)
+    apart = torch.zeros(n, rows + 3, inp // 2, dtype=torch.uint8, device=DEV)[:, :rows]   # held inputs of clients that lie apart
+    apart.copy_(x)
+    for held_x in (x, apart):
+        dx, dw, db = ops.aet_mx4_linear_backward(dy, held_x, xs, w, ws, pre, act="gelu")
+        for t, q, part in zip((flat(dx), dw[None], db[None]), want, ("dx", "dw", "db")):
+            O.near(t, q, part)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [1, 40])
 def test_one_w_for_all_clients(ops, dtype, rows):   # noqa: F811
@@ -150,6 +256,23 @@ def test_one_w_for_all_clients(ops, dtype, rows):   # noqa: F811
     O.near(got[0].view(1, 5 * rows, 96), wants[0], "dx")
     O.near(got[1][None], wants[1], "dw")
     O.near(got[2][None], wants[2], "db")
+
+
+def test_large_gradient_captured_and_replayed(ops):   # noqa: F811
+    g = torch.Generator().manual_seed(6)
+    (x, xs), (w, ws) = held(g, (1500, 1024)), held(g, (1500, 1024))
+    dy, pre = rand(g, (1500, 1500), torch.bfloat16), rand(g, (1500, 1500), torch.bfloat16)
+    step = lambda: ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act="silu")   # noqa: E731
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(4):
+        dy.copy_(rand(g, (1500, 1500), torch.bfloat16, 10.0 ** -k))   # (tops of the last replay must not stay)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, step())), k
 
 
 @pytest.mark.parametrize("rows", [3, 70, 300])
