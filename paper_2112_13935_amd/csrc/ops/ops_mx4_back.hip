@@ -22,12 +22,25 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Rows of held values as fp16, times 2^-exps[row], where exps is the exponent of the row's largest block that has a value, less 13
-// (magnitudes up to 6 become up to 49152); zeros up to a multiple of 8.  A workgroup has a row.
-__global__ __launch_bounds__(256) void k_mx4_half(Held from, _Float16 *to, int32_t *exps, int64_t rows, int cols, int line) {
-    __shared__ int lds[4];
-    const int64_t at = blockIdx.x, client = at / rows, row = at - client * rows;
-    const uint8_t *codes = (const uint8_t *)from.codes.p + client * from.codes.client + row * from.codes.row;
-    const uint8_t *scales = (const uint8_t *)from.scales.p + client * from.scales.client + row * from.scales.row;
+// (magnitudes up to 6 become up to 49152); zeros up to a multiple of 8.
+struct HalfRows {
+    Held from;
+    _Float16 *to;
+    int32_t *exps;
+    int64_t rows, all;   // of a client, and of all
+};
+// W's rows and x's, a wave each, and the places of the maxima that come next.
+__global__ __launch_bounds__(256) void k_mx4_half(HalfRows w, HalfRows x, int cols, int line, int32_t *tops, int64_t count) {
+    int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    const int64_t thread = (int64_t)blockIdx.x * 256 + threadIdx.x, threads = (int64_t)gridDim.x * 256;
+    for (int64_t i = thread; i < count; i += threads) tops[i] = INT_MIN;
+    const HalfRows &r = at < w.all ? w : x;
+    if (at >= w.all) at -= w.all;
+    if (at >= r.all) return;
+    const int lane = threadIdx.x % 64;
+    const int64_t client = at / r.rows, row = at - client * r.rows;
+    const uint8_t *codes = (const uint8_t *)r.from.codes.p + client * r.from.codes.client + row * r.from.codes.row;
+    const uint8_t *scales = (const uint8_t *)r.from.scales.p + client * r.from.scales.client + row * r.from.scales.row;
     const int blocks = (cols + 31) / 32, pieces = line / 8;
     // 8 codes from column 8 i on; past the end 0
     const auto read = [&](int i) {
@@ -44,48 +57,52 @@ __global__ __launch_bounds__(256) void k_mx4_half(Held from, _Float16 *to, int32
         return v;
     };
     int top = INT_MIN;
-    for (int i = threadIdx.x; i < pieces; i += 256) {
+#pragma unroll 4
+    for (int i = lane; i < pieces; i += 64) {
         const int scale = i / 4 < blocks ? scales[i / 4] : 255;
-        if (scale != 255 && (read(i) & 0x77777777u)) top = scale > top ? scale : top;
+        const uint32_t code = read(i);
+        if (scale != 255 && (code & 0x77777777u)) top = scale > top ? scale : top;
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) {
         const int o = __shfl_xor(top, off, 64);
         top = o > top ? o : top;
     }
-    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 4; ++w) top = lds[w] > top ? lds[w] : top;
     const int shift = (top == INT_MIN ? 127 : top) - 13;   // scales become scale - shift + 127
-    if (threadIdx.x == 0) exps[at] = shift - 127;
-    for (int i = threadIdx.x; i < pieces; i += 256) {
+    if (lane == 0) r.exps[at] = shift - 127;
+#pragma unroll 4
+    for (int i = lane; i < pieces; i += 64) {
         const int scale = i / 4 < blocks ? scales[i / 4] : 127, moved = scale - shift + 127;
-        const float by = scale == 255 ? __builtin_nanf("") : __builtin_bit_cast(float, (uint32_t)(moved > 0 ? moved : 0) << 23);
+        const float by = __builtin_bit_cast(float, (uint32_t)(scale == 255 ? 255 : moved > 0 ? moved : 0) << 23);   // (255: NaN)
         const uint32_t code = read(i);
-        half8 v;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {   // magnitudes below 2 are 0, 0.5, 1, 1.5; above (2 + bit) 2^(exponent - 2)
-            const uint32_t c = code >> (4 * e), m = c & 7;
-            const float f = m < 4 ? 0.5f * (float)m : (float)((2 + (m & 1)) << ((m >> 1) - 2));
-            v[e] = (_Float16)((c & 8 ? -f : f) * by);
-        }
-        *(half8 *)(to + at * line + (int64_t)i * 8) = v;
+        const half2v c0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, by, 0), c1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, by, 1),
+                     c2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, by, 2), c3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, by, 3);
+        *(half8 *)(r.to + at * line + (int64_t)i * 8) = half8{c0[0], c0[1], c1[0], c1[1], c2[0], c2[1], c3[0], c3[1]};
     }
 }
 
-// dz of 8 columns of a row
+// What dz of 8 columns of a row is worked out from, and dz
 template <typename T, int ACT, bool DROP>
-__device__ __forceinline__ void dz_of(const aet_mx4_linear_grad &a, const Drop &d, int64_t client, int64_t row, int col, int count, float (&v)[8]) {
-    load_some((const T *)a.dy.p + client * a.dy.client + row * a.dy.row + col, count, v);
-    if (ACT) {
-        float z[8];
-        load_some((const T *)a.pre.p + client * a.pre.client + row * a.pre.row + col, count, z);
-        slope_each<ACT>(z, v);
+struct DzPiece {
+    wide<T, 8> dy, z;
+    __device__ __forceinline__ void load(const aet_mx4_linear_grad &a, int64_t client, int64_t row, int col, int count) {
+        dy = load_raw<T, 8>((const T *)a.dy.p + client * a.dy.client + row * a.dy.row + col, count);
+        if (ACT) z = load_raw<T, 8>((const T *)a.pre.p + client * a.pre.client + row * a.pre.row + col, count);
     }
-    // last, so that what the forward pass took out has a gradient of 0 whatever z was
-    if (DROP) drop_apply(d, drop_row(d, client * a.rows + row), col, v);
-}
+    __device__ __forceinline__ void work(const aet_mx4_linear_grad &a, const Drop &d, int64_t client, int64_t row, int col, float (&v)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)dy[e];
+        if (ACT) {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = (float)z[e];
+            slope_each<ACT>(f, v);
+        }
+        // last, so that what the forward pass took out has a gradient of 0 whatever z was
+        if (DROP) drop_apply(d, drop_row(d, client * a.rows + row), col, v);
+    }
+};
+constexpr int kTopRows = 1, kDzRows = 4;   // of a thread, all on their way at once
 
 // How dz is dealt out: a workgroup has 256 columns of a strip of a client's rows, eight rows at a time.
 struct HalfShape {
@@ -112,15 +129,12 @@ struct HalfPlace {
     }
 };
 
-__global__ __launch_bounds__(256) void k_half_clear(int32_t *p, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) p[i] = INT_MIN;
-}
+constexpr int kNone = kNoExponent;
 
 // |v| < 2^exponent; nothing for 0 and what is not finite
 __device__ __forceinline__ int exponent_of(float v) {
     const bool counts = v != 0 && __builtin_fabsf(v) <= __FLT_MAX__;
-    return counts ? __builtin_amdgcn_frexp_expf(v) : -100000;
+    return counts ? __builtin_amdgcn_frexp_expf(v) : kNone;
 }
 
 // The largest exponents of rows and columns (maxima, whose order does not matter), and the sums over rows.
@@ -134,30 +148,39 @@ __global__ __launch_bounds__(256) void k_half_tops(aet_mx4_linear_grad a, Drop d
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         w[e] = s.by_rows && e < p.count ? s.w_exps[p.client * s.w_client + p.col + e] : 0;
-        col[e] = -100000;
+        col[e] = kNone;
     }
-    for (int64_t r0 = p.first; r0 < p.end; r0 += 8) {   // (all lanes as often)
-        const int64_t row = r0 + p.ty;
-        int top = -100000;
-        if (row < p.end && p.count > 0) {
-            float v[8];
-            dz_of<T, ACT, DROP>(a, d, p.client, row, p.col, p.count, v);
-            const int x = s.by_columns ? s.x_exps[p.client * a.rows + row] : 0;
+    for (int64_t r0 = p.first; r0 < p.end; r0 += 8 * kTopRows) {   // (all lanes as often)
+        DzPiece<T, ACT, DROP> piece[kTopRows];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (e >= p.count) continue;
-                const int q = exponent_of(v[e]);
-                top = q + w[e] > top ? q + w[e] : top;
-                col[e] = q + x > col[e] ? q + x : col[e];
-                sum[e] += v[e];
+        for (int i = 0; i < kTopRows; ++i) {
+            const int64_t row = r0 + 8 * i + p.ty;
+            if (p.count > 0) piece[i].load(a, p.client, row < p.end ? row : p.end - 1, p.col, p.count);
+        }
+#pragma unroll
+        for (int i = 0; i < kTopRows; ++i) {
+            const int64_t row = r0 + 8 * i + p.ty;
+            int top = kNone;
+            if (row < p.end && p.count > 0) {
+                float v[8];
+                piece[i].work(a, d, p.client, row, p.col, v);
+                const int x = s.by_columns ? s.x_exps[p.client * a.rows + row] : 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (e >= p.count) continue;
+                    const int q = exponent_of(v[e]);
+                    top = q + w[e] > top ? q + w[e] : top;
+                    col[e] = q + x > col[e] ? q + x : col[e];
+                    sum[e] += v[e];
+                }
             }
-        }
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) {
-            const int o = __shfl_xor(top, off, 64);
-            top = o > top ? o : top;
+            for (int off = 16; off > 0; off >>= 1) {
+                const int o = __shfl_xor(top, off, 64);
+                top = o > top ? o : top;
+            }
+            if (s.by_rows && threadIdx.x % 32 == 0 && row < p.end) atomicMax(s.row_top + p.client * a.rows + row, top);
         }
-        if (s.by_rows && threadIdx.x % 32 == 0 && row < p.end) atomicMax(s.row_top + p.client * a.rows + row, top);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -168,7 +191,7 @@ __global__ __launch_bounds__(256) void k_half_tops(aet_mx4_linear_grad a, Drop d
     const int mine = blockIdx.x % s.across * 256 + threadIdx.x;
     if (mine >= a.out) return;
     float total = 0;
-    int top = -100000;
+    int top = kNone;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         total += sums[i][threadIdx.x];
@@ -181,33 +204,26 @@ __global__ __launch_bounds__(256) void k_half_tops(aet_mx4_linear_grad a, Drop d
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_half_db(aet_mx4_linear_grad a, HalfShape s) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)a.n * a.out;
-    if (i >= all) return;
-    float total = 0;
-#pragma unroll 8
-    for (int k = 0; k < s.strips; ++k) total += s.partial[k * all + i];
-    ((T *)a.db.p)[i / a.out * a.db.client + i % a.out] = (T)total;
-}
-
-// The exponent that a row (column) of the result is multiplied by; no value: 0
-__device__ __forceinline__ int shift_of(int top) { return top < -50000 ? 0 : top - 15; }
-__global__ __launch_bounds__(256) void k_half_shifts(int32_t *p, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) p[i] = shift_of(p[i]);
-}
-
 // dz as its two forms, rows and columns times the powers of two that leave their largest value near 2^15.
 template <typename T, int ACT, bool DROP>
 __global__ __launch_bounds__(256) void k_half_dz(aet_mx4_linear_grad a, Drop d, HalfShape s) {
+    const int64_t blocks = (int64_t)a.n * s.across * s.strips;
+    if (blockIdx.x >= blocks) {   // beside that, the strips' sums
+        const int64_t i = (blockIdx.x - blocks) * 256 + threadIdx.x, all = (int64_t)a.n * a.out;
+        if (i >= all) return;
+        float total = 0;
+#pragma unroll 8
+        for (int k = 0; k < s.strips; ++k) total += s.partial[k * all + i];
+        ((T *)a.db.p)[i / a.out * a.db.client + i % a.out] = (T)total;
+        return;
+    }
     const HalfPlace p(s, a.rows, a.out);
     if (p.col >= s.line) return;
     int w[8], col[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         w[e] = s.by_rows && e < p.count ? s.w_exps[p.client * s.w_client + p.col + e] : 0;
-        col[e] = s.by_columns && e < p.count ? s.col_top[p.client * a.out + p.col + e] : 0;
+        col[e] = s.by_columns && e < p.count ? row_shift(s.col_top[p.client * a.out + p.col + e]) : 0;
     }
     const auto put = [&](_Float16 *to, const float (&v)[8], auto by) {
         half8 high, low;
@@ -221,17 +237,31 @@ __global__ __launch_bounds__(256) void k_half_dz(aet_mx4_linear_grad a, Drop d, 
         *(half8 *)to = high;
         if (sizeof(T) == 4) *(half8 *)(to + s.low) = low;
     };
-    for (int64_t row = p.first + p.ty; row < p.end; row += 8) {
-        float v[8];
-        dz_of<T, ACT, DROP>(a, d, p.client, row, p.col, p.count, v);
-        const int64_t at = (p.client * a.rows + row) * s.line + p.col;
-        if (s.by_rows) {
-            const int r = s.row_top[p.client * a.rows + row];
-            put(s.by_rows + at, v, [&](int e) { return w[e] - r; });
+    for (int64_t r0 = p.first + p.ty; r0 < p.end; r0 += 8 * kDzRows) {
+        DzPiece<T, ACT, DROP> piece[kDzRows];
+        int tops[kDzRows], xs[kDzRows];
+#pragma unroll
+        for (int i = 0; i < kDzRows; ++i) {
+            const int64_t row = r0 + 8 * i < p.end ? r0 + 8 * i : p.end - 1;
+            piece[i].load(a, p.client, row, p.col, p.count);
+            tops[i] = s.by_rows ? s.row_top[p.client * a.rows + row] : 0;
+            xs[i] = s.by_columns ? s.x_exps[p.client * a.rows + row] : 0;
         }
-        if (s.by_columns) {
-            const int x = s.x_exps[p.client * a.rows + row];
-            put(s.by_columns + at, v, [&](int e) { return x - col[e]; });
+#pragma unroll
+        for (int i = 0; i < kDzRows; ++i) {
+            const int64_t row = r0 + 8 * i;
+            if (row >= p.end) break;
+            float v[8];
+            piece[i].work(a, d, p.client, row, p.col, v);
+            const int64_t at = (p.client * a.rows + row) * s.line + p.col;
+            if (s.by_rows) {
+                const int r = row_shift(tops[i]);
+                put(s.by_rows + at, v, [&](int e) { return w[e] - r; });
+            }
+            if (s.by_columns) {
+                const int x = xs[i];
+                put(s.by_columns + at, v, [&](int e) { return x - col[e]; });
+            }
         }
     }
 }
@@ -316,7 +346,7 @@ bool mx4_half_pays(const aet_mx4_linear_grad &a) {
     const HalfPlan p = plan(a, (char *)256);
     if ((a.dx.p && !half_fits(p.dx)) || (a.dw.p && !half_fits(p.dw))) return false;
     if ((int64_t)a.n * a.rows > INT32_MAX || p.w_rows > INT32_MAX) return false;
-    float here = 20.0f, there = 0.0f;   // four launches more, and dz worked out twice
+    float here = 10.0f, there = 0.0f;   // two launches more, and dz worked out twice
     here += (float)a.n * (float)a.rows * (float)a.out * 2.0f * (a.dtype == AET_F32 ? 4 : 2) / 4e6f;
     for (const Product *q : {a.dx.p ? &p.dx : nullptr, a.dw.p ? &p.dw : nullptr}) {
         if (!q) continue;
@@ -333,19 +363,17 @@ template <typename T>
 static hipError_t run(const aet_mx4_linear_grad &a, char *workspace, hipStream_t s) {
     const HalfPlan p = plan(a, workspace);
     const int64_t rows = (int64_t)a.n * a.rows, blocks = (int64_t)a.n * p.s.across * p.s.strips;
-    if (blocks > INT32_MAX || p.count > (int64_t)INT32_MAX * 256) return hipErrorInvalidConfiguration;
-    if (a.dx.p) k_mx4_half<<<(int)p.w_rows, 256, 0, s>>>({a.w, a.w_scales}, p.w, p.w_exps, a.out, a.in, p.line);
-    if (a.dw.p) k_mx4_half<<<(int)rows, 256, 0, s>>>({a.x, a.x_scales}, p.x, p.x_exps, a.rows, a.in, p.line);
-    const int fill = (int)ceil_div(p.count, 256);
-    k_half_clear<<<fill, 256, 0, s>>>(p.tops, p.count);
+    if (blocks > INT32_MAX || p.w_rows + rows > INT32_MAX) return hipErrorInvalidConfiguration;
+    const HalfRows w = {{a.w, a.w_scales}, p.w, p.w_exps, a.out, p.w_rows}, x = {{a.x, a.x_scales}, p.x, p.x_exps, a.rows, a.dw.p ? rows : 0};
+    k_mx4_half<<<(int)ceil_div(w.all + x.all, 4), 256, 0, s>>>(w, x, a.in, p.line, p.tops, p.count);
+    const int64_t sums = a.db.p && p.s.strips > 1 ? ceil_div((int64_t)a.n * a.out, 256) : 0;
+    if (blocks + sums > INT32_MAX) return hipErrorInvalidConfiguration;
     const Drop d = make_drop(a.p, a.seed, a.first_row, a.out);
     const auto go = [&](auto act) {
         const auto tops = d.least ? k_half_tops<T, act, true> : k_half_tops<T, act, false>;
         const auto dz = d.least ? k_half_dz<T, act, true> : k_half_dz<T, act, false>;
         tops<<<(int)blocks, 256, 0, s>>>(a, d, p.s);
-        if (a.db.p && p.s.strips > 1) k_half_db<T><<<(int)ceil_div((int64_t)a.n * a.out, 256), 256, 0, s>>>(a, p.s);
-        k_half_shifts<<<fill, 256, 0, s>>>(p.tops, p.count);
-        dz<<<(int)blocks, 256, 0, s>>>(a, d, p.s);
+        dz<<<(int)(blocks + sums), 256, 0, s>>>(a, d, p.s);
     };
     switch (a.act) {
     case AET_ACT_RELU: go(std::integral_constant<int, AET_ACT_RELU>()); break;

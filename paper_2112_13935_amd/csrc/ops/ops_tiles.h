@@ -40,11 +40,14 @@ hipError_t launch_rows(int dtype, const Product &p, hipStream_t s);
 // Bytes of scratch that the product wants (for sums that are split along k).
 size_t product_workspace(int dtype, const Product &p);
 hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStream_t s);
-// C's rows times 2^exps[client * .client + row]
+// C's rows times 2^row_shift(tops[client * .client + row]), tops being the exponent of the largest value of the row that A stands for,
+// which was made to lie below 2^15 so (no more than kNoExponent: there is none).
 struct RowExponents {
-    const int32_t *exps;
+    const int32_t *tops;
     int64_t client;
 };
+constexpr int kNoExponent = -100000;
+__device__ __forceinline__ int row_shift(int top) { return top < kNoExponent / 2 ? 0 : top - 15; }
 // The same of fp16 operands (A in one part or two), B by columns, where both can go straight into LDS; dtype is C's.
 bool half_fits(const Product &p);
 size_t half_product_workspace(const Product &p);

@@ -116,7 +116,7 @@ struct Tile {
 };
 
 // O: the type of C and what is beside it.  HALF: the operands are fp16 (T says bf16, which lies as they do), and C's rows are
-// multiplied by 2^half.exps[row].
+// multiplied as `half` says.
 template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT, typename O = T, bool HALF = false>
 __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, const Shape &s, const Epilogue &e, int block, lds_ptr lds,
                                         const RowExponents &half = {}) {
@@ -332,7 +332,7 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
                 for (int y = 0; y < 4; ++y) v[4 * h + y] = x[y] + bias[4 * h + y];
             }
             if constexpr (HALF) {
-                const int by = row < s.M ? half.exps[client * half.client + row] : 0;
+                const int by = row < s.M ? row_shift(half.tops[client * half.client + row]) : 0;
 #pragma unroll
                 for (int y = 0; y < V; ++y) v[y] = __builtin_ldexpf(v[y], by);
             }

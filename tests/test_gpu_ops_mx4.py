@@ -201,6 +201,23 @@ def test_large_gradients_of_rows_of_all_sizes(ops, dtype):   # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_gradients_of_blocks_of_all_sizes(ops, dtype):   # noqa: F811
+    """Neighbouring blocks of W and x, whose scales are 2^-34 to 1 of the row's largest: each column of a product sees only its own blocks,
+    and dz is in as many bits for all of them."""
+    dt = TYPES[dtype]
+    n, rows, inp, out = 1, 1500, 1024, 1500
+    g = torch.Generator().manual_seed(3)
+    (x, xs), (w, ws) = held(g, (n, rows, inp)), held(g, (n, out, inp))
+    for t in (xs, ws):   # the same for all rows: a row of the contraction has its large blocks where the others have
+        t.copy_((127 - 34 * torch.arange(inp // 32) // (inp // 32 - 1)).to(torch.uint8).expand(t.shape))
+    dy, pre = rand(g, (n, rows, out), dt), rand(g, (n, rows, out), dt)
+    want = gradient(d64(dy), M.values(x, xs, inp), M.values(w, ws, inp), d64(pre), "silu", 0.0, 5, dt)
+    got = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act="silu")
+    for t, q, part in zip(got, want, ("dx", "dw", "db")):
+        O.near(t, q, part)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_large_gradients_that_are_not_finite(ops, dtype):   # noqa: F811
     dt = TYPES[dtype]
     n, rows, inp, out = 1, 1500, 1024, 1500
