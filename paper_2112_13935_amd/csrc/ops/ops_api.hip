@@ -569,7 +569,7 @@ aet_status aet_mx4_linear_forward(const aet_mx4_linear *a, void *workspace, size
 
 size_t aet_mx4_linear_backward_workspace_bytes(const aet_mx4_linear_grad *a) {
     bool shared;
-    if (check(a, &shared) != AET_OK || !a->n) return 0;
+    if (check(a, &shared) != AET_OK || (!a->n && !shared)) return 0;
     aet_mx4_linear_grad h = *a;
     if (fold(h, shared) && mx4_half_pays(h)) return mx4_half_workspace(h);
     size_t used;
@@ -580,7 +580,7 @@ size_t aet_mx4_linear_backward_workspace_bytes(const aet_mx4_linear_grad *a) {
 aet_status aet_mx4_linear_backward(const aet_mx4_linear_grad *a, void *workspace, size_t workspace_bytes, void *hip_stream) {
     bool shared;
     if (const aet_status st = check(a, &shared)) return st;
-    if (!a->n) return AET_OK;
+    if (!a->n && !shared) return AET_OK;
     aet_mx4_linear_grad h = *a;
     const bool half = fold(h, shared) && mx4_half_pays(h);
     size_t used = 0;

@@ -184,10 +184,8 @@ static int64_t line_of(int dtype, int64_t cols) { return ceil_div(cols, dtype ==
 static size_t expanded_bytes(int dtype, int64_t n, int64_t rows, int64_t cols) {
     return up256((size_t)n * rows * line_of(dtype, cols) * (dtype == AET_F32 ? 4 : 2));
 }
-static hipError_t expand(int dtype, int64_t n, int64_t rows, int64_t cols, const aet_in &codes, const aet_in &scales, void *to, aet_in *out, hipStream_t s) {
+static hipError_t expand(int dtype, int64_t n, int64_t rows, int64_t cols, const aet_in &codes, const aet_in &scales, void *to, hipStream_t s) {
     const int64_t line = line_of(dtype, cols);
-    *out = {to, n > 1 ? rows * line : 0, line};
-    if (!n || !rows || !cols) return hipSuccess;
     return launch_mx4_dequantise({dtype, (int32_t)n, (int32_t)rows, (int32_t)cols, codes, scales, {to, rows * line, line}}, s);
 }
 
@@ -201,6 +199,8 @@ hipError_t launch_mx4_linear_forward(const aet_mx4_linear &a, void *workspace, h
     return launch_mx4_product(a.dtype, forward_product(a), workspace, s);
 }
 
+// Sums over nothing: held values are not looked at.
+static bool nothing(const aet_mx4_linear_grad &a) { return !a.n || !a.rows || !a.in || !a.out; }
 aet_linear_grad mx4_plain_gradient(const aet_mx4_linear_grad &a, void *workspace, size_t *used) {
     aet_linear_grad b = {a.dtype, a.act, a.n, a.rows, a.in, a.out, a.p, a.seed, a.first_row};
     b.dy = a.dy;
@@ -209,17 +209,17 @@ aet_linear_grad mx4_plain_gradient(const aet_mx4_linear_grad &a, void *workspace
     b.dw = a.dw;
     b.db = a.db;
     const int64_t line = line_of(a.dtype, a.in), held = a.w.client ? a.n : 1;
-    const size_t x = a.dw.p ? expanded_bytes(a.dtype, a.n, a.rows, a.in) : 0;
+    const size_t x = a.dw.p && !nothing(a) ? expanded_bytes(a.dtype, a.n, a.rows, a.in) : 0;
     b.x = {workspace, a.rows * line, line};
     b.w = {(char *)workspace + x, held > 1 ? a.out * line : 0, line};
-    *used = x + (a.dx.p ? expanded_bytes(a.dtype, held, a.out, a.in) : 0);
+    *used = x + (a.dx.p && !nothing(a) ? expanded_bytes(a.dtype, held, a.out, a.in) : 0);
     return b;
 }
 hipError_t launch_mx4_expand(const aet_mx4_linear_grad &a, const aet_linear_grad &plain, hipStream_t s) {
-    aet_in out;
     hipError_t e = hipSuccess;
-    if (a.dw.p) e = expand(a.dtype, a.n, a.rows, a.in, a.x, a.x_scales, (void *)plain.x.p, &out, s);
-    if (e == hipSuccess && a.dx.p) e = expand(a.dtype, a.w.client ? a.n : 1, a.out, a.in, a.w, a.w_scales, (void *)plain.w.p, &out, s);
+    if (nothing(a)) return e;
+    if (a.dw.p) e = expand(a.dtype, a.n, a.rows, a.in, a.x, a.x_scales, (void *)plain.x.p, s);
+    if (e == hipSuccess && a.dx.p) e = expand(a.dtype, a.w.client ? a.n : 1, a.out, a.in, a.w, a.w_scales, (void *)plain.w.p, s);
     return e;
 }
 

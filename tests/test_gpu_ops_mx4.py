@@ -1,5 +1,7 @@
 """Microscaled 4-bit values, there and back, bit for bit, and the linear layer of them and its gradient against their
 definitions in 64 bits."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -333,6 +335,26 @@ def test_nothing_to_add(ops):   # noqa: F811
     assert dx.shape == (3, 0) and dw.shape == (4, 0) and bool((db == 3).all())
     c, s = ops.aet_mx4_quantise(torch.ones(2, 0, 5, device=DEV))
     assert c.shape == (2, 0, 3) and s.shape == (2, 0, 1) and ops.aet_mx4_dequantise(c, s, cols=5).shape == (2, 0, 5)
+
+
+def test_sums_over_nothing(ops):   # noqa: F811
+    """No clients with one W for all of them: its gradients are 0.  And what is not looked at need not be there."""
+    z = lambda *s: torch.zeros(*s, dtype=torch.uint8, device=DEV)   # noqa: E731
+    places = [torch.full(s, 7.0, device=DEV) for s in ((4, 16), (4,))]
+    dx, dw, db = ops.aet_mx4_linear_backward(torch.ones(0, 5, 4, device=DEV), z(0, 5, 8), z(0, 5, 1), z(4, 8), z(4, 1), out=(None, *places))
+    assert dx.shape == (0, 5, 16) and dw is places[0] and bool((dw == 0).all() and (db == 0).all())
+    lib, stream = ops.load_library(), torch.cuda.current_stream().cuda_stream
+    for rows, out in ((0, 4), (3, 0)):
+        dx, dw, db = (torch.full(s, 7.0, device=DEV) for s in ((2, max(rows, 1), 16), (2, max(out, 1), 16), (2, max(out, 1))))
+        a = ops.aet_mx4_linear_grad(0, 0, 2, rows, 16, out)
+        for f, t in (("dx", dx), ("dw", dw), ("db", db)):
+            setattr(a, f + "_p", t.data_ptr())
+            setattr(a, f + "_client", t.stride(0))
+            setattr(a, f + "_row", 16)
+        need = lib.aet_mx4_linear_backward_workspace_bytes(C.addressof(a))
+        space = torch.empty(max(need, 1), dtype=torch.uint8, device=DEV)
+        assert lib.aet_mx4_linear_backward(C.addressof(a), space.data_ptr(), need, stream) == 0
+        assert bool((dx == (0 if rows else 7)).all() and (dw == (0 if out else 7)).all() and (db == (0 if out else 7)).all())
 
 
 def test_what_is_wanted(ops):   # noqa: F811
