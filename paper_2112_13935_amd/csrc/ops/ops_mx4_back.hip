@@ -19,6 +19,8 @@ namespace aet_ops {
 typedef int i4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 
+constexpr int kNone = kNoExponent;
+
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Rows of held values as fp16, times 2^-exps[row], where exps is the exponent of the row's largest block that has a value, less 13
@@ -69,7 +71,7 @@ __global__ __launch_bounds__(256) void k_mx4_half(HalfRows w, HalfRows x, int co
         top = o > top ? o : top;
     }
     const int shift = (top == INT_MIN ? 127 : top) - 13;   // scales become scale - shift + 127
-    if (lane == 0) r.exps[at] = shift - 127;
+    if (lane == 0) r.exps[at] = top == INT_MIN ? kNone : shift - 127;   // (a row of zeros weighs nothing)
 #pragma unroll 4
     for (int i = lane; i < pieces; i += 64) {
         const int scale = i / 4 < blocks ? scales[i / 4] : 127, moved = scale - shift + 127;
@@ -128,8 +130,6 @@ struct HalfPlace {
         end = first + s.strip < rows ? first + s.strip : rows;
     }
 };
-
-constexpr int kNone = kNoExponent;
 
 // |v| < 2^exponent; nothing for 0 and what is not finite
 __device__ __forceinline__ int exponent_of(float v) {

@@ -203,6 +203,25 @@ def test_large_gradients_of_rows_of_all_sizes(ops, dtype):   # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_gradients_beside_rows_of_zeros(ops, dtype):   # noqa: F811
+    """Every second row of W and x is zeros, the others are tiny: what the zeros have for a scale is no matter."""
+    dt = TYPES[dtype]
+    n, rows, inp, out = 1, 1500, 1024, 1500
+    g = torch.Generator().manual_seed(3)
+    (x, xs), (w, ws) = held(g, (n, rows, inp)), held(g, (n, out, inp))
+    for c, s in ((x, xs), (w, ws)):
+        s -= 70
+        c[:, ::2] = 0
+    dy, pre = rand(g, (n, rows, out), dt), rand(g, (n, rows, out), dt)
+    want = gradient(d64(dy), M.values(x, xs, inp), M.values(w, ws, inp), d64(pre), "silu", 0.0, 5, dt)
+    got = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act="silu")
+    for t, (v, bound), part in zip(got, want, ("dx", "dw", "db")):
+        # (beside the bound: 2^-39 of the largest term of the row of the contraction, for each)
+        room = 2.0 ** -39 * v.abs().amax(-1, keepdim=True) * 1500 if part != "db" else 0
+        O.near(t, (v, bound + room), part)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_large_gradients_of_blocks_of_all_sizes(ops, dtype):   # noqa: F811
     """Neighbouring blocks of W and x, whose scales are 2^-34 to 1 of the row's largest: each column of a product sees only its own blocks,
     and dz is in as many bits for all of them."""
