@@ -302,7 +302,7 @@ static aet_status check(const aet_orthogonal *a) {
     if (a->rows > kMostSide || a->cols > kMostSide) return fail(AET_EINVAL, "a side of the matrices is over 2^20");
     if (a->steps < 0 || a->steps > 100) return fail(AET_EINVAL, "steps is not in [0, 100]");
     if (!(a->eps >= 0) || !isfinite(a->eps)) return fail(AET_EINVAL, "eps is negative or not finite");
-    if (!isfinite(a->a) || !isfinite(a->b) || !isfinite(a->c) || !isfinite(a->keep) || !isfinite(a->scale))
+    if (!isfinite(a->a) || !isfinite(a->b) || !isfinite(a->c) || !isfinite((float)a->keep) || !isfinite(a->scale))
         return fail(AET_EINVAL, "a, b, c, keep and scale have to be finite");
     if (!orthogonal_bounded(*a)) return fail(AET_EINVAL, "singular values up to 1 grow beyond 2^30 under this polynomial");
     if (!a->n || !a->rows || !a->cols) return AET_OK;

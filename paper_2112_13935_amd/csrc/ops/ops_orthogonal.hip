@@ -99,11 +99,12 @@ bool orthogonal_bounded(const aet_orthogonal &o) {
     return true;
 }
 // A power of two that takes a value of this bound to 2^14 or more and less than 2^15, of a type whose largest value is nearly 2^16.
+// (Below 2^-400 no more: what is multiplied with it stays in 64 bits' range, and is nothing in the result.)
 __device__ inline double room_of(double bound) {
     if (!(bound > 0)) return 1;
     int e;
     frexp(bound, &e);
-    return ldexp(1.0, 15 - e);
+    return ldexp(1.0, 15 - (e > -400 ? e : -400));
 }
 
 // The largest |a + b q + c q^2| over q in [0, top^2]: how much a step makes of a singular value, at most

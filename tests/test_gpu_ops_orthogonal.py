@@ -134,6 +134,15 @@ def test_other_polynomials(ops):   # noqa: F811
               torch.float32, f"{polynomial}")
 
 
+def test_an_eps_far_above_the_gradient(ops):   # noqa: F811
+    """Singular values whose squares are nothing in 64 bits."""
+    gen = torch.Generator().manual_seed(4)
+    g, w = rand(gen, (2, 60, 90), torch.float32), rand(gen, (2, 60, 90), torch.float32)
+    for eps in (1e30, 1e100, 1e150, 1e156, 1e160, 1e165, 1e200, 1e308):
+        for polynomial in (MUON, (0.0, 1.0, 0.0)):
+            assert torch.equal(ops.aet_orthogonalise(g, w=w, keep=0.5, eps=eps, polynomial=polynomial), 0.5 * w), eps
+
+
 def test_nothing_to_do(ops):   # noqa: F811
     for shape in ((0, 3, 4), (2, 0, 4), (2, 3, 0), (0, 5)):
         assert ops.aet_orthogonalise(torch.ones(*shape, device=DEV)).shape == shape

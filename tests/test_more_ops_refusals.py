@@ -132,7 +132,7 @@ def orthogonal(**k):
 
 @pytest.mark.parametrize("wrong", SIZES + [dict(cols=-1), dict(cols=(1 << 20) + 1), dict(rows=(1 << 20) + 1), dict(steps=-1), dict(steps=101), dict(eps=-1.0),
                                            dict(eps=float("nan")), dict(eps=float("inf")), dict(a=float("nan")), dict(b=float("inf")), dict(c=float("nan")),
-                                           dict(keep=float("inf")), dict(scale=float("nan")), dict(a=1e7), dict(c=1e30), dict(b=-1e30), dict(g_p=None),
+                                           dict(keep=float("inf")), dict(keep=1e39), dict(scale=float("nan")), dict(a=1e7), dict(c=1e30), dict(b=-1e30), dict(g_p=None),
                                            dict(y_p=None), dict(g_p=P + 2), dict(w_p=P + 1), dict(g_row=-1), dict(w_client=-1), dict(y_row=7), dict(y_client=23)],
                          ids=str)
 def test_orthogonalise_refused(lib, wrong):   # noqa: F811
