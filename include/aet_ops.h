@@ -12,11 +12,13 @@
  *     calls that need scratch memory take a workspace (size from aet_*_workspace_bytes,
  *     256-byte aligned; NULL where that is 0).  It keeps nothing between calls.
  *   - All tensors of a call have the call's dtype, but for the statistics of a normalisation
- *     (fp32).  Products, sums, statistics and everything between a call's inputs and its
- *     outputs are fp32 or wider; an output is rounded once, to its type.  Two exceptions: dz in
- *     the gradient of a linear layer in bf16 (named there); and fp32 products of more than 32
- *     rows, and all of fp32 gradients, take their operands to within 2^-134, which is less
- *     than 24 bits of one below 2^-110 (forward products of up to 32 rows take all of them).
+ *     (fp32), and held values (bytes).  Products, sums, statistics and everything between a
+ *     call's inputs and its outputs are fp32 or wider; an output is rounded once, to its type.
+ *     Exceptions: dz in the gradient of a linear layer in bf16, dz in that of a layer of held
+ *     values, and the matrices between the steps of an orthogonalised update (named there);
+ *     and fp32 products of more than 32 rows, and all of fp32 gradients, take their operands
+ *     to within 2^-134, which is less than 24 bits of one below 2^-110 (forward products of up
+ *     to 32 rows take all of them).
  *   - Strides are in elements; the last axis has stride 1.  Inputs may have any strides that
  *     are not negative (0: the same values for every row or client).  Outputs must not
  *     overlap themselves, nor an input, except where a call says so.  Any alignment that
@@ -240,9 +242,9 @@ aet_status aet_orthogonalise(const aet_orthogonal *a, void *workspace, size_t wo
  *   codes   a byte for two columns, the even one in its lower half: the sign's bit, and the place of the
  *           magnitude in the list above.  ceil(cols / 2) bytes a row; a half that is left is 0, and not read.
  *   scales  a byte for a block: x + 127, or 255 for NaN.  ceil(cols / 32) bytes a row.
- * (The OCP Microscaling Formats specification's MXFP4.)  Their strides are in bytes, of any alignment; codes
- * at multiples of 16 and scales at multiples of 4 bytes, rows too, are faster in products.  Any bytes are
- * legal codes and scales. */
+ * (The OCP Microscaling Formats specification's MXFP4.)  Their strides are in bytes, of any alignment;
+ * products of more than 32 rows are faster where the columns are a multiple of 512, and rows of codes and of scales begin
+ * at multiples of 16 bytes: else they are first copied so, into the workspace.  Any bytes are legal codes and scales. */
 
 /* x, n x rows x cols, to codes and scales. */
 typedef struct {
@@ -282,8 +284,9 @@ aet_status aet_mx4_linear_forward(const aet_mx4_linear *a, void *workspace, size
 
 /* Its gradient with regard to what the codes stand for, from the codes: dx = dz W, dw = dz^T x, db = sum of dz over
  * rows.  (That of the values that were quantised is the same where rounding is taken to have a slope of 1.)  dtype is that
- * of dy, pre, dx, dw and db; all else as in aet_linear_grad, where x, if dw is wanted, and w, if dx is, stand for rows
- * that lie one after another. */
+ * of dy, pre, dx, dw and db; all else as in aet_linear_grad, but x may lie anyhow also where one W is for all.  The products
+ * take dz to within 2^-11 of each value where dtype is AET_BF16, else 2^-22, or to within 2^-39 of the largest term of its row (of dx)
+ * or column (of dw), whichever is more, and leave out blocks of a row of W or x below 2^-36 of the largest one of the row. */
 typedef struct {
     int32_t dtype, act;
     int32_t n, rows, in, out;

@@ -3,6 +3,8 @@
 // Bound by memory.  Four lanes have a block of 32 values, 8 each: their largest magnitude's exponent by two exchanges
 // between neighbours, then the hardware's conversions, which divide by the scale (given by its exponent alone; 0 is 2^-127,
 // 255 NaN), round to the nearest of the 16 values, ties to the even code, and end at 6.
+//   16384 x 4096 of bf16 to codes and scales 32 us (5.3 TB/s); 16384 x 8192 there and back 140 us, at a large copy's rate
+//   (5.0 TB/s) 136; 128 x 784 of fp32 there and back 9.8 us, the two calls.
 #include "ops_internal.h"
 #include "ops_mx4.h"
 
@@ -13,7 +15,12 @@ namespace aet_ops {
 typedef bf16 bf2 __attribute__((ext_vector_type(2)));
 typedef float f2 __attribute__((ext_vector_type(2)));
 
-constexpr int kRows = 4;   // of a thread, all on their way at once
+// Rows of a thread, all on their way at once.  16384 x 8192, microseconds for 1, 2, 4 rows: of bf16 to codes 81, 67, 67 (half as many
+// columns 36, 31, 33) and back 87, 71, 66; of fp32, twice the bytes a row, 105, 111, 115 and 140, 153, 159.
+template <typename T>
+constexpr int kToRows = sizeof(T) == 2 ? 2 : 1;
+template <typename T>
+constexpr int kBackRows = sizeof(T) == 2 ? 4 : 1;
 
 struct Mx4Shape {
     int pieces, wide;         // pieces of 8 columns in a row, whole blocks; threads side by side (a power of two, 4 and more)
@@ -24,12 +31,13 @@ struct Mx4Place {
     int64_t client, row0;
     int col, high;
 };
+template <int ROWS>
 __device__ __forceinline__ bool place_of(const Mx4Shape &s, Mx4Place &p) {
     const int64_t per = s.across * s.down, b = blockIdx.x % per;
     p.client = blockIdx.x / per;
     const int piece = (int)(b % s.across) * s.wide + (threadIdx.x & (s.wide - 1));
     p.high = 256 / s.wide;
-    p.row0 = b / s.across * (p.high * kRows) + threadIdx.x / s.wide;
+    p.row0 = b / s.across * (p.high * ROWS) + threadIdx.x / s.wide;
     p.col = piece * 8;
     return piece < s.pieces;   // (the same for the four lanes of a block)
 }
@@ -69,20 +77,21 @@ __device__ __forceinline__ uint32_t quantise8(const wide<T, 8> &v, uint32_t &sca
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_quantise(aet_mx4_values a, Mx4Shape s) {
+    constexpr int ROWS = kToRows<T>;
     Mx4Place p;
-    if (!place_of(s, p)) return;
+    if (!place_of<ROWS>(s, p)) return;
     const T *x = (const T *)a.x.p + p.client * a.x.client + p.col;
     uint8_t *codes = (uint8_t *)a.codes.p + p.client * a.codes.client + p.col / 2;
     uint8_t *scales = (uint8_t *)a.scales.p + p.client * a.scales.client + p.col / 32;
     const int count = a.cols - p.col, bytes = (count + 1) / 2;
-    wide<T, 8> v[kRows];
+    wide<T, 8> v[ROWS];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
         const int64_t row = p.row0 + i * p.high;
         if (row < a.rows) v[i] = load_raw<T, 8>(x + row * a.x.row, count);
     }
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
         const int64_t row = p.row0 + i * p.high;
         if (row >= a.rows) continue;
         uint32_t scale;
@@ -115,15 +124,16 @@ __device__ __forceinline__ wide<T, 8> expand8(uint32_t code, uint32_t scale) {
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_dequantise(aet_mx4_codes a, Mx4Shape s) {
+    constexpr int ROWS = kBackRows<T>;
     Mx4Place p;
-    if (!place_of(s, p) || p.col >= a.cols) return;
+    if (!place_of<ROWS>(s, p) || p.col >= a.cols) return;
     const uint8_t *codes = (const uint8_t *)a.codes.p + p.client * a.codes.client + p.col / 2;
     const uint8_t *scales = (const uint8_t *)a.scales.p + p.client * a.scales.client + p.col / 32;
     T *y = (T *)a.y.p + p.client * a.y.client + p.col;
     const int count = a.cols - p.col, bytes = (count + 1) / 2;
-    uint32_t code[kRows], scale[kRows];
+    uint32_t code[ROWS], scale[ROWS];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
         const int64_t row = p.row0 + i * p.high;
         if (row >= a.rows) continue;
         const uint8_t *from = codes + row * a.codes.row;
@@ -137,7 +147,7 @@ __global__ __launch_bounds__(256) void k_mx4_dequantise(aet_mx4_codes a, Mx4Shap
         scale[i] = scales[row * a.scales.row];
     }
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
         const int64_t row = p.row0 + i * p.high;
         if (row >= a.rows) continue;
         const wide<T, 8> v = expand8<T>(code[i], scale[i]);
@@ -150,18 +160,18 @@ __global__ __launch_bounds__(256) void k_mx4_dequantise(aet_mx4_codes a, Mx4Shap
     }
 }
 
-static bool shape_of(int64_t n, int64_t rows, int64_t cols, Mx4Shape *s, int64_t *blocks) {
+static bool shape_of(int64_t n, int64_t rows, int64_t cols, int each, Mx4Shape *s, int64_t *blocks) {
     *s = {(int)ceil_div(cols, 32) * 4, 4, 0, 0};
     while (s->wide < s->pieces && s->wide < 256) s->wide *= 2;
     s->across = ceil_div(s->pieces, s->wide);
-    s->down = ceil_div(rows, 256 / s->wide * kRows);
+    s->down = ceil_div(rows, 256 / s->wide * each);
     *blocks = n * s->across * s->down;
     return *blocks <= INT32_MAX;
 }
 hipError_t launch_mx4_quantise(const aet_mx4_values &a, hipStream_t s) {
     Mx4Shape d;
     int64_t blocks;
-    if (!shape_of(a.n, a.rows, a.cols, &d, &blocks)) return hipErrorInvalidConfiguration;
+    if (!shape_of(a.n, a.rows, a.cols, a.dtype == AET_F32 ? kToRows<float> : kToRows<bf16>, &d, &blocks)) return hipErrorInvalidConfiguration;
     if (a.dtype == AET_F32) k_mx4_quantise<float><<<(int)blocks, 256, 0, s>>>(a, d);
     else k_mx4_quantise<bf16><<<(int)blocks, 256, 0, s>>>(a, d);
     return hipGetLastError();
@@ -169,7 +179,7 @@ hipError_t launch_mx4_quantise(const aet_mx4_values &a, hipStream_t s) {
 hipError_t launch_mx4_dequantise(const aet_mx4_codes &a, hipStream_t s) {
     Mx4Shape d;
     int64_t blocks;
-    if (!shape_of(a.n, a.rows, a.cols, &d, &blocks)) return hipErrorInvalidConfiguration;
+    if (!shape_of(a.n, a.rows, a.cols, a.dtype == AET_F32 ? kBackRows<float> : kBackRows<bf16>, &d, &blocks)) return hipErrorInvalidConfiguration;
     if (a.dtype == AET_F32) k_mx4_dequantise<float><<<(int)blocks, 256, 0, s>>>(a, d);
     else k_mx4_dequantise<bf16><<<(int)blocks, 256, 0, s>>>(a, d);
     return hipGetLastError();
