@@ -3,6 +3,11 @@
 // C[m][n] = sum over k of A(m, k) B(n, k), both as codes by rows with a scale for each 32 k.  A lane of
 // v_mfma_scale_f32_32x32x64_f8f6f4 has the 16 bytes and the scale of one block of a row: the codes go as they lie in
 // memory from there to LDS and to the unit, four times the values a byte of bf16 products.
+//
+// Bound by the matrix unit where there is enough to do: a loop of its instructions alone runs at 5.0 to 5.8 PF/s with random codes (8.7
+// with zeros: the clock gives way).  To bf16: 16384 x 4096 x 4096 198 to 211 us (2.7 PF/s; with bias and GELU 225), 8192^3 317 (3.5).
+// A tile of 256 x 256 takes 2.0 us for 256 k, of which the unit has 1.5, and some 10 from its first load to its last store beside
+// that, a quarter of 16 stages' time; two tiles at once, which would hide that, do not fit into LDS.
 #include "ops_internal.h"
 #include "ops_mx4.h"
 #include "ops_stage.h"
@@ -19,7 +24,9 @@ __device__ __forceinline__ i8v widen(i4 v) { return __builtin_shufflevector(v, v
 
 // ---- tiles -------------------------------------------------------------------------------
 
-constexpr int kDeep = 256, kGroup = 4;   // k of a stage, 128 bytes of codes a row; stages whose scales come together, 32 bytes a row
+// k of a stage, 128 bytes of codes a row (64 bytes a row, half the k: all kinds of tiles at 2.2 PF/s); stages whose scales come
+// together, 32 bytes a row
+constexpr int kDeep = 256, kGroup = 4;
 constexpr int kUnit = 512;               // sums are whole ones of these: 16 bytes of scales a row
 
 // Scales of BM rows of A and BN of B, a group of stages at a time.  (8 bytes a row and stage would be a line of memory for each.)
@@ -243,6 +250,7 @@ __global__ __launch_bounds__(64 * WR * WC, BM == 64 ? 4 : 2) void k_mx4_tiles(He
 
 // ---- few rows ----------------------------------------------------------------------------
 
+// Up to 32 rows: bound by reading W once, and by latency.  One row by 4096 x 4096 5.3 us (8.9 MB: 1.7 TB/s; the call alone takes 5).
 // 16 outputs a workgroup and all rows, its waves parts of the sum; operands go from memory straight into the lanes that want them
 // (v_mfma_scale_f32_16x16x128_f8f6f4: a lane has a block of a row), several steps ahead of their use.  Any alignment, any end of a sum.
 struct HeldRows {
@@ -329,7 +337,9 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_mx4_rows(Held oa, Held ob, H
 static bool rows_fit(const HeldProduct &p) { return p.M <= 32 || p.K >= 1 << 24; }
 
 // Kinds of tiles, as in ops_tiles.hip: microseconds for a stage where a compute unit has one workgroup, for each further one
-// up to the `fit` that it holds, and for each workgroup's epilogue.
+// up to the `fit` that it holds, and for each workgroup's epilogue.  Of 24 sizes between 64 x 512 x 512 and 8192 x 8192 x 4096 the choice is
+// the fastest kind and split or within 8 % of it; e. g. in tiles of 256, 128, 64: 512 x 4096 x 4096 34, 17, 12.6 us; 2048 x 4096 x 4096 37,
+// 27, 34; 4096^3 43, 49, 66; 512 x 512 x 16384 in 4 parts 37, 21, 15 (whole 111, 47, 31).
 struct Kind {
     int bm, bn, fit;
     float alone, more, end;

@@ -16,6 +16,10 @@
 // noise, five steps (two such runs): 1e-5 to 6e-5; step by step 4e-6 to 3e-5, with products in fp32 6e-6 to 5e-5 (a run of all five: 3e-2).
 //
 // All matrices of a call lie in the workspace with zeros up to whole tiles, so that no product has to look where they end.
+//
+// Five steps, y = keep w + scale X: 4096 x 4096 of fp32 4.2 to 4.5 ms (the matrix unit at 920 to 990 TF/s), 4 x 1024 x 4096 in bf16 760 to 800 us
+// (step by step 1120; the products of 1024^3 in tiles of 64, whose operands come from the L2s at 12.7 TB/s: 22 of 31 us each), 3 x 1001 x 515
+// of fp32 190 to 205 (18 launches: 4 us each to begin and to end), 16 x 128 x 784 of fp32 125 (the same).
 #include <math.h>
 
 #include <type_traits>
@@ -551,12 +555,14 @@ __global__ __launch_bounds__(256) void k_half_join(HalfProduct p, int tiles) {
 // ---- the steps ---------------------------------------------------------------------------
 
 // Kinds of tiles: microseconds for 32 k where a compute unit has one workgroup (`busy`: more when all units have one), for each further
-// one up to the `fit` that it holds, and for a workgroup's beginning and end.  Measured on products of 64 to 4096.
+// one up to the `fit` that it holds, and for a workgroup's beginning and end.  Measured on products of 64 to 4096.  (Tiles of 64 with three
+// stages on their way, of which a unit holds three: 1024 x 1024 3 % slower than with four.  With twice the waves, each of a pair with every
+// other 16 k: 16 x 128 x 784 130 us, 3 x 1001 x 515 188, as with one.)
 struct Kind {
-    int tile, deep, fit;
+    int tile, fit;
     float alone, busy, more, end;
 };
-static const Kind kKinds[] = {{256, 2, 1, 1.7f, 0.8f, 0.0f, 8.0f}, {128, 2, 2, 0.58f, 0.2f, 0.62f, 5.0f}, {64, 4, 2, 0.22f, 0.0f, 0.13f, 3.5f}, {64, 2, 4, 0.42f, 0.0f, 0.11f, 3.5f}};
+static const Kind kKinds[] = {{256, 1, 1.7f, 0.8f, 0.0f, 8.0f}, {128, 2, 0.58f, 0.2f, 0.62f, 5.0f}, {64, 2, 0.22f, 0.0f, 0.13f, 3.5f}};
 struct Choice {
     const Kind *kind;
     int slices;
@@ -729,7 +735,7 @@ static hipError_t product(const Choice &c, HalfProduct p, hipStream_t s) {
     hipError_t e;
     if (t == 256) e = run_half<256, 2, 4, 2, SYM, !SYM>(p, s);
     else if (t == 128) e = run_half<128, 2, 2, 2, SYM, false>(p, s);
-    else e = c.kind->deep == 2 ? run_half<64, 2, 2, 2, SYM, false>(p, s) : run_half<64, 2, 2, 4, SYM, false>(p, s);
+    else e = run_half<64, 2, 2, 4, SYM, false>(p, s);
     if (e != hipSuccess || p.slices == 1) return e;
     k_half_join<SYM><<<(int)(joins * p.clients), 256, 0, s>>>(p, (int)joins);
     return hipGetLastError();
