@@ -52,9 +52,10 @@ __device__ __forceinline__ int row_shift(int top) { return top < kNoExponent / 2
 bool half_fits(const Product &p);
 size_t half_product_workspace(const Product &p);
 hipError_t launch_half_product(int dtype, const Product &p, const RowExponents &half, void *workspace, hipStream_t s);
-// Microseconds that the two are expected to take.
+// Microseconds that products are expected to take; of a layer's gradients (the operands of launch_product in one piece, or by
+// launch_pair), those that have clients.
 float half_product_time(const Product &p);
-float product_time(int dtype, const Product &p);
+float gradients_time(int dtype, const Product &x, const Product &w);
 // Both gradients of a layer in one launch, where both are small (taken).
 hipError_t launch_pair(int dtype, const Product &x, const Product &w, hipStream_t s, bool *taken);
 

@@ -539,7 +539,6 @@ size_t half_product_workspace(const Product &p) {
     return slices > 1 ? (size_t)slices * p.clients * p.M * p.N * sizeof(float) : 0;
 }
 float half_product_time(const Product &p) { return choose(AET_BF16, p, true).time; }
-float product_time(int dtype, const Product &p) { return choose(dtype, p, dtype == AET_BF16).time; }
 
 template <typename O, int BM, int BN, int WR, int WC, bool TA>
 static hipError_t run_half(const Product &p, const Shape &s, const RowExponents &half, hipStream_t stream) {
@@ -578,6 +577,20 @@ hipError_t launch_half_product(int dtype, const Product &p, const RowExponents &
     return p.a.by_columns ? run_half<bf16, true>(p, half, workspace, s) : run_half<bf16, false>(p, half, workspace, s);
 }
 
+// Two products in one launch, in tiles of the smallest kind, sums in one piece
+static float pair_time(const Kind &k, const Product &x, const Shape &sx, const Product &w, const Shape &sw) {
+    return time_of(k, ceil_div(x.K > w.K ? x.K : w.K, k.bk) * (x.a.low ? 2 : 1), (int64_t)sx.blocks + sw.blocks);
+}
+float gradients_time(int dtype, const Product &x, const Product &w) {
+    const bool d = dtype == AET_BF16;
+    const float one = (x.clients ? choose(dtype, x, d).time : 0.0f) + (w.clients ? choose(dtype, w, d).time : 0.0f);
+    const Choice pair = {d ? &kKinds16[3] : &kKinds32[2], 1};
+    Shape sx, sw;
+    if (!x.clients || !w.clients || !shape_of(x, pair, nullptr, &sx) || !shape_of(w, pair, nullptr, &sw)) return one;
+    const float both = pair_time(*pair.kind, x, sx, w, sw);
+    return both < one + 3.0f ? both : one + 3.0f;
+}
+
 template <typename T>
 static hipError_t run_pair(const Product &x, const Product &w, hipStream_t stream, bool *taken) {
     const int dtype = sizeof(T) == 4 ? AET_F32 : AET_BF16;
@@ -590,7 +603,7 @@ static hipError_t run_pair(const Product &x, const Product &w, hipStream_t strea
     if (d != straight<T>(w) || !shape_of(x, one, nullptr, &sx) || !shape_of(w, one, nullptr, &sw) || !sx.blocks || !sw.blocks ||
         sx.blocks > INT32_MAX - sw.blocks)
         return hipSuccess;
-    if (time_of(k, ceil_div(x.K > w.K ? x.K : w.K, k.bk) * (x.a.low ? 2 : 1), (int64_t)sx.blocks + sw.blocks) > choose(dtype, x, d).time + choose(dtype, w, d).time + 3.0f)
+    if (pair_time(k, x, sx, w, sw) > choose(dtype, x, d).time + choose(dtype, w, d).time + 3.0f)
         return hipSuccess;
     *taken = true;
     constexpr int BK = sizeof(T) == 4 ? 32 : 64;
