@@ -3,7 +3,7 @@
 // Bound by memory.  Four lanes have a block of 32 values, 8 each: their largest magnitude's exponent by two exchanges
 // between neighbours, then the hardware's conversions, which divide by the scale (given by its exponent alone; 0 is 2^-127,
 // 255 NaN), round to the nearest of the 16 values, ties to the even code, and end at 6.
-//   16384 x 4096 of bf16 to codes and scales 32 us (5.3 TB/s); 16384 x 8192 there and back 140 us, at a large copy's rate
+//   16384 x 4096 of bf16 to codes and scales 31 us (5.5 TB/s); 16384 x 8192 there and back 139 us, at a large copy's rate
 //   (5.0 TB/s) 136; 128 x 784 of fp32 there and back 9.8 us, the two calls.
 #include "ops_internal.h"
 #include "ops_mx4.h"
