@@ -1,6 +1,6 @@
 // Microscaled 4-bit floating point: values to codes and scales, and back.
 //
-// Bound by memory.  Four lanes have a block of 32 values, 8 each: their largest magnitude's exponent by two exchanges
+// Bound by memory.  To codes four lanes have a block of 32 values, 8 each: their largest magnitude's exponent by two exchanges
 // between neighbours, then the hardware's conversions, which divide by the scale (given by its exponent alone; 0 is 2^-127,
 // 255 NaN), round to the nearest of the 16 values, ties to the even code, and end at 6.
 //   16384 x 4096 of bf16 to codes and scales 31 us (5.5 TB/s); 16384 x 8192 there and back 139 us, at a large copy's rate
@@ -15,15 +15,16 @@ namespace aet_ops {
 typedef bf16 bf2 __attribute__((ext_vector_type(2)));
 typedef float f2 __attribute__((ext_vector_type(2)));
 
-// Rows of a thread, all on their way at once.  16384 x 8192, microseconds for 1, 2, 4 rows: of bf16 to codes 81, 67, 67 (half as many
-// columns 36, 31, 33) and back 87, 71, 66; of fp32, twice the bytes a row, 105, 111, 115 and 140, 153, 159.
+// Rows of a thread, all on their way at once, and its columns.  16384 x 8192, microseconds for 1, 2, 4 rows: 8 columns of bf16 to codes 81, 67, 67 (of
+// half as many 36, 31, 33) and back 87, 71, 66; of fp32, where that is 32 bytes, 105, 111, 115 and 140, 153, 159; 4 columns of fp32
+// 145, 118, 121 and 156, 132, 125.
 template <typename T>
 constexpr int kToRows = sizeof(T) == 2 ? 2 : 1;
 template <typename T>
-constexpr int kBackRows = sizeof(T) == 2 ? 4 : 1;
+constexpr int kBackPiece = 16 / sizeof(T);
 
 struct Mx4Shape {
-    int pieces, wide;         // pieces of 8 columns in a row, whole blocks; threads side by side (a power of two, 4 and more)
+    int pieces, wide;         // pieces of V columns in a row, whole blocks; threads side by side (a power of two, a block's and more)
     int64_t across, down;     // workgroups: of a row of pieces, of a client
 };
 
@@ -31,15 +32,15 @@ struct Mx4Place {
     int64_t client, row0;
     int col, high;
 };
-template <int ROWS>
+template <int V, int ROWS>
 __device__ __forceinline__ bool place_of(const Mx4Shape &s, Mx4Place &p) {
     const int64_t per = s.across * s.down, b = blockIdx.x % per;
     p.client = blockIdx.x / per;
     const int piece = (int)(b % s.across) * s.wide + (threadIdx.x & (s.wide - 1));
     p.high = 256 / s.wide;
     p.row0 = b / s.across * (p.high * ROWS) + threadIdx.x / s.wide;
-    p.col = piece * 8;
-    return piece < s.pieces;   // (the same for the four lanes of a block)
+    p.col = piece * V;
+    return piece < s.pieces;   // (the same for the lanes of a block)
 }
 
 // 8 values to codes; the block's scale
@@ -79,7 +80,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_quantise(aet_mx4_values a, Mx4Shape s) {
     constexpr int ROWS = kToRows<T>;
     Mx4Place p;
-    if (!place_of<ROWS>(s, p)) return;
+    if (!place_of<8, ROWS>(s, p)) return;
     const T *x = (const T *)a.x.p + p.client * a.x.client + p.col;
     uint8_t *codes = (uint8_t *)a.codes.p + p.client * a.codes.client + p.col / 2;
     uint8_t *scales = (uint8_t *)a.scales.p + p.client * a.scales.client + p.col / 32;
@@ -107,26 +108,23 @@ __global__ __launch_bounds__(256) void k_mx4_quantise(aet_mx4_values a, Mx4Shape
 }
 
 template <typename T>
-__device__ __forceinline__ wide<T, 8> expand8(uint32_t code, uint32_t scale) {
+__device__ __forceinline__ wide<T, kBackPiece<T>> expand_piece(uint32_t code, uint32_t scale) {
     const float by = __builtin_bit_cast(float, scale << 23);
-    wide<T, 8> v;
     if constexpr (sizeof(T) == 2) {
         const bf2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, by, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, by, 1),
                   c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, by, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, by, 3);
-        v = wide<T, 8>{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+        return wide<T, 8>{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     } else {
-        const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, by, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, by, 1),
-                 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, by, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, by, 3);
-        v = wide<T, 8>{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+        const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, by, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, by, 1);
+        return wide<T, 4>{a[0], a[1], b[0], b[1]};
     }
-    return v;
 }
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_dequantise(aet_mx4_codes a, Mx4Shape s) {
-    constexpr int ROWS = kBackRows<T>;
+    constexpr int ROWS = 4, V = kBackPiece<T>;
     Mx4Place p;
-    if (!place_of<ROWS>(s, p) || p.col >= a.cols) return;
+    if (!place_of<V, ROWS>(s, p) || p.col >= a.cols) return;
     const uint8_t *codes = (const uint8_t *)a.codes.p + p.client * a.codes.client + p.col / 2;
     const uint8_t *scales = (const uint8_t *)a.scales.p + p.client * a.scales.client + p.col / 32;
     T *y = (T *)a.y.p + p.client * a.y.client + p.col;
@@ -137,12 +135,14 @@ __global__ __launch_bounds__(256) void k_mx4_dequantise(aet_mx4_codes a, Mx4Shap
         const int64_t row = p.row0 + i * p.high;
         if (row >= a.rows) continue;
         const uint8_t *from = codes + row * a.codes.row;
-        if (bytes >= 4) {
-            code[i] = __builtin_bit_cast(uint32_t, (uint8_t __attribute__((ext_vector_type(4))))(*(const wide<uint8_t, 4> *)from));
-        } else {
-            code[i] = 0;
+        code[i] = 0;
+        if (bytes >= V / 2) {
+            const wide<uint8_t, V / 2> all = *(const wide<uint8_t, V / 2> *)from;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) code[i] |= (uint32_t)from[e < bytes ? e : bytes - 1] << (8 * e);
+            for (int e = 0; e < V / 2; ++e) code[i] |= (uint32_t)all[e] << (8 * e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V / 2; ++e) code[i] |= (uint32_t)from[e < bytes ? e : bytes - 1] << (8 * e);
         }
         scale[i] = scales[row * a.scales.row];
     }
@@ -150,40 +150,42 @@ __global__ __launch_bounds__(256) void k_mx4_dequantise(aet_mx4_codes a, Mx4Shap
     for (int i = 0; i < ROWS; ++i) {
         const int64_t row = p.row0 + i * p.high;
         if (row >= a.rows) continue;
-        const wide<T, 8> v = expand8<T>(code[i], scale[i]);
+        const wide<T, V> v = expand_piece<T>(code[i], scale[i]);
         T *const to = y + row * a.y.row;
-        if (count >= 8) *(wide<T, 8> *)to = v;
+        if (count >= V) *(wide<T, V> *)to = v;
         else
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+            for (int e = 0; e < V; ++e)
                 if (e < count) to[e] = v[e];
     }
 }
 
-static bool shape_of(int64_t n, int64_t rows, int64_t cols, int each, Mx4Shape *s, int64_t *blocks) {
-    *s = {(int)ceil_div(cols, 32) * 4, 4, 0, 0};
+static bool shape_of(int64_t n, int64_t rows, int64_t cols, int piece, int each, Mx4Shape *s, int64_t *blocks) {
+    *s = {(int)ceil_div(cols, 32) * (32 / piece), 32 / piece, 0, 0};
     while (s->wide < s->pieces && s->wide < 256) s->wide *= 2;
     s->across = ceil_div(s->pieces, s->wide);
     s->down = ceil_div(rows, 256 / s->wide * each);
     *blocks = n * s->across * s->down;
     return *blocks <= INT32_MAX;
 }
-hipError_t launch_mx4_quantise(const aet_mx4_values &a, hipStream_t s) {
+template <typename T>
+static hipError_t quantise(const aet_mx4_values &a, hipStream_t s) {
     Mx4Shape d;
     int64_t blocks;
-    if (!shape_of(a.n, a.rows, a.cols, a.dtype == AET_F32 ? kToRows<float> : kToRows<bf16>, &d, &blocks)) return hipErrorInvalidConfiguration;
-    if (a.dtype == AET_F32) k_mx4_quantise<float><<<(int)blocks, 256, 0, s>>>(a, d);
-    else k_mx4_quantise<bf16><<<(int)blocks, 256, 0, s>>>(a, d);
+    if (!shape_of(a.n, a.rows, a.cols, 8, kToRows<T>, &d, &blocks)) return hipErrorInvalidConfiguration;
+    k_mx4_quantise<T><<<(int)blocks, 256, 0, s>>>(a, d);
     return hipGetLastError();
 }
-hipError_t launch_mx4_dequantise(const aet_mx4_codes &a, hipStream_t s) {
+template <typename T>
+static hipError_t dequantise(const aet_mx4_codes &a, hipStream_t s) {
     Mx4Shape d;
     int64_t blocks;
-    if (!shape_of(a.n, a.rows, a.cols, a.dtype == AET_F32 ? kBackRows<float> : kBackRows<bf16>, &d, &blocks)) return hipErrorInvalidConfiguration;
-    if (a.dtype == AET_F32) k_mx4_dequantise<float><<<(int)blocks, 256, 0, s>>>(a, d);
-    else k_mx4_dequantise<bf16><<<(int)blocks, 256, 0, s>>>(a, d);
+    if (!shape_of(a.n, a.rows, a.cols, kBackPiece<T>, 4, &d, &blocks)) return hipErrorInvalidConfiguration;
+    k_mx4_dequantise<T><<<(int)blocks, 256, 0, s>>>(a, d);
     return hipGetLastError();
 }
+hipError_t launch_mx4_quantise(const aet_mx4_values &a, hipStream_t s) { return a.dtype == AET_F32 ? quantise<float>(a, s) : quantise<bf16>(a, s); }
+hipError_t launch_mx4_dequantise(const aet_mx4_codes &a, hipStream_t s) { return a.dtype == AET_F32 ? dequantise<float>(a, s) : dequantise<bf16>(a, s); }
 
 // ---- the linear layer --------------------------------------------------------------------
 
