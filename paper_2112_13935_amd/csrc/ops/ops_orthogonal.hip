@@ -19,7 +19,7 @@
 //
 // Five steps, y = keep w + scale X: 4096 x 4096 of fp32 4.2 to 4.5 ms (the matrix unit at 920 to 990 TF/s), 4 x 1024 x 4096 in bf16 760 to 800 us
 // (step by step 1120; the products of 1024^3 in tiles of 64, whose operands come from the L2s at 12.7 TB/s: 22 of 31 us each), 3 x 1001 x 515
-// of fp32 190 to 205 (18 launches: 4 us each to begin and to end), 16 x 128 x 784 of fp32 125 (the same).
+// of fp32 190 to 205 (18 launches: 4 us each to begin and to end), 16 x 128 x 784 of fp32 112 (13 launches).
 #include <math.h>
 
 #include <type_traits>
@@ -105,9 +105,8 @@ bool orthogonal_bounded(const aet_orthogonal &o) {
 // A power of two that takes a value of this bound to 2^14 or more and less than 2^15, of a type whose largest value is nearly 2^16.
 // (Below 2^-400 no more: what is multiplied with it stays in 64 bits' range, and is nothing in the result.)
 __device__ inline double room_of(double bound) {
-    if (!(bound > 0)) return 1;
-    int e;
-    frexp(bound, &e);
+    int e = -400;
+    if (bound > 0) frexp(bound, &e);
     return ldexp(1.0, 15 - (e > -400 ? e : -400));
 }
 
@@ -126,6 +125,7 @@ __host__ __device__ inline double most_growth(double a, double b, double c, doub
 struct Scales {
     float a_by;                                     // A = X X^T
     float b_by, b_plus, x_plus;                     // a step by itself: B = b A + c A A, X = a X + B X
+    float ax_by, x_ax, x_aax;                       // the same as a X + b (A X) + c A (A X)
     float p_by, p_plus, p_diagonal;                 // several by A alone: P
     float q_by, t_by, n_by;                         // Q P, A P, (A P) P
     float x_by;                                     // B X or Q X
@@ -153,6 +153,10 @@ __device__ inline void scales_of(const aet_orthogonal &o, const Runs &runs, doub
             t.b_plus = (float)(o.b * sb / sa);
             t.x_by = (float)(next / (sb * sx));
             t.x_plus = (float)(o.a * next / sx);
+            const double st = room_of(x * b.a);
+            t.ax_by = (float)(st / (sa * sx));
+            t.x_ax = (float)(o.b * next / (sa * sx));
+            t.x_aax = (float)(o.c * next / (sa * st));
             sx = next;
         } else {
             const double p = most_growth(o.a, o.b, o.c, x), sp = room_of(p), st = room_of(x * b.next), sn = room_of(b.next * b.next);
@@ -514,6 +518,137 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_half(HalfProduct p) {
     }
 }
 
+// Y = a X + b T + c A T, T = A X, of small A, all of which lies in LDS: 64 columns a workgroup.  A launch instead of two (B, and B X).  Five
+// steps: 1 x 64 x 64 73 -> 50 us, 300 x 64 x 512 257 -> 225, 16 x 128 x 784 128 -> 112; 64 x 128 x 784, four workgroups a unit one after the
+// other, 224 -> 256.
+struct HalfApply {
+    Parts a, xt, x, y, yt;         // yt.p = NULL: not wanted
+    const Scales *by;              // of the first client
+    int steps, tiles, blocks;      // steps: between clients' scales
+};
+template <int M>
+struct ApplyTile {
+    using SA = Stage<M, 64, false>;
+    using SB = Stage<64, 64, false>;
+    static constexpr int kDeep = M / 32, FM = M / 64, LINE = 36;
+    static constexpr int kX = kDeep * SA::kBytes, kTurn = kX + kDeep * SB::kBytes, kLds = kTurn + 4 * 32 * LINE * 4;
+};
+template <int M>
+__global__ __launch_bounds__(256) void k_half_apply(HalfApply p) {
+    using L = ApplyTile<M>;
+    using SA = typename L::SA;
+    using SB = typename L::SB;
+    constexpr int FM = L::FM, LINE = L::LINE;
+    extern __shared__ __attribute__((aligned(1024))) char lds_[];
+    const lds_ptr lds = (lds_ptr)lds_;
+    const int id = xcd_order(blockIdx.x, p.blocks), n0 = id % p.tiles * 64;
+    const int64_t client = id / p.tiles;
+    const Scales &by = p.by[client * p.steps];
+    const float ax_by = by.ax_by, x_ax = by.x_ax, x_aax = by.x_aax, plus = by.x_plus;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wr = wave / 2, wc = wave % 2;
+
+    DirectStage<M, 64, false, 256> la;
+    DirectStage<64, 64, false, 256> lb;
+    la.begin({p.a.p, p.a.client, p.a.line, false, true, 0}, client, 0, 1 << 30, 0, 0);
+    lb.begin({p.xt.p, p.xt.client, p.xt.line, false, true, 0}, client, n0, 1 << 30, 0, 0);
+#pragma unroll
+    for (int i = 0; i < L::kDeep; ++i) {
+        la.load(lds + i * SA::kBytes);
+        lb.load(lds + L::kX + i * SB::kBytes);
+    }
+    const auto arrived = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // the small products apart from high high
+    struct Sums {
+        f16v s[2][FM];
+        __device__ __forceinline__ float at(int j, int e) const { return s[0][j][e] + s[1][j][e]; }
+    };
+    const auto multiply = [&](Sums &c) {
+#pragma unroll
+        for (int j = 0; j < FM; ++j) c.s[0][j] = c.s[1][j] = f16v{};
+#pragma unroll
+        for (int i = 0; i < 2 * L::kDeep; ++i) {
+            half8 a[FM][2], b[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                b[q] = __builtin_bit_cast(half8, SB::fragment(lds + L::kX + i / 2 * SB::kBytes, wc, i % 2 + 2 * q, lane));
+#pragma unroll
+                for (int j = 0; j < FM; ++j) a[j][q] = __builtin_bit_cast(half8, SA::fragment(lds + i / 2 * SA::kBytes, wr * FM + j, i % 2 + 2 * q, lane));
+            }
+#pragma unroll
+            for (int q = 0; q < 3; ++q)   // low high, high high, high low
+#pragma unroll
+                for (int j = 0; j < FM; ++j) {
+                    f16v &o = c.s[q != 1][j];
+                    o = __builtin_amdgcn_mfma_f32_32x32x16_f16(b[q == 0], a[j][q == 2], o, 0, 0, 0);
+                }
+        }
+    };
+    // A lane has, of row lane % 32 of a fragment, four columns at a time: through LDS, a wave for itself, by columns or by rows
+    __attribute__((address_space(3))) float *const mine = (__attribute__((address_space(3))) float *)(lds + L::kTurn) + wave * (32 * LINE);
+    const auto settle = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    };
+    const auto put = [&](auto value) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *(__attribute__((address_space(3))) f4 *)(mine + (lane & 31) * LINE + 8 * q + 4 * (lane >> 5)) = f4{value(4 * q), value(4 * q + 1), value(4 * q + 2), value(4 * q + 3)};
+        settle();
+    };
+    // calls f(column, 8 rows' values)
+    const auto turned = [&](auto f) {
+#pragma unroll
+        for (int c = lane / 4; c < 32; c += 16) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = mine[(lane % 4 * 8 + e) * LINE + c];
+            f(c, v);
+        }
+        settle();
+    };
+    Sums t, u;
+    arrived();
+    multiply(t);
+    arrived();   // T takes X's place
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+        put([&](int e) { return t.at(j, e) * ax_by; });
+        turned([&](int c, const float (&v)[8]) {
+            half8 high, low;
+            split_half(v, high, low);
+            const lds_ptr to = lds + L::kX + (wr * FM + j) * SB::kBytes;
+            *(__attribute__((address_space(3))) half8 *)(to + SB::slot(wc * 32 + c, lane % 4) * 16) = high;
+            *(__attribute__((address_space(3))) half8 *)(to + SB::slot(wc * 32 + c, 4 + lane % 4) * 16) = low;
+        });
+    }
+    arrived();
+    multiply(u);
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+        put([&](int e) { return __builtin_fmaf(u.at(j, e), x_aax, t.at(j, e) * x_ax); });
+        const int row0 = (wr * FM + j) * 32, col0 = n0 + wc * 32;
+#pragma unroll
+        for (int r = 0; r < 32; r += 16) {
+            const int line = r + lane / 4, c = lane % 4 * 8;
+            __attribute__((address_space(3))) f4 *const at = (__attribute__((address_space(3))) f4 *)(mine + line * LINE + c);
+            float v[8], o[8];
+            get_parts(p.x, client, row0 + line, col0 + c, o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(o[e], plus, at[e / 4][e % 4]);
+            put_parts(p.y, client, row0 + line, col0 + c, v);
+            at[0] = f4{v[0], v[1], v[2], v[3]};
+            at[1] = f4{v[4], v[5], v[6], v[7]};
+        }
+        settle();
+        if (p.yt.p) turned([&](int c, const float (&v)[8]) { put_parts(p.yt, client, col0 + c, row0 + lane % 4 * 8, v); });
+    }
+}
+
 // Adds the slices of a split sum, in their order, and ends it: 64 x 64 of C a workgroup.
 template <bool SYM>
 __global__ __launch_bounds__(256) void k_half_join(HalfProduct p, int tiles) {
@@ -598,6 +733,7 @@ struct OrthoPlan {
     Whole w;
     Choice gram, square, pair, times;   // X X^T, A A, two of those, B X
     bool runs;                          // several steps by A alone
+    bool apply;                         // steps by themselves without B
     Parts x[2], xt[2], a[2], b, p[2], q[2], t;   // xt: X's transpose, where B X wants that
     bool turned() const { return times.kind->tile < 256; }
     float *partial;
@@ -657,6 +793,8 @@ static OrthoPlan plan(const aet_orthogonal &o, char *workspace) {
         best = q.runs ? b : a;
         p = q;
     }
+    // (128 rows fill a compute unit's LDS: where that is more than one round of workgroups, products by themselves are faster)
+    p.apply = o.steps && !p.runs && (p.w.mp == 64 || (p.w.mp == 128 && (int64_t)o.n * (p.w.kp / 64) <= 256));
     // parts of the sum of squares: some 2048 workgroups, each with values for its threads
     const int64_t pieces = ceil_div(o.cols, o.dtype == AET_F32 ? 4 : 8) * o.rows, wanted = ceil_div(2048, o.n > 0 ? o.n : 1);
     p.w.parts = (int)(wanted < 256 ? wanted : 256);
@@ -676,7 +814,7 @@ static OrthoPlan plan(const aet_orthogonal &o, char *workspace) {
         if (p.turned()) for (Parts &t : p.xt) t = parts(p.w.kp, p.w.mp);
         const auto squares = [&](Parts &t) { t = parts(p.w.mp, p.w.mp); };
         squares(p.a[0]);
-        squares(p.b);
+        if (!p.apply) squares(p.b);
         if (p.runs) {
             squares(p.a[1]);
             for (int i = 0; i < 2; ++i) squares(p.p[i]), squares(p.q[i]);
@@ -719,6 +857,25 @@ static hipError_t run_half(const HalfProduct &p, hipStream_t stream) {
     kernel<<<p.blocks, 64 * WR * WC, lds, stream>>>(p);
     return hipGetLastError();
 }
+template <int M>
+static hipError_t run_apply(const HalfApply &p, hipStream_t stream) {
+    const auto kernel = k_half_apply<M>;
+    constexpr int lds = ApplyTile<M>::kLds;
+    if constexpr (lds > 64 * 1024) {
+        static aet::PerDevice allowed;
+        int dev = 0, ok = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        e = allowed.get(dev, &ok, [&](int *v) {
+            *v = 1;
+            return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        });
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<p.blocks, 256, lds, stream>>>(p);
+    return hipGetLastError();
+}
+
 template <bool SYM>   // SYM: A = B
 static hipError_t product(const Choice &c, HalfProduct p, hipStream_t s) {
     const int t = c.kind->tile;
@@ -769,7 +926,11 @@ static hipError_t run(const aet_orthogonal &o, char *workspace, hipStream_t s) {
         const bool end = p.w.runs.end(i);
         if (i == first && !step(product<true>(p.gram, one({x, x, p.a[at], none, p.a[at], &by->a_by}, mp, kp), s))) return e;
         const Parts &a = p.a[at];
-        if (i == first && end) {   // a step by itself
+        if (i == first && end && p.apply) {
+            const int tiles = kp / 64, blocks = o.n * tiles;   // (no more than `firsts`)
+            const HalfApply h = {a, xt, x, y, yt, by, o.steps, tiles, blocks};
+            if (!step(mp == 64 ? run_apply<64>(h, s) : run_apply<128>(h, s))) return e;
+        } else if (i == first && end) {   // a step by itself
             if (!step(product<true>(p.square, one({a, a, p.b, a, p.b, &by->b_by, &by->b_plus}, mp, mp), s))) return e;
             if (!step(product<false>(p.times, one({p.b, xt, y, x, yt, &by->x_by, &by->x_plus}, kp, mp), s))) return e;
         } else {
