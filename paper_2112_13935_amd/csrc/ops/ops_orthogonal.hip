@@ -102,12 +102,12 @@ bool orthogonal_bounded(const aet_orthogonal &o) {
     }
     return true;
 }
-// A power of two that takes a value of this bound to 2^14 or more and less than 2^15, of a type whose largest value is nearly 2^16.
+// The exponent of a power of two that takes a value of this bound to 2^14 or more and less than 2^15, of a type whose largest value is nearly 2^16.
 // (Below 2^-400 no more: what is multiplied with it stays in 64 bits' range, and is nothing in the result.)
-__device__ inline double room_of(double bound) {
+__device__ inline int room_of(double bound) {
     int e = -400;
     if (bound > 0) frexp(bound, &e);
-    return ldexp(1.0, 15 - (e > -400 ? e : -400));
+    return 15 - (e > -400 ? e : -400);
 }
 
 // The largest |a + b q + c q^2| over q in [0, top^2]: how much a step makes of a singular value, at most
@@ -135,43 +135,47 @@ struct Runs {
     uint64_t ends[2];
     __host__ __device__ bool end(int i) const { return ends[i / 64] >> (i % 64) & 1; }
 };
-// Of a client whose X begins with singular values up to x; the last X's own scale is taken out of *y_by.
+// Of a client whose X begins with singular values up to x; the last X's own scale is taken out of *y_by.  (A thread's time, about as much as
+// a launch: powers of two are divided by as exponents.)
 __device__ inline void scales_of(const aet_orthogonal &o, const Runs &runs, double x, Scales *to, double *y_by) {
-    double sx = room_of(x), sa = 0, q = 0, sq = 0;
+    int sx = room_of(x), sa = 0, sq = 0;
+    double q = 0;
     bool first = true;   // of a run
+    const auto times = [](double v, int e) { return (float)ldexp(v, e); };
     for (int i = 0; i < o.steps; ++i) {
         const Bounds b = bounds_of(o, x);
-        const double next = room_of(b.next);
+        const int next = room_of(b.next);
         Scales t = {};
         if (first) {
             sa = room_of(b.a);
-            t.a_by = (float)(sa / (sx * sx));
+            t.a_by = times(1, sa - 2 * sx);
         }
         if (first && runs.end(i)) {
-            const double sb = room_of(b.b);
-            t.b_by = (float)(o.c * sb / (sa * sa));
-            t.b_plus = (float)(o.b * sb / sa);
-            t.x_by = (float)(next / (sb * sx));
-            t.x_plus = (float)(o.a * next / sx);
-            const double st = room_of(x * b.a);
-            t.ax_by = (float)(st / (sa * sx));
-            t.x_ax = (float)(o.b * next / (sa * sx));
-            t.x_aax = (float)(o.c * next / (sa * st));
+            const int sb = room_of(b.b), st = room_of(x * b.a);
+            t.b_by = times(o.c, sb - 2 * sa);
+            t.b_plus = times(o.b, sb - sa);
+            t.x_by = times(1, next - sb - sx);
+            t.x_plus = times(o.a, next - sx);
+            t.ax_by = times(1, st - sa - sx);
+            t.x_ax = times(o.b, next - sa - sx);
+            t.x_aax = times(o.c, next - sa - st);
             sx = next;
         } else {
-            const double p = most_growth(o.a, o.b, o.c, x), sp = room_of(p), st = room_of(x * b.next), sn = room_of(b.next * b.next);
-            t.p_by = (float)(o.c * sp / (sa * sa));
-            t.p_plus = (float)(o.b * sp / sa);
-            t.p_diagonal = (float)(o.a * sp);
-            const double more = first ? p : kRoom * q * p, s = first ? sp : room_of(more);
-            t.q_by = first ? 0.0f : (float)(s / (sq * sp));
-            t.t_by = (float)(st / (sa * sp));
-            t.n_by = (float)(sn / (st * sp));
+            const double p = most_growth(o.a, o.b, o.c, x);
+            const int sp = room_of(p), st = room_of(x * b.next), sn = room_of(b.next * b.next);
+            t.p_by = times(o.c, sp - 2 * sa);
+            t.p_plus = times(o.b, sp - sa);
+            t.p_diagonal = times(o.a, sp);
+            const double more = first ? p : kRoom * q * p;
+            const int s = first ? sp : room_of(more);
+            t.q_by = first ? 0.0f : times(1, s - sq - sp);
+            t.t_by = times(1, st - sa - sp);
+            t.n_by = times(1, sn - st - sp);
             q = more;
             sq = s;
             sa = sn;
             if (runs.end(i)) {
-                t.x_by = (float)(next / (sq * sx));
+                t.x_by = times(1, next - sq - sx);
                 sx = next;
             }
         }
@@ -179,7 +183,7 @@ __device__ inline void scales_of(const aet_orthogonal &o, const Runs &runs, doub
         first = runs.end(i);
         x = b.next;
     }
-    *y_by = o.scale / sx;
+    *y_by = ldexp(o.scale, -sx);
 }
 
 // ---- the norm, the first X, and the result -----------------------------------------------
@@ -222,9 +226,11 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_ortho_first(aet_orthogonal a, Whole w, Parts straight, Parts turned) {
     __shared__ double lds[4];
     __shared__ float tile[64][65];
+    // the first workgroups, one a client, work out the scales
     const int rows = w.tall ? w.kp : w.mp, cols = w.tall ? w.mp : w.kp, across = cols / 64, tiles = across * (rows / 64);
-    const int64_t client = blockIdx.x / tiles;
-    const int t = blockIdx.x % tiles, r0 = t / across * 64, c0 = t % across * 64;
+    const bool scales = blockIdx.x < (unsigned)a.n;
+    const int64_t client = scales ? blockIdx.x : (blockIdx.x - a.n) / tiles;
+    const int t = scales ? 0 : (blockIdx.x - a.n) % tiles, r0 = t / across * 64, c0 = t % across * 64;
     double sum = threadIdx.x < w.parts ? w.sums[client * w.parts + threadIdx.x] : 0;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
@@ -233,9 +239,12 @@ __global__ __launch_bounds__(256) void k_ortho_first(aet_orthogonal a, Whole w, 
     const double own = __builtin_sqrt((lds[0] + lds[1]) + (lds[2] + lds[3])), norm = own + a.eps;
     // singular values are at most the norm's share of norm + eps, and the scales go by that: also a gradient far below eps keeps its bits
     const double top = own > 0 && norm < INFINITY ? kRoom * own / norm : 0;
-    if (t == 0 && threadIdx.x == 0) scales_of(a, w.runs, top, w.scales + client * a.steps, w.y_by + client);
+    if (scales) {
+        if (threadIdx.x == 0) scales_of(a, w.runs, top, w.scales + client * a.steps, w.y_by + client);
+        return;
+    }
     // (values that are not finite: all of X is NaN)
-    const double by = own < INFINITY ? (top > 0 ? room_of(top) / norm : 0) : __builtin_nan("");
+    const double by = own < INFINITY ? (top > 0 ? ldexp(1.0, room_of(top)) / norm : 0) : __builtin_nan("");
     const T *g = (const T *)a.g.p + client * a.g.client;
     for (int i = threadIdx.x; i < 64 * 8; i += 256) {
         const int r = i / 8, c = i % 8 * 8;
@@ -903,9 +912,9 @@ static hipError_t run(const aet_orthogonal &o, char *workspace, hipStream_t s) {
     const OrthoPlan p = plan(o, workspace);
     const int64_t norms = (int64_t)o.n * p.w.parts, firsts = (int64_t)o.n * (p.w.mp / 64) * (p.w.kp / 64),
                   lasts = (int64_t)o.n * ceil_div(p.w.m, 64) * ceil_div(p.w.k, 64);
-    if (norms > INT32_MAX || firsts > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (norms > INT32_MAX || firsts + o.n > INT32_MAX) return hipErrorInvalidConfiguration;
     k_ortho_norm<T><<<(int)norms, 256, 0, s>>>(o, p.w);
-    k_ortho_first<T><<<(int)firsts, 256, 0, s>>>(o, p.w, p.w.tall ? p.xt[0] : p.x[0], p.w.tall ? p.x[0] : p.xt[0]);
+    k_ortho_first<T><<<(int)(o.n + firsts), 256, 0, s>>>(o, p.w, p.w.tall ? p.xt[0] : p.x[0], p.w.tall ? p.x[0] : p.xt[0]);
     hipError_t e = hipGetLastError();
     const Parts none = {};
     const int apart = o.steps * (int)(sizeof(Scales) / sizeof(float)), mp = p.w.mp, kp = p.w.kp;
