@@ -77,8 +77,9 @@ __global__ __launch_bounds__(256) void k_mx4_half(HalfRows w, HalfRows x, int co
     if (lane == 0) r.exps[at] = top == INT_MIN ? kNone : shift - 127;   // (a row of zeros weighs nothing)
 #pragma unroll 4
     for (int i = lane; i < pieces; i += 64) {
-        const int scale = i / 4 < blocks ? scales[i / 4] : 127, moved = scale - shift + 127;
-        const float by = __builtin_bit_cast(float, (uint32_t)(scale == 255 ? 255 : moved > 0 ? moved : 0) << 23);   // (255: NaN)
+        // (a block that has a value is moved to no more than 2^13; zeros may have any scale, which must not become 255, NaN)
+        const int scale = i / 4 < blocks ? scales[i / 4] : 127, moved = scale - shift + 127, most = 127 + 13;
+        const float by = __builtin_bit_cast(float, (uint32_t)(scale == 255 ? 255 : moved < 0 ? 0 : moved < most ? moved : most) << 23);
         const uint32_t code = read(i);
         const half2v c0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, by, 0), c1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, by, 1),
                      c2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, by, 2), c3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, by, 3);
