@@ -1,14 +1,13 @@
 // The gradient of the linear layer of values held in 4 bits.
 //
-// dx = dz W and dw = dz^T x, dz = dropout'(dy) act'(z).  W and x have two bits a value and dz more, so a product takes W and x in one
-// part, and dz in as few as hold it: one fp16 value for results in bf16 (to within 2^-11 of it, 2e-4 in the root mean square, where rounding
-// the result is 1.7e-3), two for results in fp32 (22 bits).  fp16 has few exponents, so that both operands are scaled by powers of two that
+// dx = dz W and dw = dz^T x, dz = dropout'(dy) act'(z), in fp32.  W and x have two bits a value and dz more, so a product takes W and x in
+// one part, and dz in two (22 bits).  fp16 has few exponents, so that both operands are scaled by powers of two that
 // move from one to the other: a row of the contraction in W by the exponent that its largest block has, which its column of dz is
 // multiplied by; then a row of dz so that its largest value is near 2^15, which the row of the result is multiplied by.  What is lost
 // of a value is below 2^-39 of the largest of its row, and blocks of W (or x) less than 2^-36 of the largest of their row.
 //
-// 8192 x 4096 x 4096 in bf16 behind SiLU 660 to 690 us: W and x to fp16 38, the largest values 41 and dz 59 (memory: 134 and 268 MB), the
-// products 280 to 300 each (950 TF/s; a loop of the unit's instructions alone runs at 1670).  With dz in two bf16 values 1010.
+// 8192 x 4096 x 4096 behind SiLU 1.37 ms.  In bf16 one fp16 value would do it in 660 us, but is 2^-11 of dz off, which shows where terms
+// cancel; two bf16 values take 1.01 ms, and no more by the linear layer's own way.
 #include "ops_internal.h"
 #include "ops_mx4.h"
 #include "ops_stage.h"
@@ -342,23 +341,20 @@ static HalfPlan plan(const aet_mx4_linear_grad &a, char *workspace) {
     return p;
 }
 
-// Where it can be done and is faster than with the values in dz's own type: two bf16 values behind an activation or dropout (one else, which
-// is exact), three of six products in fp32.
+// Where it can be done and is faster than with the values in dz's own type: two of six products in fp32.
 bool mx4_half_pays(const aet_mx4_linear_grad &a) {
-    if (!a.n || !a.rows || !a.in || !a.out || !(a.dx.p || a.dw.p)) return false;
-    if (a.dtype == AET_BF16 && a.act == AET_ACT_NONE && a.p == 0) return false;
+    if (a.dtype != AET_F32 || !a.n || !a.rows || !a.in || !a.out || !(a.dx.p || a.dw.p)) return false;
     const HalfPlan p = plan(a, (char *)256);
     if ((a.dx.p && !half_fits(p.dx)) || (a.dw.p && !half_fits(p.dw))) return false;
     if ((int64_t)a.n * a.rows > INT32_MAX || p.w_rows > INT32_MAX) return false;
     // Launches more, and dz worked out twice and written in a form for each product.  (Measured against the other way at 50 sizes of 0.3 to 100 G
-    // products, both wanted, in microseconds and for a million values: 3 to 18 and 2 to 3 in bf16, 8 to 18 and 5 to 7 in fp32.  The
-    // choice is the faster way or within 17 % of it.)
+    // products, both wanted, in microseconds and for a million values: 8 to 18 and 5 to 7.  The choice is the faster way or within 17 % of it.)
     const float values = (float)a.n * (float)a.rows * (float)a.out * 1e-6f, forms = (a.dx.p ? 1.0f : 0.0f) + (a.dw.p ? 1.0f : 0.0f);
-    float here = a.dtype == AET_F32 ? 2.0f + 2.1f * values + (4.0f + 1.7f * values) * forms : 1.0f + 0.2f * values + (3.0f + 0.9f * values) * forms;
+    float here = 2.0f + 2.1f * values + (4.0f + 1.7f * values) * forms;
     Product x = p.dx, w = p.dw;
     if (a.dx.p) here += half_product_time(x);
     if (a.dw.p) here += half_product_time(w);
-    x.a.low = w.a.low = a.dtype == AET_BF16 ? 1 : 0;
+    x.a.low = w.a.low = 0;
     return here < gradients_time(a.dtype, x, w);
 }
 size_t mx4_half_workspace(const aet_mx4_linear_grad &a) { return plan(a, nullptr).bytes; }
@@ -386,12 +382,10 @@ static hipError_t run(const aet_mx4_linear_grad &a, char *workspace, hipStream_t
     default: go(std::integral_constant<int, AET_ACT_NONE>());
     }
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && a.dx.p) e = launch_half_product(a.dtype, p.dx, {p.s.row_top, a.rows}, p.more, s);
-    if (e == hipSuccess && a.dw.p) e = launch_half_product(a.dtype, p.dw, {p.s.col_top, a.out}, p.more, s);
+    if (e == hipSuccess && a.dx.p) e = launch_half_product(p.dx, {p.s.row_top, a.rows}, p.more, s);
+    if (e == hipSuccess && a.dw.p) e = launch_half_product(p.dw, {p.s.col_top, a.out}, p.more, s);
     return e;
 }
-hipError_t launch_mx4_half(const aet_mx4_linear_grad &a, void *workspace, hipStream_t s) {
-    return a.dtype == AET_F32 ? run<float>(a, (char *)workspace, s) : run<bf16>(a, (char *)workspace, s);
-}
+hipError_t launch_mx4_half(const aet_mx4_linear_grad &a, void *workspace, hipStream_t s) { return run<float>(a, (char *)workspace, s); }
 
 }  // namespace aet_ops

@@ -48,10 +48,10 @@ struct RowExponents {
 };
 constexpr int kNoExponent = -100000;
 __device__ __forceinline__ int row_shift(int top) { return top < kNoExponent / 2 ? 0 : top - 15; }
-// The same of fp16 operands (A in one part or two), B by columns, where both can go straight into LDS; dtype is C's.
+// The same of fp16 operands (A in one part or two), B by columns, where both can go straight into LDS; C is fp32.
 bool half_fits(const Product &p);
 size_t half_product_workspace(const Product &p);
-hipError_t launch_half_product(int dtype, const Product &p, const RowExponents &half, void *workspace, hipStream_t s);
+hipError_t launch_half_product(const Product &p, const RowExponents &half, void *workspace, hipStream_t s);
 // Microseconds that products are expected to take; of a layer's gradients (the operands of launch_product in one piece, or by
 // launch_pair), those that have clients.
 float half_product_time(const Product &p);

@@ -572,9 +572,8 @@ static hipError_t run_half(const Product &p, const RowExponents &half, void *wor
     if (e != hipSuccess || s.slices == 1) return e;
     return launch_join(sizeof(O) == 4 ? AET_F32 : AET_BF16, s, p.e, stream);
 }
-hipError_t launch_half_product(int dtype, const Product &p, const RowExponents &half, void *workspace, hipStream_t s) {
-    if (dtype == AET_F32) return p.a.by_columns ? run_half<float, true>(p, half, workspace, s) : run_half<float, false>(p, half, workspace, s);
-    return p.a.by_columns ? run_half<bf16, true>(p, half, workspace, s) : run_half<bf16, false>(p, half, workspace, s);
+hipError_t launch_half_product(const Product &p, const RowExponents &half, void *workspace, hipStream_t s) {
+    return p.a.by_columns ? run_half<float, true>(p, half, workspace, s) : run_half<float, false>(p, half, workspace, s);
 }
 
 // Two products in one launch, in tiles of the smallest kind, sums in one piece

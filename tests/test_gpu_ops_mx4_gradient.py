@@ -34,3 +34,41 @@ def test_zeros_of_every_scale(ops, size, dtype):   # noqa: F811
         s[300:555] = every[:, None]
     got = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act="silu")
     assert all(bool(t.isfinite().all()) and torch.equal(t, q) for t, q in zip(got, want))
+
+
+def held_differences(rows, cols):
+    """Codes and scales of a matrix whose column i is 1 in row 2 i and -1 in row 2 i + 1."""
+    v = torch.zeros(rows, cols, dtype=torch.uint8, device=DEV)
+    i = torch.arange(min(cols, rows // 2), device=DEV)
+    v[2 * i, i], v[2 * i + 1, i] = 0x2, 0xA
+    return v[:, 0::2] | v[:, 1::2] << 4, torch.full((rows, (cols + 31) // 32), 127, dtype=torch.uint8, device=DEV)
+
+
+def pairs(g, shape, dt):
+    """Values of which neighbouring rows, and columns, differ by some percent."""
+    v = torch.randn(shape[0] // 2, shape[1] // 2, generator=g).repeat_interleave(2, 0).repeat_interleave(2, 1)
+    v[1::2] *= 1 + 2.0 ** -6
+    v[:, 1::2] *= 1 - 2.0 ** -5
+    return v.to(dt).to(DEV)
+
+
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_differences_of_nearly_equal_terms(ops, size, dtype):   # noqa: F811
+    """What a product takes of dz shows where its terms cancel: in bf16 two bf16 values (2^-16 of it), in fp32 all 24 bits."""
+    rows, inp, out = size
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(2)
+    x, w = held_differences(rows, inp), held_differences(out, inp)
+    dy, pre = pairs(g, (rows, out), dt), pairs(g, (rows, out), dt)
+    dx, dw, _ = ops.aet_mx4_linear_backward(dy, *x, *w, pre, act="silu")
+    dz = d64(dy) * O.slope(d64(pre), "silu")
+    # dz itself as the oracle bounds it (the slope, which may be near 0, is off by up to 10 U32 (|z| + 1), not by a share of it: that times dy),
+    # and its parts; a sum of two terms, of up to three parts each
+    off = d64(dy).abs() * (4 * 1.13 + 10 * (d64(pre).abs() + 1)) * O.U32 + dz.abs() * (2.0 ** -16 if dt == torch.bfloat16 else O.U32)
+    for got, d, o in ((dx, dz, off), (dw, dz.t(), off.t())):
+        n = min(inp, d.shape[1] // 2)
+        v, b = d[:, :2 * n:2] - d[:, 1:2 * n:2], (o + 6 * O.U32 * d.abs())
+        b = b[:, :2 * n:2] + b[:, 1:2 * n:2]
+        O.near(got[:, :n], (v, b + O.ROUND[dt] * (v.abs() + b)), "sums of two")
+        assert not bool(got[:, n:].any())
