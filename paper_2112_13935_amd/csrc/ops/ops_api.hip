@@ -377,22 +377,32 @@ static void fold(aet_mx4_linear &a) {
     a.n = 1;
 }
 
-// One W for all clients: the clients are one, if the rows of held inputs lie one after another, too.
-static bool fold(aet_mx4_linear_grad &a, bool shared) {
-    if (!shared) return true;
+// One W for all clients: the clients are one.  (Held inputs are read as they were given.)
+static void fold(aet_mx4_linear_grad &a, bool shared) {
+    if (!shared) return;
     if (a.rows == 1) {
         a.dy.row = a.dy.client;
-        a.x.row = a.x.client;
-        a.x_scales.row = a.x_scales.client;
         a.pre.row = a.pre.client;
         a.dx.row = a.dx.client;
-    } else if (a.dw.p && (a.x.client != a.rows * a.x.row || a.x_scales.client != a.rows * a.x_scales.row)) {
-        return false;
     }
     a.rows *= a.n;
     a.n = 1;
-    return true;
 }
+
+// The gradient as the linear layer has it; x and w stand for any that are as large.
+static aet_linear_grad plain_gradient(const aet_mx4_linear_grad &a) {
+    aet_linear_grad b = {a.dtype, a.act, a.n, a.rows, a.in, a.out, a.p, a.seed, a.first_row};
+    b.dy = a.dy;
+    b.x = {(void *)256, (int64_t)a.rows * a.in, a.in};
+    b.w = {(void *)256, a.w.client && a.n > 1 ? (int64_t)a.out * a.in : 0, a.in};
+    b.pre = a.pre;
+    b.dx = a.dx;
+    b.dw = a.dw;
+    b.db = a.db;
+    return b;
+}
+// Sums over nothing, and no products: held values are not looked at.
+static bool nothing(const aet_mx4_linear_grad &a) { return !a.n || !a.rows || !a.in || !a.out; }
 
 static aet_status check(const aet_mx4_linear_grad *a, bool *shared) {
     const char *why;
@@ -410,8 +420,7 @@ static aet_status check(const aet_mx4_linear_grad *a, bool *shared) {
                 return fail(AET_EINVAL, "w and w_scales: either both or none are the same for all clients (client = 0)");
         }
     }
-    size_t used;
-    const aet_linear_grad b = mx4_plain_gradient(*a, (void *)256, &used);
+    const aet_linear_grad b = plain_gradient(*a);
     return check(&b, shared);
 }
 
@@ -570,29 +579,30 @@ aet_status aet_mx4_linear_forward(const aet_mx4_linear *a, void *workspace, size
 size_t aet_mx4_linear_backward_workspace_bytes(const aet_mx4_linear_grad *a) {
     bool shared;
     if (check(a, &shared) != AET_OK || (!a->n && !shared)) return 0;
-    aet_mx4_linear_grad h = *a;
-    if (fold(h, shared) && mx4_half_pays(h)) return mx4_half_workspace(h);
-    size_t used;
-    aet_linear_grad b = mx4_plain_gradient(*a, nullptr, &used);
+    if (nothing(*a)) {
+        aet_linear_grad b = plain_gradient(*a);
+        fold(b, shared);
+        return linear_backward_workspace(b);
+    }
+    aet_mx4_linear_grad b = *a;
     fold(b, shared);
-    return used + linear_backward_workspace(b);
+    return mx4_gradient_workspace(b, *a);
 }
 aet_status aet_mx4_linear_backward(const aet_mx4_linear_grad *a, void *workspace, size_t workspace_bytes, void *hip_stream) {
     bool shared;
     if (const aet_status st = check(a, &shared)) return st;
     if (!a->n && !shared) return AET_OK;
-    aet_mx4_linear_grad h = *a;
-    const bool half = fold(h, shared) && mx4_half_pays(h);
-    size_t used = 0;
-    const aet_linear_grad plain = mx4_plain_gradient(*a, workspace, &used);
-    aet_linear_grad b = plain;
-    fold(b, shared);
-    const size_t need = half ? mx4_half_workspace(h) : used + linear_backward_workspace(b);
+    const size_t need = aet_mx4_linear_backward_workspace_bytes(a);
     if (bad_workspace(workspace, workspace_bytes, need))
         return fail(AET_ENOMEM, "the workspace needs %zu bytes, 256-byte aligned; got %zu", need, workspace_bytes);
-    if (half) return done(launch_mx4_half(h, workspace, (hipStream_t)hip_stream));
-    const hipError_t e = launch_mx4_expand(*a, plain, (hipStream_t)hip_stream);
-    return done(e != hipSuccess ? e : launch_linear_backward(b, (char *)workspace + used, (hipStream_t)hip_stream));
+    if (nothing(*a)) {
+        aet_linear_grad b = plain_gradient(*a);
+        fold(b, shared);
+        return done(launch_linear_backward(b, workspace, (hipStream_t)hip_stream));
+    }
+    aet_mx4_linear_grad b = *a;
+    fold(b, shared);
+    return done(launch_mx4_gradient(b, *a, workspace, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

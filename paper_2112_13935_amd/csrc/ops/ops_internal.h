@@ -42,13 +42,8 @@ hipError_t launch_mx4_quantise(const aet_mx4_values &a, hipStream_t s);
 hipError_t launch_mx4_dequantise(const aet_mx4_codes &a, hipStream_t s);
 size_t mx4_linear_forward_workspace(const aet_mx4_linear &a);
 hipError_t launch_mx4_linear_forward(const aet_mx4_linear &a, void *workspace, hipStream_t s);
-// The gradient with all operands in fp16, where that pays.
-bool mx4_half_pays(const aet_mx4_linear_grad &a);
-size_t mx4_half_workspace(const aet_mx4_linear_grad &a);
-hipError_t launch_mx4_half(const aet_mx4_linear_grad &a, void *workspace, hipStream_t s);
-// The gradient of the layer with the held values in `workspace` as they stand for (used: bytes of it), and the launches that
-// put them there.
-aet_linear_grad mx4_plain_gradient(const aet_mx4_linear_grad &a, void *workspace, size_t *used);
-hipError_t launch_mx4_expand(const aet_mx4_linear_grad &a, const aet_linear_grad &plain, hipStream_t s);
+// a: with the clients as one where W is one for all; given: as the caller has it.  Neither is empty.
+size_t mx4_gradient_workspace(const aet_mx4_linear_grad &a, const aet_mx4_linear_grad &given);
+hipError_t launch_mx4_gradient(const aet_mx4_linear_grad &a, const aet_mx4_linear_grad &given, void *workspace, hipStream_t s);
 
 }  // namespace aet_ops

@@ -189,18 +189,6 @@ hipError_t launch_mx4_dequantise(const aet_mx4_codes &a, hipStream_t s) { return
 
 // ---- the linear layer --------------------------------------------------------------------
 
-// The held values as they stand for: every one of them is a value of bf16 (2 bits of it, down to 2^-128), rows a multiple
-// of 16 bytes apart.
-static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
-static int64_t line_of(int dtype, int64_t cols) { return ceil_div(cols, dtype == AET_F32 ? 4 : 8) * (dtype == AET_F32 ? 4 : 8); }
-static size_t expanded_bytes(int dtype, int64_t n, int64_t rows, int64_t cols) {
-    return up256((size_t)n * rows * line_of(dtype, cols) * (dtype == AET_F32 ? 4 : 2));
-}
-static hipError_t expand(int dtype, int64_t n, int64_t rows, int64_t cols, const aet_in &codes, const aet_in &scales, void *to, hipStream_t s) {
-    const int64_t line = line_of(dtype, cols);
-    return launch_mx4_dequantise({dtype, (int32_t)n, (int32_t)rows, (int32_t)cols, codes, scales, {to, rows * line, line}}, s);
-}
-
 static HeldProduct forward_product(const aet_mx4_linear &a) {
     HeldProduct p = {{a.x, a.x_scales}, {a.w, a.w_scales}, a.n, a.rows, a.out, a.in};
     p.e = {a.bias, a.residual, a.y, a.pre, a.rows, a.act, make_drop(a.p, a.seed, a.first_row, a.out)};
@@ -209,30 +197,6 @@ static HeldProduct forward_product(const aet_mx4_linear &a) {
 size_t mx4_linear_forward_workspace(const aet_mx4_linear &a) { return mx4_product_workspace(forward_product(a)); }
 hipError_t launch_mx4_linear_forward(const aet_mx4_linear &a, void *workspace, hipStream_t s) {
     return launch_mx4_product(a.dtype, forward_product(a), workspace, s);
-}
-
-// Sums over nothing: held values are not looked at.
-static bool nothing(const aet_mx4_linear_grad &a) { return !a.n || !a.rows || !a.in || !a.out; }
-aet_linear_grad mx4_plain_gradient(const aet_mx4_linear_grad &a, void *workspace, size_t *used) {
-    aet_linear_grad b = {a.dtype, a.act, a.n, a.rows, a.in, a.out, a.p, a.seed, a.first_row};
-    b.dy = a.dy;
-    b.pre = a.pre;
-    b.dx = a.dx;
-    b.dw = a.dw;
-    b.db = a.db;
-    const int64_t line = line_of(a.dtype, a.in), held = a.w.client ? a.n : 1;
-    const size_t x = a.dw.p && !nothing(a) ? expanded_bytes(a.dtype, a.n, a.rows, a.in) : 0;
-    b.x = {workspace, a.rows * line, line};
-    b.w = {(char *)workspace + x, held > 1 ? a.out * line : 0, line};
-    *used = x + (a.dx.p && !nothing(a) ? expanded_bytes(a.dtype, held, a.out, a.in) : 0);
-    return b;
-}
-hipError_t launch_mx4_expand(const aet_mx4_linear_grad &a, const aet_linear_grad &plain, hipStream_t s) {
-    hipError_t e = hipSuccess;
-    if (nothing(a)) return e;
-    if (a.dw.p) e = expand(a.dtype, a.n, a.rows, a.in, a.x, a.x_scales, (void *)plain.x.p, s);
-    if (e == hipSuccess && a.dx.p) e = expand(a.dtype, a.w.client ? a.n : 1, a.out, a.in, a.w, a.w_scales, (void *)plain.w.p, s);
-    return e;
 }
 
 }  // namespace aet_ops

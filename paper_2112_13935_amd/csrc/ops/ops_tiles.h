@@ -6,13 +6,15 @@ namespace aet_ops {
 
 // By rows: element (r, k) is at p + client * c + row * r + k.  By columns: at p + client * c + row * k + r.  Padded: what
 // lies side by side goes on with zeros up to a multiple of 8.  low: where not 0, the values are in two bf16 parts, whose second
-// lies that many elements behind the first (A of a product with B by columns only).
+// lies that many elements behind the first (A of a product with B by columns only); third: and a third one as far behind the second.
 struct Operand {
     const void *p;
     int64_t client, row;
     bool by_columns, padded;
     int64_t low;
+    bool third;
 };
+__host__ __device__ inline int parts_of(const Operand &o) { return o.low ? (o.third ? 3 : 2) : 1; }
 
 struct Product {
     Operand a, b;
@@ -40,23 +42,13 @@ hipError_t launch_rows(int dtype, const Product &p, hipStream_t s);
 // Bytes of scratch that the product wants (for sums that are split along k).
 size_t product_workspace(int dtype, const Product &p);
 hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStream_t s);
-// C's rows times 2^row_shift(tops[client * .client + row]), tops being the exponent of the largest value of the row that A stands for,
-// which was made to lie below 2^15 so (no more than kNoExponent: there is none).
-struct RowExponents {
-    const int32_t *tops;
-    int64_t client;
-};
-constexpr int kNoExponent = -100000;
-__device__ __forceinline__ int row_shift(int top) { return top < kNoExponent / 2 ? 0 : top - 15; }
-// The same of fp16 operands (A in one part or two), B by columns, where both can go straight into LDS; C is fp32.
-bool half_fits(const Product &p);
-size_t half_product_workspace(const Product &p);
-hipError_t launch_half_product(const Product &p, const RowExponents &half, void *workspace, hipStream_t s);
-// Microseconds that products are expected to take; of a layer's gradients (the operands of launch_product in one piece, or by
-// launch_pair), those that have clients.
-float half_product_time(const Product &p);
-float gradients_time(int dtype, const Product &x, const Product &w);
 // Both gradients of a layer in one launch, where both are small (taken).
 hipError_t launch_pair(int dtype, const Product &x, const Product &w, hipStream_t s, bool *taken);
+
+// Both gradients of a layer whose W and x lie expanded (bf16, B of w and x): A, which is dz, in up to three parts; those that have a
+// place.  The results are of `dtype`.  In one launch where both are small.
+bool held_straight(const Operand &dz, int rows, int out);   // whether dz can be read as it lies
+size_t held_products_workspace(const Product &x, const Product &w);
+hipError_t launch_held_products(int dtype, const Product &x, const Product &w, void *workspace, hipStream_t s);
 
 }  // namespace aet_ops

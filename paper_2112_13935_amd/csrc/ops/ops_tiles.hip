@@ -115,11 +115,9 @@ struct Tile {
     static constexpr int kLds = kStage * kBuffers > kEpilogue ? kStage * kBuffers : kEpilogue;
 };
 
-// O: the type of C and what is beside it.  HALF: the operands are fp16 (T says bf16, which lies as they do), and C's rows are
-// multiplied as `half` says.
-template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT, typename O = T, bool HALF = false>
-__device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, const Shape &s, const Epilogue &e, int block, lds_ptr lds,
-                                        const RowExponents &half = {}) {
+// O: the type of C and what is beside it.  HELD: A in up to three parts.
+template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT, typename O = T, bool HELD = false>
+__device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, const Shape &s, const Epilogue &e, int block, lds_ptr lds) {
     using L = Tile<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>;
     constexpr int FM = L::FM, FN = L::FN, P = L::kParts;
     using SA = typename L::SA;
@@ -164,12 +162,7 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
 #pragma unroll
             for (int i = 0; i < FN; ++i)
 #pragma unroll
-                for (int j = 0; j < FM; ++j) {
-                    if constexpr (HALF)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, f.b[i][0]), __builtin_bit_cast(half8, f.a[j][0]), acc[i][j], 0, 0, 0);
-                    else
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[i][0], f.a[j][0], acc[i][j], 0, 0, 0);
-                }
+                for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[i][0], f.a[j][0], acc[i][j], 0, 0, 0);
         } else {
 #pragma unroll
             for (int q = 0; q < 6; ++q)
@@ -288,8 +281,18 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
             }
         }
     };
-    sum(oa);
-    if constexpr (TB && sizeof(T) == 2) {   // A in two parts: the sum over the second on top
+    if constexpr (HELD) {   // the smallest part first, so that its terms are not rounded at the others' size
+#pragma unroll 1
+        for (int part = parts_of(oa) - 1; part >= 0; --part) {
+            Operand one = oa;
+            one.p = (const T *)oa.p + part * oa.low;
+            sum(one);
+            if (part) __syncthreads();   // the last stage has been read
+        }
+    } else {
+        sum(oa);
+    }
+    if constexpr (!HELD && TB && sizeof(T) == 2) {   // A in two parts: the sum over the second on top
         if (oa.low) {
             Operand low = oa;
             low.p = (const T *)oa.p + oa.low;
@@ -331,11 +334,6 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
 #pragma unroll
                 for (int y = 0; y < 4; ++y) v[4 * h + y] = x[y] + bias[4 * h + y];
             }
-            if constexpr (HALF) {
-                const int by = row < s.M ? row_shift(half.tops[client * half.client + row]) : 0;
-#pragma unroll
-                for (int y = 0; y < V; ++y) v[y] = __builtin_ldexpf(v[y], by);
-            }
             if (row < s.M && count > 0) {
                 if (s.slices > 1) store_some(s.partial + (((int64_t)slice * s.clients + client) * s.M + row) * s.N + col, count, v);
                 else finish<O>(e, client, row, col, count, v);
@@ -352,20 +350,20 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand o
     tile_of<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>(oa, ob, s, e, blockIdx.x, (lds_ptr)lds);
 }
 
-// Operands in fp16, B by columns.
-template <typename O, int BM, int BN, int WR, int WC, bool TA>
-__global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles_half(Operand oa, Operand ob, Shape s, Epilogue e, RowExponents half) {
+// A in up to three parts, B by columns; C is of type O.
+template <typename O, int BM, int BN, int WR, int WC, bool TA, bool DIRECT>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles_held(Operand oa, Operand ob, Shape s, Epilogue e) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    tile_of<bf16, BM, BN, 64, WR, WC, TA, true, true, O, true>(oa, ob, s, e, blockIdx.x, (lds_ptr)lds, half);
+    tile_of<bf16, BM, BN, 64, WR, WC, TA, true, DIRECT, O, true>(oa, ob, s, e, blockIdx.x, (lds_ptr)lds);
 }
 
 // Two small products in one launch: the gradients of a layer's inputs (B by columns) and of its weights (both by columns).
-template <typename T, int BM, int BN, int BK, int WR, int WC, bool DIRECT>
+template <typename T, int BM, int BN, int BK, int WR, int WC, bool DIRECT, typename O = T, bool HELD = false>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles_pair(Product x, Shape sx, Product w, Shape sw) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int block = blockIdx.x;
-    if (block < sx.blocks) tile_of<T, BM, BN, BK, WR, WC, false, true, DIRECT>(x.a, x.b, sx, x.e, block, (lds_ptr)lds);
-    else tile_of<T, BM, BN, BK, WR, WC, true, true, DIRECT>(w.a, w.b, sw, w.e, block - sx.blocks, (lds_ptr)lds);
+    if (block < sx.blocks) tile_of<T, BM, BN, BK, WR, WC, false, true, DIRECT, O, HELD>(x.a, x.b, sx, x.e, block, (lds_ptr)lds);
+    else tile_of<T, BM, BN, BK, WR, WC, true, true, DIRECT, O, HELD>(w.a, w.b, sw, w.e, block - sx.blocks, (lds_ptr)lds);
 }
 
 // Adds the slices of a split sum, in their order, and ends it.  A thread has 16 bytes of C.  Bound by memory: two slices of
@@ -455,21 +453,20 @@ static float time_of(const Kind &k, int64_t stages, int64_t blocks) {
     const float stage = waves <= k.fit ? k.alone + (waves - 1) * k.more : (k.alone + (k.fit - 1) * k.more) * waves / k.fit;
     return (float)stages * stage + waves * k.end;
 }
+static void consider(Choice &best, const Kind &k, const Product &p) {
+    const int64_t tiles = p.clients * ceil_div(p.M, k.bm) * ceil_div(p.N, k.bn), stages = ceil_div(p.K, k.bk);
+    const float sums = (float)p.clients * (float)p.M * (float)p.N * 4.0f;
+    for (int64_t slices = 1; slices == 1 || (slices <= 64 && stages / slices >= 2); slices *= 2) {
+        float t = time_of(k, ceil_div(stages, slices) * parts_of(p.a), tiles * slices);
+        if (slices > 1) t += 4.0f + (float)(2 * slices + 1) * sums / 6e6f;
+        if (!best.kind || t < best.time) best = {&k, (int)slices, t};
+    }
+}
 static Choice choose(int dtype, const Product &p, bool straight) {
     Choice best = {};
-    const auto consider = [&](const Kind &k) {
-        const int64_t tiles = p.clients * ceil_div(p.M, k.bm) * ceil_div(p.N, k.bn), stages = ceil_div(p.K, k.bk);
-        const float sums = (float)p.clients * (float)p.M * (float)p.N * 4.0f;
-        const int parts = p.a.low ? 2 : 1;
-        for (int64_t slices = 1; slices == 1 || (slices <= 64 && stages / slices >= 2); slices *= 2) {
-            float t = time_of(k, ceil_div(stages, slices) * parts, tiles * slices);
-            if (slices > 1) t += 4.0f + (float)(2 * slices + 1) * sums / 6e6f;
-            if (!best.kind || t < best.time) best = {&k, (int)slices, t};
-        }
-    };
-    if (dtype == AET_F32) for (const Kind &k : kKinds32) consider(k);
-    else if (straight) for (const Kind &k : kKinds16) consider(k);
-    else for (const Kind &k : kKinds16Any) if (k.bm < 256 || !p.b.by_columns) consider(k);
+    if (dtype == AET_F32) for (const Kind &k : kKinds32) consider(best, k, p);
+    else if (straight) for (const Kind &k : kKinds16) consider(best, k, p);
+    else for (const Kind &k : kKinds16Any) if (k.bm < 256 || !p.b.by_columns) consider(best, k, p);
     return best;
 }
 
@@ -532,62 +529,9 @@ hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStrea
     return f32 ? run_product<float, true, true>(p, workspace, s) : run_product<bf16, true, true>(p, workspace, s);
 }
 
-// Products of fp16 operands, B by columns, both as stages go straight into LDS.
-bool half_fits(const Product &p) { return direct(p.a, p.M, p.K, 64) && direct(p.b, p.N, p.K, 64); }
-size_t half_product_workspace(const Product &p) {
-    const int slices = choose(AET_BF16, p, true).slices;
-    return slices > 1 ? (size_t)slices * p.clients * p.M * p.N * sizeof(float) : 0;
-}
-float half_product_time(const Product &p) { return choose(AET_BF16, p, true).time; }
-
-template <typename O, int BM, int BN, int WR, int WC, bool TA>
-static hipError_t run_half(const Product &p, const Shape &s, const RowExponents &half, hipStream_t stream) {
-    using L = Tile<bf16, BM, BN, 64, WR, WC, TA, true, true>;
-    const auto kernel = k_tiles_half<O, BM, BN, WR, WC, TA>;
-    if constexpr (L::kLds > 64 * 1024) {
-        static aet::PerDevice allowed;
-        int dev = 0, ok = 0;
-        hipError_t e = hipGetDevice(&dev);
-        if (e != hipSuccess) return e;
-        e = allowed.get(dev, &ok, [&](int *v) {
-            *v = 1;
-            return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kLds);
-        });
-        if (e != hipSuccess) return e;
-    }
-    kernel<<<s.blocks, L::kThreads, L::kLds, stream>>>(p.a, p.b, s, p.e, half);
-    return hipGetLastError();
-}
-template <typename O, bool TA>
-static hipError_t run_half(const Product &p, const RowExponents &half, void *workspace, hipStream_t stream) {
-    const Choice c = choose(AET_BF16, p, true);
-    Shape s;
-    if (!shape_of(p, c, workspace, &s)) return hipErrorInvalidConfiguration;
-    if (!s.blocks) return hipSuccess;
-    hipError_t e;
-    if (c.kind->bm == 256) e = run_half<O, 256, 256, 2, 4, TA>(p, s, half, stream);
-    else if (c.kind->bm == 128) e = run_half<O, 128, 128, 2, 2, TA>(p, s, half, stream);
-    else if (c.kind->bn == 128) e = run_half<O, 64, 128, 2, 2, TA>(p, s, half, stream);
-    else e = run_half<O, 64, 64, 2, 2, TA>(p, s, half, stream);
-    if (e != hipSuccess || s.slices == 1) return e;
-    return launch_join(sizeof(O) == 4 ? AET_F32 : AET_BF16, s, p.e, stream);
-}
-hipError_t launch_half_product(const Product &p, const RowExponents &half, void *workspace, hipStream_t s) {
-    return p.a.by_columns ? run_half<float, true>(p, half, workspace, s) : run_half<float, false>(p, half, workspace, s);
-}
-
 // Two products in one launch, in tiles of the smallest kind, sums in one piece
 static float pair_time(const Kind &k, const Product &x, const Shape &sx, const Product &w, const Shape &sw) {
-    return time_of(k, ceil_div(x.K > w.K ? x.K : w.K, k.bk) * (x.a.low ? 2 : 1), (int64_t)sx.blocks + sw.blocks);
-}
-float gradients_time(int dtype, const Product &x, const Product &w) {
-    const bool d = dtype == AET_BF16;
-    const float one = (x.clients ? choose(dtype, x, d).time : 0.0f) + (w.clients ? choose(dtype, w, d).time : 0.0f);
-    const Choice pair = {d ? &kKinds16[3] : &kKinds32[2], 1};
-    Shape sx, sw;
-    if (!x.clients || !w.clients || !shape_of(x, pair, nullptr, &sx) || !shape_of(w, pair, nullptr, &sw)) return one;
-    const float both = pair_time(*pair.kind, x, sx, w, sw);
-    return both < one + 3.0f ? both : one + 3.0f;
+    return time_of(k, ceil_div(x.K > w.K ? x.K : w.K, k.bk) * parts_of(x.a), (int64_t)sx.blocks + sw.blocks);
 }
 
 template <typename T>
@@ -621,6 +565,87 @@ static hipError_t run_pair(const Product &x, const Product &w, hipStream_t strea
 }
 hipError_t launch_pair(int dtype, const Product &x, const Product &w, hipStream_t s, bool *taken) {
     return dtype == AET_F32 ? run_pair<float>(x, w, s, taken) : run_pair<bf16>(x, w, s, taken);
+}
+
+// ---- products of expanded 4-bit values ---------------------------------------------------
+
+// The kinds as those of bf16; an operand whose lines are too far apart for stages that go straight into LDS has the smallest through registers.
+static bool held_straight(const Product &p) { return direct(p.a, p.M, p.K, 64) && direct(p.b, p.N, p.K, 64); }
+bool held_straight(const Operand &dz, int rows, int out) {
+    Operand turned = dz;
+    turned.by_columns = true;
+    return direct(dz, rows, out, 64) && direct(turned, out, rows, 64);
+}
+static Choice choose_held(const Product &p, bool straight) {
+    Choice best = {};
+    if (straight) for (const Kind &k : kKinds16) consider(best, k, p);
+    else consider(best, kKinds16Any[3], p);
+    return best;
+}
+static size_t held_partial(const Product &p) {
+    const int a = choose_held(p, true).slices, b = choose_held(p, false).slices, slices = a > b ? a : b;
+    return slices > 1 ? (size_t)slices * p.clients * p.M * p.N * sizeof(float) : 0;
+}
+size_t held_products_workspace(const Product &x, const Product &w) {
+    const size_t a = x.e.y.p ? held_partial(x) : 0, b = w.e.y.p ? held_partial(w) : 0;
+    return a > b ? a : b;
+}
+
+template <typename O, int BM, int BN, int WR, int WC, bool TA, bool DIRECT>
+static hipError_t run_held(const Product &p, const Shape &s, hipStream_t stream) {
+    using L = Tile<bf16, BM, BN, 64, WR, WC, TA, true, DIRECT>;
+    const auto kernel = k_tiles_held<O, BM, BN, WR, WC, TA, DIRECT>;
+    if constexpr (L::kLds > 64 * 1024) {
+        static aet::PerDevice allowed;
+        int dev = 0, ok = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        e = allowed.get(dev, &ok, [&](int *v) {
+            *v = 1;
+            return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kLds);
+        });
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<s.blocks, L::kThreads, L::kLds, stream>>>(p.a, p.b, s, p.e);
+    return hipGetLastError();
+}
+template <typename O, bool TA>
+static hipError_t run_held(const Product &p, const Choice &c, bool straight, void *workspace, hipStream_t stream) {
+    Shape s;
+    if (!shape_of(p, c, workspace, &s)) return hipErrorInvalidConfiguration;
+    hipError_t e;
+    if (!straight) e = run_held<O, 64, 64, 2, 2, TA, false>(p, s, stream);
+    else if (c.kind->bm == 256) e = run_held<O, 256, 256, 2, 4, TA, true>(p, s, stream);
+    else if (c.kind->bm == 128) e = run_held<O, 128, 128, 2, 2, TA, true>(p, s, stream);
+    else if (c.kind->bn == 128) e = run_held<O, 64, 128, 2, 2, TA, true>(p, s, stream);
+    else e = run_held<O, 64, 64, 2, 2, TA, true>(p, s, stream);
+    if (e != hipSuccess || s.slices == 1) return e;
+    return launch_join(sizeof(O) == 4 ? AET_F32 : AET_BF16, s, p.e, stream);
+}
+template <typename O>
+static hipError_t run_held_products(const Product &x, const Product &w, void *workspace, hipStream_t stream) {
+    const bool d = held_straight(x) && held_straight(w);
+    const Choice cx = choose_held(x, d), cw = choose_held(w, d), one = {d ? &kKinds16[3] : &kKinds16Any[3], 1};
+    Shape sx, sw;
+    if (x.e.y.p && w.e.y.p && shape_of(x, one, nullptr, &sx) && shape_of(w, one, nullptr, &sw) && sx.blocks <= INT32_MAX - sw.blocks &&
+        pair_time(*one.kind, x, sx, w, sw) <= cx.time + cw.time + 3.0f) {
+        const int blocks = sx.blocks + sw.blocks;
+        if (d) {
+            using L = Tile<bf16, 64, 64, 64, 2, 2, true, true, true>;
+            k_tiles_pair<bf16, 64, 64, 64, 2, 2, true, O, true><<<blocks, L::kThreads, L::kLds, stream>>>(x, sx, w, sw);
+        } else {
+            using L = Tile<bf16, 64, 64, 64, 2, 2, true, true, false>;
+            k_tiles_pair<bf16, 64, 64, 64, 2, 2, false, O, true><<<blocks, L::kThreads, L::kLds, stream>>>(x, sx, w, sw);
+        }
+        return hipGetLastError();
+    }
+    hipError_t e = hipSuccess;
+    if (x.e.y.p) e = run_held<O, false>(x, cx, d, workspace, stream);
+    if (e == hipSuccess && w.e.y.p) e = run_held<O, true>(w, cw, d, workspace, stream);
+    return e;
+}
+hipError_t launch_held_products(int dtype, const Product &x, const Product &w, void *workspace, hipStream_t s) {
+    return dtype == AET_F32 ? run_held_products<float>(x, w, workspace, s) : run_held_products<bf16>(x, w, workspace, s);
 }
 
 }  // namespace aet_ops

@@ -1,5 +1,5 @@
 """The gradient of the linear layer of 4-bit values where its products' operands are hard to hold: blocks of zeros of any scale, differences of
-nearly equal terms."""
+nearly equal terms, blocks far below their row's largest."""
 import pytest
 import torch
 
@@ -52,7 +52,7 @@ def pairs(g, shape, dt):
     return v.to(dt).to(DEV)
 
 
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("size", SIZES, ids=str)
 def test_differences_of_nearly_equal_terms(ops, size, dtype):   # noqa: F811
     """What a product takes of dz shows where its terms cancel: in bf16 two bf16 values (2^-16 of it), in fp32 all 24 bits."""
@@ -72,3 +72,47 @@ def test_differences_of_nearly_equal_terms(ops, size, dtype):   # noqa: F811
         b = b[:, :2 * n:2] + b[:, 1:2 * n:2]
         O.near(got[:, :n], (v, b + O.ROUND[dt] * (v.abs() + b)), "sums of two")
         assert not bool(got[:, n:].any())
+
+
+def tiny_blocks(g, rows, cols):
+    """Codes without zeros, whose second blocks are 2^-60 and whose third ones 2^-45 of the others."""
+    codes = torch.randint(1, 8, (rows, cols), generator=g, dtype=torch.uint8)
+    codes += 8 * torch.randint(0, 2, (rows, cols), generator=g, dtype=torch.uint8)
+    scales = torch.full((rows, cols // 32), 127, dtype=torch.uint8)
+    scales[:, 1], scales[:, 2] = 67, 82
+    return (codes[:, 0::2] | codes[:, 1::2] << 4).to(DEV), scales.to(DEV)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_blocks_far_below_their_rows_largest(ops, size, dtype):   # noqa: F811
+    """Columns of W, and of x, are sums of their own: that others are 2^60 times as large is no matter to them."""
+    rows, inp, out = size
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(3)
+    x, w = tiny_blocks(g, rows, inp), tiny_blocks(g, out, inp)
+    dy = rand(g, (rows, out), dt)
+    dy[3] *= 2.0 ** -50
+    dx, dw, _ = ops.aet_mx4_linear_backward(dy, *x, *w)
+    d, vx, vw = (t.to(DEV) for t in (d64(dy), M.values(*x, inp), M.values(*w, inp)))
+    for got, a, b in ((dx, d, vw), (dw, d.t().contiguous(), vx)):
+        v = a @ b
+        # dz is held whole; three parts of each term at most, in fp32
+        off = (3 * a.shape[1] + 4) * O.U32 * (a.abs() @ b.abs())
+        O.near(got, (v.cpu(), (off + O.ROUND[dt] * (v.abs() + off)).cpu()), "with tiny blocks")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_an_infinite_gradient_beside_tiny_blocks(ops, size, dtype):   # noqa: F811
+    """Infinity times a value that is not 0 is infinity, however small the value."""
+    rows, inp, out = size
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(3)
+    x, w = tiny_blocks(g, rows, inp), tiny_blocks(g, out, inp)
+    dy = rand(g, (rows, out), dt)
+    dy[4, 7] = float("inf")
+    dx, dw, _ = ops.aet_mx4_linear_backward(dy, *x, *w)
+    assert torch.equal(dx[4].double().cpu(), float("inf") * M.values(*w, inp)[7].sign())
+    assert torch.equal(dw[7].double().cpu(), float("inf") * M.values(*x, inp)[4].sign())
+    assert bool(dx[5:].isfinite().all() and dw[8:].isfinite().all())
