@@ -285,7 +285,8 @@ aet_status aet_mx4_linear_forward(const aet_mx4_linear *a, void *workspace, size
 /* Its gradient with regard to what the codes stand for, from the codes: dx = dz W, dw = dz^T x, db = sum of dz over
  * rows.  (That of the values that were quantised is the same where rounding is taken to have a slope of 1.)  dtype is that
  * of dy, pre, dx, dw and db; all else as in aet_linear_grad, but x may lie anyhow also where one W is for all.  The products
- * take dz whole where dtype is AET_F32 (to within 2^-134), else as those of aet_linear_grad do. */
+ * take dz whole where dtype is AET_F32 (to within 2^-134), else as those of aet_linear_grad do, and what codes stand for as it
+ * is; sums below 2^-124 may be 0. */
 typedef struct {
     int32_t dtype, act;
     int32_t n, rows, in, out;

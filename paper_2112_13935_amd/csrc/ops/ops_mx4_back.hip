@@ -1,6 +1,6 @@
 // The gradient of the linear layer of values held in 4 bits.
 //
-// dx = dz W and dw = dz^T x, dz = dropout'(dy) act'(z).  Every value that codes stand for is one of bf16 (2 bits of it), so the products
+// dx = dz W and dw = dz^T x, dz = dropout'(dy) act'(z).  A quarter of every value that codes stand for is one of bf16 (2 bits of it), so the products
 // are of the matrix unit's bf16 instructions with W and x in one part, and with dz in as many as it takes: two for results in bf16 (to
 // within 2^-16 of it), as in the linear layer's gradient, three for results in fp32 (24 bits, where that layer's fp32 products, whose
 // operands both have 24, are six).  Without activation and dropout a dz in bf16 is dy as it is.
@@ -106,7 +106,8 @@ __global__ __launch_bounds__(256) void k_held_dz(aet_mx4_linear_grad a, Drop d, 
 
 // ---- W and x -----------------------------------------------------------------------------
 
-// Rows of held values as bf16, with zeros up to a multiple of 8.
+// Rows of held values as bf16, with zeros up to a multiple of 8.  They are a quarter of what they stand for, which the products make up for:
+// 6 x 2^127, the largest, is beyond bf16's (and fp32's) largest value, while the smallest, 2^-128, leaves it room below.
 struct HeldRows16 {
     Held from;
     bf16 *to;
@@ -146,7 +147,7 @@ __global__ __launch_bounds__(256) void k_held_values(HeldRows16 w, HeldRows16 x,
         bf8 v;
         const auto two = [&](f2 q, int e) {
 #pragma unroll
-            for (int y = 0; y < 2; ++y) v[e + y] = e + y < left ? (bf16)(scale == 255 ? __builtin_nanf("") : __builtin_ldexpf(q[y], scale - 127)) : (bf16)0.0f;
+            for (int y = 0; y < 2; ++y) v[e + y] = e + y < left ? (bf16)(scale == 255 ? __builtin_nanf("") : __builtin_ldexpf(q[y], scale - 129)) : (bf16)0.0f;
         };
         two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 0), 0);
         two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 1), 2);

@@ -45,7 +45,7 @@ hipError_t launch_product(int dtype, const Product &p, void *workspace, hipStrea
 // Both gradients of a layer in one launch, where both are small (taken).
 hipError_t launch_pair(int dtype, const Product &x, const Product &w, hipStream_t s, bool *taken);
 
-// Both gradients of a layer whose W and x lie expanded (bf16, B of w and x): A, which is dz, in up to three parts; those that have a
+// Both gradients of a layer whose W and x lie expanded (bf16, a quarter of their values; B of w and x): A, which is dz, in up to three parts; those that have a
 // place.  The results are of `dtype`.  In one launch where both are small.
 bool held_straight(const Operand &dz, int rows, int out);   // whether dz can be read as it lies
 size_t held_products_workspace(const Product &x, const Product &w);

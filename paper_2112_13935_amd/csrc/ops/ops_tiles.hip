@@ -115,7 +115,7 @@ struct Tile {
     static constexpr int kLds = kStage * kBuffers > kEpilogue ? kStage * kBuffers : kEpilogue;
 };
 
-// O: the type of C and what is beside it.  HELD: A in up to three parts.
+// O: the type of C and what is beside it.  HELD: A in up to three parts, B's values a quarter of what they stand for.
 template <typename T, int BM, int BN, int BK, int WR, int WC, bool TA, bool TB, bool DIRECT, typename O = T, bool HELD = false>
 __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, const Shape &s, const Epilogue &e, int block, lds_ptr lds) {
     using L = Tile<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>;
@@ -334,6 +334,9 @@ __device__ __forceinline__ void tile_of(const Operand &oa, const Operand &ob, co
 #pragma unroll
                 for (int y = 0; y < 4; ++y) v[4 * h + y] = x[y] + bias[4 * h + y];
             }
+            if constexpr (HELD)
+#pragma unroll
+                for (int y = 0; y < V; ++y) v[y] *= 4.0f;
             if (row < s.M && count > 0) {
                 if (s.slices > 1) store_some(s.partial + (((int64_t)slice * s.clients + client) * s.M + row) * s.N + col, count, v);
                 else finish<O>(e, client, row, col, count, v);
@@ -350,7 +353,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles(Operand oa, Operand o
     tile_of<T, BM, BN, BK, WR, WC, TA, TB, DIRECT>(oa, ob, s, e, blockIdx.x, (lds_ptr)lds);
 }
 
-// A in up to three parts, B by columns; C is of type O.
+// A in up to three parts, B a quarter, by columns; C is of type O.
 template <typename O, int BM, int BN, int WR, int WC, bool TA, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_tiles_held(Operand oa, Operand ob, Shape s, Epilogue e) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];

@@ -116,3 +116,26 @@ def test_an_infinite_gradient_beside_tiny_blocks(ops, size, dtype):   # noqa: F8
     assert torch.equal(dx[4].double().cpu(), float("inf") * M.values(*w, inp)[7].sign())
     assert torch.equal(dw[7].double().cpu(), float("inf") * M.values(*x, inp)[4].sign())
     assert bool(dx[5:].isfinite().all() and dw[8:].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("scale,power", [(254, -40), (253, -40), (0, 100), (1, 100), (2, 100)])
+def test_largest_and_smallest_scales(ops, size, act, dtype, scale, power):   # noqa: F811
+    """Codes stand for values beyond fp32's largest, and below its smallest normal one, whose gradients are ordinary."""
+    rows, inp, out = size
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(4)
+    (x, xs), (w, ws) = held(g, (rows, inp)), held(g, (out, inp))
+    for s in (xs, ws):
+        s.fill_(scale)
+    dy, pre = rand(g, (rows, out), dt, 2.0 ** power), rand(g, (rows, out), dt)
+    dx, dw, _ = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act=act)
+    d = d64(dy) * (O.slope(d64(pre), act) if act != "none" else 1.0)
+    doff = d64(dy).abs() * (4 * 1.13 + 10 * (d64(pre).abs() + 1)) * O.U32 + (d.abs() * 2.0 ** -16 if dt == torch.bfloat16 and act != "none" else 0)
+    d, doff, vx, vw = (t.to(DEV) for t in (d, doff, M.values(x, xs, inp), M.values(w, ws, inp)))
+    for got, a, o, b in ((dx, d, doff, vw), (dw, d.t().contiguous(), doff.t().contiguous(), vx)):
+        v = a @ b
+        off = o @ b.abs() + (3 * a.shape[1] + 4) * O.U32 * (a.abs() @ b.abs())
+        O.near(got, (v.cpu(), (off + O.ROUND[dt] * (v.abs() + off)).cpu()), f"scales of {scale}")
