@@ -628,10 +628,14 @@ static hipError_t run_held(const Product &p, const Choice &c, bool straight, voi
 template <typename O>
 static hipError_t run_held_products(const Product &x, const Product &w, void *workspace, hipStream_t stream) {
     const bool d = held_straight(x) && held_straight(w);
-    const Choice cx = choose_held(x, d), cw = choose_held(w, d), one = {d ? &kKinds16[3] : &kKinds16Any[3], 1};
+    // By the sizes alone, whether or not both are wanted: the order of a sum does not depend on what is wanted beside it.
+    Choice cx = choose_held(x, d), cw = choose_held(w, d);
+    const Choice one = {d ? &kKinds16[3] : &kKinds16Any[3], 1};
     Shape sx, sw;
-    if (x.e.y.p && w.e.y.p && shape_of(x, one, nullptr, &sx) && shape_of(w, one, nullptr, &sw) && sx.blocks <= INT32_MAX - sw.blocks &&
-        pair_time(*one.kind, x, sx, w, sw) <= cx.time + cw.time + 3.0f) {
+    const bool pair = shape_of(x, one, nullptr, &sx) && shape_of(w, one, nullptr, &sw) && sx.blocks <= INT32_MAX - sw.blocks &&
+                      pair_time(*one.kind, x, sx, w, sw) <= cx.time + cw.time + 3.0f;
+    if (pair) cx = cw = one;
+    if (pair && x.e.y.p && w.e.y.p) {
         const int blocks = sx.blocks + sw.blocks;
         if (d) {
             using L = Tile<bf16, 64, 64, 64, 2, 2, true, true, true>;

@@ -139,3 +139,18 @@ def test_largest_and_smallest_scales(ops, size, act, dtype, scale, power):   # n
         v = a @ b
         off = o @ b.abs() + (3 * a.shape[1] + 4) * O.U32 * (a.abs() @ b.abs())
         O.near(got, (v.cpu(), (off + O.ROUND[dt] * (v.abs() + off)).cpu()), f"scales of {scale}")
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(1, 1000, 64, 64), (1, 700, 96, 130), (1, 40, 64, 1500), (16, 257, 512, 1000), (3, 1030, 1030, 1030), (2, 2055, 512, 1543)], ids=str)
+def test_results_do_not_depend_on_what_else_is_wanted(ops, size, dtype, act):   # noqa: F811
+    n, rows, inp, out = size
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(5)
+    (x, xs), (w, ws) = held(g, (n, rows, inp)), held(g, (n, out, inp))
+    dy, pre = rand(g, (n, rows, out), dt), rand(g, (n, rows, out), dt)
+    want = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act=act)
+    for need in ((True, False, False), (False, True, False), (False, False, True), (False, True, True), (True, True, False)):
+        got = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act=act, need=need)
+        assert all(torch.equal(t, q) if yes else t is None for t, q, yes in zip(got, want, need)), need
