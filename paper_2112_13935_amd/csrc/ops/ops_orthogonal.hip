@@ -12,12 +12,14 @@
 // Where X is wide and the result bf16, several steps go by the matrices of m x m alone: X X^T once, then with P = a + b A + c A A
 // of each step Q <- Q P and A <- (A P) P, all of them polynomials of the first A, which commute and are symmetric; at the end
 // X <- Q X.  What A is off by is not corrected there, and grows as the square of what small singular values do, so X is worked out in
-// between where that has come to 2e3.  Relative 2-norm against 64 bits before the result is rounded, gradients of rank 2 to 512 with bf16's
-// noise, five steps (two such runs): 1e-5 to 6e-5; step by step 4e-6 to 3e-5, with products in fp32 6e-6 to 5e-5 (a run of all five: 3e-2).
+// between before that has come to 200: two steps a run with the default polynomial.  Relative 2-norm against 64 bits before the result is
+// rounded, five steps of gradients with bf16's noise, of rank 1, of rank 16 to all, and over five decades: 4e-5 to 1e-4, 3e-6 to 4e-5, and 5e-6
+// to 8e-6, with products in fp32 6e-5 to 1.7e-4, 1e-6 to 5e-5, and 4e-6 to 7e-6.  (Up to 2e3, three steps a run, it was up to four times that, and with
+// other polynomials and more steps up to 50 times what products in fp32 are off by; a run of all five 3e-2.)
 //
 // All matrices of a call lie in the workspace with zeros up to whole tiles, so that no product has to look where they end.
 //
-// Five steps, y = keep w + scale X: 4096 x 4096 of fp32 4.2 to 4.5 ms (the matrix unit at 920 to 990 TF/s), 4 x 1024 x 4096 in bf16 740 to 800 us
+// Five steps, y = keep w + scale X: 4096 x 4096 of fp32 4.2 to 4.5 ms (the matrix unit at 920 to 990 TF/s), 4 x 1024 x 4096 in bf16 850 to 930 us
 // (step by step 1120; the products of 1024^3 in tiles of 64, whose operands come from the L2s at 12.7 TB/s: 22 of 31 us each), 3 x 1001 x 515
 // of fp32 182 to 200 (18 launches: 4 us each to begin and to end), 16 x 128 x 784 of fp32 109 (13 launches).
 #include <math.h>
@@ -757,7 +759,7 @@ static Runs runs_of(const aet_orthogonal &o, bool any) {
         grown *= square(most_growth(o.a, o.b, o.c, x));
         x = bounds_of(o, x).next;
         // (the last step is one, too)
-        const bool end = !any || i + 1 == o.steps || grown * square(most_growth(o.a, o.b, o.c, x)) > 2e3;
+        const bool end = !any || i + 1 == o.steps || grown * square(most_growth(o.a, o.b, o.c, x)) > 200;
         if (end) {
             r.ends[i / 64] |= UINT64_C(1) << (i % 64);
             grown = 1;
