@@ -20,6 +20,7 @@ static aet_status fail(aet_status st, const char *fmt, ...) {
 }
 
 static aet_status done(hipError_t e) {
+    if (e == hipErrorInvalidConfiguration) return fail(AET_EHIP, "the call is too large: a launch of it has 2^32 threads or more");
     return e == hipSuccess ? AET_OK : fail(AET_EHIP, "%s", hipGetErrorString(e));
 }
 

@@ -58,7 +58,7 @@ static hipError_t run(const aet_dropout &a, hipStream_t s) {
     d.across = ceil_div(d.pieces, d.wide);
     d.down = ceil_div(a.rows, 256 / d.wide * kRows);
     const int64_t blocks = a.n * d.across * d.down;
-    if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
     k_dropout<T, V><<<(int)blocks, 256, 0, s>>>(a, make_drop(a.p, a.seed, a.first_row, a.cols), d);
     return hipGetLastError();
 }

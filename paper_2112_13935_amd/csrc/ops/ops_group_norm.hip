@@ -692,11 +692,17 @@ static bool odd_pieces(const NormShape &s) {
     return s.channels % V || (s.spans > 1 && s.span % V);
 }
 
+static bool launches_fit(const NormPlan &p, int64_t samples, int groups) {
+    const int64_t blocks = samples * p.s.spans * p.s.strips, parts = samples * p.s.spans * p.s.parts, all = samples * groups;
+    if (parts > INT32_MAX || all > INT32_MAX || !grid_fits(blocks, p.s.threads)) return false;
+    return p.whole || (grid_fits(parts, p.s.threads) && grid_fits(all, 256));
+}
 template <typename T, bool ODD>
 static hipError_t forward(const aet_group_norm &a, char *workspace, hipStream_t s) {
     constexpr int V = 16 / sizeof(T);
     const int64_t samples = (int64_t)a.n * a.batch;
     if (!a.positions) {
+        if (!grid_fits(ceil_div(samples * a.groups, 256), 256)) return hipErrorInvalidConfiguration;
         if (a.mean || a.rstd) k_norm_nothing<<<(int)ceil_div(samples * a.groups, 256), 256, 0, s>>>(a.mean, a.rstd, a.eps, samples * a.groups);
         return hipGetLastError();
     }
@@ -704,7 +710,7 @@ static hipError_t forward(const aet_group_norm &a, char *workspace, hipStream_t 
     p.s.sums = (float *)workspace;
     p.s.stats = (float *)(workspace + p.sums_bytes);
     const int64_t blocks = samples * p.s.spans * p.s.strips;
-    if (blocks > INT32_MAX || samples * p.s.spans * p.s.parts > INT32_MAX || samples * a.groups > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (!launches_fit(p, samples, a.groups)) return hipErrorInvalidConfiguration;
     if (p.whole) {
         if (p.n <= 4) k_norm_whole<T, V, 4, ODD><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
         else if (p.n <= 8) k_norm_whole<T, V, 8, ODD><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
@@ -734,7 +740,7 @@ static hipError_t backward(const aet_group_norm_grad &a, char *workspace, hipStr
         p.s.sums = (float *)workspace;
         p.s.stats = (float *)(workspace + p.sums_bytes);
         const int64_t blocks = samples * p.s.spans * p.s.strips;
-        if (blocks > INT32_MAX || samples * p.s.spans * p.s.parts > INT32_MAX || samples * a.groups > INT32_MAX) return hipErrorInvalidConfiguration;
+        if (!launches_fit(p, samples, a.groups)) return hipErrorInvalidConfiguration;
         if (p.whole) {
             if (p.n <= 4) k_norm_back_whole<T, V, 4, ODD><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
             else k_norm_back_whole<T, V, 8, ODD><<<(int)blocks, p.s.threads, p.lds, s>>>(a, p.s);
@@ -748,7 +754,7 @@ static hipError_t backward(const aet_group_norm_grad &a, char *workspace, hipStr
         const bool shared = (a.dgamma.p && !a.dgamma.client) || (a.dbeta.p && !a.dbeta.client);
         const int clients = shared ? 1 : a.n, across = (int)ceil_div(channels, 64);
         if (!clients) return hipSuccess;
-        if ((int64_t)clients * across > INT32_MAX) return hipErrorInvalidConfiguration;
+        if (!grid_fits((int64_t)clients * across, 256)) return hipErrorInvalidConfiguration;
         k_norm_params<T><<<clients * across, 256, 0, s>>>(a, p.s.sums, (int64_t)p.s.strips * 2 * channels, (int)channels, across, samples / clients);
     }
     return hipGetLastError();

@@ -10,6 +10,9 @@ namespace aet_ops {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Whether a launch can be as large.  (Threads are counted in 32 bits: 2^24 + 8 workgroups of 256 run as 8, and nobody says so.)
+inline bool grid_fits(int64_t blocks, int64_t threads) { return blocks <= UINT32_MAX / threads; }
+
 // Whether vectors of 16 bytes can be read at p + any multiples of the strides (elements of e bytes).
 inline bool aligned16(const void *p, int64_t e, int64_t s1, int64_t s2, int64_t s3 = 0) {
     return ((uintptr_t)p | (uintptr_t)(s1 * e) | (uintptr_t)(s2 * e) | (uintptr_t)(s3 * e)) % 16 == 0;

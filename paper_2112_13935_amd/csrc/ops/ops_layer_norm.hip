@@ -231,7 +231,7 @@ static hipError_t forward(const aet_layer_norm &a, hipStream_t s) {
     const bool held = a.cols > 0 && for_width<false>(ceil_div(a.cols, V), [&](auto L, auto W, auto NP) {
         constexpr int threads = threads_of(W), R = threads / (L * W);
         const int64_t blocks = ceil_div(rows, R);
-        if (blocks > INT32_MAX) {
+        if (!grid_fits(blocks, threads)) {
             e = hipErrorInvalidConfiguration;
             return;
         }
@@ -239,7 +239,7 @@ static hipError_t forward(const aet_layer_norm &a, hipStream_t s) {
         kernel<<<(int)blocks, threads, 0, s>>>(a, inv);
     });
     if (!held) {
-        if (rows > INT32_MAX) return hipErrorInvalidConfiguration;
+        if (!grid_fits(rows, kLong)) return hipErrorInvalidConfiguration;
         k_ln_long<T><<<(int)rows, kLong, 0, s>>>(a, a.cols ? 1.0 / a.cols : 0.0);
     }
     return e != hipSuccess ? e : hipGetLastError();
@@ -551,7 +551,7 @@ static hipError_t backward(const aet_layer_norm_grad &a, void *workspace, hipStr
     if (!a.cols) return hipSuccess;
     if (!a.n || !a.rows) {
         const int64_t blocks = ceil_div(sums * a.cols, 256);
-        if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+        if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
         if (params && blocks) k_ln_none<T><<<(int)blocks, 256, 0, stream>>>(a, sums);
         return hipGetLastError();
     }
@@ -559,8 +559,12 @@ static hipError_t backward(const aet_layer_norm_grad &a, void *workspace, hipStr
     const StripShape s = strips_of(a, workspace);
     const float inv = (float)(1.0 / a.cols);
     const int64_t blocks = (int64_t)a.n * s.strips;
-    if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+    hipError_t e = hipSuccess;
     const auto go = [&](auto sums, auto L, auto W, auto NP) {
+        if (!grid_fits(blocks, threads_of(W))) {
+            e = hipErrorInvalidConfiguration;
+            return;
+        }
         const auto kernel = a.cols % V ? k_ln_back<T, L, W, NP, true, sums> : k_ln_back<T, L, W, NP, false, sums>;
         kernel<<<(int)blocks, threads_of(W), 0, stream>>>(a, s, inv);
     };
@@ -568,14 +572,15 @@ static hipError_t backward(const aet_layer_norm_grad &a, void *workspace, hipStr
                              : for_width<false>(ceil_div(a.cols, V), [&](auto... g) { go(std::false_type(), g...); });
     if (!held) {
         const int64_t rows = (int64_t)a.n * a.rows, across = ceil_div(a.cols, 256 * V);
-        if (rows > INT32_MAX || blocks * across > INT32_MAX) return hipErrorInvalidConfiguration;
+        if ((a.dx.p && !grid_fits(rows, kLong)) || (params && !grid_fits(blocks * across, 256))) return hipErrorInvalidConfiguration;
         // first, while dy has its values (dx may be dy)
         if (params) k_ln_params_long<T><<<(int)(blocks * across), 256, 0, stream>>>(a, s, (int)across);
         if (a.dx.p) k_ln_back_long<T><<<(int)rows, kLong, 0, stream>>>(a, 1.0 / a.cols);
     }
+    if (e != hipSuccess) return e;
     if (params && !s.direct) {
         const int64_t across = ceil_div(a.cols, 32), joins = 2 * across * sums;
-        if (joins > INT32_MAX) return hipErrorInvalidConfiguration;
+        if (!grid_fits(joins, 256)) return hipErrorInvalidConfiguration;
         k_ln_join<T><<<(int)joins, 256, 0, stream>>>(a, s, a.n * s.strips / sums, (int)across);
     }
     return hipGetLastError();

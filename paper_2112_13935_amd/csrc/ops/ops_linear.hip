@@ -202,7 +202,7 @@ static hipError_t backward(const aet_linear_grad &a, char *workspace, hipStream_
     hipError_t e = hipSuccess;
     if (a.out && (b.dz_bytes || a.db.p)) {
         const int64_t blocks = (int64_t)a.n * b.dz.across * b.dz.strips;
-        if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+        if (!grid_fits(blocks, 256) || (a.db.p && b.dz.strips > 1 && !grid_fits(ceil_div((int64_t)a.n * a.out, 256), 256))) return hipErrorInvalidConfiguration;
         const Drop d = make_drop(a.p, a.seed, a.first_row, a.out);
         const auto dz = [&](auto act) {
             const auto kernel = d.least ? k_dz<T, act, true> : k_dz<T, act, false>;

@@ -166,7 +166,7 @@ static bool shape_of(int64_t n, int64_t rows, int64_t cols, int piece, int each,
     s->across = ceil_div(s->pieces, s->wide);
     s->down = ceil_div(rows, 256 / s->wide * each);
     *blocks = n * s->across * s->down;
-    return *blocks <= INT32_MAX;
+    return grid_fits(*blocks, 256);
 }
 template <typename T>
 static hipError_t quantise(const aet_mx4_values &a, hipStream_t s) {

@@ -232,7 +232,7 @@ static hipError_t run(const aet_mx4_linear_grad &a, const aet_mx4_linear_grad &g
     int lanes = 0;
     while (lanes < 6 && 8 << lanes < p.line) ++lanes;
     const int64_t values = ceil_div((p.w.all + p.x.all) << lanes, 256), sums = a.db.p && p.dz.strips > 1 ? ceil_div((int64_t)a.n * a.out, 256) : 0;
-    if (blocks > INT32_MAX || values + sums > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (!grid_fits(blocks, 256) || !grid_fits(values + sums, 256)) return hipErrorInvalidConfiguration;
     if (p.dz.to || a.db.p) {
         const Drop d = make_drop(a.p, a.seed, a.first_row, a.out);
         const auto go = [&](auto act) {

@@ -404,7 +404,7 @@ static size_t lay_bytes(const Held &o, int64_t clients, int64_t rows, int64_t K)
 }
 static hipError_t lay(Held &o, int64_t clients, int64_t rows, int64_t K, char *to, hipStream_t s) {
     const int64_t units = ceil_div(K, kUnit), lines = lines_of(o, clients, rows), n = lines / rows, pieces = units * (kUnit / 32), blocks = ceil_div(lines * pieces, 256);
-    if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
     Held d;
     d.codes = {to, n > 1 ? rows * units * (kUnit / 2) : 0, units * (kUnit / 2)};
     d.scales = {to + up256((size_t)lines * units * (kUnit / 2)), n > 1 ? rows * units * (kUnit / 32) : 0, units * (kUnit / 32)};
@@ -444,7 +444,7 @@ template <typename T>
 static hipError_t run(HeldProduct p, char *workspace, hipStream_t stream) {
     if (rows_fit(p)) {
         const int64_t tiles_n = ceil_div(p.N, 16), tiles = tiles_n * ceil_div(p.M, p.M <= 16 ? 16 : 32), blocks = tiles * p.clients;
-        if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+        if (!grid_fits(blocks, 64 * kRowWaves)) return hipErrorInvalidConfiguration;
         const HeldRows s = {p.M, p.N, p.K, (int)tiles_n, (int)tiles};
         if (p.M <= 16) k_mx4_rows<T, 1><<<(int)blocks, 64 * kRowWaves, 0, stream>>>(p.a, p.b, s, p.e);
         else k_mx4_rows<T, 2><<<(int)blocks, 64 * kRowWaves, 0, stream>>>(p.a, p.b, s, p.e);
@@ -453,7 +453,7 @@ static hipError_t run(HeldProduct p, char *workspace, hipStream_t stream) {
     const Choice c = choose(p);
     const Kind &k = *c.kind;
     const int64_t tiles_n = ceil_div(p.N, k.bn), tiles = ceil_div(p.M, k.bm) * tiles_n, blocks = tiles * p.clients * c.slices;
-    if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (!grid_fits(blocks, k.bm == 256 ? 512 : 256)) return hipErrorInvalidConfiguration;
     hipError_t e = hipSuccess;
     if (p.K && !aligned(p.a, p.K)) {
         const size_t bytes = lay_bytes(p.a, p.clients, p.M, p.K);

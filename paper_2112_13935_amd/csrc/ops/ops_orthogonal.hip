@@ -892,7 +892,7 @@ static hipError_t product(const Choice &c, HalfProduct p, hipStream_t s) {
     const int t = c.kind->tile;
     const int64_t tm = p.M / t, tn = p.N / t, tiles = SYM ? tm * (tm + 1) / 2 : tm * tn;
     const int64_t am = p.M / 64, joins = SYM ? am * (am + 1) / 2 : am * (p.N / 64);
-    if (tiles * p.clients * c.slices > INT32_MAX || joins * p.clients > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (!grid_fits(tiles * p.clients * c.slices, t == 256 ? 512 : 256) || !grid_fits(joins * p.clients, 256)) return hipErrorInvalidConfiguration;
     p.tiles_m = (int)tm;
     p.tiles_n = (int)tn;
     p.tiles = (int)tiles;
@@ -914,7 +914,7 @@ static hipError_t run(const aet_orthogonal &o, char *workspace, hipStream_t s) {
     const OrthoPlan p = plan(o, workspace);
     const int64_t norms = (int64_t)o.n * p.w.parts, firsts = (int64_t)o.n * (p.w.mp / 64) * (p.w.kp / 64),
                   lasts = (int64_t)o.n * ceil_div(p.w.m, 64) * ceil_div(p.w.k, 64);
-    if (norms > INT32_MAX || firsts + o.n > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (!grid_fits(norms, 256) || !grid_fits(firsts + o.n, 256)) return hipErrorInvalidConfiguration;
     k_ortho_norm<T><<<(int)norms, 256, 0, s>>>(o, p.w);
     k_ortho_first<T><<<(int)(o.n + firsts), 256, 0, s>>>(o, p.w, p.w.tall ? p.xt[0] : p.x[0], p.w.tall ? p.x[0] : p.xt[0]);
     hipError_t e = hipGetLastError();

@@ -165,10 +165,10 @@ static hipError_t run(const Product &p, hipStream_t stream) {
     const RowsShape s = {p.M, p.N, p.K, (int)ceil_div(p.N, 16)};
     const int64_t blocks = (int64_t)p.clients * s.tiles_n;
     if (!blocks || !p.M) return hipSuccess;
-    if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
     // waves: 16 where each has 4 steps or more (32 rows of 4096 x 4096 in bf16 14 us, with 4 waves 16; 64 x (256 x 256) in
     // fp32 with 16 waves 8.2, with 4 5.0)
     const bool deep = p.K >= 16 * 4 * Step<T>::kDepth;
+    if (!grid_fits(blocks, deep ? 1024 : 256)) return hipErrorInvalidConfiguration;
     const auto go = [&](auto odd) {
         if (p.M <= 16) {
             if (deep) k_rows<T, 1, 16, odd><<<(int)blocks, 1024, 0, stream>>>(p.a, p.b, s, p.e);

@@ -393,7 +393,9 @@ __global__ __launch_bounds__(256) void k_join(Shape s, Epilogue e) {
 
 template <typename T>
 static hipError_t run_join(const Shape &s, const Epilogue &e, hipStream_t stream) {
-    k_join<T><<<(int)ceil_div((int64_t)s.clients * s.M * ceil_div(s.N, 16 / sizeof(T)), 256), 256, 0, stream>>>(s, e);
+    const int64_t blocks = ceil_div((int64_t)s.clients * s.M * ceil_div(s.N, 16 / sizeof(T)), 256);
+    if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+    k_join<T><<<(int)blocks, 256, 0, stream>>>(s, e);
     return hipGetLastError();
 }
 hipError_t launch_join(int dtype, const Shape &s, const Epilogue &e, hipStream_t stream) {
@@ -492,7 +494,7 @@ static bool shape_of(const Product &p, const Choice &c, void *workspace, Shape *
     s->slices = c.slices;
     s->slice_k = (int)ceil_div(ceil_div(p.K, k.bk), c.slices) * k.bk;
     s->partial = (float *)workspace;
-    return blocks <= INT32_MAX;
+    return grid_fits(blocks, k.bm == 256 ? 512 : 256);
 }
 template <typename T>
 static bool straight(const Product &p) {
@@ -547,7 +549,7 @@ static hipError_t run_pair(const Product &x, const Product &w, hipStream_t strea
     *taken = false;
     Shape sx, sw;
     if (d != straight<T>(w) || !shape_of(x, one, nullptr, &sx) || !shape_of(w, one, nullptr, &sw) || !sx.blocks || !sw.blocks ||
-        sx.blocks > INT32_MAX - sw.blocks)
+        !grid_fits((int64_t)sx.blocks + sw.blocks, 256))
         return hipSuccess;
     if (pair_time(k, x, sx, w, sw) > choose(dtype, x, d).time + choose(dtype, w, d).time + 3.0f)
         return hipSuccess;
@@ -632,7 +634,7 @@ static hipError_t run_held_products(const Product &x, const Product &w, void *wo
     Choice cx = choose_held(x, d), cw = choose_held(w, d);
     const Choice one = {d ? &kKinds16[3] : &kKinds16Any[3], 1};
     Shape sx, sw;
-    const bool pair = shape_of(x, one, nullptr, &sx) && shape_of(w, one, nullptr, &sw) && sx.blocks <= INT32_MAX - sw.blocks &&
+    const bool pair = shape_of(x, one, nullptr, &sx) && shape_of(w, one, nullptr, &sw) && grid_fits((int64_t)sx.blocks + sw.blocks, 256) &&
                       pair_time(*one.kind, x, sx, w, sw) <= cx.time + cw.time + 3.0f;
     if (pair) cx = cw = one;
     if (pair && x.e.y.p && w.e.y.p) {
