@@ -17,7 +17,7 @@ CALLS = {
     "aet_layer_norm_forward": norm(n=1, rows=1 << 23, cols=20000, x_row=20000, residual_p=None, h_p=None, y_row=20000),
     "aet_layer_norm_backward": norm_grad(n=N, rows=1),
     "aet_orthogonalise": orthogonal(n=N),
-    "aet_dropout_forward": ops.aet_dropout(0, N, 1, 8, 0.0, 0, 0, P, 8, 8, None, 0, 0, P, 8, 8),
+    "aet_dropout_forward": ops.aet_dropout(0, N, 2, 8, 0.0, 0, 0, P, 24, 8, None, 0, 0, P, 24, 8),
 }
 
 
