@@ -478,7 +478,7 @@ __global__ __launch_bounds__(256) void k_ln_params_long(aet_layer_norm_grad a, S
         if (e < count) put_sum<T>(a, s, client, strip, (int)col + e, dg[e], db[e]);
 }
 
-// Adds the strips' sums in their order: 32 runs of them side by side, then the runs.  A workgroup has 32 columns.
+// Adds the strips' sums: 32 runs of them side by side, in their order, then the runs by twos.  A workgroup has 32 columns.
 template <typename T>
 __global__ __launch_bounds__(256) void k_ln_join(aet_layer_norm_grad a, StripShape s, int64_t count, int across) {
     __shared__ f4 lds[32][8];
@@ -497,10 +497,14 @@ __global__ __launch_bounds__(256) void k_ln_join(aet_layer_norm_grad a, StripSha
     __syncthreads();
     const int col = blockIdx.x / 2 % across * 32 + threadIdx.x;
     if (threadIdx.x >= 32 || !out.p || col >= a.cols) return;
-    float total = 0;
+    float total[32];
 #pragma unroll
-    for (int k = 0; k < 32; ++k) total += lds[k][threadIdx.x / 4][threadIdx.x % 4];
-    ((T *)out.p)[client * out.client + col] = (T)total;
+    for (int k = 0; k < 32; ++k) total[k] = lds[k][threadIdx.x / 4][threadIdx.x % 4];
+#pragma unroll
+    for (int off = 16; off > 0; off /= 2)
+#pragma unroll
+        for (int k = 0; k < off; ++k) total[k] += total[k + off];
+    ((T *)out.p)[client * out.client + col] = (T)total[0];
 }
 
 // Parameters' gradients over nothing.
