@@ -4,6 +4,10 @@
 // are of the matrix unit's bf16 instructions with W and x in one part, and with dz in as many as it takes: two for results in bf16 (to
 // within 2^-16 of it), as in the linear layer's gradient, three for results in fp32 (24 bits, where that layer's fp32 products, whose
 // operands both have 24, are six).  Without activation and dropout a dz in bf16 is dy as it is.
+//
+// Bound by the products: 8192 x 4096 x 4096 behind SiLU in bf16 976 to 1050 us, of which dz takes 55 (268 MB: 4.8 TB/s), W and x 32, dx and dw 519
+// and 510 (1060 TF/s; the matrix unit is busy for 55 % of the cycles); in fp32 1.50 to 1.59 ms, of which dz takes 85 (5.5 TB/s), dx and dw 786 and 766.
+// With dy as it is in bf16 482 to 515.  16 x 32 x 784 x 128 17 in bf16 and 19 in fp32: three launches of 5, 5 and 8 to 10.
 #include "ops_internal.h"
 #include "ops_mx4.h"
 #include "ops_stage.h"

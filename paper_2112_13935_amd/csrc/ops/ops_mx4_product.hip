@@ -4,10 +4,11 @@
 // v_mfma_scale_f32_32x32x64_f8f6f4 has the 16 bytes and the scale of one block of a row: the codes go as they lie in
 // memory from there to LDS and to the unit, four times the values a byte of bf16 products.
 //
-// Bound by the matrix unit where there is enough to do: a loop of its instructions alone runs at 5.0 to 5.8 PF/s with random codes (8.7
-// with zeros: the clock gives way).  To bf16: 16384 x 4096 x 4096 198 to 211 us (2.7 PF/s; with bias and GELU 225), 8192^3 317 (3.5).
-// A tile of 256 x 256 takes 2.0 us for 256 k, of which the unit has 1.5, and some 10 from its first load to its last store beside
-// that, a quarter of 16 stages' time; two tiles at once, which would hide that, do not fit into LDS.
+// Bound by the parts of a tile one after the other; no unit is full.  Over the whole of 16384 x 4096 x 4096 with bias and GELU the matrix unit is
+// busy for 30 % of the cycles, LDS for 26 %, and waves are at a wait for 35 % of their time.  A tile of 256 x 256 takes 2.0 us for 256 k, and some 10
+// from its first load to its last store beside that, a quarter of 16 stages' time; two tiles at once, which would hide that, do not fit
+// into LDS.  That size takes 181 to 225 us to bf16 (2.4 to 3.0 PF/s) and 195 to fp32, 8192^3 299 to 317 (3.5 to 3.7).  (A loop of the unit's instructions
+// alone runs at 5.0 to 5.8 PF/s with random codes and at 8.7 with zeros: the clock gives way.)
 #include "ops_internal.h"
 #include "ops_mx4.h"
 #include "ops_stage.h"
@@ -337,7 +338,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_mx4_rows(Held oa, Held ob, H
 static bool rows_fit(const HeldProduct &p) { return p.M <= 32 || p.K >= 1 << 24; }
 
 // Kinds of tiles, as in ops_tiles.hip: microseconds for a stage where a compute unit has one workgroup, for each further one
-// up to the `fit` that it holds, and for each workgroup's epilogue.  Of 24 sizes between 64 x 512 x 512 and 8192 x 8192 x 4096 the choice is
+// up to the `fit` that it holds, and for each workgroup's epilogue.  (They rank the kinds, and are no forecast: with all units busy a stage of 256 x
+// 256 takes 2.0, and a tile's beginning and end 10.)  Of 24 sizes between 64 x 512 x 512 and 8192 x 8192 x 4096 the choice is
 // the fastest kind and split or within 8 % of it; e. g. in tiles of 256, 128, 64: 512 x 4096 x 4096 34, 17, 12.6 us; 2048 x 4096 x 4096 37,
 // 27, 34; 4096^3 43, 49, 66; 512 x 512 x 16384 in 4 parts 37, 21, 15 (whole 111, 47, 31).
 struct Kind {

@@ -19,7 +19,7 @@
 //
 // All matrices of a call lie in the workspace with zeros up to whole tiles, so that no product has to look where they end.
 //
-// Five steps, y = keep w + scale X: 4096 x 4096 of fp32 4.2 to 4.5 ms (the matrix unit at 920 to 990 TF/s), 4 x 1024 x 4096 in bf16 850 to 930 us
+// Five steps, y = keep w + scale X: 4096 x 4096 of fp32 4.2 to 4.5 ms (the matrix unit at 920 to 990 TF/s), 4 x 1024 x 4096 in bf16 820 to 930 us
 // (step by step 1120; the products of 1024^3 in tiles of 64, whose operands come from the L2s at 12.7 TB/s: 22 of 31 us each), 3 x 1001 x 515
 // of fp32 182 to 200 (18 launches: 4 us each to begin and to end), 16 x 128 x 784 of fp32 109 (13 launches).
 #include <math.h>
