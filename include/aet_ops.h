@@ -14,8 +14,8 @@
  *   - All tensors of a call have the call's dtype, but for the statistics of a normalisation
  *     (fp32), and held values (bytes).  Products, sums, statistics and everything between a
  *     call's inputs and its outputs are fp32 or wider; an output is rounded once, to its type.
- *     Exceptions: dz in the gradient of a linear layer in bf16, dz in that of a layer of held
- *     values, and the matrices between the steps of an orthogonalised update (named there);
+ *     Exceptions: dz in the gradient of a linear layer in bf16, of held values or not, and the
+ *     matrices between the steps of an orthogonalised update (named there);
  *     and fp32 products of more than 32 rows, and all of fp32 gradients, take their operands
  *     to within 2^-134, which is less than 24 bits of one below 2^-110 (forward products of up
  *     to 32 rows take all of them).

@@ -154,3 +154,40 @@ def test_results_do_not_depend_on_what_else_is_wanted(ops, size, dtype, act):   
     for need in ((True, False, False), (False, True, False), (False, False, True), (False, True, True), (True, True, False)):
         got = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act=act, need=need)
         assert all(torch.equal(t, q) if yes else t is None for t, q, yes in zip(got, want, need)), need
+
+
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("dtype,act", [("f32", "none"), ("f32", "silu"), ("bf16", "none"), ("bf16", "silu")])
+def test_the_largest_gradients(ops, size, act, dtype):   # noqa: F811
+    """A finite dz is finite in the products, also where its first part by itself would round to infinity."""
+    rows, inp, out = size
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(6)
+    (x, xs), (w, ws) = held(g, (rows, inp)), held(g, (out, inp))
+    for s in (xs, ws):
+        s.fill_(127 - 40)
+    most = torch.finfo(dt).max
+    dy = torch.where(torch.rand(rows, out, generator=g) < 0.5, most, -most).to(dt).to(DEV)
+    pre = torch.full((rows, out), 30.0, dtype=dt, device=DEV)   # where SiLU's slope is 1
+    dx, dw, db = ops.aet_mx4_linear_backward(dy, x, xs, w, ws, pre, act=act)
+    d, vx, vw = (t.to(DEV) for t in (d64(dy), M.values(x, xs, inp), M.values(w, ws, inp)))
+    for got, a, b in ((dx, d, vw), (dw, d.t().contiguous(), vx)):
+        v, S = a @ b, a.abs() @ b.abs()
+        off = ((3 * a.shape[1] + 4) * O.U32 + (2.0 ** -16 if dt == torch.bfloat16 else 2 * O.U32)) * S
+        assert bool(((got.double() - v).abs() <= off + O.ROUND[dt] * (v.abs() + off)).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_what_the_dropout_took_out_has_no_gradient(ops, size, dtype):   # noqa: F811
+    """Whatever dy and z are there: infinities and NaN do not come through."""
+    rows, inp, out = size
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(7)
+    (x, xs), (w, ws) = held(g, (rows, inp)), held(g, (out, inp))
+    dy, pre = rand(g, (rows, out), dt), rand(g, (rows, out), dt)
+    gone = ops.aet_dropout_forward(torch.ones(rows, out, dtype=dt, device=DEV), p=0.4, seed=9, first_row=2) == 0
+    want = ops.aet_mx4_linear_backward(torch.where(gone, 0, dy), x, xs, w, ws, torch.where(gone, 0, pre), act="gelu", p=0.4, seed=9, first_row=2)
+    bad = [torch.where(gone, v, t) for t, v in ((dy, float("inf")), (pre, float("nan")))]
+    got = ops.aet_mx4_linear_backward(bad[0], x, xs, w, ws, bad[1], act="gelu", p=0.4, seed=9, first_row=2)
+    assert bool(gone.any()) and all(torch.equal(a, b) for a, b in zip(got, want))
